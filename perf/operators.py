@@ -1,7 +1,7 @@
 """Speed cases of the operators between a last stage's logits and a loss on log-probabilities.
 
   logprob       token_logprob: per row of logits the target's log-probability, the entropy and the row's
-                maximum and log-sum
+                maximum logit and log-sum
   logprob_grad  token_logprob_backward: the gradient of those log-probabilities and entropies in the logits
   head          head_logprob: the same as logprob from hidden states and the head's matrix
   policy        policy_loss: the clipped surrogate with a KL term and an entropy bonus, and its gradients
@@ -100,10 +100,9 @@ def draw(rng):
         return _policy(_log(rng, 1, max(1, min(2048, 2.0e6 / length))), length, rng.random() < 0.7,
                        rng.random() < 0.5, rng.random() < 0.5, rng.random() < 0.5,
                        rng.choice([0.0, 0.0, 4096.0]))
-    length = _log(rng, 1, 16384)
-    return _pref(_log(rng, 1, max(1, min(1024, 1.0e6 / length))), length, rng.random() < 0.7,
-                 rng.choice(["sigmoid", "sigmoid", "hinge", "square"]), rng.choice([0.0, 0.1]),
-                 rng.choice([0.0, 0.5]), rng.random() < 0.5)
+    length, kind = _log(rng, 1, 16384), rng.choice(["sigmoid", "sigmoid", "hinge", "square"])
+    return _pref(_log(rng, 1, max(1, min(1024, 1.0e6 / length))), length, rng.random() < 0.7, kind,
+                 rng.choice([0.0, 0.1]) if kind == "sigmoid" else 0.0, rng.choice([0.0, 0.5]), rng.random() < 0.5)
 
 
 # ------------------------------------------------------------------------------------------ inputs
@@ -158,10 +157,10 @@ def prepare(case, seed):
             s["out"] = _row_outputs(n)
         else:
             # what the forward left, and a gradient as a loss over the batch gives it
-            z = x.float() * case["inv_temp"]
-            m = z.amax(1)
-            logs = torch.log(torch.exp(z - m[:, None]).sum(1, dtype=torch.float64))
-            q = z.double() - m.double()[:, None] - logs[:, None]
+            m = x.float().amax(1)
+            z = (x.float() - m[:, None]) * case["inv_temp"]
+            logs = torch.log(torch.exp(z).sum(1, dtype=torch.float64))
+            q = z.double() - logs[:, None]
             ent = -(q.exp() * q).sum(1)
             on = t >= 0
             s["stats"] = torch.where(on[:, None], torch.stack([m, logs.float()], 1), 0.0)
@@ -210,9 +209,9 @@ def prepare(case, seed):
 # ------------------------------------------------------------------------------------------ plain forms
 def _plain_logprob(x, t, inv_temp):
     on = t >= 0
-    z = x.float() * inv_temp
+    z = x.float()
     m = z.amax(1)
-    z = z - m[:, None]
+    z = (z - m[:, None]) * inv_temp
     e = torch.exp(z)
     total = e.sum(1)
     logs = torch.log(total)
@@ -226,7 +225,7 @@ def _plain_grad(s):
     c, t = s["case"], s["targets"]
     st = s["stats"]
     on = t >= 0
-    q = s["logits"].float() * c["inv_temp"] - st[:, :1] - st[:, 1:]
+    q = (s["logits"].float() - st[:, :1]) * c["inv_temp"] - st[:, 1:]
     p = torch.exp(q)
     d = -p * s["dlogp"][:, None]
     d[torch.arange(c["rows"], device=DEV), t.clamp(min=0).long()] += s["dlogp"]
@@ -371,26 +370,27 @@ def work(case):
 
 
 # ------------------------------------------------------------------------------------------ exact
-def _exact_rows(z, t):
+def _exact_rows(x, t, inv_temp):
     """Log-probabilities, entropies and statistics of rows of 64-bit logits."""
     on = t >= 0
+    z = x * inv_temp
     m = z.amax(1)
     lse = torch.logsumexp(z, 1)
     q = z - lse[:, None]
     ent = -(q.exp() * q).sum(1)
     logp = q[torch.arange(z.shape[0], device=DEV), t.clamp(min=0).long()]
     keep = lambda v: torch.where(on, v, torch.zeros_like(v))  # noqa: E731
-    return dict(logp=keep(logp), entropy=keep(ent), stats=torch.stack([keep(m), keep(lse - m)], 1))
+    return dict(logp=keep(logp), entropy=keep(ent), stats=torch.stack([keep(x.amax(1)), keep(lse - m)], 1))
 
 
 def exact(case, seed):
     s = prepare(case, seed)
     op, c = case["op"], case
     if op == "logprob":
-        return _exact_rows(s["logits"].double() * c["inv_temp"], s["targets"])
+        return _exact_rows(s["logits"].double(), s["targets"], c["inv_temp"])
     if op == "head":
-        z = s["x"].double() @ s["weight"].double().t()
-        return _exact_rows(z * c["inv_temp"], s["targets"])
+        x = s["x"].double() @ s["weight"].double().t()
+        return _exact_rows(x, s["targets"], c["inv_temp"])
     if op == "logprob_grad":
         x = s["logits"].double().requires_grad_(True)
         q = torch.log_softmax(x * c["inv_temp"], 1)

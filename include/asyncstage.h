@@ -273,6 +273,123 @@ int grad_norm_flat_noalloc(int64_t n, const void* g, int32_t g_is_bf16, float cl
  * flight per thread - the practical HBM ceiling the update pass's bandwidth is reported against. */
 int hbm_stream_copy(void* dst, const void* src, size_t bytes, void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Log-probabilities and the losses on them: fine-tuning by rewards or preferences on the stage that
+ * otherwise trains on next-token cross-entropy.  A last stage runs them in its own paths
+ * (stage_forward_logprob, stage_backward_logprob, stage_score_logprob); these calls take a caller's
+ * arrays.
+ *
+ * Common rules: every call is stateless, enqueues on hip_stream of the current device and allocates
+ * nothing.  `workspace` is device scratch of at least the bytes the matching *_workspace_bytes call
+ * gives (it may be NULL where that is 0), 256-byte aligned, written before it is read; calls that share
+ * one must not overlap.  Arrays need the alignment of their element type only; an output may not
+ * overlap an input unless said.  Sizes of 0 are allowed.  The *_workspace_bytes calls give 0 on sizes
+ * their operator refuses.  Results are the same bit for bit from call to call.
+ */
+
+/* Log-probability of targets[r] under row r of logits, at inv_temperature s > 0: log p = s (x_t - m) -
+ * log S with m the row's largest logit and S = sum_j exp(s (x_j - m)), and the entropy H = -sum p log p.
+ *   logits      [rows, vocab] fp32, or bf16 when logits_bf16; rows ld >= vocab elements apart;
+ *               vocab in [1, 2^24], ld <= 2^28
+ *   targets     [rows] int32; a row whose target is outside [0, vocab) is ignored: its logits are not
+ *               read and its outputs are 0
+ *   logp        [rows] fp32;  entropy [rows] fp32, may be NULL
+ *   stats       [rows, 2] fp32, m and log S (read by token_logprob_backward); may be NULL
+ * A logit of -inf is a token that cannot occur (logp -inf for such a target); a row of only -inf has
+ * logp -inf, entropy 0 and stats (-inf, 0).  A NaN or +inf among a row's logits makes its logp and
+ * entropy NaN. */
+size_t token_logprob_workspace_bytes(int64_t rows, int64_t vocab);
+int token_logprob(int64_t rows, int64_t vocab, const void* logits, int64_t ld, int32_t logits_bf16,
+                  const int32_t* targets, float inv_temperature, float* logp, float* entropy, float* stats,
+                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient in the logits of any function of the log-probabilities and entropies of token_logprob:
+ * dlogits[r, j] = s (g (1[j = t] - p_j) - h p_j (log p_j + H)), g = dlogp[r], h = dentropy[r].
+ * logits, targets and inv_temperature as in the forward, stats (and, with dentropy, entropy) what it
+ * wrote; dentropy may be NULL (then entropy too).  dlogits: fp32, or bf16 (one rounding, to nearest)
+ * when out_bf16, rows ld_out >= vocab elements apart, columns past vocab left as they are; it may be
+ * logits itself (same type and row stride).  A row that is ignored, has only -inf, or has g = h = 0
+ * gets zeros and its logits are not read. */
+int token_logprob_backward(int64_t rows, int64_t vocab, const void* logits, int64_t ld, int32_t logits_bf16,
+                           const int32_t* targets, const float* stats, const float* entropy,
+                           const float* dlogp, const float* dentropy, float inv_temperature, void* dlogits,
+                           int64_t ld_out, int32_t out_bf16, void* hip_stream);
+
+/* token_logprob of the logits x W^T of a head, which are never all in memory: x [rows, d] hidden states
+ * (after the final norm), W [vocab, d] the head's matrix, both fp32 or both bf16 (is_bf16), rows ldx and
+ * ldw >= d elements apart; the products accumulate in fp32.  d in [1, 2^20], ldx and ldw <= 2^24; the other arguments as in
+ * token_logprob.  For log-probabilities no gradient flows through: those of a reference policy, or
+ * of the policy an answer was sampled from. */
+size_t head_logprob_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int32_t is_bf16);
+int head_logprob(int64_t rows, int64_t vocab, int64_t d, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                 int32_t is_bf16, const int32_t* targets, float inv_temperature, float* logp, float* entropy,
+                 float* stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Policy loss of answers [seqs, len] against the policy they were sampled from, and its gradients.
+ * Per token with mask != 0, x = logp - old_logp, r = e^x, A its advantage, d = ref_logp - logp:
+ *   l = max(-r A, -clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - 1 - d) - entropy_coef H
+ *   loss = sum w l, with w = 1 / N over the N tokens that count (reduction 0), or 1 / (B n_b) for a
+ *   sequence of n_b > 0 such tokens among B sequences that have any (reduction 1); norm > 0 takes the
+ *   place of N or B (a count over the whole step, where it is split into microbatches)
+ *   dlogp = grad_scale w (-r A [not clipped] + kl_coef (1 - e^d)),  dentropy = -grad_scale w entropy_coef
+ * A token is clipped where A > 0 and x > log(1 + clip_high), or A < 0 and x < log(1 - clip_low); it then
+ * has no gradient from the first term. */
+typedef struct {
+  float clip_low, clip_high; /* clip_low in [0, 1], clip_high >= 0 */
+  float kl_coef, entropy_coef;
+  double norm;               /* 0: the counts of this call */
+  double grad_scale;         /* multiplies the gradients, not the loss */
+  int32_t reduction;         /* 0: mean over tokens, 1: mean over sequences of their means */
+  int32_t advantage_per_token;
+} policy_hparams_t;
+
+/*   logp, old_logp      [seqs, len] fp32
+ *   ref_logp            [seqs, len] fp32 or NULL (then kl_coef must be 0)
+ *   entropy             [seqs, len] fp32 or NULL (then entropy_coef must be 0)
+ *   advantages          [seqs] fp32, or [seqs, len] with hp->advantage_per_token
+ *   mask                [seqs, len] uint8; where it is 0 the other arrays may hold anything, and the
+ *                       gradients are 0
+ *   loss                one fp32;  dlogp [seqs, len] fp32
+ *   dentropy            [seqs, len] fp32 (NULL exactly when entropy is)
+ *   metrics             6 fp32, sums of w times: the clipped surrogate, the KL term to ref_logp, the
+ *                       entropy, whether the token is clipped, e^x - 1 - x, r
+ *   counts              2 int64: tokens and sequences that count
+ * seqs in [0, 2^31), len in [0, 2^31), seqs len < 2^40.  No token that counts: everything is 0. */
+size_t policy_loss_workspace_bytes(int64_t seqs, int64_t len);
+int policy_loss(int64_t seqs, int64_t len, const float* logp, const float* old_logp, const float* ref_logp,
+                const float* entropy, const float* advantages, const uint8_t* mask, const policy_hparams_t* hp,
+                float* loss, float* dlogp, float* dentropy, float* metrics, int64_t* counts, void* workspace,
+                size_t workspace_bytes, void* hip_stream);
+
+/* Preference loss of pairs of answers, and its gradient.  Rows 0 .. pairs - 1 of the arrays are the
+ * chosen answers, row pairs + p the rejected one of pair p.  A row's score is the sum of logp - ref_logp
+ * over its tokens with mask != 0 (divided by their number with length_normalize); for a pair,
+ * delta = score(chosen) - score(rejected) and h = beta delta - margin:
+ *   kind 0 (sigmoid)  l = -(1 - e) log sigmoid(h) - e log sigmoid(-h), e = label_smoothing
+ *   kind 1 (hinge)    l = max(0, 1 - h)
+ *   kind 2 (square)   l = ((h - 1/2) / beta)^2
+ * loss = the mean of l over the pairs whose rows both have tokens; the others (padding of a batch) have
+ * loss, rewards and gradients 0.  norm > 0 divides instead of their number. */
+typedef struct {
+  float beta; /* > 0 */
+  float label_smoothing; /* [0, 1]; kind 0 only */
+  float margin;
+  int32_t kind, length_normalize;
+  double norm, grad_scale;
+} preference_hparams_t;
+
+/*   logp       [2 pairs, len] fp32;  ref_logp the same or NULL (no reference: logp alone)
+ *   mask       [2 pairs, len] uint8; where it is 0 the other arrays may hold anything
+ *   loss       one fp32;  dlogp [2 pairs, len] fp32 = grad_scale dloss/dlogp
+ *   pair_loss  [pairs] fp32;  rewards [2 pairs] fp32 = beta score
+ *   metrics    4 fp32, means over the same pairs: delta > 0, reward of the chosen, of the rejected, h
+ *   counts     1 int64: pairs that count
+ * pairs in [0, 2^24], len in [0, 2^31), 2 pairs len < 2^40. */
+size_t preference_loss_workspace_bytes(int64_t pairs, int64_t len);
+int preference_loss(int64_t pairs, int64_t len, const float* logp, const float* ref_logp, const uint8_t* mask,
+                    const preference_hparams_t* hp, float* loss, float* dlogp, float* pair_loss, float* rewards,
+                    float* metrics, int64_t* counts, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Ascending unique token ids of the microbatch in `slot` and their counts (after its backward
  * on a first stage).  ids, counts: device int32 arrays of >= micro_batch*seq_len entries;
  * n_unique: device int32. */

@@ -12,6 +12,7 @@ Contents
   ops     primitive operations of a decoder block (App. E.2) and the tied head
   model   stage forward / backward (stack of blocks, embedding, head)
   update  Alg. 1 of §2 with AdamW and the Error-Feedback correction of §3.2 / App. A.4
+  losses  log-probabilities of tokens, the policy and preference losses on them
   run()   the training loop: fwd/bwd at x_t, then the delayed update, for T iterations
 """
 from __future__ import annotations
@@ -20,7 +21,7 @@ from typing import Callable, Dict, List, Optional
 
 import numpy as np
 
-from . import model, ops, update  # noqa: F401
+from . import losses, model, ops, update  # noqa: F401
 from .update import HParams, OptState, iteration_update
 
 

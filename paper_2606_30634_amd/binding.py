@@ -19,7 +19,9 @@ EXPORTS = ["stage_required_bytes", "stage_init", "stage_num_tensors", "stage_ten
            "stage_grad_norm", "stage_profile_enable", "stage_profile_read", "stage_last_error",
            "stage_destroy", "stage_set_update_overlap", "stage_join_update", "stage_resume",
            "grad_norm_flat_workspace_bytes", "grad_norm_flat", "hbm_stream_copy", "delayed_update_flat_adan",
-           "grad_norm_flat_noalloc"]
+           "grad_norm_flat_noalloc", "token_logprob_workspace_bytes", "token_logprob", "token_logprob_backward",
+           "head_logprob_workspace_bytes", "head_logprob", "policy_loss_workspace_bytes", "policy_loss",
+           "preference_loss_workspace_bytes", "preference_loss"]
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_UPDATE, PROF_NORM, PROF_OTHER, PROF_NS = range(7)
 
 
@@ -37,6 +39,18 @@ class UpdateHParams(C.Structure):
                                                           ("momentum", C.c_float), ("update_rms", C.c_float),
                                                           ("ns_steps", C.c_int32), ("predict", C.c_int32),
                                                           ("nadam_psi", C.c_float), ("beta3", C.c_float)]
+
+
+class PolicyHParams(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef")] + [
+        (n, C.c_double) for n in ("norm", "grad_scale")] + [
+        (n, C.c_int32) for n in ("reduction", "advantage_per_token")]
+
+
+class PreferenceHParams(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("beta", "label_smoothing", "margin")] + [
+        (n, C.c_int32) for n in ("kind", "length_normalize")] + [
+        (n, C.c_double) for n in ("norm", "grad_scale")]
 
 
 class StageError(RuntimeError):
@@ -80,6 +94,17 @@ def _load():
         "delayed_update_flat_adan": (C.c_int, [i64, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, i64,
                                                C.POINTER(UpdateHParams), vp, vp]),
         "stage_profile_read": (C.c_int, [vp, i32, C.POINTER(C.c_double), C.POINTER(i64), C.POINTER(C.c_double)]),
+        "token_logprob_workspace_bytes": (sz, [i64, i64]),
+        "token_logprob": (C.c_int, [i64, i64, vp, i64, i32, vp, C.c_float, vp, vp, vp, vp, sz, vp]),
+        "token_logprob_backward": (C.c_int, [i64, i64, vp, i64, i32, vp, vp, vp, vp, vp, C.c_float, vp, i64, i32, vp]),
+        "head_logprob_workspace_bytes": (sz, [i64, i64, i64, i32]),
+        "head_logprob": (C.c_int, [i64, i64, i64, vp, i64, vp, i64, i32, vp, C.c_float, vp, vp, vp, vp, sz, vp]),
+        "policy_loss_workspace_bytes": (sz, [i64, i64]),
+        "policy_loss": (C.c_int, [i64, i64, vp, vp, vp, vp, vp, vp, C.POINTER(PolicyHParams), vp, vp, vp, vp, vp,
+                                  vp, sz, vp]),
+        "preference_loss_workspace_bytes": (sz, [i64, i64]),
+        "preference_loss": (C.c_int, [i64, i64, vp, vp, vp, C.POINTER(PreferenceHParams), vp, vp, vp, vp, vp, vp,
+                                      vp, sz, vp]),
         "stage_last_error": (C.c_char_p, []),
         "stage_destroy": (None, [vp]),
     }
@@ -179,6 +204,52 @@ def grad_norm_flat_noalloc(n, g, g_is_bf16, clip_norm, out_dev, nonfinite_dev, s
 
 def hbm_stream_copy(dst, src, nbytes, stream) -> None:
     _call("hbm_stream_copy", dst, src, nbytes, stream)
+
+
+def token_logprob_workspace_bytes(rows, vocab) -> int:
+    return LIB.token_logprob_workspace_bytes(rows, vocab)
+
+
+def token_logprob(rows, vocab, logits, ld, logits_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
+                  workspace_bytes, stream) -> None:
+    _call("token_logprob", rows, vocab, logits, ld, int(logits_bf16), targets, inv_temperature, logp, entropy, stats,
+          workspace, workspace_bytes, stream)
+
+
+def token_logprob_backward(rows, vocab, logits, ld, logits_bf16, targets, stats, entropy, dlogp, dentropy,
+                           inv_temperature, dlogits, ld_out, out_bf16, stream) -> None:
+    _call("token_logprob_backward", rows, vocab, logits, ld, int(logits_bf16), targets, stats, entropy, dlogp,
+          dentropy, inv_temperature, dlogits, ld_out, int(out_bf16), stream)
+
+
+def head_logprob_workspace_bytes(rows, vocab, d, is_bf16) -> int:
+    return LIB.head_logprob_workspace_bytes(rows, vocab, d, int(is_bf16))
+
+
+def head_logprob(rows, vocab, d, x, ldx, w, ldw, is_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
+                 workspace_bytes, stream) -> None:
+    _call("head_logprob", rows, vocab, d, x, ldx, w, ldw, int(is_bf16), targets, inv_temperature, logp, entropy,
+          stats, workspace, workspace_bytes, stream)
+
+
+def policy_loss_workspace_bytes(seqs, length) -> int:
+    return LIB.policy_loss_workspace_bytes(seqs, length)
+
+
+def policy_loss(seqs, length, logp, old_logp, ref_logp, entropy, advantages, mask, hp: PolicyHParams, loss, dlogp,
+                dentropy, metrics, counts, workspace, workspace_bytes, stream) -> None:
+    _call("policy_loss", seqs, length, logp, old_logp, ref_logp, entropy, advantages, mask, C.byref(hp), loss, dlogp,
+          dentropy, metrics, counts, workspace, workspace_bytes, stream)
+
+
+def preference_loss_workspace_bytes(pairs, length) -> int:
+    return LIB.preference_loss_workspace_bytes(pairs, length)
+
+
+def preference_loss(pairs, length, logp, ref_logp, mask, hp: PreferenceHParams, loss, dlogp, pair_loss, rewards,
+                    metrics, counts, workspace, workspace_bytes, stream) -> None:
+    _call("preference_loss", pairs, length, logp, ref_logp, mask, C.byref(hp), loss, dlogp, pair_loss, rewards,
+          metrics, counts, workspace, workspace_bytes, stream)
 
 
 def stage_embed_indices(s: int, slot: int, ids, counts, n_unique) -> None:

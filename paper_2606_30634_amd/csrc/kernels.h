@@ -220,3 +220,50 @@ void launch_muon_apply(bool bf, const MuonMat* mats, int nmat, int ntile, int fi
                        void* shadow, const int* flag, float lr, float wd, float rms, bool ef, float lam,
                        hipStream_t st);
 
+
+// ------------------------------------------------------------------ log-probabilities (logprob.hip)
+// rows x vocab logits (row stride ld elements, any alignment of the element type), int32 targets; a row
+// whose target is outside [0, vocab) is ignored.  logp [rows]; ent [rows] and stats [rows, 2] (maximum
+// logit, log of the sum of exponentials relative to it) may be null.
+size_t logprob_ws_bytes(int64_t rows, int64_t vocab);
+void launch_logprob(bool bf, int64_t rows, int vocab, const void* logits, int64_t ld, const int32_t* targets,
+                    float inv_temp, float* logp, float* ent, float* stats, void* ws, hipStream_t st);
+// zero_to > vocab: the columns [vocab, zero_to) of dlogits get zeros; dent (with ent) may be null
+void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, int64_t ld, const int32_t* targets,
+                        const float* stats, const float* ent, const float* dlogp, const float* dent, float inv_temp,
+                        bool out_bf, void* dlogits, int64_t ldo, int zero_to, hipStream_t st);
+// launch_logprob of the logits x W^T (x [rows, d], W [vocab, d], rows of ldx and ldw elements)
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d);
+void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
+                         int64_t ldw, const int32_t* targets, float inv_temp, float* logp, float* ent, float* stats,
+                         void* ws, hipStream_t st);
+
+// ------------------------------------------------------------------ losses (losses.hip)
+// Arrays [seqs, len] (preference: [2 pairs, len], chosen rows first); the pointers noted may be null.
+struct PolicyArgs {
+  int64_t seqs, len;
+  const float *logp, *old, *ref, *ent, *adv;  // ref, ent: null or not
+  const uint8_t* mask;
+  int per_token, seq_mean;
+  float clip_low, clip_high, kl_coef, ent_coef;
+  double log_lo, log_hi, norm, grad_scale;  // log(1 - clip_low), log(1 + clip_high)
+  float *loss, *dlogp, *dent, *metrics;     // dent: null without ent
+  int64_t* counts;
+};
+size_t policy_ws_bytes(int64_t seqs, int64_t len);
+void launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t st);
+struct PreferenceArgs {
+  int64_t pairs, len;
+  const float *logp, *ref;  // ref: null or not
+  const uint8_t* mask;
+  int kind, normalize;
+  double beta, smoothing, margin, norm, grad_scale;
+  float *loss, *dlogp, *pair_loss, *rewards, *metrics;
+  int64_t* counts;
+};
+size_t preference_ws_bytes(int64_t pairs, int64_t len);
+void launch_preference_loss(const PreferenceArgs& a, void* ws, hipStream_t st);
+
+// ------------------------------------------------------------------ errors (stage.hip)
+// Sets the message stage_last_error() returns and gives the code back.
+int set_error(int code, const char* msg);

@@ -1,0 +1,333 @@
+// Log-probabilities of given tokens under rows of logits, and their gradient in the logits.
+//
+// For a row x of V logits, s = inv_temperature > 0, m = max x and S = sum exp(s (x_j - m)):
+//   log p_j = s (x_j - m) - log S,   H = log S - sum p_j s (x_j - m)   (both terms >= 0: no cancellation)
+//   dx_j = s (g (1[j = t] - p_j) - h p_j (log p_j + H))   for upstream g = dlogp, h = dentropy.
+// Everything is taken relative to m: x_j - m is exact where it matters, so logits of any magnitude
+// lose nothing, and log p_t = s (x_t - m) - log S is small where p_t is near 1.  Exponentials are base 2
+// with c = s log2(e); sums are fp32.
+//
+// What a row may hold: -inf adds nothing; the running maximum starts at the lowest finite value, so a row
+// of only -inf ends with S = 0 (told apart from one of lowest finite values, which is uniform); a NaN or
+// +inf makes the row NaN through S.
+#include "common.h"
+#include "kernels.h"
+#include <algorithm>
+#include <cfloat>
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float TINY_T = -1e30f;  // a finite stand-in for -inf where it meets a zero factor
+
+// 8 elements at any element alignment
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16> {
+  typedef bf16 raw __attribute__((ext_vector_type(8), aligned(2)));
+  static __device__ __forceinline__ void load(const bf16* p, float (&v)[8]) {
+    const raw r = *reinterpret_cast<const raw*>(p);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = (float)r[q];
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float (&v)[8]) {
+    raw r;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) r[q] = (bf16)v[q];
+    *reinterpret_cast<raw*>(p) = r;
+  }
+};
+template <> struct Vec8<float> {
+  typedef float raw __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
+    const raw a = reinterpret_cast<const raw*>(p)[0], b = reinterpret_cast<const raw*>(p)[1];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = a[q], v[q + 4] = b[q];
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+    reinterpret_cast<raw*>(p)[0] = raw{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<raw*>(p)[1] = raw{v[4], v[5], v[6], v[7]};
+  }
+};
+
+// Running statistics of a part of a row: maximum m, s = sum 2^t, w = sum t 2^t with t = c (x - m).
+struct Part { float m, s, w; };
+__device__ __forceinline__ Part part_empty() { return {-FLT_MAX, 0.f, 0.f}; }
+
+// a's sums relative to the maximum mx >= a.m (an empty part's shift is -inf or NaN: it has nothing to move)
+__device__ __forceinline__ void part_raise(Part& a, float mx, float c) {
+  const float d = fmaxf((a.m - mx) * c, TINY_T), k = __builtin_amdgcn_exp2f(d);
+  a.w = k * (a.w + d * a.s);
+  a.s *= k;
+  a.m = mx;
+}
+__device__ __forceinline__ void part_merge(Part& a, Part b, float c) {
+  const float mx = fmaxf(a.m, b.m);
+  part_raise(a, mx, c);
+  part_raise(b, mx, c);
+  a.s += b.s;
+  a.w += b.w;
+}
+template <int N>
+__device__ __forceinline__ void part_add(Part& a, const float (&v)[N], float c) {
+  float mx = v[0];
+#pragma unroll
+  for (int q = 1; q < N; ++q) mx = fmaxf(mx, v[q]);
+  if (mx > a.m) part_raise(a, mx, c);
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    const float t = (v[q] - a.m) * c, e = __builtin_amdgcn_exp2f(t);
+    a.s += e;
+    a.w += e * fmaxf(t, TINY_T);
+  }
+}
+template <int LANES>
+__device__ __forceinline__ void part_lanes(Part& a, float c) {  // the same in every lane of the group
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    const Part b{__shfl_xor(a.m, o, WAVE), __shfl_xor(a.s, o, WAVE), __shfl_xor(a.w, o, WAVE)};
+    part_merge(a, b, c);
+  }
+}
+
+// What a row's statistics say about its target (x_t its logit).
+__device__ __forceinline__ void row_finish(const Part& a, float xt, float c, int64_t row, float* logp, float* ent,
+                                           float* stats) {
+  const float ls = logf(a.s);
+  const bool none = a.s == 0.f;  // every logit -inf: no distribution
+  logp[row] = none ? -INFINITY : (xt - a.m) * c * LN2 - ls;
+  if (ent) ent[row] = none ? 0.f : ls - a.w / a.s * LN2;
+  if (stats) {
+    stats[2 * row] = none ? -INFINITY : a.m;
+    stats[2 * row + 1] = none ? 0.f : ls;
+  }
+}
+__device__ __forceinline__ void row_ignored(int64_t row, float* logp, float* ent, float* stats) {
+  logp[row] = 0.f;
+  if (ent) ent[row] = 0.f;
+  if (stats) stats[2 * row] = 0.f, stats[2 * row + 1] = 0.f;
+}
+
+// One row (or one of nsplit equal parts of it) per group of NT threads of a block; a block holds RPB groups.
+template <typename T, int NT, int RPB>
+__global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
+                                                         const int32_t* __restrict__ tg, float c, int nsplit, int per,
+                                                         Part* __restrict__ parts, float* __restrict__ logp,
+                                                         float* __restrict__ ent, float* __restrict__ stats) {
+  constexpr int NW = NT / WAVE, U = 4;
+  static_assert(NW == 1 || RPB == 1, "groups of one wave, or one group per block");
+  __shared__ Part sm[NW];
+  const int tid = threadIdx.x % NT;
+  const int64_t items = rows * nsplit;
+  for (int64_t it = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; it < items; it += (int64_t)gridDim.x * RPB) {
+    const int64_t row = it / nsplit;
+    const int sp = (int)(it % nsplit), t = tg[row];
+    if (t < 0 || t >= V) {
+      if (nsplit == 1 && tid == 0) row_ignored(row, logp, ent, stats);
+      continue;
+    }
+    const T* z = x + row * ld + (int64_t)sp * per;
+    const int n = min(per, V - sp * per), nv = n / 8;
+    Part a = part_empty();
+    int j = tid;
+    for (; j + (U - 1) * NT < nv; j += U * NT) {
+      float v[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) Vec8<T>::load(z + (int64_t)(j + u * NT) * 8, v[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) part_add(a, v[u], c);
+    }
+    for (; j < nv; j += NT) {
+      float v[8];
+      Vec8<T>::load(z + (int64_t)j * 8, v);
+      part_add(a, v, c);
+    }
+    if (tid < n - nv * 8) {
+      const float v[1] = {to_f32(z[nv * 8 + tid])};
+      part_add(a, v, c);
+    }
+    part_lanes<WAVE>(a, c);
+    if constexpr (NW > 1) {
+      __syncthreads();  // the row before has been read
+      if (tid % WAVE == 0) sm[tid / WAVE] = a;
+      __syncthreads();
+      if (tid < WAVE) {
+        a = tid < NW ? sm[tid] : part_empty();
+        part_lanes<WAVE>(a, c);
+      }
+    }
+    if (tid == 0) {
+      if (nsplit > 1) parts[it] = a;
+      else row_finish(a, to_f32(x[row * ld + t]), c, row, logp, ent, stats);
+    }
+  }
+}
+
+// Joins the nsplit <= 64 parts of every row, a wave per row.
+template <typename T>
+__global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
+                                                    const int32_t* __restrict__ tg, float c, int nsplit,
+                                                    const Part* __restrict__ parts, float* __restrict__ logp,
+                                                    float* __restrict__ ent, float* __restrict__ stats) {
+  const int lane = threadIdx.x % WAVE;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE; row < rows; row += (int64_t)gridDim.x * 4) {
+    const int t = tg[row];
+    if (t < 0 || t >= V) {
+      if (lane == 0) row_ignored(row, logp, ent, stats);
+      continue;
+    }
+    Part a = lane < nsplit ? parts[row * nsplit + lane] : part_empty();
+    part_lanes<WAVE>(a, c);
+    if (lane == 0) row_finish(a, to_f32(x[row * ld + t]), c, row, logp, ent, stats);
+  }
+}
+
+// The gradient, element by element: a wave takes U x 512 consecutive logits of a row.  A row without a
+// target, without a distribution or with zero upstream gradients gets zeros and is not read.  zero_to > V:
+// the columns [V, zero_to) get zeros.  dx may be x (same type and rows): a lane writes only what it has read.
+template <typename T, typename OutT>
+__global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T* x, int64_t ld,
+                                                   const int32_t* __restrict__ tg, const float* __restrict__ stats,
+                                                   const float* __restrict__ ent, const float* __restrict__ dlogp,
+                                                   const float* __restrict__ dent, float s, OutT* dx, int64_t ldo,
+                                                   int zero_to) {
+  constexpr int U = 4, CH = U * 512;
+  const int lane = threadIdx.x % WAVE, W = max(V, zero_to);
+  const int64_t per_row = (W + CH - 1) / CH, items = rows * per_row;
+  const int64_t w0 = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  for (int64_t it = w0; it < items; it += (int64_t)gridDim.x * 4) {
+    const int64_t row = it / per_row;
+    const int j0 = (int)(it % per_row) * CH;
+    const int t = tg[row];
+    const float m = stats[2 * row], l2 = stats[2 * row + 1] * LOG2E, c = s * LOG2E;
+    const bool on = t >= 0 && t < V && m != -INFINITY;
+    const float g = on ? dlogp[row] * s : 0.f, h = on && dent ? dent[row] * s : 0.f, H = h != 0.f ? ent[row] : 0.f;
+    const bool zero = g == 0.f && h == 0.f;
+    const T* z = x + row * ld;
+    OutT* o = dx + row * ldo;
+    auto grad = [&](float v, int j) {
+      const float q = (v - m) * c - l2, p = __builtin_amdgcn_exp2f(q), lp = fmaxf(q, TINY_T) * LN2;
+      float d = -p * (h != 0.f ? g + h * (lp + H) : g);
+      if (j == t) d = g * -expm1f(q * LN2) - (h != 0.f ? p * h * (lp + H) : 0.f);
+      return d;
+    };
+    float v[U][8];
+    const bool whole = j0 + CH <= V;
+    if (whole && !zero) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) Vec8<T>::load(z + j0 + (u * WAVE + lane) * 8, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + (u * WAVE + lane) * 8;
+      if (j + 8 <= V) {
+        if (!whole && !zero) Vec8<T>::load(z + j, v[u]);
+        float d[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) d[q] = zero ? 0.f : grad(v[u][q], j + q);
+        Vec8<OutT>::store(o + j, d);
+      } else {
+        for (int q = 0; q < 8 && j + q < W; ++q)
+          o[j + q] = from_f32<OutT>(zero || j + q >= V ? 0.f : grad(to_f32(z[j + q]), j + q));
+      }
+    }
+  }
+}
+
+// Parts of a row: none with enough rows to fill the chip.
+int row_splits(int64_t rows, int64_t V) {
+  (void)V;
+  (void)rows;
+  return 1;
+}
+
+constexpr int64_t GRID = 1 << 20;  // blocks of a launch at most; the kernels walk their rows
+
+template <typename T>
+void logprob_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg, float s, float* logp, float* ent,
+               float* stats, void* ws, hipStream_t st) {
+  const float c = s * LOG2E;
+  const int ns = row_splits(rows, V);
+  const int per = (int)(cdiv(cdiv(V, ns), 8) * 8);
+  const T* z = (const T*)x;
+  Part* parts = (Part*)ws;
+  if (V <= 2048)
+    logprob_rows<T, 64, 4><<<(unsigned)std::min(GRID, cdiv(rows * ns, 4)), 256, 0, st>>>(
+        rows, V, z, ld, tg, c, ns, per, parts, logp, ent, stats);
+  else
+    logprob_rows<T, 256, 1><<<(unsigned)std::min(GRID, rows * ns), 256, 0, st>>>(rows, V, z, ld, tg, c, ns, per,
+                                                                                  parts, logp, ent, stats);
+  if (ns > 1)
+    logprob_join<T><<<(unsigned)std::min(GRID, cdiv(rows, 4)), 256, 0, st>>>(rows, V, z, ld, tg, c, ns, parts, logp,
+                                                                              ent, stats);
+}
+
+template <typename T, typename OutT>
+void logprob_bwd_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg, const float* stats,
+                   const float* ent, const float* dlogp, const float* dent, float s, void* dx, int64_t ldo,
+                   int zero_to, hipStream_t st) {
+  const int64_t waves = rows * cdiv(std::max(V, zero_to), 2048);
+  logprob_bwd<T, OutT><<<(unsigned)std::min(GRID, cdiv(waves, 4)), 256, 0, st>>>(
+      rows, V, (const T*)x, ld, tg, stats, ent, dlogp, dent, s, (OutT*)dx, ldo, zero_to);
+}
+
+}  // namespace
+
+size_t logprob_ws_bytes(int64_t rows, int64_t vocab) {
+  const int ns = row_splits(rows, vocab);
+  return ns > 1 ? (size_t)rows * ns * sizeof(Part) : 0;
+}
+
+void launch_logprob(bool bf, int64_t rows, int vocab, const void* logits, int64_t ld, const int32_t* targets,
+                    float inv_temp, float* logp, float* ent, float* stats, void* ws, hipStream_t st) {
+  if (rows <= 0) return;
+  if (bf) logprob_t<bf16>(rows, vocab, logits, ld, targets, inv_temp, logp, ent, stats, ws, st);
+  else logprob_t<float>(rows, vocab, logits, ld, targets, inv_temp, logp, ent, stats, ws, st);
+}
+
+void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, int64_t ld, const int32_t* targets,
+                        const float* stats, const float* ent, const float* dlogp, const float* dent, float inv_temp,
+                        bool out_bf, void* dlogits, int64_t ldo, int zero_to, hipStream_t st) {
+  if (rows <= 0) return;
+#define B_(T, O) \
+  logprob_bwd_t<T, O>(rows, vocab, logits, ld, targets, stats, ent, dlogp, dent, inv_temp, dlogits, ldo, zero_to, st)
+  if (bf && out_bf) B_(bf16, bf16);
+  else if (bf) B_(bf16, float);
+  else if (out_bf) B_(float, bf16);
+  else B_(float, float);
+#undef B_
+}
+
+// ------------------------------------------------------------------ from hidden states
+// Rows of logits that fit the workspace at once: x W^T in fp32, then their statistics.
+constexpr int64_t HEAD_CHUNK_BYTES = 256 << 20;
+static int64_t head_chunk(int64_t rows, int64_t vocab) {
+  return std::max<int64_t>(1, std::min(rows, HEAD_CHUNK_BYTES / (4 * vocab) / 256 * 256 > 0
+                                                 ? HEAD_CHUNK_BYTES / (4 * vocab) / 256 * 256
+                                                 : HEAD_CHUNK_BYTES / (4 * vocab)));
+}
+
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d) {
+  (void)bf;
+  (void)d;
+  const int64_t r = head_chunk(rows, vocab);
+  return (size_t)(r * vocab * 4 + 255) / 256 * 256 + logprob_ws_bytes(r, vocab);
+}
+
+void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
+                         int64_t ldw, const int32_t* targets, float inv_temp, float* logp, float* ent, float* stats,
+                         void* ws, hipStream_t st) {
+  const int64_t r = head_chunk(rows, vocab);
+  float* logits = (float*)ws;
+  void* parts = (char*)ws + (size_t)(r * vocab * 4 + 255) / 256 * 256;
+  for (int64_t r0 = 0; r0 < rows; r0 += r) {
+    const int64_t n = std::min(r, rows - r0);
+    GemmArgs g{};
+    g.M = (int)n; g.N = vocab; g.K = d;
+    g.A = (const char*)x + r0 * ldx * (bf ? 2 : 4); g.lda = (int)ldx; g.a_kmajor = true;
+    g.B = w; g.ldb = (int)ldw; g.b_kmajor = true;
+    g.C = logits; g.ldc = vocab; g.out_f32 = true; g.beta = 0.f;
+    launch_gemm(bf, g, st);
+    launch_logprob(false, n, vocab, logits, vocab, targets + r0, inv_temp, logp + r0, ent ? ent + r0 : nullptr,
+                   stats ? stats + 2 * r0 : nullptr, parts, st);
+  }
+}

@@ -703,6 +703,15 @@ void block_backward(stage* S, int vi, BlockAct& b, const BlockOff& w, const void
 
 }  // namespace
 
+int set_error(int code, const char* msg) {
+  try {
+    g_err = msg;
+  } catch (...) {  // no memory for the message: the code alone
+    g_err.clear();
+  }
+  return code;
+}
+
 extern "C" {
 
 const char* stage_last_error(void) { return g_err.c_str(); }

@@ -1,0 +1,443 @@
+"""Log-probability and loss operators on the GPU against the oracle in float64, at the sizes, strides and masks
+where they can go wrong.
+
+Tolerances count roundings, u = 2^-24.  With t = s (x - m) the exponent of a logit: x - m, its factor, the
+product and the hardware's 2^t err by at most 8 u (1 + |t|) of p together.  A row's sum adds n terms of one sign
+per thread (n <= V / 64 with a wave per row) and a tree: (n + 64) u.  So log S, log p and each p are
+within E = u (V / 64 + 64 + 8 |log p|) (log p absolutely, p relatively), the entropy within E (2 + 2 log V) and the
+gradient within E times the sum of the magnitudes of its terms, plus its output's rounding."""
+import numpy as np
+import pytest
+
+from gpu_common import log
+from oracle import losses as L
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _matrix(a, bf16, pad=0, lead=0):
+    """A device matrix of float64 a's values (rounded to the type), rows pad elements apart beyond their
+    width, starting lead elements into its allocation; and the values it holds."""
+    torch = _torch()
+    dt = torch.bfloat16 if bf16 else torch.float32
+    n, v = a.shape
+    buf = torch.full((lead + n * (v + pad) + 8,), float("nan"), dtype=dt, device="cuda:0")
+    m = buf[lead:lead + n * (v + pad)].view(n, v + pad)[:, :v]
+    m.copy_(torch.from_numpy(np.ascontiguousarray(a)).to(dt))
+    return m, m.double().cpu().numpy()
+
+
+def _i32(a):
+    return _torch().tensor(np.asarray(a), dtype=_torch().int32, device="cuda:0")
+
+
+def _f32(a):
+    t = _torch().from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to("cuda:0")
+    return t, t.double().cpu().numpy()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _err(V, logp):
+    return U * (V / 64 + 64 + 8 * np.abs(logp))
+
+
+def _check_rows(got, ref, V):
+    """got: LogProb of device tensors; ref: (logp, entropy, stats) in float64."""
+    for name, g, r in zip(("logp", "entropy", "stats"), got, ref):
+        g = _np(g)
+        same = np.isfinite(g) == np.isfinite(r)
+        assert same.all(), (name, g[~same][:4], r[~same][:4])
+        np.testing.assert_array_equal(g[~np.isfinite(r)], r[~np.isfinite(r)], err_msg=name)
+    fin = np.isfinite(ref[0])
+    d = np.abs(_np(got[0])[fin] - ref[0][fin])
+    assert (d <= _err(V, ref[0][fin])).all(), ("logp", d.max())
+    spread = np.abs(ref[2][:, 1]) + 1 + np.log(V)
+    d = np.abs(_np(got[1]) - ref[1])
+    assert (d <= 2 * _err(V, 0.0) * spread)[np.isfinite(ref[1])].all(), ("entropy", np.nanmax(d))
+    np.testing.assert_array_equal(_np(got[2])[:, 0], ref[2][:, 0])  # a maximum is exact
+    d = np.abs(_np(got[2])[:, 1] - ref[2][:, 1])
+    assert (d <= _err(V, 0.0)).all(), ("log sum", d.max())
+
+
+def _logits(r, n, v, scale=3.0):
+    x = r.normal(size=(n, v)) * scale
+    t = r.integers(0, v, size=n)
+    x[np.arange(n), t] += r.uniform(0, 12, size=n)
+    if n > 3:
+        t[1], t[n - 1] = -1, v
+    return x, t
+
+
+SHAPES = [(1, 1), (3, 2), (5, 7), (6, 8), (4, 63), (5, 64), (9, 65), (70, 513), (4, 2047), (5, 2049), (4, 4104),
+          (3, 16387), (300, 1111), (2, 32001), (1, 128256), (257, 9001)]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,v", SHAPES)
+def test_token_logprob_and_gradient(n, v, bf16):
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n * 1000003 + v)
+    x, t = _logits(r, n, v)
+    for pad, lead, s in ((0, 0, 1.0), (5, 3, 1.75)):
+        log(f"rows {n} vocab {v} bf16 {bf16} pad {pad} lead {lead} scale {s}")
+        m, xv = _matrix(x, bf16, pad, lead)
+        got = losses.token_logprob(m, _i32(t), inv_temperature=s)
+        ref = L.token_logprob(xv, t, s)
+        _check_rows(got, ref, v)
+        g, gv = _f32(r.normal(size=n) * 1e-2)
+        h, hv = _f32(r.normal(size=n) * 1e-3)
+        g[n // 2], gv[n // 2] = 0.0, 0.0
+        for out in ("f32", "bf16"):
+            for dent in (False, True):
+                o = torch.full((n, v + 3), 7.0, dtype=torch.float32 if out == "f32" else torch.bfloat16, device="cuda:0")
+                losses.token_logprob_backward(m, _i32(t), got, g, h if dent else None, inv_temperature=s, out=o[:, :v])
+                want = L.token_logprob_bwd(xv, t, s, gv, hv if dent else None)
+                lp = np.log(np.maximum(np.exp(s * (xv - xv.max(1, keepdims=True))), 1e-300))
+                lp = lp - np.log(np.exp(lp).sum(1, keepdims=True))
+                p = np.exp(lp)
+                hh = np.abs(hv)[:, None] if dent else 0.0
+                mag = p * (np.abs(gv)[:, None] + hh * (np.abs(lp) + 2 + 2 * np.log(v)))
+                tol = s * _err(v, lp) * mag + np.abs(want) * (HALF_STEP[out] + 8 * U) + 1e-37
+                d = np.abs(_np(o[:, :v]) - want)
+                assert (d <= tol).all(), (out, dent, (d - tol).max(), d.max())
+                assert (o[:, v:] == 7).all()  # the columns past the vocabulary
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("v", [5, 100, 2500, 40007])
+def test_rows_of_masks_and_nonfinite_values(v, bf16):
+    """-inf and the type's lowest value as masks, rows that are nothing else, +inf and NaN."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(v)
+    lowest = float(torch.finfo(torch.bfloat16 if bf16 else torch.float32).min)
+    n = 9
+    x, _ = _logits(r, n, v)
+    t = r.integers(0, v, size=n)
+    x[0, :] = -np.inf                                   # nothing left
+    x[1, :] = -np.inf; x[1, v // 2] = 3.0; t[1] = v // 2  # one token left
+    x[2, :] = lowest                                    # uniform
+    x[3, :] = lowest; x[3, 0] = 1.0; t[3] = 0
+    x[4, t[4]] = -np.inf                                # the target cannot occur
+    x[5, 0] = np.inf
+    x[6, v - 1] = np.nan
+    x[7, ::2] = -np.inf; t[7] = 1
+    x[8] += 30000.0                                     # large logits
+    for s in (1.0, 2.0):
+        m, xv = _matrix(x, bf16)
+        got = losses.token_logprob(m, _i32(t), inv_temperature=s)
+        ref = L.token_logprob(xv, t, s)
+        for k in (5, 6):
+            assert np.isnan(_np(got.logp)[k]) and np.isnan(_np(got.entropy)[k])
+        keep = [0, 1, 2, 3, 4, 7, 8]
+        _check_rows([a[keep] for a in got], [a[keep] for a in ref], v)
+        g, gv = _f32(np.full(n, 0.5))
+        h, hv = _f32(np.full(n, -0.25))
+        out = _np(losses.token_logprob_backward(m, _i32(t), got, g, h, inv_temperature=s,
+                                                out=torch.empty(n, v, dtype=torch.float32, device="cuda:0")))
+        assert np.isnan(out[5]).any() and np.isnan(out[6]).any() and not out[0].any()
+        want = L.token_logprob_bwd(xv, t, s, gv, hv)
+        tol = 4 * s * U * (v / 64 + 64 + 100) * (3 + 2 * np.log(v)) + np.zeros_like(want)
+        assert (np.abs(out - want) <= tol)[keep].all()
+        # rows with no gradient, and ignored ones, are zeros whatever they hold
+        zero = torch.zeros(n, device="cuda:0")
+        none = losses.token_logprob_backward(m, _i32(t), got, zero, None, inv_temperature=s)
+        assert (none == 0).all()
+        gone = losses.token_logprob(m, _i32(np.full(n, -7)), inv_temperature=s)
+        assert all((a == 0).all() for a in gone)
+        assert (losses.token_logprob_backward(m, _i32(np.full(n, v)), gone, g, h, inv_temperature=s) == 0).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_gradient_in_place(bf16):
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(5)
+    x, t = _logits(r, 33, 5003)
+    m, _ = _matrix(x, bf16, pad=2)
+    fwd = losses.token_logprob(m, _i32(t))
+    g, _ = _f32(r.normal(size=33))
+    apart = losses.token_logprob_backward(m, _i32(t), fwd, g)
+    losses.token_logprob_backward(m, _i32(t), fwd, g, out=m)
+    assert (m == apart).all()
+
+
+def test_a_row_past_32_bits():
+    """Rows whose offsets pass 2^31 elements, at both ends of a tall matrix."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    n, v = 70000, 32768
+    x = torch.zeros(n, v, dtype=torch.bfloat16, device="cuda:0")
+    t = torch.full((n,), -1, dtype=torch.int32, device="cuda:0")
+    r = np.random.default_rng(8)
+    rows = [0, n // 2, n - 1]
+    vals = r.normal(size=(3, v)) * 2
+    for k, row in enumerate(rows):
+        x[row] = torch.from_numpy(vals[k]).to(torch.bfloat16)
+        t[row] = 17 + k
+    xv, tv = _np(x[rows]), np.array([17, 18, 19])
+    got = losses.token_logprob(x, t)
+    _check_rows([a[rows] for a in got], L.token_logprob(xv, tv, 1.0), v)
+    assert int((got.logp != 0).sum()) == 3
+    g = torch.ones(n, device="cuda:0")
+    losses.token_logprob_backward(x, t, got, g, out=x)
+    want = L.token_logprob_bwd(xv, tv, 1.0, np.ones(3))
+    assert (np.abs(_np(x[rows]) - want) <= np.abs(want) * (2.0 ** -8 + 1e-4) + 1e-7).all()
+    assert int((x != 0).any(1).sum()) == 3
+
+
+# ------------------------------------------------------------------ from hidden states
+def _head_tol(d, x, w, s):
+    """Bound on a logit's error times s: the products of both types are exact in fp32 or round once, the sum
+    of d of them errs by at most (d + 2) u of the sum of their magnitudes."""
+    return s * U * (d + 2) * float((np.abs(x) @ np.abs(w).T).max())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (1, 300, 64), (2, 128, 72), (5, 1000, 64), (17, 129, 8), (33, 4097, 256),
+                                   (64, 2048, 520), (129, 1111, 136), (130, 257, 33), (300, 777, 1000), (1, 40001, 512),
+                                   (256, 512, 128)])
+def test_head_logprob(n, v, d, bf16):
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n * 7919 + v + d)
+    x, w = r.normal(size=(n, d)), r.normal(size=(v, d)) * (3 / np.sqrt(d))
+    t = r.integers(0, v, size=n)
+    if n > 3:
+        t[2], t[n - 1] = -1, v
+    for padx, padw, lead, s in ((0, 0, 0, 1.0), (8, 16, 8, 1.5), (3, 1, 1, 0.75)):
+        log(f"rows {n} vocab {v} d {d} bf16 {bf16} pads {padx} {padw} lead {lead} scale {s}")
+        mx, xv = _matrix(x, bf16, padx, lead)
+        mw, wv = _matrix(w, bf16, padw, lead)
+        got = losses.head_logprob(mx, mw, _i32(t), inv_temperature=s)
+        ref = L.token_logprob(xv @ wv.T, t, s)
+        e = _head_tol(d, xv, wv, s)
+        live = (t >= 0) & (t < v)
+        assert (np.abs(_np(got.logp) - ref[0]) <= 2 * e + _err(v, ref[0])).all()
+        assert (np.abs(_np(got.stats)[:, 0] - ref[2][:, 0]) <= e / s).all()
+        assert (np.abs(_np(got.stats)[:, 1] - ref[2][:, 1]) <= 2 * e + _err(v, 0.0)).all()
+        spread = np.abs(ref[2][:, 1]) + 1 + np.log(v)
+        assert (np.abs(_np(got.entropy) - ref[1]) <= (2 * e + 2 * _err(v, 0.0)) * 2 * spread).all()
+        assert not _np(got.logp)[~live].any() and not _np(got.stats)[~live].any()
+
+
+# ------------------------------------------------------------------ losses
+def _close(name, got, want, rel, floor=0.0):
+    d = np.abs(_np(got) - want)
+    tol = rel * np.abs(want) + floor
+    assert (d <= tol).all(), (name, float((d - tol).max()), float(d.max()))
+
+
+def _answers(r, b, s, empty=()):
+    start = r.integers(0, max(1, s // 2), size=(b, 1))
+    stop = start + 1 + (r.random((b, 1)) * (s - start)).astype(int)
+    k = np.arange(s)[None]
+    on = (k >= start) & (k < stop) & (r.random((b, s)) < 0.9)
+    for e in empty:
+        if e < b:
+            on[e] = False
+    return on
+
+
+GRIDS = [(1, 1), (1, 3), (2, 1), (3, 5), (4, 64), (8, 1024), (37, 111), (1025, 3), (5000, 1), (2, 40001), (1, 20000),
+         (600, 66), (130, 127), (9, 4096)]
+
+
+@pytest.mark.parametrize("reduction", ["token", "sequence"])
+@pytest.mark.parametrize("b,s", GRIDS)
+def test_policy_loss(b, s, reduction):
+    """The gradients' terms: e^x and e^d - 1 within 2 u plus the rounding of their arguments, u |x|; three products
+    and a sum: 8 u of the terms' magnitudes for |x| <= 2.  The sums are in double over such terms."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(b * 31 + s)
+    for empty, ref_on, ent_on, per_token, norm, gs in (((0, 2), True, True, True, 0.0, 1.0), ((), False, False, False, 0.0, 0.5),
+                                                       ((1,), True, False, False, 77.0, 1.0), ((), False, True, True, 0.0, 1.0)):
+        log(f"sequences {b} length {s} {reduction} ref {ref_on} entropy {ent_on} per token {per_token} norm {norm}")
+        on = _answers(r, b, s, empty)
+        lp = -np.abs(r.normal(size=(b, s)))
+        old, ref, ent = lp + 0.2 * r.normal(size=(b, s)), lp + 0.3 * r.normal(size=(b, s)), np.abs(lp) * 0.7
+        adv = r.normal(size=(b, s) if per_token else (b,))
+        for a in (lp, old, ref, ent) + ((adv,) if per_token else ()):
+            a[~on] = r.choice([np.nan, np.inf, -np.inf, 3e38], size=int((~on).sum()))  # anything may stand there
+        T = {k: _f32(a) for k, a in dict(lp=lp, old=old, ref=ref, ent=ent, adv=adv).items()}
+        kw = dict(clip_low=0.125, clip_high=0.25, kl_coef=0.5 if ref_on else 0.0, entropy_coef=0.25 if ent_on else 0.0,
+                  reduction=reduction, norm=norm, grad_scale=gs)
+        mask = torch.from_numpy(on).to("cuda:0")
+        got = losses.policy_loss(T["lp"][0], T["old"][0], T["adv"][0], mask, ref_logp=T["ref"][0] if ref_on else None,
+                                 entropy=T["ent"][0] if ent_on else None, **kw)
+        want = L.policy_loss(T["lp"][1], T["old"][1], T["adv"][1], on, ref=T["ref"][1] if ref_on else None,
+                             entropy=T["ent"][1] if ent_on else None, **kw)
+        w = np.abs(want["dlogp"]).max() if on.any() else 0.0
+        _close("dlogp", got.dlogp, want["dlogp"], 16 * U, 16 * U * w)
+        if ent_on:
+            _close("dentropy", got.dentropy, want["dentropy"], 4 * U)
+        else:
+            assert got.dentropy is None
+        big = np.abs(want["metrics"]).max() + 1
+        _close("metrics", got.metrics, want["metrics"], 16 * U, 4 * U * big * 4)
+        _close("loss", got.loss, np.array([want["loss"]]), 16 * U, 16 * U * big)
+        assert got.counts.tolist() == want["counts"].tolist()
+        again = losses.policy_loss(T["lp"][0], T["old"][0], T["adv"][0], mask.view(torch.uint8) * 200,
+                                   ref_logp=T["ref"][0] if ref_on else None, entropy=T["ent"][0] if ent_on else None, **kw)
+        assert all(x is y is None or torch.equal(x, y) for x, y in zip(got, again))
+
+
+def test_policy_loss_at_the_clip():
+    """Tokens a rounding away from the clip on either side, and far ratios: the side is that of the exact
+    difference of the two log-probabilities."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    hi, lo = np.float32(0.25), np.float32(0.125)
+    edge = np.float32(np.log1p(float(hi)))
+    low = np.float32(np.log1p(-float(lo)))
+    x = np.array([[np.nextafter(edge, np.float32(-9)), edge, np.nextafter(edge, np.float32(9)),
+                   np.nextafter(low, np.float32(-9)), low, np.nextafter(low, np.float32(9)), 60.0, -60.0]], np.float32)
+    for a in (1.5, -1.5, 0.0):
+        lp, lpv = _f32(x)
+        old, oldv = _f32(np.zeros_like(x))
+        adv, advv = _f32(np.array([a]))
+        on = np.ones(x.shape, bool)
+        kw = dict(clip_low=float(lo), clip_high=float(hi))
+        got = losses.policy_loss(lp, old, adv, torch.from_numpy(on).to("cuda:0"), **kw)
+        want = L.policy_loss(lpv, oldv, advv, on, **kw)
+        assert ((_np(got.dlogp) == 0) == (want["dlogp"] == 0)).all()
+        # e^60: the argument is exact, the exponential within 2 u, two products
+        _close("dlogp", got.dlogp, want["dlogp"], 8 * U)
+        _close("metrics", got.metrics, want["metrics"], 16 * U, 1e-6)
+
+
+@pytest.mark.parametrize("kind,smoothing,normalize", [("sigmoid", 0.0, False), ("sigmoid", 0.25, True), ("hinge", 0.0, True),
+                                                      ("square", 0.0, False)])
+@pytest.mark.parametrize("p,s", [(1, 1), (1, 7), (2, 100), (3, 4), (32, 128), (33, 129), (256, 5), (300, 40), (1, 50001),
+                                 (5, 9999), (2000, 3)])
+def test_preference_loss(p, s, kind, smoothing, normalize):
+    """Scores are sums in double of exact differences; every output is one rounding of a double, 2 u with the scale's."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(p * 17 + s)
+    for ref_on, norm, gs, empty in ((True, 0.0, 1.0, (1,)), (False, 12.0, 0.5, (0, p + 2))):
+        log(f"pairs {p} length {s} {kind} smoothing {smoothing} normalize {normalize} ref {ref_on} norm {norm}")
+        on = _answers(r, 2 * p, s, empty)
+        lp = -np.abs(r.normal(size=(2 * p, s)))
+        ref = lp + 0.3 * r.normal(size=(2 * p, s))
+        for a in (lp, ref):
+            a[~on] = r.choice([np.nan, np.inf, -np.inf], size=int((~on).sum()))
+        lp, lpv = _f32(lp)
+        ref, refv = _f32(ref)
+        kw = dict(kind=kind, beta=0.25, label_smoothing=smoothing, margin=0.125, length_normalize=normalize, norm=norm,
+                  grad_scale=gs)
+        mask = torch.from_numpy(on).to("cuda:0")
+        got = losses.preference_loss(lp, mask, ref_logp=ref if ref_on else None, **kw)
+        want = L.preference_loss(lpv, on, ref=refv if ref_on else None, **kw)
+        for name in ("dlogp", "pair_loss", "rewards", "metrics"):
+            floor = 1e-12 * (1 + np.abs(want[name]).max())  # double sums of s terms in another order
+            _close(name, getattr(got, name), want[name], 2 * U, floor)
+        _close("loss", got.loss, np.array([want["loss"]]), 2 * U, 1e-12)
+        assert got.counts.tolist() == want["counts"].tolist()
+        again = losses.preference_loss(lp, mask, ref_logp=ref if ref_on else None, **kw)
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+def test_no_tokens():
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    for b, s in ((0, 0), (0, 5), (2, 0), (6, 40), (2000, 20), (3000, 0)):
+        z = torch.full((b, s), float("nan"), device="cuda:0")
+        off = torch.zeros(b, s, dtype=torch.bool, device="cuda:0")
+        out = losses.policy_loss(z, z, torch.ones(b, device="cuda:0"), off, ref_logp=z, kl_coef=0.5)
+        assert float(out.loss) == 0 and not out.dlogp.any() and not out.metrics.any() and out.counts.tolist() == [0, 0]
+        out = losses.preference_loss(z, off, ref_logp=z)
+        assert float(out.loss) == 0 and not out.dlogp.any() and not out.pair_loss.any() and not out.rewards.any()
+        assert not out.metrics.any() and out.counts.tolist() == [0]
+
+
+# ------------------------------------------------------------------ together
+def _chain(losses, x, w, t, old, ref, adv, mask, ws):
+    """One step as a training loop makes it, on given buffers: the reference's log-probabilities from the
+    hidden states, the policy's from its logits, the loss, the gradient in the logits."""
+    B, S = mask.shape
+    out = {}
+    out["ref"] = losses.head_logprob(x, w, t, out=ws["ref"], workspace=ws["head"])
+    out["lp"] = losses.token_logprob(ws["logits"], t, out=ws["lp"], workspace=ws["rows"])
+    out["loss"] = losses.policy_loss(out["lp"].logp.view(B, S), old, adv, mask, ref_logp=out["ref"].logp.view(B, S),
+                                     entropy=out["lp"].entropy.view(B, S), kl_coef=0.125, entropy_coef=0.01,
+                                     out=ws["loss"], workspace=ws["policy"])
+    out["grad"] = losses.token_logprob_backward(ws["logits"], t, out["lp"], out["loss"].dlogp.view(-1),
+                                                out["loss"].dentropy.view(-1), out=ws["grad"])
+    out["pref"] = losses.preference_loss(out["lp"].logp.view(B, S), mask, ref_logp=out["ref"].logp.view(B, S),
+                                         out=ws["pref"], workspace=ws["preference"])
+    return out
+
+
+def _chain_buffers(losses, B, S, V, d, x, w):
+    torch = _torch()
+    from paper_2606_30634_amd import binding as Bd
+    n = B * S
+    f = lambda *s: torch.empty(*s, device="cuda:0")  # noqa: E731
+    u = lambda k: torch.empty(max(k, 1), dtype=torch.uint8, device="cuda:0")  # noqa: E731
+    i = lambda k: torch.empty(k, dtype=torch.int64, device="cuda:0")  # noqa: E731
+    return dict(logits=(x.float() @ w.float().t()) * 1.01, ref=losses.LogProb(f(n), f(n), f(n, 2)),
+                lp=losses.LogProb(f(n), f(n), f(n, 2)), loss=losses.PolicyLoss(f(1), f(B, S), f(B, S), f(6), i(2)),
+                pref=losses.PreferenceLoss(f(1), f(B, S), f(B // 2), f(B), f(4), i(1)),
+                grad=torch.empty(n, V, dtype=torch.bfloat16, device="cuda:0"),
+                head=u(Bd.head_logprob_workspace_bytes(n, V, d, True)), rows=u(Bd.token_logprob_workspace_bytes(n, V)),
+                policy=u(Bd.policy_loss_workspace_bytes(B, S)), preference=u(Bd.preference_loss_workspace_bytes(B // 2, S)))
+
+
+def _leaves(out):
+    for v in out.values():
+        for a in (v if isinstance(v, tuple) else (v,)):
+            yield a
+
+
+@pytest.mark.parametrize("B,S,V,d", [(4, 33, 1003, 128), (24, 512, 600, 64), (2, 1, 70001, 64)])
+def test_captured_chain(B, S, V, d):
+    """The operators captured as one graph and replayed on new inputs, with eager work between the
+    replays, against the eager results bit for bit; and a second stream beside the first."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda:0")  # noqa: E731
+    x, w = rnd(B * S, d).bfloat16(), (rnd(V, d) * (3 / d ** 0.5)).bfloat16()
+    t = torch.randint(-1, V, (B * S,), generator=g, device="cuda:0", dtype=torch.int32)
+    old, ref, adv = -rnd(B, S).abs(), None, rnd(B)
+    mask = torch.rand(B, S, generator=g, device="cuda:0") < 0.7
+    ws = _chain_buffers(losses, B, S, V, d, x, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _chain(losses, x, w, t, old, ref, adv, mask, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _chain(losses, x, w, t, old, ref, adv, mask, ws)
+    for k in range(4):
+        x.copy_(rnd(B * S, d))
+        ws["logits"].copy_(rnd(B * S, V) * 2)
+        t.copy_(torch.randint(-1, V, (B * S,), generator=g, device="cuda:0", dtype=torch.int32))
+        old.copy_(-rnd(B, S).abs())
+        mask.copy_(torch.rand(B, S, generator=g, device="cuda:0") < 0.5)
+        for a in _leaves(out):
+            a.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [a.clone() for a in _leaves(out)]
+        # the eager step on another stream with its own workspaces
+        ws2 = _chain_buffers(losses, B, S, V, d, x, w)
+        ws2["logits"].copy_(ws["logits"])
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            eager = _chain(losses, x, w, t, old, ref, adv, mask, ws2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, _leaves(eager))), k

@@ -190,6 +190,30 @@ int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
 int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out,
                    int32_t microbatches_per_step);
 
+/* The last stage under a loss on the log-probabilities of its targets instead of the mean cross-entropy
+ * (reward or preference fine-tuning; the losses are policy_loss and preference_loss below).
+ * stage_forward_logprob is stage_forward up to the logits, then
+ *   logp     [micro_batch, seq_len] fp32, device: log-probability of each target at inv_temperature > 0
+ *            (token_logprob's rules; a target outside [0, vocab) is ignored: 0)
+ *   entropy  the same shape, or NULL
+ * and leaves the slot pending for stage_backward_logprob, which takes
+ *   dlogp, dentropy  [micro_batch, seq_len] fp32, device: the loss's gradients (dentropy may be NULL), with
+ *            whatever scale the caller's loss has; microbatches_per_step only places the chunks of overlap
+ *            mode 2
+ * and otherwise is stage_backward.  The two kinds of forward and backward do not mix on one slot
+ * (STAGE_ESTATE). */
+int stage_forward_logprob(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
+                          const int32_t* targets, float inv_temperature, float* logp, float* entropy);
+int stage_backward_logprob(stage_t* s, int32_t slot, const float* dlogp, const float* dentropy, void* dx_out,
+                           int32_t microbatches_per_step);
+
+/* The log-probabilities of stage_forward_logprob without a backward to follow (a reference policy, or the
+ * policy an answer was sampled from): the logits are never all in memory (head_logprob).  `slot` must
+ * hold no pending microbatch; its activations are overwritten and it stays free.  In the delayed update's
+ * order this is a use of the weights of `step` like any forward. */
+int stage_score_logprob(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
+                        const int32_t* targets, float inv_temperature, float* logp, float* entropy);
+
 /* Second half of iteration t of Alg. 1: with delay tau >= 1 consume g_{t-tau} (the gradient of
  * step t-tau, complete), with delay 0 consume g_t; clip by the global norm; AdamW (or Muon);
  * standard or lambda-EF update of the master weights (EF once tau earlier updates exist: the

@@ -21,7 +21,8 @@ EXPORTS = ["stage_required_bytes", "stage_init", "stage_num_tensors", "stage_ten
            "grad_norm_flat_workspace_bytes", "grad_norm_flat", "hbm_stream_copy", "delayed_update_flat_adan",
            "grad_norm_flat_noalloc", "token_logprob_workspace_bytes", "token_logprob", "token_logprob_backward",
            "head_logprob_workspace_bytes", "head_logprob", "policy_loss_workspace_bytes", "policy_loss",
-           "preference_loss_workspace_bytes", "preference_loss"]
+           "preference_loss_workspace_bytes", "preference_loss", "stage_forward_logprob", "stage_backward_logprob",
+           "stage_score_logprob"]
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_UPDATE, PROF_NORM, PROF_OTHER, PROF_NS = range(7)
 
 
@@ -77,6 +78,9 @@ def _load():
         "stage_sync_weights": (C.c_int, [vp]),
         "stage_forward": (C.c_int, [vp, i32, i64, vp, vp, vp, vp, vp]),
         "stage_backward": (C.c_int, [vp, i32, vp, vp, i32]),
+        "stage_forward_logprob": (C.c_int, [vp, i32, i64, vp, vp, vp, C.c_float, vp, vp]),
+        "stage_backward_logprob": (C.c_int, [vp, i32, vp, vp, vp, i32]),
+        "stage_score_logprob": (C.c_int, [vp, i32, i64, vp, vp, vp, C.c_float, vp, vp]),
         "delayed_update": (C.c_int, [vp, i64, C.POINTER(UpdateHParams)]),
         "delayed_update_flat": (C.c_int, [i64, vp, vp, i32, vp, vp, vp, vp, i32, i64,
                                           C.POINTER(UpdateHParams), vp, vp]),
@@ -171,6 +175,20 @@ def stage_forward(s: int, slot: int, step: int, tokens=None, x_in=None, targets=
 
 def stage_backward(s: int, slot: int, dy=None, dx_out=None, microbatches_per_step: int = 1) -> None:
     _call("stage_backward", s, slot, dy, dx_out, microbatches_per_step)
+
+
+def stage_forward_logprob(s: int, slot: int, step: int, tokens, x_in, targets, inv_temperature: float, logp,
+                          entropy=None) -> None:
+    _call("stage_forward_logprob", s, slot, step, tokens, x_in, targets, inv_temperature, logp, entropy)
+
+
+def stage_backward_logprob(s: int, slot: int, dlogp, dentropy=None, dx_out=None, microbatches_per_step: int = 1) -> None:
+    _call("stage_backward_logprob", s, slot, dlogp, dentropy, dx_out, microbatches_per_step)
+
+
+def stage_score_logprob(s: int, slot: int, step: int, tokens, x_in, targets, inv_temperature: float, logp,
+                        entropy=None) -> None:
+    _call("stage_score_logprob", s, slot, step, tokens, x_in, targets, inv_temperature, logp, entropy)
 
 
 def delayed_update(s: int, t: int, hp: UpdateHParams) -> None:

@@ -54,6 +54,11 @@ struct Slot {
   void* y;          // output of the last block [T, d]
   void *hf;         // final norm output (last stage)
   float *rstdf, *logits, *lse_ce;  // head: final-norm statistics, fp32 logits, their row lse
+  // head under a loss on log-probabilities: the rows' maxima and log-sums, their entropies, and whether
+  // the pending forward was one (at which inverse temperature)
+  float *lp_stats, *lp_ent;
+  bool lp = false;
+  float inv_temp = 1.f;
   int32_t *tokens, *targets;
   // first stage: the microbatch's positions sorted by token (stable) and the start of each token's
   // run, sorted at forward time on the weight-gradient stream (the tokens are known then); the
@@ -143,6 +148,7 @@ struct stage {
   // scratch
   void *dA, *dB, *dh, *dn, *dgu, *do_, *dqkv, *dlog, *dhf;
   float *delta, *rms_part, *row_loss, *cos_t, *sin_t, *norm_out, *upd_norm_out;
+  void* lp_ws = nullptr;  // workspace of the log-probabilities' rows
   double *norm_part, *upd_norm_part;
   float* gemm_ws;
   float* act_ws;  // split-K partials of the [T, d_model] activation products (null: none are split)
@@ -395,8 +401,13 @@ size_t layout(stage* S, char* base) {
     sl.targets = sh.last_stage ? (int32_t*)carve(T * 4) : nullptr;
     sl.hf = sh.last_stage ? carve(T * d * esz) : nullptr;
     sl.rstdf = sh.last_stage ? (float*)carve(T * 4) : nullptr;
-    sl.logits = sh.last_stage ? (float*)carve(T * (int64_t)sh.vocab * 4) : nullptr;
+    // scoring takes the logits' memory for its workspace
+    sl.logits = sh.last_stage ? (float*)carve(std::max<int64_t>(T * (int64_t)sh.vocab * 4,
+                                                                (int64_t)head_logprob_ws_bytes(sh.dtype == 1, T, sh.vocab, d)))
+                              : nullptr;
     sl.lse_ce = sh.last_stage ? (float*)carve(T * 4) : nullptr;
+    sl.lp_stats = sh.last_stage ? (float*)carve(T * 8) : nullptr;
+    sl.lp_ent = sh.last_stage ? (float*)carve(T * 4) : nullptr;
   }
   // scratch shared by all calls
   S->dA = carve(T * d * esz);
@@ -432,6 +443,8 @@ size_t layout(stage* S, char* base) {
   S->dlog = sh.last_stage ? carve(T * S->lddlog * esz) : nullptr;
   S->dhf = sh.last_stage ? carve(T * d * esz) : nullptr;
   S->row_loss = sh.last_stage ? (float*)carve(T * 4) : nullptr;
+  const size_t lp_ws = sh.last_stage ? logprob_ws_bytes(T, sh.vocab) : 0;
+  S->lp_ws = lp_ws ? carve((int64_t)lp_ws) : nullptr;
   // Muon: every block's wq, wk, wv, wo, wgate, wup, wdown; a group per wide-orientation shape
   // (m = min(rows, cols) <= n) holds the matrices' fp32 Newton-Schulz iterates [m, n] (ping-pong
   // on the fp32 stage; on the bf16 stage one, plus the bf16 hi/lo operand form [m, 2n]: ping-pong
@@ -861,8 +874,12 @@ int stage_sync_weights(stage_t* s) {
   return STAGE_OK;
 }
 
-int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
-                  const int32_t* targets, void* y_out, float* loss_dev) {
+}  // extern "C"
+
+namespace {
+
+// What every forward asks of its stage, slot, step and inputs
+int check_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in) {
   if (!s) return fail(STAGE_EINVAL, "null stage");
   const stage_shape_t& sh = s->sh;
   if (slot < 0 || slot >= sh.max_inflight) return fail(STAGE_EINVAL, "slot out of range");
@@ -870,10 +887,21 @@ int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
     return fail(STAGE_ESTATE, "weights of step " + std::to_string(step) + " are not resident");
   if (sh.first_stage && !tokens) return fail(STAGE_EINVAL, "first stage needs tokens");
   if (!sh.first_stage && !x_in) return fail(STAGE_EINVAL, "non-first stage needs x_in");
-  if (sh.last_stage && (!targets || !loss_dev)) return fail(STAGE_EINVAL, "last stage needs targets and loss_dev");
-  Slot& sl = s->slots[slot];
-  if (sl.pending) return fail(STAGE_ESTATE, "slot holds a microbatch whose backward is pending");
-  const int vi = (int)(step % 2);
+  return STAGE_OK;
+}
+
+int check_logprob(stage_t* s, const int32_t* targets, float inv_temperature, const float* logp) {
+  if (!s->sh.last_stage) return fail(STAGE_EINVAL, "log-probabilities need a last stage");
+  if (!targets || !logp) return fail(STAGE_EINVAL, "null targets or logp");
+  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature))
+    return fail(STAGE_EINVAL, "inv_temperature must be positive and finite");
+  return STAGE_OK;
+}
+
+// The slot's input and blocks at weight version vi.  keep: a backward follows (a first stage's
+// tokens are held and sorted for the embedding gradient).
+int forward_blocks(stage_t* s, Slot& sl, int vi, const int32_t* tokens, const void* x_in, bool keep) {
+  const stage_shape_t& sh = s->sh;
   if (vi == s->pend.vout) flush_pending(s);  // the deferred pass writes this version
   if (s->upd_owed_v[vi]) {
     HIP_OK(hipStreamWaitEvent(s->st, s->ev_upd_v[vi], 0));
@@ -883,8 +911,12 @@ int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
   hipStream_t st = s->st;
   void* x0 = sh.n_blocks > 0 ? sl.blk[0].x : sl.y;
   if (sh.first_stage) {
-    HIP_OK(hipMemcpyAsync(sl.tokens, tokens, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
-    launch_embed_gather(s->bf, sl.tokens, s->wptr(vi, s->off_embed), x0, T, d, sh.vocab, st);
+    if (keep) HIP_OK(hipMemcpyAsync(sl.tokens, tokens, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
+    launch_embed_gather(s->bf, keep ? sl.tokens : tokens, s->wptr(vi, s->off_embed), x0, T, d, sh.vocab, st);
+  } else {
+    HIP_OK(hipMemcpyAsync(x0, x_in, (size_t)T * d * s->esz, hipMemcpyDeviceToDevice, st));
+  }
+  if (sh.first_stage && keep) {
     // the embedding gradient's sort needs only the tokens: beside the forward, where there is a
     // second stream
     hipStream_t ss = s->wgrad_side ? s->wst : st;
@@ -895,36 +927,28 @@ int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
     launch_token_sort(sl.tokens, T, sh.vocab, s->sort_ws, sl.sorted_tok, sl.sorted_pos, ss);
     launch_token_runs(sl.sorted_tok, T, sh.vocab, sl.row_start, nullptr, nullptr, nullptr, ss);
     HIP_OK(hipEventRecord(sl.ev_sort, ss));
-  } else {
-    HIP_OK(hipMemcpyAsync(x0, x_in, (size_t)T * d * s->esz, hipMemcpyDeviceToDevice, st));
   }
   for (int i = 0; i < sh.n_blocks; ++i) {
     void* y = i + 1 < sh.n_blocks ? sl.blk[i + 1].x : sl.y;
     block_forward(s, vi, sl.blk[i], s->boff[i], y);
   }
-  if (sh.last_stage) {
-    HIP_OK(hipMemcpyAsync(sl.targets, targets, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
-    launch_rmsnorm_fwd(s->bf, sl.y, s->wptr(vi, s->off_final), sl.hf, sl.rstdf, T, d, sh.rms_eps, st);
-    run_gemm(s, gemm(T, sh.vocab, d, sl.hf, d, true, s->wptr(vi, s->off_head), d, true,
-                            sl.logits, sh.vocab, true, 0.f));
-    launch_ce_fwd(sl.logits, sl.targets, T, sh.vocab, sl.lse_ce, s->row_loss, st);
-    launch_mean(s->row_loss, T, loss_dev, st);
-  }
-  if (y_out && !sh.last_stage)
-    HIP_OK(hipMemcpyAsync(y_out, sl.y, (size_t)T * d * s->esz, hipMemcpyDeviceToDevice, st));
-  HIP_OK(hipGetLastError());
-  sl.step = step;
-  sl.pending = true;
   return STAGE_OK;
 }
 
-int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out, int32_t microbatches_per_step) {
-  if (!s) return fail(STAGE_EINVAL, "null stage");
+// The final norm and the fp32 logits of the slot's last activations
+void head_logits(stage_t* s, Slot& sl, int vi) {
   const stage_shape_t& sh = s->sh;
-  if (slot < 0 || slot >= sh.max_inflight) return fail(STAGE_EINVAL, "slot out of range");
-  Slot& sl = s->slots[slot];
-  if (!sl.pending) return fail(STAGE_ESTATE, "slot holds no pending forward");
-  if (!sh.last_stage && !dy) return fail(STAGE_EINVAL, "non-last stage needs dy");
+  const int T = s->T, d = sh.d_model;
+  launch_rmsnorm_fwd(s->bf, sl.y, s->wptr(vi, s->off_final), sl.hf, sl.rstdf, T, d, sh.rms_eps, s->st);
+  run_gemm(s, gemm(T, sh.vocab, d, sl.hf, d, true, s->wptr(vi, s->off_head), d, true,
+                          sl.logits, sh.vocab, true, 0.f));
+}
+
+// The backward of the slot's pending forward, from dy (a stage without a head), from the mean
+// cross-entropy, or from the gradients of the log-probabilities and entropies (dlogp set).
+int backward_run(stage_t* s, Slot& sl, const void* dy, const float* dlogp, const float* dentropy, void* dx_out,
+                 int32_t microbatches_per_step) {
+  const stage_shape_t& sh = s->sh;
   if (microbatches_per_step <= 0) return fail(STAGE_EINVAL, "microbatches_per_step must be positive");
   const int64_t step = sl.step;
   const int gb = (int)(step % s->ng), vi = (int)(step % 2);
@@ -951,8 +975,12 @@ int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out, int32
   bool head_wrote_embed = false;
   s->colsums = 0;
   if (sh.last_stage) {
-    launch_ce_bwd(bf, sl.logits, sl.targets, sl.lse_ce, T, sh.vocab, 1.0f / ((float)T * microbatches_per_step),
-                  s->dlog, s->lddlog, st);
+    if (dlogp)
+      launch_logprob_bwd(false, T, sh.vocab, sl.logits, sh.vocab, sl.targets, sl.lp_stats, sl.lp_ent, dlogp, dentropy,
+                         sl.inv_temp, bf, s->dlog, s->lddlog, (int)s->lddlog, st);
+    else
+      launch_ce_bwd(bf, sl.logits, sl.targets, sl.lse_ce, T, sh.vocab, 1.0f / ((float)T * microbatches_per_step),
+                    s->dlog, s->lddlog, st);
     // dhf = dlogits W ; dW (+)= dlogits^T hf   (W the head matrix, or the tied embedding)
     GemmArgs gd = gemm(T, d, sh.vocab, s->dlog, s->lddlog, true, s->wptr(vi, s->off_head), d, false, s->dhf, d);
     gd.a_padded = true;
@@ -992,6 +1020,100 @@ int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out, int32
   s->grad_count[gb] += 1;
   sl.pending = false;
   return STAGE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
+                  const int32_t* targets, void* y_out, float* loss_dev) {
+  if (int rc = check_forward(s, slot, step, tokens, x_in)) return rc;
+  const stage_shape_t& sh = s->sh;
+  if (sh.last_stage && (!targets || !loss_dev)) return fail(STAGE_EINVAL, "last stage needs targets and loss_dev");
+  Slot& sl = s->slots[slot];
+  if (sl.pending) return fail(STAGE_ESTATE, "slot holds a microbatch whose backward is pending");
+  const int vi = (int)(step % 2), T = s->T, d = sh.d_model;
+  hipStream_t st = s->st;
+  if (int rc = forward_blocks(s, sl, vi, tokens, x_in, true)) return rc;
+  if (sh.last_stage) {
+    HIP_OK(hipMemcpyAsync(sl.targets, targets, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
+    head_logits(s, sl, vi);
+    launch_ce_fwd(sl.logits, sl.targets, T, sh.vocab, sl.lse_ce, s->row_loss, st);
+    launch_mean(s->row_loss, T, loss_dev, st);
+  }
+  if (y_out && !sh.last_stage)
+    HIP_OK(hipMemcpyAsync(y_out, sl.y, (size_t)T * d * s->esz, hipMemcpyDeviceToDevice, st));
+  HIP_OK(hipGetLastError());
+  sl.step = step;
+  sl.pending = true;
+  sl.lp = false;
+  return STAGE_OK;
+}
+
+int stage_forward_logprob(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
+                          const int32_t* targets, float inv_temperature, float* logp, float* entropy) {
+  if (int rc = check_forward(s, slot, step, tokens, x_in)) return rc;
+  if (int rc = check_logprob(s, targets, inv_temperature, logp)) return rc;
+  Slot& sl = s->slots[slot];
+  if (sl.pending) return fail(STAGE_ESTATE, "slot holds a microbatch whose backward is pending");
+  const int vi = (int)(step % 2), T = s->T;
+  hipStream_t st = s->st;
+  if (int rc = forward_blocks(s, sl, vi, tokens, x_in, true)) return rc;
+  HIP_OK(hipMemcpyAsync(sl.targets, targets, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
+  head_logits(s, sl, vi);
+  launch_logprob(false, T, s->sh.vocab, sl.logits, s->sh.vocab, sl.targets, inv_temperature, logp, sl.lp_ent,
+                 sl.lp_stats, s->lp_ws, st);
+  if (entropy) HIP_OK(hipMemcpyAsync(entropy, sl.lp_ent, (size_t)T * 4, hipMemcpyDeviceToDevice, st));
+  HIP_OK(hipGetLastError());
+  sl.step = step;
+  sl.pending = true;
+  sl.lp = true;
+  sl.inv_temp = inv_temperature;
+  return STAGE_OK;
+}
+
+int stage_score_logprob(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
+                        const int32_t* targets, float inv_temperature, float* logp, float* entropy) {
+  if (int rc = check_forward(s, slot, step, tokens, x_in)) return rc;
+  if (int rc = check_logprob(s, targets, inv_temperature, logp)) return rc;
+  Slot& sl = s->slots[slot];
+  if (sl.pending) return fail(STAGE_ESTATE, "slot holds a microbatch whose backward is pending");
+  const stage_shape_t& sh = s->sh;
+  const int vi = (int)(step % 2), T = s->T, d = sh.d_model;
+  hipStream_t st = s->st;
+  if (int rc = forward_blocks(s, sl, vi, tokens, x_in, false)) return rc;
+  launch_rmsnorm_fwd(s->bf, sl.y, s->wptr(vi, s->off_final), sl.hf, sl.rstdf, T, d, sh.rms_eps, st);
+  timed(s, STAGE_PROF_GEMM, 2.0 * T * sh.vocab * d, [&] {
+    launch_head_logprob(s->bf, T, sh.vocab, d, sl.hf, d, s->wptr(vi, s->off_head), d, targets, inv_temperature, logp,
+                        entropy, nullptr, sl.logits, st);
+  });
+  // the update that overwrites this weight version waits for this read of it
+  HIP_OK(hipEventRecord(s->ev_bwd[vi], st));
+  s->ev_bwd_set[vi] = true;
+  HIP_OK(hipGetLastError());
+  return STAGE_OK;
+}
+
+int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out, int32_t microbatches_per_step) {
+  if (!s) return fail(STAGE_EINVAL, "null stage");
+  const stage_shape_t& sh = s->sh;
+  if (slot < 0 || slot >= sh.max_inflight) return fail(STAGE_EINVAL, "slot out of range");
+  Slot& sl = s->slots[slot];
+  if (!sl.pending) return fail(STAGE_ESTATE, "slot holds no pending forward");
+  if (sl.lp) return fail(STAGE_ESTATE, "the slot's forward was stage_forward_logprob: stage_backward_logprob");
+  if (!sh.last_stage && !dy) return fail(STAGE_EINVAL, "non-last stage needs dy");
+  return backward_run(s, sl, dy, nullptr, nullptr, dx_out, microbatches_per_step);
+}
+
+int stage_backward_logprob(stage_t* s, int32_t slot, const float* dlogp, const float* dentropy, void* dx_out,
+                           int32_t microbatches_per_step) {
+  if (!s) return fail(STAGE_EINVAL, "null stage");
+  if (slot < 0 || slot >= s->sh.max_inflight) return fail(STAGE_EINVAL, "slot out of range");
+  Slot& sl = s->slots[slot];
+  if (!sl.pending || !sl.lp) return fail(STAGE_ESTATE, "slot holds no pending stage_forward_logprob");
+  if (!dlogp) return fail(STAGE_EINVAL, "null dlogp");
+  return backward_run(s, sl, nullptr, dlogp, dentropy, dx_out, microbatches_per_step);
 }
 
 }  // extern "C"

@@ -79,6 +79,25 @@ class Stage:
         p = lambda t: None if t is None else t.data_ptr()
         B.stage_backward(self.handle, slot, p(dy), p(dx_out), microbatches_per_step)
 
+    def forward_logprob(self, slot: int, step: int, targets, logp, tokens=None, x_in=None, entropy=None,
+                        inv_temperature: float = 1.0):
+        """forward() of a last stage up to the log-probabilities (and entropies) of its targets, for a loss
+        on them (losses.policy_loss, losses.preference_loss); backward_logprob() takes its gradients."""
+        p = lambda t: None if t is None else t.data_ptr()
+        B.stage_forward_logprob(self.handle, slot, step, p(tokens), p(x_in), p(targets), inv_temperature, p(logp),
+                                p(entropy))
+
+    def backward_logprob(self, slot: int, dlogp, dentropy=None, dx_out=None, microbatches_per_step: int = 1):
+        p = lambda t: None if t is None else t.data_ptr()
+        B.stage_backward_logprob(self.handle, slot, p(dlogp), p(dentropy), p(dx_out), microbatches_per_step)
+
+    def score_logprob(self, slot: int, step: int, targets, logp, tokens=None, x_in=None, entropy=None,
+                      inv_temperature: float = 1.0):
+        """The log-probabilities alone, with no backward to follow and no logits in memory."""
+        p = lambda t: None if t is None else t.data_ptr()
+        B.stage_score_logprob(self.handle, slot, step, p(tokens), p(x_in), p(targets), inv_temperature, p(logp),
+                              p(entropy))
+
     def update(self, t: int, hp: B.UpdateHParams):
         B.delayed_update(self.handle, t, hp)
 

@@ -59,7 +59,8 @@ __device__ __forceinline__ void tri_origin(const GemmArgs& g, int b, int& m0, in
 // GemmArgs::epi): bf16 output as is, SwiGLU backward, RoPE, SwiGLU forward, attention delta, plus
 // a residual row added, alpha (A B) + beta D.
 enum { EPI_PLAIN = 0, EPI_SWIGLU_BWD = 1, EPI_ROPE = 2, EPI_SWIGLU_FWD = 3, EPI_DELTA = 4, EPI_RESID = 5,
-       EPI_AXPBY = GEMM_EPI_AXPBY, EPI_AXPBY_DUP = GEMM_EPI_AXPBY_DUP, EPI_NS_SPLIT = GEMM_EPI_NS_SPLIT };
+       EPI_AXPBY = GEMM_EPI_AXPBY, EPI_AXPBY_DUP = GEMM_EPI_AXPBY_DUP, EPI_NS_SPLIT = GEMM_EPI_NS_SPLIT,
+       EPI_ROWSTAT = GEMM_EPI_ROWSTAT };
 
 // Output chunks leave with non-temporal stores and read-once epilogue operands arrive with
 // non-temporal loads: a product streams 10-150 MB of them through the 4 MB L2 of each XCD, which
@@ -357,6 +358,73 @@ __device__ __forceinline__ void dma_epilogue(const GemmArgs& g, f32x16 (&acc)[WM
   });
 }
 
+// Epilogue 9: the maximum and the two sums of every row over the wave's WN columns (kernels.h).  A part
+// of RP rows goes through the wave's LDS staging as above and comes back as 64 / RP lanes per row, each
+// with every (64 / RP)-th 16-byte chunk of it, so that a row's exponentials are spread over few lanes and
+// its sums take 2 or 3 exchanges.
+template <int BM, int BN, int WM, int WN, int RP>
+__device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[WM / 32][WN / 32], float* stage, int m0,
+                                              int n0, int wm0, int wn0) {
+  constexpr int FM = WM / 32, FN = WN / 32, EP = WN + 4, NP = 32 / RP, EPP = 16 / NP, NPART = FM * NP;
+  constexpr int LPR = 64 / RP, CI = WN / (4 * LPR);
+  static_assert(CI * 4 * LPR == WN, "whole chunks per lane");
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int r = lane / LPR, k = lane % LPR, c0 = n0 + wn0;
+  if (c0 >= g.N) return;  // no column of the wave is in C
+  const bool edge = c0 + WN > g.N;
+  float* stg = stage + wave * RP * EP;
+  const int64_t panel = (int64_t)(c0 / WN) * g.M;
+  const float c = g.stat_c;
+  int tgt[NPART];
+#pragma unroll
+  for (int p = 0; p < NPART; ++p) {
+    const int row = m0 + wm0 + (p / NP) * 32 + RP * (p % NP) + r;
+    tgt[p] = row < g.M ? g.targets[row] : -1;
+  }
+  static_for<NPART>([&](auto P) {
+    constexpr int p = P, i = p / NP, h = p % NP;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int e = EPP * h; e < EPP * h + EPP; ++e)
+        stg[(8 * (e / 4) - RP * h + 4 * (lane / 32) + (e % 4)) * EP + j * 32 + lane % 32] = acc[i][j][e];
+    asm volatile("" ::: "memory");
+    const int row = m0 + wm0 + i * 32 + RP * h + r;
+    f32x4 v[CI];
+    float m = -3.402823466e38f;
+#pragma unroll
+    for (int q = 0; q < CI; ++q) {
+      v[q] = *reinterpret_cast<const f32x4*>(stg + r * EP + 4 * (k + LPR * q));
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c0 + 4 * (k + LPR * q) + u >= g.N) v[q][u] = -INFINITY;
+      }
+      m = fmaxf(m, fmaxf(fmaxf(v[q][0], v[q][1]), fmaxf(v[q][2], v[q][3])));
+    }
+    const int tc = tgt[p] - c0;
+    if (k == 0 && tc >= 0 && tc < WN && tgt[p] < g.N) g.stat_xt[row] = stg[r * EP + tc];
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    float s = 0.f, w = 0.f;
+#pragma unroll
+    for (int q = 0; q < CI; ++q)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float t = (v[q][u] - m) * c, e = __builtin_amdgcn_exp2f(t);
+        s += e;
+        w += e * fmaxf(t, -1e30f);
+      }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) {
+      s += __shfl_xor(s, o, 64);
+      w += __shfl_xor(w, o, 64);
+    }
+    if (k == 0 && row < g.M) g.stats[panel + row] = RowPart{m, s, w};
+  });
+}
+
 // ---------------------------------------------------------------------------------------------
 // Kernel with direct-to-LDS operand loads (gfx950 global_load_lds_dwordx4): each lane's
 // 16 bytes land at the wave's LDS base + 16 * lane, so a tile is written in lane order and the
@@ -481,7 +549,7 @@ gemm_dma_kernel(GemmArgs g) {
   constexpr int RP = C_::RP, CPP = RP * WN / (sizeof(OutT) == 2 ? 8 : 4);  // 16-byte chunks per part
   static_assert(CPP % 64 == 0, "every lane stores the same number of chunks per part");
   // (RAG: a wave outside C issues none)
-  constexpr int EPI_OPS = RAG ? 0 : FM * (32 / RP) * (CPP / 64);
+  constexpr int EPI_OPS = RAG || EPI == EPI_ROWSTAT ? 0 : FM * (32 / RP) * (CPP / 64);
   static_assert((NS - 2) * (PA + PB) + EPI_OPS < 64, "vmcnt range");
   extern __shared__ __align__(16) unsigned char smem[];
   bf16* S = reinterpret_cast<bf16*>(smem);  // [NS][A tile | B tile]
@@ -623,12 +691,13 @@ gemm_dma_kernel(GemmArgs g) {
           for (int j = 0; j < FN; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[c][i], bfr[c][j], acc[i][j], 0, 0, 0);
         if constexpr (ks + 1 < BKT / 16) {
-          static_assert(FM * FN >= FM + FN, "one MFMA ahead of every fragment read");
-          static_for<FM + FN>([&](auto) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
-          });
-          __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - (FM + FN), 0);
+          if constexpr (FM * FN >= FM + FN) {  // one MFMA ahead of every fragment read
+            static_for<FM + FN>([&](auto) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
+              __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
+            });
+            __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - (FM + FN), 0);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -643,7 +712,8 @@ gemm_dma_kernel(GemmArgs g) {
     }
     wait_vm_lds<63>();
     block_barrier();
-    dma_epilogue<BM, BN, WM, WN, OutT, EPI, C_::RP, RAG>(g, acc, stg, m0, n0, wm0, wn0, t - g.tile0);
+    if constexpr (EPI == EPI_ROWSTAT) stat_epilogue<BM, BN, WM, WN, C_::RP>(g, acc, stg, m0, n0, wm0, wn0);
+    else dma_epilogue<BM, BN, WM, WN, OutT, EPI, C_::RP, RAG>(g, acc, stg, m0, n0, wm0, wn0, t - g.tile0);
     if (!next) break;
     t = tn; m0 = m1; n0 = n1; at = atn; bt = btn;
   }
@@ -985,5 +1055,45 @@ bool gemm_mfma_try(const GemmArgs& g0, hipStream_t st) {
   if (rope_after)
     launch_rope(!g.out_f32, g.C, g.M, g.rope_S, g.rope_cols / g.rope_hd, g.rope_hd, g.ldc, g.rope_cos,
                 g.rope_sin, false, st);
+  return true;
+}
+
+// ------------------------------------------------------------------ row statistics (epilogue 9)
+namespace {
+// 0: 32-row tiles, 1: 64, 2: 128 x 128, 3: 256 x 256
+int rowstat_config(int64_t M, int64_t N, int64_t K) {
+  if (M <= 32) return 0;
+  if (M <= 64) return 1;
+  const int64_t t256 = cdiv(M, 256) * cdiv(N, 256);
+  return K >= 1024 && t256 >= 512 ? 3 : 2;
+}
+
+template <int BM, int BN, int WM, int WN, int NS>
+void launch_rowstat(const GemmArgs& g, hipStream_t st) {
+  const int nblk = (int)(cdiv(g.M, BM) * cdiv(g.N, BN));
+  if (g.M % BM == 0 && g.N % BN == 0 && g.K % BKT == 0)
+    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI_ROWSTAT, false>(g, nblk, st);
+  else
+    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI_ROWSTAT, true>(g, nblk, st);
+}
+}  // namespace
+
+int gemm_rowstat_panel(int64_t M, int64_t N, int64_t K) {
+  const int panel[] = {32, 32, 64, 128};
+  return panel[rowstat_config(M, N, K)];
+}
+
+bool gemm_rowstat_try(const GemmArgs& g0, hipStream_t st) {
+  GemmArgs g = g0;
+  g.out_f32 = true;
+  g.epi = 0;
+  g.ksplit = 1;
+  if (!g.a_kmajor || !g.b_kmajor || !dma_operands(g)) return false;
+  switch (rowstat_config(g.M, g.N, g.K)) {
+    case 0: launch_rowstat<32, 128, 32, 32, 4>(g, st); break;
+    case 1: launch_rowstat<64, 128, 64, 32, 3>(g, st); break;
+    case 2: launch_rowstat<128, 128, 64, 64, 2>(g, st); break;
+    default: launch_rowstat<256, 256, 64, 128, 2>(g, st); break;
+  }
   return true;
 }

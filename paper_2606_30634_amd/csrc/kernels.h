@@ -91,6 +91,10 @@ void launch_ce_bwd(bool bf, const float* logits, const int32_t* targets, const f
                    float scale, void* dlogits, int ld, hipStream_t st);
 void launch_mean(const float* v, int n, float* out, hipStream_t st);
 
+// Statistics of a part of a row of logits: its maximum m, s = sum 2^t and w = sum t 2^t, t = c (x - m);
+// m is the lowest finite value where there is nothing above it
+struct RowPart { float m, s, w; };
+
 // ------------------------------------------------------------------ GEMM (gemm.hip)
 // C[m, n] (+)= sum_k A(m, k) B(n, k).  A(m,k) = a_kmajor ? A[m*lda + k] : A[k*lda + m];
 // B(n,k) = b_kmajor ? B[n*ldb + k] : B[k*ldb + n].  Inputs bf16 or fp32 (bf), accumulation fp32.
@@ -140,6 +144,14 @@ struct GemmArgs {
   // the tiles on and above the diagonal only and write each off-diagonal one also transposed; a
   // product of partial tiles ignores the flag (and computes every tile)
   int sym = 0;
+  // epilogue 9 (row statistics): nothing of the product is stored.  Per row and panel of
+  // gemm_rowstat_panel() columns, panel p of row m writes its maximum x0 and the sums of 2^t and of
+  // t 2^t, t = stat_c (x - x0), to stats[p M + m], and the row's logit of column targets[m] goes to
+  // stat_xt[m] (nothing where targets[m] is outside [0, N)).
+  RowPart* stats = nullptr;
+  float stat_c = 0.f;
+  const int32_t* targets = nullptr;
+  float* stat_xt = nullptr;
 };
 constexpr int GEMM_EPI_AXPBY = 6;
 // epilogue 7 (AXPBY with duplicated columns): C[r, 2c] = C[r, 2c + 1] = alpha (A B)[r, c] +
@@ -154,6 +166,12 @@ inline bool gemm_batched_tiles(int M, int N, int K) { return M % 128 == 0 && N %
 // y = alpha y + beta x over rows x cols (row stride ld), in place, bf16 or fp32 storage
 void launch_axpby(bool bf, void* y, const void* x, float alpha, float beta, int rows, int cols, int ld,
                   hipStream_t st);
+constexpr int GEMM_EPI_ROWSTAT = 9;
+// Columns of a panel of epilogue 9 for a product of these sizes, and the product itself (bf16, both operands
+// k-contiguous): false if the kernels do not take the operands (K, lda, ldb multiples of 8, 16-byte
+// aligned; gemm_mfma.hip)
+int gemm_rowstat_panel(int64_t M, int64_t N, int64_t K);
+bool gemm_rowstat_try(const GemmArgs& g, hipStream_t st);
 constexpr int64_t GEMM_WS_ELEMS = 16 << 20;  // 64 MiB of fp32 split-K partials per stage
 void launch_gemm(bool bf, const GemmArgs& g, hipStream_t st);
 

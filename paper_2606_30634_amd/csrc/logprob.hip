@@ -49,8 +49,8 @@ template <> struct Vec8<float> {
   }
 };
 
-// Running statistics of a part of a row: maximum m, s = sum 2^t, w = sum t 2^t with t = c (x - m).
-struct Part { float m, s, w; };
+// Running statistics of a part of a row
+typedef RowPart Part;
 __device__ __forceinline__ Part part_empty() { return {-FLT_MAX, 0.f, 0.f}; }
 
 // a's sums relative to the maximum mx >= a.m (an empty part's shift is -inf or NaN: it has nothing to move)
@@ -298,34 +298,112 @@ void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, in
 }
 
 // ------------------------------------------------------------------ from hidden states
-// Rows of logits that fit the workspace at once: x W^T in fp32, then their statistics.
-constexpr int64_t HEAD_CHUNK_BYTES = 256 << 20;
-static int64_t head_chunk(int64_t rows, int64_t vocab) {
-  return std::max<int64_t>(1, std::min(rows, HEAD_CHUNK_BYTES / (4 * vocab) / 256 * 256 > 0
-                                                 ? HEAD_CHUNK_BYTES / (4 * vocab) / 256 * 256
-                                                 : HEAD_CHUNK_BYTES / (4 * vocab)));
+namespace {
+
+// Joins the panels of every row (parts[p rows + row]): RJ rows per block of 256, 256 / RJ threads on each.
+template <int RJ>
+__global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panels, const int32_t* __restrict__ tg, float c,
+                                                  const Part* __restrict__ parts, const float* __restrict__ xt,
+                                                  float* __restrict__ logp, float* __restrict__ ent,
+                                                  float* __restrict__ stats) {
+  constexpr int TR = 256 / RJ;  // threads per row
+  __shared__ Part sm[256];
+  const int r = threadIdx.x % RJ, k = threadIdx.x / RJ;
+  const int64_t row = (int64_t)blockIdx.x * RJ + r;
+  Part a = part_empty();
+  if (row < rows) {
+    int p = k;
+    for (; p + 3 * TR < panels; p += 4 * TR) {
+      Part b[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) b[u] = parts[(int64_t)(p + u * TR) * rows + row];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) part_merge(a, b[u], c);
+    }
+    for (; p < panels; p += TR) part_merge(a, parts[(int64_t)p * rows + row], c);
+  }
+  sm[threadIdx.x] = a;
+  __syncthreads();
+#pragma unroll
+  for (int o = TR / 2; o > 0; o >>= 1) {
+    if (k < o) {
+      part_merge(a, sm[threadIdx.x + o * RJ], c);
+      sm[threadIdx.x] = a;
+    }
+    __syncthreads();
+  }
+  if (k == 0 && row < rows) {
+    const int t = tg[row];
+    if (t < 0 || t >= V) row_ignored(row, logp, ent, stats);
+    else row_finish(a, xt[row], c, row, logp, ent, stats);
+  }
 }
 
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Rows of fp32 logits held at once where they go through memory: within `bytes`, whole 128s if more than that
+int64_t head_chunk(int64_t rows, int64_t vocab, int64_t bytes) {
+  const int64_t r = bytes / (4 * vocab);
+  return std::max<int64_t>(1, std::min(rows, r > 128 ? r / 128 * 128 : r));
+}
+constexpr int64_t HEAD_F32_BYTES = 256 << 20;  // fp32 heads; a chunk stays in the last-level cache
+constexpr int64_t HEAD_ODD_BYTES = 32 << 20;   // bf16 heads of unaligned rows
+
+constexpr int64_t HEAD_ROWS = 16384;  // rows of one fused product: bounds its parts' memory
+
+size_t fused_bytes(int64_t n, int64_t vocab, int64_t d) {
+  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(n, vocab, d)) * n * sizeof(Part);
+}
+size_t chunk_bytes(int64_t r, int64_t vocab) { return align256((size_t)(r * vocab * 4)) + logprob_ws_bytes(r, vocab); }
+
+}  // namespace
+
 size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d) {
-  (void)bf;
-  (void)d;
-  const int64_t r = head_chunk(rows, vocab);
-  return (size_t)(r * vocab * 4 + 255) / 256 * 256 + logprob_ws_bytes(r, vocab);
+  const size_t chunked = chunk_bytes(head_chunk(rows, vocab, bf ? HEAD_ODD_BYTES : HEAD_F32_BYTES), vocab);
+  if (!bf) return chunked;
+  const int64_t first = std::min(rows, HEAD_ROWS), last = (rows - 1) % HEAD_ROWS + 1;
+  return std::max({fused_bytes(first, vocab, d), fused_bytes(last, vocab, d), chunked});
 }
 
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
                          int64_t ldw, const int32_t* targets, float inv_temp, float* logp, float* ent, float* stats,
                          void* ws, hipStream_t st) {
-  const int64_t r = head_chunk(rows, vocab);
+  if (rows <= 0) return;
+  GemmArgs g{};
+  g.N = vocab; g.K = d;
+  g.lda = (int)ldx; g.a_kmajor = true;
+  g.B = w; g.ldb = (int)ldw; g.b_kmajor = true;
+  // the rows' statistics in the product's epilogue, a part per panel of columns
+  bool fused = bf;
+  for (int64_t r0 = 0; fused && r0 < rows; r0 += HEAD_ROWS) {
+    const int64_t n = std::min(HEAD_ROWS, rows - r0);
+    g.M = (int)n;
+    g.A = (const char*)x + r0 * ldx * 2;
+    g.stat_c = inv_temp * LOG2E;
+    g.targets = targets + r0;
+    g.stat_xt = (float*)ws;
+    g.stats = (Part*)((char*)ws + align256((size_t)n * 4));
+    fused = gemm_rowstat_try(g, st);  // takes all chunks or none: they differ in n alone
+    if (!fused) break;
+    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(n, vocab, d));
+    float* e = ent ? ent + r0 : nullptr;
+    float* q = stats ? stats + 2 * r0 : nullptr;
+    if (n >= 256)
+      panel_join<16><<<(unsigned)cdiv(n, 16), 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt,
+                                                            logp + r0, e, q);
+    else
+      panel_join<1><<<(unsigned)n, 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, logp + r0, e,
+                                                 q);
+  }
+  if (fused) return;
+  const int64_t r = head_chunk(rows, vocab, bf ? HEAD_ODD_BYTES : HEAD_F32_BYTES);
   float* logits = (float*)ws;
-  void* parts = (char*)ws + (size_t)(r * vocab * 4 + 255) / 256 * 256;
+  void* parts = (char*)ws + align256((size_t)(r * vocab * 4));
+  g.C = logits; g.ldc = vocab; g.out_f32 = true; g.beta = 0.f;
   for (int64_t r0 = 0; r0 < rows; r0 += r) {
     const int64_t n = std::min(r, rows - r0);
-    GemmArgs g{};
-    g.M = (int)n; g.N = vocab; g.K = d;
-    g.A = (const char*)x + r0 * ldx * (bf ? 2 : 4); g.lda = (int)ldx; g.a_kmajor = true;
-    g.B = w; g.ldb = (int)ldw; g.b_kmajor = true;
-    g.C = logits; g.ldc = vocab; g.out_f32 = true; g.beta = 0.f;
+    g.M = (int)n;
+    g.A = (const char*)x + r0 * ldx * (bf ? 2 : 4);
     launch_gemm(bf, g, st);
     launch_logprob(false, n, vocab, logits, vocab, targets + r0, inv_temp, logp + r0, ent ? ent + r0 : nullptr,
                    stats ? stats + 2 * r0 : nullptr, parts, st);

@@ -441,3 +441,19 @@ def test_captured_chain(B, S, V, d):
             eager = _chain(losses, x, w, t, old, ref, adv, mask, ws2)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, _leaves(eager))), k
+
+
+def test_head_logprob_of_more_rows_than_one_product_takes():
+    """Rows of both chunks of a tall input, at the chunk's border and at its end, in a small head."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    n, v, d = 16384 + 70, 300, 64
+    r = np.random.default_rng(12)
+    mx, xv = _matrix(r.normal(size=(n, d)), True)
+    mw, wv = _matrix(r.normal(size=(v, d)) * 0.4, True)
+    t = r.integers(-1, v, size=n)
+    got = losses.head_logprob(mx, mw, _i32(t))
+    ref = L.token_logprob(xv @ wv.T, t, 1.0)
+    e = _head_tol(d, xv, wv, 1.0)
+    assert (np.abs(_np(got.logp) - ref[0]) <= 2 * e + _err(v, ref[0])).all()
+    assert (np.abs(_np(got.stats)[:, 0] - ref[2][:, 0]) <= e).all()

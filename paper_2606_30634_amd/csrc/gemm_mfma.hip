@@ -1060,12 +1060,16 @@ bool gemm_mfma_try(const GemmArgs& g0, hipStream_t st) {
 
 // ------------------------------------------------------------------ row statistics (epilogue 9)
 namespace {
-// 0: 32-row tiles, 1: 64, 2: 128 x 128, 3: 256 x 256
-int rowstat_config(int64_t M, int64_t N, int64_t K) {
-  if (M <= 32) return 0;
-  if (M <= 64) return 1;
-  const int64_t t256 = cdiv(M, 256) * cdiv(N, 256);
-  return K >= 1024 && t256 >= 512 ? 3 : 2;
+// Tiles of the statistics product.  Up to 32 rows it streams W: 32 x 256 tiles in 3 stages, two blocks per
+// CU (one row, d 4096, N 128256: 173.5 us, 6.1 TB/s; 32 x 128 in 4 stages 181, 128 x 128 179).  Above, rounds
+// decide: a round of 256 blocks of 256 x 256 takes 1.5 to 1.75 times one of 512 of 128 x 128.  128 against
+// 256, us: N 32000, K 768: M 256 23 : 30, M 512 38 : 35; N 49152, K 2048: M 256 63 : 58, M 512 105 : 107, M 8192
+// 1609 : 1370; N 128256, K 4096: M 128 198 : 250, M 256 342 : 274; N 4000, K 512: M 2048 20 : 26, M 8192 56 : 49.
+enum { ROWSTAT_32, ROWSTAT_128, ROWSTAT_256 };
+int rowstat_config(int64_t M, int64_t N) {
+  if (M <= 32) return ROWSTAT_32;
+  const int64_t r128 = cdiv(cdiv(M, 128) * cdiv(N, 128), 512), r256 = cdiv(cdiv(M, 256) * cdiv(N, 256), 256);
+  return 8 * r256 <= 5 * r128 ? ROWSTAT_256 : ROWSTAT_128;
 }
 
 template <int BM, int BN, int WM, int WN, int NS>
@@ -1078,10 +1082,7 @@ void launch_rowstat(const GemmArgs& g, hipStream_t st) {
 }
 }  // namespace
 
-int gemm_rowstat_panel(int64_t M, int64_t N, int64_t K) {
-  const int panel[] = {32, 32, 64, 128};
-  return panel[rowstat_config(M, N, K)];
-}
+int gemm_rowstat_panel(int64_t M, int64_t N) { return rowstat_config(M, N) == ROWSTAT_256 ? 128 : 64; }
 
 bool gemm_rowstat_try(const GemmArgs& g0, hipStream_t st) {
   GemmArgs g = g0;
@@ -1089,10 +1090,9 @@ bool gemm_rowstat_try(const GemmArgs& g0, hipStream_t st) {
   g.epi = 0;
   g.ksplit = 1;
   if (!g.a_kmajor || !g.b_kmajor || !dma_operands(g)) return false;
-  switch (rowstat_config(g.M, g.N, g.K)) {
-    case 0: launch_rowstat<32, 128, 32, 32, 4>(g, st); break;
-    case 1: launch_rowstat<64, 128, 64, 32, 3>(g, st); break;
-    case 2: launch_rowstat<128, 128, 64, 64, 2>(g, st); break;
+  switch (rowstat_config(g.M, g.N)) {
+    case ROWSTAT_32: launch_rowstat<32, 256, 32, 64, 3>(g, st); break;
+    case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2>(g, st); break;
     default: launch_rowstat<256, 256, 64, 128, 2>(g, st); break;
   }
   return true;

@@ -170,7 +170,7 @@ constexpr int GEMM_EPI_ROWSTAT = 9;
 // Columns of a panel of epilogue 9 for a product of these sizes, and the product itself (bf16, both operands
 // k-contiguous): false if the kernels do not take the operands (K, lda, ldb multiples of 8, 16-byte
 // aligned; gemm_mfma.hip)
-int gemm_rowstat_panel(int64_t M, int64_t N, int64_t K);
+int gemm_rowstat_panel(int64_t M, int64_t N);
 bool gemm_rowstat_try(const GemmArgs& g, hipStream_t st);
 constexpr int64_t GEMM_WS_ELEMS = 16 << 20;  // 64 MiB of fp32 split-K partials per stage
 void launch_gemm(bool bf, const GemmArgs& g, hipStream_t st);
@@ -251,7 +251,7 @@ void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, in
                         const float* stats, const float* ent, const float* dlogp, const float* dent, float inv_temp,
                         bool out_bf, void* dlogits, int64_t ldo, int zero_to, hipStream_t st);
 // launch_logprob of the logits x W^T (x [rows, d], W [vocab, d], rows of ldx and ldw elements)
-size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d);
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab);
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
                          int64_t ldw, const int32_t* targets, float inv_temp, float* logp, float* ent, float* stats,
                          void* ws, hipStream_t st);

@@ -351,18 +351,18 @@ constexpr int64_t HEAD_ODD_BYTES = 32 << 20;   // bf16 heads of unaligned rows
 
 constexpr int64_t HEAD_ROWS = 16384;  // rows of one fused product: bounds its parts' memory
 
-size_t fused_bytes(int64_t n, int64_t vocab, int64_t d) {
-  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(n, vocab, d)) * n * sizeof(Part);
+size_t fused_bytes(int64_t n, int64_t vocab) {
+  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(n, vocab)) * n * sizeof(Part);
 }
 size_t chunk_bytes(int64_t r, int64_t vocab) { return align256((size_t)(r * vocab * 4)) + logprob_ws_bytes(r, vocab); }
 
 }  // namespace
 
-size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d) {
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab) {
   const size_t chunked = chunk_bytes(head_chunk(rows, vocab, bf ? HEAD_ODD_BYTES : HEAD_F32_BYTES), vocab);
   if (!bf) return chunked;
   const int64_t first = std::min(rows, HEAD_ROWS), last = (rows - 1) % HEAD_ROWS + 1;
-  return std::max({fused_bytes(first, vocab, d), fused_bytes(last, vocab, d), chunked});
+  return std::max({fused_bytes(first, vocab), fused_bytes(last, vocab), chunked});
 }
 
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
@@ -385,7 +385,7 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
     g.stats = (Part*)((char*)ws + align256((size_t)n * 4));
     fused = gemm_rowstat_try(g, st);  // takes all chunks or none: they differ in n alone
     if (!fused) break;
-    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(n, vocab, d));
+    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(n, vocab));
     float* e = ent ? ent + r0 : nullptr;
     float* q = stats ? stats + 2 * r0 : nullptr;
     if (n >= 256)

@@ -37,6 +37,38 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// Sum over the wave's lanes in lane order by data-parallel moves (no LDS round trips), in every lane.
+// Four row shifts sum each 16 lanes into their last one, two broadcasts carry those on to lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T dpp_add(T v) {
+  uint32_t w[sizeof(T) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
+#pragma unroll
+  for (unsigned k = 0; k < sizeof(T) / 4; ++k) w[k] = dpp_or_zero<CTRL, ROWS>(w[k]);
+  T o;
+  __builtin_memcpy(&o, w, sizeof(T));
+  return v + o;
+}
+template <typename T>
+__device__ __forceinline__ T wave_total(T v) {
+  v = dpp_add<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);  // lane 15 of rows 0 and 2 to rows 1 and 3
+  v = dpp_add<0x143, 0xc>(v);  // lane 31 to rows 2 and 3
+  uint32_t w[sizeof(T) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
+#pragma unroll
+  for (unsigned k = 0; k < sizeof(T) / 4; ++k) w[k] = (uint32_t)__builtin_amdgcn_readlane((int)w[k], 63);
+  __builtin_memcpy(&v, w, sizeof(T));
+  return v;
+}
+
 // Block-wide sum for blockDim.x a multiple of 64 (<= 1024); result valid in every thread.
 template <typename T>
 __device__ __forceinline__ T block_sum(T v, T* smem /* >= 16 entries */) {

@@ -20,34 +20,23 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float TINY_T = -1e30f;  // a finite stand-in for -inf where it meets a zero factor
 
-// 8 elements at any element alignment
-template <typename T> struct Vec8;
-template <> struct Vec8<bf16> {
-  typedef bf16 raw __attribute__((ext_vector_type(8), aligned(2)));
-  static __device__ __forceinline__ void load(const bf16* p, float (&v)[8]) {
-    const raw r = *reinterpret_cast<const raw*>(p);
+// 16 bytes of elements at any element alignment (8 bf16, 4 fp32); N of them, of either type
+template <typename T> constexpr int VE = 16 / (int)sizeof(T);
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[N]) {
+  typedef T raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  const raw r = *reinterpret_cast<const raw*>(p);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = (float)r[q];
-  }
-  static __device__ __forceinline__ void store(bf16* p, const float (&v)[8]) {
-    raw r;
+  for (int q = 0; q < N; ++q) v[q] = to_f32(r[q]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[N]) {
+  typedef T raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  raw r;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) r[q] = (bf16)v[q];
-    *reinterpret_cast<raw*>(p) = r;
-  }
-};
-template <> struct Vec8<float> {
-  typedef float raw __attribute__((ext_vector_type(4), aligned(4)));
-  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
-    const raw a = reinterpret_cast<const raw*>(p)[0], b = reinterpret_cast<const raw*>(p)[1];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = a[q], v[q + 4] = b[q];
-  }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
-    reinterpret_cast<raw*>(p)[0] = raw{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<raw*>(p)[1] = raw{v[4], v[5], v[6], v[7]};
-  }
-};
+  for (int q = 0; q < N; ++q) r[q] = from_f32<T>(v[q]);
+  *reinterpret_cast<raw*>(p) = r;
+}
 
 // Running statistics of a part of a row
 typedef RowPart Part;
@@ -113,7 +102,7 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
                                                          const int32_t* __restrict__ tg, float c, int nsplit, int per,
                                                          Part* __restrict__ parts, float* __restrict__ logp,
                                                          float* __restrict__ ent, float* __restrict__ stats) {
-  constexpr int NW = NT / WAVE, U = 4;
+  constexpr int NW = NT / WAVE, E = VE<T>, U = 32 / E;
   static_assert(NW == 1 || RPB == 1, "groups of one wave, or one group per block");
   __shared__ Part sm[NW];
   const int tid = threadIdx.x % NT;
@@ -126,23 +115,23 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
       continue;
     }
     const T* z = x + row * ld + (int64_t)sp * per;
-    const int n = min(per, V - sp * per), nv = n / 8;
+    const int n = max(0, min(per, V - sp * per)), nv = n / E;
     Part a = part_empty();
     int j = tid;
     for (; j + (U - 1) * NT < nv; j += U * NT) {
-      float v[U][8];
+      float v[U][E];
 #pragma unroll
-      for (int u = 0; u < U; ++u) Vec8<T>::load(z + (int64_t)(j + u * NT) * 8, v[u]);
+      for (int u = 0; u < U; ++u) load_vec(z + (int64_t)(j + u * NT) * E, v[u]);
 #pragma unroll
       for (int u = 0; u < U; ++u) part_add(a, v[u], c);
     }
     for (; j < nv; j += NT) {
-      float v[8];
-      Vec8<T>::load(z + (int64_t)j * 8, v);
+      float v[E];
+      load_vec(z + (int64_t)j * E, v);
       part_add(a, v, c);
     }
-    if (tid < n - nv * 8) {
-      const float v[1] = {to_f32(z[nv * 8 + tid])};
+    if (tid < n - nv * E) {
+      const float v[1] = {to_f32(z[nv * E + tid])};
       part_add(a, v, c);
     }
     part_lanes<WAVE>(a, c);
@@ -151,8 +140,8 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
       if (tid % WAVE == 0) sm[tid / WAVE] = a;
       __syncthreads();
       if (tid < WAVE) {
-        a = tid < NW ? sm[tid] : part_empty();
-        part_lanes<WAVE>(a, c);
+        a = sm[tid % NW];
+        part_lanes<NW>(a, c);
       }
     }
     if (tid == 0) {
@@ -181,16 +170,18 @@ __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T
   }
 }
 
-// The gradient, element by element: a wave takes U x 512 consecutive logits of a row.  A row without a
-// target, without a distribution or with zero upstream gradients gets zeros and is not read.  zero_to > V:
-// the columns [V, zero_to) get zeros.  dx may be x (same type and rows): a lane writes only what it has read.
+// The gradient, element by element: a wave takes U x 64 x 16 bytes of consecutive logits of a row.  A row
+// without a target, without a distribution or with zero upstream gradients gets zeros and is not read.
+// zero_to > V: the columns [V, zero_to) get zeros.  dx may be x (same type and rows): a lane writes only
+// what it has read.
+template <typename T> constexpr int BWD_U = 4;
 template <typename T, typename OutT>
 __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T* x, int64_t ld,
                                                    const int32_t* __restrict__ tg, const float* __restrict__ stats,
                                                    const float* __restrict__ ent, const float* __restrict__ dlogp,
                                                    const float* __restrict__ dent, float s, OutT* dx, int64_t ldo,
                                                    int zero_to) {
-  constexpr int U = 4, CH = U * 512;
+  constexpr int U = BWD_U<T>, E = VE<T>, CH = U * E * WAVE;
   const int lane = threadIdx.x % WAVE, W = max(V, zero_to);
   const int64_t per_row = (W + CH - 1) / CH, items = rows * per_row;
   const int64_t w0 = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -201,43 +192,71 @@ __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T*
     const float m = stats[2 * row], l2 = stats[2 * row + 1] * LOG2E, c = s * LOG2E;
     const bool on = t >= 0 && t < V && m != -INFINITY;
     const float g = on ? dlogp[row] * s : 0.f, h = on && dent ? dent[row] * s : 0.f, H = h != 0.f ? ent[row] : 0.f;
-    const bool zero = g == 0.f && h == 0.f;
     const T* z = x + row * ld;
     OutT* o = dx + row * ldo;
-    auto grad = [&](float v, int j) {
-      const float q = (v - m) * c - l2, p = __builtin_amdgcn_exp2f(q), lp = fmaxf(q, TINY_T) * LN2;
-      float d = -p * (h != 0.f ? g + h * (lp + H) : g);
-      if (j == t) d = g * -expm1f(q * LN2) - (h != 0.f ? p * h * (lp + H) : 0.f);
-      return d;
-    };
-    float v[U][8];
-    const bool whole = j0 + CH <= V;
-    if (whole && !zero) {
+    if (g == 0.f && h == 0.f) {
+      const float zero[E] = {};
 #pragma unroll
-      for (int u = 0; u < U; ++u) Vec8<T>::load(z + j0 + (u * WAVE + lane) * 8, v[u]);
+      for (int u = 0; u < U; ++u) {
+        const int j = j0 + (u * WAVE + lane) * E;
+        if (j + E <= W) store_vec(o + j, zero);
+        else
+          for (int q = j; q < W; ++q) o[q] = from_f32<OutT>(0.f);
+      }
+      continue;
     }
+    // without an entropy gradient an element is -g p; the target's is written apart, after its wave's stores
+    // (1 - p_t is -(e^lp - 1), which keeps its bits where p_t is near 1)
+    auto grad = [&](float v) {
+      const float q = (v - m) * c - l2, p = __builtin_amdgcn_exp2f(q);
+      return h == 0.f ? -g * p : -p * (g + h * (fmaxf(q, TINY_T) * LN2 + H));
+    };
+    const bool mine = t >= j0 && t < j0 + CH;
+    float dt = 0.f;
+    if (mine) {
+      const float q = (to_f32(z[t]) - m) * c - l2;
+      dt = -g * expm1f(q * LN2);
+      if (h != 0.f) dt -= __builtin_amdgcn_exp2f(q) * h * (fmaxf(q, TINY_T) * LN2 + H);
+    }
+    if (j0 + CH <= V) {
+      float v[U][E];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + (u * WAVE + lane) * 8;
-      if (j + 8 <= V) {
-        if (!whole && !zero) Vec8<T>::load(z + j, v[u]);
-        float d[8];
+      for (int u = 0; u < U; ++u) load_vec(z + j0 + (u * WAVE + lane) * E, v[u]);
+      if (h == 0.f) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) d[q] = zero ? 0.f : grad(v[u][q], j + q);
-        Vec8<OutT>::store(o + j, d);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int q = 0; q < E; ++q) v[u][q] = -g * __builtin_amdgcn_exp2f((v[u][q] - m) * c - l2);
       } else {
-        for (int q = 0; q < 8 && j + q < W; ++q)
-          o[j + q] = from_f32<OutT>(zero || j + q >= V ? 0.f : grad(to_f32(z[j + q]), j + q));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int q = 0; q < E; ++q) v[u][q] = grad(v[u][q]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) store_vec(o + j0 + (u * WAVE + lane) * E, v[u]);
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < U; ++u) {
+        const int j = j0 + (u * WAVE + lane) * E;
+        if (j + E <= V) {
+          float v[E];
+          load_vec(z + j, v);
+#pragma unroll
+          for (int q = 0; q < E; ++q) v[q] = grad(v[q]);
+          store_vec(o + j, v);
+        } else {
+          for (int q = j; q < min(j + E, W); ++q) o[q] = from_f32<OutT>(q >= V ? 0.f : grad(to_f32(z[q])));
+        }
       }
     }
+    if (mine && lane == (t - j0) / E % WAVE) o[t] = from_f32<OutT>(dt);  // the lane that stored around it
   }
 }
 
 // Parts of a row: none with enough rows to fill the chip.
 int row_splits(int64_t rows, int64_t V) {
-  (void)V;
-  (void)rows;
-  return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, V / 4096, 1024 / std::max<int64_t>(rows, 1)}));
 }
 
 constexpr int64_t GRID = 1 << 20;  // blocks of a launch at most; the kernels walk their rows
@@ -265,7 +284,7 @@ template <typename T, typename OutT>
 void logprob_bwd_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg, const float* stats,
                    const float* ent, const float* dlogp, const float* dent, float s, void* dx, int64_t ldo,
                    int zero_to, hipStream_t st) {
-  const int64_t waves = rows * cdiv(std::max(V, zero_to), 2048);
+  const int64_t waves = rows * cdiv(std::max(V, zero_to), BWD_U<T> * VE<T> * WAVE);
   logprob_bwd<T, OutT><<<(unsigned)std::min(GRID, cdiv(waves, 4)), 256, 0, st>>>(
       rows, V, (const T*)x, ld, tg, stats, ent, dlogp, dent, s, (OutT*)dx, ldo, zero_to);
 }
@@ -307,7 +326,7 @@ __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panel
                                                   float* __restrict__ logp, float* __restrict__ ent,
                                                   float* __restrict__ stats) {
   constexpr int TR = 256 / RJ;  // threads per row
-  __shared__ Part sm[256];
+  __shared__ Part sm[4 * RJ];
   const int r = threadIdx.x % RJ, k = threadIdx.x / RJ;
   const int64_t row = (int64_t)blockIdx.x * RJ + r;
   Part a = part_empty();
@@ -322,15 +341,17 @@ __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panel
     }
     for (; p < panels; p += TR) part_merge(a, parts[(int64_t)p * rows + row], c);
   }
-  sm[threadIdx.x] = a;
-  __syncthreads();
+  // a wave holds 64 / RJ threads of each of the block's rows
+  constexpr int LR = WAVE / RJ;
 #pragma unroll
-  for (int o = TR / 2; o > 0; o >>= 1) {
-    if (k < o) {
-      part_merge(a, sm[threadIdx.x + o * RJ], c);
-      sm[threadIdx.x] = a;
-    }
-    __syncthreads();
+  for (int o = LR / 2 * RJ; o >= RJ; o >>= 1) {
+    const Part b{__shfl_xor(a.m, o, WAVE), __shfl_xor(a.s, o, WAVE), __shfl_xor(a.w, o, WAVE)};
+    part_merge(a, b, c);
+  }
+  if (threadIdx.x % WAVE < RJ) sm[threadIdx.x / WAVE * RJ + r] = a;
+  __syncthreads();
+  if (k == 0) {
+    for (int w = 1; w < 4; ++w) part_merge(a, sm[w * RJ + r], c);
   }
   if (k == 0 && row < rows) {
     const int t = tg[row];

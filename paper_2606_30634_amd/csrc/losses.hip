@@ -13,9 +13,9 @@ namespace {
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint8_t u8x4u __attribute__((ext_vector_type(4), aligned(1)));
 
-// e^x - 1 - x >= 0: its series up to x^9 where e^x - 1 and x cancel (next term below 3e-9 of the value)
-__device__ __forceinline__ float kl_term(float x) {
-  if (fabsf(x) >= 0.5f) return expm1f(x) - x;
+// e^x - 1 - x >= 0, given ex = e^x: the series up to x^9 where the difference cancels (next term below 3e-9 of
+// the value; from |x| = 1/2 on the difference keeps all but 2 bits).  With x added it is e^x - 1.
+__device__ __forceinline__ float kl_term(float x, float ex) {
   float p = 1.f / 362880.f;
   p = p * x + 1.f / 40320.f;
   p = p * x + 1.f / 5040.f;
@@ -24,32 +24,26 @@ __device__ __forceinline__ float kl_term(float x) {
   p = p * x + 1.f / 24.f;
   p = p * x + 1.f / 6.f;
   p = p * x + 0.5f;
-  return p * x * x;
+  return fabsf(x) >= 0.5f ? (ex - 1.f) - x : p * x * x;
 }
 
-// Block-wide sums of N doubles, for blocks of whole waves; valid in thread 0.
+// Block-wide sums of N doubles, for blocks of whole waves; valid in the first wave.
 template <int N>
 __device__ __forceinline__ void block_sums(double (&v)[N], double* sm /* N x 16 */) {
   const int w = threadIdx.x / WAVE, l = threadIdx.x % WAVE, nw = blockDim.x / WAVE;
-  __syncthreads();
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    v[k] = wave_sum(v[k]);
-    if (l == 0) sm[k * 16 + w] = v[k];
+  for (int k = 0; k < N; ++k) v[k] = wave_total(v[k]);
+  if (nw == 1) return;
+  __syncthreads();
+  if (l == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) sm[k * 16 + w] = v[k];
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (w == 0) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      v[k] = 0.0;
-      for (int i = 0; i < nw; ++i) v[k] += sm[k * 16 + i];
-    }
+    for (int k = 0; k < N; ++k) v[k] = wave_total(l < nw ? sm[k * 16 + l] : 0.0);
   }
-}
-__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor((long long)v, o, WAVE);
-  return v;
 }
 
 // Tokens of mask[0, n) that count, summed over the lanes of a group of NT threads' own shares.
@@ -67,111 +61,135 @@ __device__ __forceinline__ int count_share(const uint8_t* m, int64_t n, int tid)
       c += __popc(b);
     }
   }
-  if (tid < n - nv * 16) c += m[nv * 16 + tid] != 0;
+  for (int64_t j = nv * 16 + tid; j < n; j += NT) c += m[j] != 0;
   return c;
 }
 
 // ------------------------------------------------------------------ policy loss
-constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = 256;
-constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024;
+constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE;
+// policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024
+constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024, POL_EAGER_TOKENS = 1 << 19;
 
-// Weight of a token of a sequence with n tokens that count.
-__device__ __forceinline__ double token_weight(const PolicyArgs& a, double tokens, double seqs, int n) {
-  if (n == 0) return 0.0;
-  if (a.seq_mean) return 1.0 / ((a.norm > 0 ? a.norm : seqs) * n);
-  return 1.0 / (a.norm > 0 ? a.norm : tokens);
+// 1 / n for n > 0, to 2^-44: one step of Newton's method from the hardware's 2^-23
+__device__ __forceinline__ double inverse(int n) {
+  const double d = n, y = (double)__builtin_amdgcn_rcpf((float)n);
+  return y * (2.0 - d * y);
+}
+// 1 / what the mean divides by, the number of tokens or of sequences that count or norm (0 where nothing
+// counts): the weight of a token, or of a sequence with seq_mean
+__device__ __forceinline__ double mean_scale(const PolicyArgs& a, int64_t tokens, int64_t seqs) {
+  const double d = a.norm > 0 ? a.norm : (double)(a.seq_mean ? seqs : tokens);
+  return d > 0 ? 1.0 / d : 0.0;
 }
 
-// Token i of sequence b at weight w: its terms into acc, its gradients returned.
-// Which side of the clip a token is on is decided in the logarithm, on the exact difference of the two
-// log-probabilities, so that the gradient's jump there does not hang on the rounding of e^x.
-__device__ __forceinline__ void policy_token(const PolicyArgs& a, float lp, float old, float adv, float ref, float ent,
-                                             double w, double (&acc)[POL_SUMS], float& g, float& ge) {
+// A token's terms, times om, added to f where it counts (whatever the others hold), and its gradient
+// apart from the weight.  Which side of the clip a token is on is decided in the logarithm, on the exact
+// difference of the two log-probabilities, so that the gradient's jump there does not hang on the rounding of
+// e^x.
+__device__ __forceinline__ float policy_token(const PolicyArgs& a, bool on, float om, float lp, float old, float adv, float ref,
+                                              float ent, float (&f)[POL_SUMS]) {
   const double x = (double)lp - (double)old;
   const float xf = (float)x, r = expf(xf);
-  const bool rise = adv > 0.f && x > a.log_hi, fall = adv < 0.f && x < a.log_lo;
+  const bool rise = adv > 0.f && x > a.log_hi, fall = adv < 0.f && x < a.log_lo, cut = rise || fall;
   const float held = rise ? 1.f + a.clip_high : fall ? 1.f - a.clip_low : r;
-  float d = rise || fall ? 0.f : -r * adv;
-  acc[0] += w * (double)(-held * adv);
-  acc[3] += rise || fall ? w : 0.0;
-  acc[4] += w * (double)kl_term(xf);
-  acc[5] += w * (double)r;
+  float d = cut ? 0.f : -r * adv;
+  f[0] -= on ? om * (held * adv) : 0.f;
+  f[3] += on && cut ? om : 0.f;
+  f[4] += on ? om * kl_term(xf, r) : 0.f;
+  f[5] += on ? om * r : 0.f;
   if (a.ref) {
-    const float q = (float)((double)ref - (double)lp);
-    acc[1] += w * (double)kl_term(q);
-    if (a.kl_coef != 0.f) d -= a.kl_coef * expm1f(q);
+    const float q = ref - lp, eq = expf(q), k = kl_term(q, eq);
+    f[1] += on ? om * k : 0.f;
+    if (a.kl_coef != 0.f) d -= a.kl_coef * (fabsf(q) >= 0.5f ? eq - 1.f : k + q);
   }
-  if (a.ent) acc[2] += w * (double)ent;
-  const float gw = (float)(w * a.grad_scale);
-  g = gw * d;
-  ge = -a.ent_coef * gw;
+  if (a.ent) f[2] += on ? om * ent : 0.f;
+  return on ? d : 0.f;
 }
 
-// Vectors j0, j0 + step, ... of 4 tokens
-__device__ __forceinline__ void policy_walk(const PolicyArgs& a, int64_t j0, int64_t step, const int* nb, double tokens,
-                                            double seqs, double (&acc)[POL_SUMS]) {
-  const int64_t n = a.seqs * a.len;
-  for (int64_t j = j0; 4 * j < n; j += step) {
-    const int64_t i = 4 * j;
-    int64_t b = (uint64_t)i >> 32 ? i / a.len : (int64_t)((uint32_t)i / (uint32_t)a.len);
-    int64_t left = (b + 1) * a.len - i;  // tokens of sequence b from i on
-    float g[4] = {0.f, 0.f, 0.f, 0.f}, ge[4] = {0.f, 0.f, 0.f, 0.f};
-    const int m = (int)min((int64_t)4, n - i);
-    uint8_t on[4] = {0, 0, 0, 0};
-    if (m == 4) {
-      const u8x4u v = *reinterpret_cast<const u8x4u*>(a.mask + i);
+// sequence of token i
+__device__ __forceinline__ int64_t seq_of(int64_t i, int64_t len) {
+  return (uint64_t)i >> 32 ? i / len : (int64_t)((uint32_t)i / (uint32_t)len);
+}
+
+// 4 consecutive tokens i .. i + 3 of the flat arrays: the first in sequence b, those from token `turn` on in
+// b + 1; the two sequences' counts and advantages.  vec: all four exist and sequences are at least that long (the
+// others are taken one by one, from memory).
+struct Tokens {
+  u8x4u on;
+  f32x4u lp, old, ref, ent, adv;
+  int turn, nb0, nb1;
+  float ab0, ab1;
+  bool vec;
+};
+__device__ __forceinline__ void tokens_start(Tokens& v, const PolicyArgs& a, int64_t i, int64_t n, const int* nb) {
+  v.vec = i + 4 <= n && a.len >= 4;
+  if (!v.vec) return;
+  const int64_t b = seq_of(i, a.len), left = (b + 1) * a.len - i;
+  v.turn = left < 4 ? (int)left : 4;
+  v.on = *reinterpret_cast<const u8x4u*>(a.mask + i);
+  const int64_t b1 = v.turn < 4 ? b + 1 : b;
+  if (nb && a.seq_mean) v.nb0 = nb[b], v.nb1 = nb[b1];
+  if (!a.per_token) v.ab0 = a.adv[b], v.ab1 = a.adv[b1];
+}
+__device__ __forceinline__ bool tokens_any(const Tokens& v) {
+  return v.vec && (v.on[0] | v.on[1] | v.on[2] | v.on[3]);
+}
+__device__ __forceinline__ void tokens_load(Tokens& v, const PolicyArgs& a, int64_t i) {
+  if (!v.vec) return;
+  auto get = [&](const float* p) { return *reinterpret_cast<const f32x4u*>(p + i); };
+  v.lp = get(a.logp);
+  v.old = get(a.old);
+  if (a.ref) v.ref = get(a.ref);
+  if (a.ent) v.ent = get(a.ent);
+  if (a.per_token) v.adv = get(a.adv);
+}
+
+// Their sums (fp32 over four tokens, in weights relative to the first one's, then in double) and gradients; nb: the
+// sequences' counts.
+__device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v, int64_t i, int64_t n, const int* nb,
+                                           double scale, double (&acc)[POL_SUMS]) {
+  auto weigh = [&](double w, float (&f)[POL_SUMS]) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) on[q] = v[q];
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (q < m) on[q] = a.mask[i + q];
-    }
-    if (on[0] | on[1] | on[2] | on[3]) {
-      float lp[4] = {}, old[4] = {}, ref[4] = {}, ent[4] = {}, adv[4] = {};
-      auto get = [&](const float* p, float (&v)[4]) {
-        if (m == 4) {
-          const f32x4u u = *reinterpret_cast<const f32x4u*>(p + i);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] = u[q];
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (q < m) v[q] = p[i + q];
-        }
-      };
-      get(a.logp, lp);
-      get(a.old, old);
-      if (a.ref) get(a.ref, ref);
-      if (a.ent) get(a.ent, ent);
-      if (a.per_token) get(a.adv, adv);
-      double w = token_weight(a, tokens, seqs, nb[b]);
-      float ab = a.per_token ? 0.f : a.adv[b];
+    for (int k = 0; k < POL_SUMS; ++k) acc[k] += w * (double)f[k];
+  };
+  if (v.vec) {
+    f32x4u g = {0.f, 0.f, 0.f, 0.f}, ge = g;
+    if (tokens_any(v)) {
+      // a sequence whose count is 0 has no token here: its weight is not used
+      const double w0 = a.seq_mean ? scale * inverse(max(v.nb0, 1)) : scale;
+      const double w1 = a.seq_mean ? scale * inverse(max(v.nb1, 1)) : scale;
+      const float g0 = (float)(w0 * a.grad_scale), g1 = (float)(w1 * a.grad_scale);
+      const float om = a.seq_mean ? (float)max(v.nb0, 1) * __builtin_amdgcn_rcpf((float)max(v.nb1, 1)) : 1.f;
+      float f[POL_SUMS] = {};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        if (q < m) {
-          if (left == 0) {
-            ++b;
-            left = a.len;
-            w = token_weight(a, tokens, seqs, nb[b]);
-            if (!a.per_token) ab = a.adv[b];
-          }
-          --left;
-          if (on[q]) policy_token(a, lp[q], old[q], a.per_token ? adv[q] : ab, ref[q], ent[q], w, acc, g[q], ge[q]);
-        }
+        const bool first = q < v.turn;
+        const float gw = first ? g0 : g1, ab = first ? v.ab0 : v.ab1;
+        g[q] = v.on[q] ? gw * policy_token(a, v.on[q], first ? 1.f : om, v.lp[q], v.old[q], a.per_token ? v.adv[q] : ab,
+                                           v.ref[q], v.ent[q], f) : 0.f;
+        ge[q] = v.on[q] ? -a.ent_coef * gw : 0.f;
       }
+      weigh(w0, f);
     }
-    auto put = [&](float* p, const float (&v)[4]) {
-      if (m == 4) {
-        *reinterpret_cast<f32x4u*>(p + i) = f32x4u{v[0], v[1], v[2], v[3]};
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < m) p[i + q] = v[q];
-      }
-    };
-    put(a.dlogp, g);
-    if (a.dent) put(a.dent, ge);
+    *reinterpret_cast<f32x4u*>(a.dlogp + i) = g;
+    if (a.dent) *reinterpret_cast<f32x4u*>(a.dent + i) = ge;
+    return;
+  }
+#pragma unroll 1
+  for (int64_t j = i; j < min(i + 4, n); ++j) {
+    float g = 0.f, ge = 0.f;
+    if (a.mask[j]) {
+      const int64_t b = seq_of(j, a.len);
+      const double w = a.seq_mean ? scale * inverse(nb[b]) : scale;
+      const float gw = (float)(w * a.grad_scale);
+      float f[POL_SUMS] = {};
+      g = gw * policy_token(a, true, 1.f, a.logp[j], a.old[j], a.adv[a.per_token ? j : b], a.ref ? a.ref[j] : 0.f,
+                            a.ent ? a.ent[j] : 0.f, f);
+      ge = -a.ent_coef * gw;
+      weigh(w, f);
+    }
+    a.dlogp[j] = g;
+    if (a.dent) a.dent[j] = ge;
   }
 }
 
@@ -195,21 +213,20 @@ __global__ void __launch_bounds__(1024) policy_count(PolicyArgs a, int* nb, int6
   if (a.len >= 16384) {
     __shared__ int part[16];
     for (int64_t b = blockIdx.x; b < a.seqs; b += gridDim.x) {
-      const int c = (int)wave_sum64(count_share<1024>(a.mask + b * a.len, a.len, threadIdx.x));
+      const int c = wave_total(count_share<1024>(a.mask + b * a.len, a.len, threadIdx.x));
       __syncthreads();
       if (lane == 0) part[wave] = c;
       __syncthreads();
-      if (threadIdx.x == 0) {
-        int n = 0;
-        for (int w = 0; w < 16; ++w) n += part[w];
-        nb[b] = n;
+      if (wave == 0) {
+        const int n = wave_total(lane < 16 ? part[lane] : 0);
+        if (lane == 0) nb[b] = n;
         tokens += n;
         seqs += n > 0;
       }
     }
   } else {
     for (int64_t b = (int64_t)blockIdx.x * 16 + wave; b < a.seqs; b += (int64_t)gridDim.x * 16) {
-      const int n = (int)wave_sum64(count_share<WAVE>(a.mask + b * a.len, a.len, lane));
+      const int n = wave_total(count_share<WAVE>(a.mask + b * a.len, a.len, lane));
       if (lane == 0) {
         nb[b] = n;
         tokens += n;
@@ -219,80 +236,153 @@ __global__ void __launch_bounds__(1024) policy_count(PolicyArgs a, int* nb, int6
   }
   if (lane == 0) sm[0][wave] = tokens, sm[1][wave] = seqs;
   __syncthreads();
-  if (threadIdx.x < 2) {
-    int64_t v = 0;
-    for (int w = 0; w < 16; ++w) v += sm[threadIdx.x][w];
-    totals[2 * blockIdx.x + threadIdx.x] = v;
+  if (wave == 0) {
+    tokens = wave_total(lane < 16 ? sm[0][lane] : (int64_t)0);
+    seqs = wave_total(lane < 16 ? sm[1][lane] : (int64_t)0);
+    if (lane == 0) totals[2 * blockIdx.x] = tokens, totals[2 * blockIdx.x + 1] = seqs;
   }
 }
 
-// The sum of the count blocks' totals, in every thread (blockDim.x >= nblk).
+// Totals of the count's blocks (at most a wave's lanes of them), in every thread of full waves.
 __device__ __forceinline__ void policy_totals(const int64_t* totals, int nblk, int64_t& tokens, int64_t& seqs) {
-  __shared__ int64_t sm[2][16];
-  const bool in = (int)threadIdx.x < nblk;
-  const int64_t t = wave_sum64(in ? totals[2 * threadIdx.x] : 0), s = wave_sum64(in ? totals[2 * threadIdx.x + 1] : 0);
-  if (threadIdx.x % WAVE == 0) sm[0][threadIdx.x / WAVE] = t, sm[1][threadIdx.x / WAVE] = s;
-  __syncthreads();
-  tokens = seqs = 0;
-  for (int w = 0; w < (int)blockDim.x / WAVE; ++w) tokens += sm[0][w], seqs += sm[1][w];
+  const int l = threadIdx.x % WAVE;
+  tokens = wave_total(l < nblk ? totals[2 * l] : (int64_t)0);
+  seqs = wave_total(l < nblk ? totals[2 * l + 1] : (int64_t)0);
 }
 
+// The tokens' pass.  EAGER: a thread's tokens are requested together with their mask, one round trip to memory
+// instead of two, where that and not the bytes of the tokens that do not count is what takes time.
+template <bool EAGER>
 __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb, const int64_t* totals, int ncount,
                                                      double* sums) {
   __shared__ double sm[POL_SUMS * 16];
+  const int64_t n = a.seqs * a.len, step = 1024 * (int64_t)gridDim.x;
+  int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  Tokens v = {}, next = {};
+  if (i < n) {
+    tokens_start(v, a, i, n, nb);
+    if (EAGER || tokens_any(v)) tokens_load(v, a, i);
+  }
   int64_t tokens, seqs;
   policy_totals(totals, ncount, tokens, seqs);
+  const double scale = mean_scale(a, tokens, seqs);
   double acc[POL_SUMS] = {};
-  policy_walk(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, nb, (double)tokens, (double)seqs, acc);
+  while (i < n) {
+    const int64_t in = i + step;
+    if (in < n) {  // the next mask is on its way while these tokens are worked on
+      tokens_start(next, a, in, n, nb);
+      if (EAGER) tokens_load(next, a, in);
+    }
+    tokens_run(a, v, i, n, nb, scale, acc);
+    v = next;
+    i = in;
+    if (!EAGER && i < n && tokens_any(v)) tokens_load(v, a, i);
+  }
   block_sums(acc, sm);
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int k = 0; k < POL_SUMS; ++k) sums[POL_SUMS * blockIdx.x + k] = acc[k];
+    for (int k = 0; k < POL_SUMS; ++k) sums[(int64_t)k * gridDim.x + blockIdx.x] = acc[k];
   }
 }
 
-__global__ void __launch_bounds__(256) policy_finish(PolicyArgs a, const int64_t* totals, int ncount, const double* sums,
-                                                     int nblk) {
+__global__ void __launch_bounds__(1024) policy_finish(PolicyArgs a, const int64_t* totals, int ncount, const double* sums,
+                                                      int nblk) {
   __shared__ double sm[POL_SUMS * 16];
+  double acc[POL_SUMS] = {};
+  for (int i = threadIdx.x; i < nblk; i += blockDim.x)
+#pragma unroll
+    for (int k = 0; k < POL_SUMS; ++k) acc[k] += sums[(int64_t)k * nblk + i];
   int64_t tokens, seqs;
   policy_totals(totals, ncount, tokens, seqs);
-  double acc[POL_SUMS] = {};
-  for (int i = threadIdx.x; i < nblk; i += 256)
-#pragma unroll
-    for (int k = 0; k < POL_SUMS; ++k) acc[k] += sums[POL_SUMS * i + k];
   block_sums(acc, sm);
   if (threadIdx.x == 0) policy_out(a, acc, tokens, seqs);
 }
 
-// Few tokens: one block does all of it.
+// Sets nb[0, seqs) in LDS to the tokens that count of every sequence of a mask of n <= 64 blockDim.x bytes,
+// and tot to the totals.  The counts are integers, whose atomic sums have no order.
+__device__ __forceinline__ void count_block(const PolicyArgs& a, int n, int* nb, int* tot) {
+  typedef uint8_t u8x16u __attribute__((ext_vector_type(16), aligned(1)));
+  const int nt = blockDim.x, len = (int)a.len;
+  u8x16u v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {  // all requested at once
+    const int i = 16 * (threadIdx.x + k * nt);
+    if (i + 16 <= n) v[k] = *reinterpret_cast<const u8x16u*>(a.mask + i);
+  }
+  for (int b = threadIdx.x; b < (int)a.seqs; b += nt) nb[b] = 0;
+  if (threadIdx.x < 2) tot[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = 16 * (threadIdx.x + k * nt);
+    if (i < n) {
+      int b = (uint32_t)i / (uint32_t)len, left = (b + 1) * len - i, c = 0;
+      if (i + 16 <= n && left >= 16) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) c += v[k][q] != 0;
+      } else {
+#pragma unroll 1
+        for (int j = i; j < min(i + 16, n); ++j) {
+          if (left == 0) {
+            if (c) atomicAdd(&nb[b], c);
+            ++b, left = len, c = 0;
+          }
+          --left;
+          c += a.mask[j] != 0;
+        }
+      }
+      if (c) atomicAdd(&nb[b], c);
+    }
+  }
+  __syncthreads();
+  int tokens = 0, seqs = 0;
+  for (int b = threadIdx.x; b < (int)a.seqs; b += nt) tokens += nb[b], seqs += nb[b] > 0;
+  tokens = wave_total(tokens);
+  seqs = wave_total(seqs);
+  if (threadIdx.x % WAVE == 0 && tokens > 0) {
+    atomicAdd(&tot[0], tokens);
+    atomicAdd(&tot[1], seqs);
+  }
+  __syncthreads();
+}
+
+// Few tokens: one block does all of it.  A thread's tokens are requested before the counts are known, so that
+// the block waits for memory once.
 __global__ void __launch_bounds__(1024) policy_small(PolicyArgs a) {
-  __shared__ int nb[POL_SMALL_SEQS];
+  __shared__ int nb[POL_SMALL_SEQS], tot[2];
   __shared__ double sm[POL_SUMS * 16];
-  __shared__ int64_t tot[2][16];
-  const int n = (int)(a.seqs * a.len);
-  for (int b = threadIdx.x; b < (int)a.seqs; b += 1024) nb[b] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += 1024)
-    if (a.mask[i]) atomicAdd(&nb[i / (int)a.len], 1);
-  __syncthreads();
-  int64_t tokens = 0, seqs = 0;
-  for (int b = threadIdx.x; b < (int)a.seqs; b += 1024) tokens += nb[b], seqs += nb[b] > 0;
-  tokens = wave_sum64(tokens);
-  seqs = wave_sum64(seqs);
-  if (threadIdx.x % WAVE == 0) tot[0][threadIdx.x / WAVE] = tokens, tot[1][threadIdx.x / WAVE] = seqs;
-  __syncthreads();
-  tokens = seqs = 0;
-  for (int w = 0; w < 16; ++w) tokens += tot[0][w], seqs += tot[1][w];
+  constexpr int PER = POL_SMALL_TOKENS / 4096;
+  const int n = (int)(a.seqs * a.len), nt = blockDim.x;
+  Tokens v[PER] = {};
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = 4 * (threadIdx.x + k * nt);
+    if (i < n) {
+      tokens_start(v[k], a, i, n, nullptr);
+      tokens_load(v[k], a, i);
+    }
+  }
+  count_block(a, n, nb, tot);
   double acc[POL_SUMS] = {};
-  policy_walk(a, threadIdx.x, 1024, nb, (double)tokens, (double)seqs, acc);
+  const double scale = mean_scale(a, tot[0], tot[1]);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = 4 * (threadIdx.x + k * nt);
+    if (i < n) {
+      const int b = (uint32_t)i / (uint32_t)a.len;
+      v[k].nb0 = nb[b];
+      v[k].nb1 = nb[v[k].turn < 4 ? b + 1 : b];
+      tokens_run(a, v[k], i, n, nb, scale, acc);
+    }
+  }
   block_sums(acc, sm);
-  if (threadIdx.x == 0) policy_out(a, acc, tokens, seqs);
+  if (threadIdx.x == 0) policy_out(a, acc, tot[0], tot[1]);
 }
 
 bool policy_is_small(int64_t seqs, int64_t len) { return seqs <= POL_SMALL_SEQS && seqs * len <= POL_SMALL_TOKENS; }
 
 // ------------------------------------------------------------------ preference loss
-constexpr int PREF_SUMS = 6, PREF_SMALL_ROWS = 512, PREF_SMALL_TOKENS = 8192;
+constexpr int PREF_SUMS = 6, PREF_SMALL_ROWS = 512, PREF_SMALL_TOKENS = 8192, PREF_ROWS_PAIRS = 2048;
 
 // Sum of logp - ref over the tokens of [t0, t1) of a row that count, and their number: this thread's share.
 template <int NT>
@@ -324,16 +414,13 @@ __device__ __forceinline__ void pref_share(const PreferenceArgs& a, int64_t row,
   }
 }
 
-// Pair p from its rows' sums and counts: its loss, rewards and terms; coef receives the rows' token gradients
-// apart from the mean's 1 / pairs.
-__device__ __forceinline__ void pref_pair(const PreferenceArgs& a, int64_t p, double sw, int nw, double sl, int nl,
-                                          double (&acc)[PREF_SUMS], double& cw, double& cl) {
+// A pair from its rows' sums and counts: its loss and rewards; its terms go to acc, and cw and cl receive the rows'
+// token gradients apart from the mean's 1 / pairs.
+struct PairOut { float loss, rw, rl; };
+__device__ __forceinline__ PairOut pref_pair(const PreferenceArgs& a, double sw, int nw, double sl, int nl,
+                                             double (&acc)[PREF_SUMS], double& cw, double& cl) {
   cw = cl = 0.0;
-  if (nw == 0 || nl == 0) {
-    a.pair_loss[p] = 0.f;
-    a.rewards[p] = a.rewards[p + a.pairs] = 0.f;
-    return;
-  }
+  if (nw == 0 || nl == 0) return {0.f, 0.f, 0.f};
   if (a.normalize) sw /= nw, sl /= nl;
   const double delta = sw - sl, h = a.beta * delta - a.margin, e = a.smoothing;
   double loss, dh;
@@ -354,15 +441,18 @@ __device__ __forceinline__ void pref_pair(const PreferenceArgs& a, int64_t p, do
   cw = a.beta * dh;
   cl = -cw;
   if (a.normalize) cw /= nw, cl /= nl;
-  a.pair_loss[p] = (float)loss;
-  a.rewards[p] = (float)(a.beta * sw);
-  a.rewards[p + a.pairs] = (float)(a.beta * sl);
   acc[0] += loss;
   acc[1] += delta > 0.0 ? 1.0 : 0.0;
   acc[2] += a.beta * sw;
   acc[3] += a.beta * sl;
   acc[4] += h;
   acc[5] += 1.0;
+  return {(float)loss, (float)(a.beta * sw), (float)(a.beta * sl)};
+}
+__device__ __forceinline__ void pair_out(const PreferenceArgs& a, int64_t p, const PairOut& o) {
+  a.pair_loss[p] = o.loss;
+  a.rewards[p] = o.rw;
+  a.rewards[p + a.pairs] = o.rl;
 }
 
 // 1 / the number the mean divides by
@@ -430,24 +520,29 @@ __global__ void __launch_bounds__(1024) pref_pairs(PreferenceArgs a, int cps, do
   __shared__ double sm[PREF_SUMS * 16];
   __shared__ double scale;
   if (cps > 1) {  // a wave per row joins its chunks (into the first)
-    for (int64_t row = threadIdx.x / WAVE; row < 2 * a.pairs; row += 16) {
+    for (int64_t row = threadIdx.x / WAVE; row < 2 * a.pairs; row += blockDim.x / WAVE) {
       double s = 0.0;
       int64_t n = 0;
       for (int k = threadIdx.x % WAVE; k < cps; k += WAVE) s += sums[row * cps + k], n += ns[row * cps + k];
-      s = wave_sum(s);
-      n = wave_sum64(n);
+      s = wave_total(s);
+      n = wave_total(n);
       if (threadIdx.x % WAVE == 0) sums[row * cps] = s, ns[row * cps] = (int)n;
     }
     __threadfence_block();
     __syncthreads();
   }
-  double acc[PREF_SUMS] = {};
-  for (int64_t p = threadIdx.x; p < a.pairs; p += 1024) {
+  double acc[PREF_SUMS] = {}, cw0 = 0.0, cl0 = 0.0;
+  const int nt = blockDim.x;
+  for (int64_t p = threadIdx.x; p < a.pairs; p += nt) {
     const int64_t w = p * cps, l = (p + a.pairs) * cps;
     double cw, cl;
-    pref_pair(a, p, sums[w], ns[w], sums[l], ns[l], acc, cw, cl);
-    raw[p] = cw;
-    raw[p + a.pairs] = cl;
+    pair_out(a, p, pref_pair(a, sums[w], ns[w], sums[l], ns[l], acc, cw, cl));
+    if (p < nt) {  // a thread's first pair stays in its registers
+      cw0 = cw, cl0 = cl;
+    } else {
+      raw[p] = cw;
+      raw[p + a.pairs] = cl;
+    }
   }
   block_sums(acc, sm);
   if (threadIdx.x == 0) {
@@ -455,14 +550,53 @@ __global__ void __launch_bounds__(1024) pref_pairs(PreferenceArgs a, int cps, do
     scale = pref_scale(a, acc[5]) * a.grad_scale;
   }
   __syncthreads();
-  for (int64_t p = threadIdx.x; p < a.pairs; p += 1024) {
-    coef[p] = (float)(raw[p] * scale);
-    coef[p + a.pairs] = (float)(raw[p + a.pairs] * scale);
+  for (int64_t p = threadIdx.x; p < a.pairs; p += nt) {
+    coef[p] = (float)((p < nt ? cw0 : raw[p]) * scale);
+    coef[p + a.pairs] = (float)((p < nt ? cl0 : raw[p + a.pairs]) * scale);
   }
 }
 
 __global__ void __launch_bounds__(256) pref_tokens(PreferenceArgs a, const float* coef) {
   pref_walk(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, [&](int64_t r) { return coef[r]; });
+}
+
+// The same two steps in one launch, for few pairs of one chunk a row: block b < 2 pairs cpr takes a share of row
+// b / cpr and finds the row's coefficient itself, the last block writes the pairs' outputs.
+__global__ void __launch_bounds__(256) pref_rows(PreferenceArgs a, int cpr, int64_t per, const double* sums,
+                                                 const int* ns) {
+  __shared__ double sm[PREF_SUMS * 16];
+  __shared__ int live[4];
+  const int P = (int)a.pairs;
+  if ((int64_t)blockIdx.x == 2 * a.pairs * cpr) {
+    double acc[PREF_SUMS] = {}, cw, cl;
+    for (int p = threadIdx.x; p < P; p += 256) {
+      const PairOut o = pref_pair(a, sums[p], ns[p], sums[p + P], ns[p + P], acc, cw, cl);
+      pair_out(a, p, o);
+    }
+    block_sums(acc, sm);
+    if (threadIdx.x == 0) pref_out(a, acc);
+    return;
+  }
+  const int64_t row = blockIdx.x / cpr, p = row < P ? row : row - P;
+  const int64_t t0 = (blockIdx.x % cpr) * per, t1 = min(a.len, t0 + per), o = row * a.len;
+  int n = 0;
+  for (int q = threadIdx.x; q < P; q += 256) n += ns[q] > 0 && ns[q + P] > 0;
+  double acc[PREF_SUMS] = {}, cw, cl;
+  pref_pair(a, sums[p], ns[p], sums[p + P], ns[p + P], acc, cw, cl);
+  n = wave_total(n);
+  if (threadIdx.x % WAVE == 0) live[threadIdx.x / WAVE] = n;
+  __syncthreads();
+  n = live[0] + live[1] + live[2] + live[3];
+  const float c = (float)((row < P ? cw : cl) * (pref_scale(a, n) * a.grad_scale));
+  for (int64_t t = t0 + 4 * threadIdx.x; t < t1; t += 1024) {
+    if (t + 4 <= t1) {
+      const u8x4u on = *reinterpret_cast<const u8x4u*>(a.mask + o + t);
+      *reinterpret_cast<f32x4u*>(a.dlogp + o + t) =
+          f32x4u{on[0] ? c : 0.f, on[1] ? c : 0.f, on[2] ? c : 0.f, on[3] ? c : 0.f};
+    } else {
+      for (int64_t u = t; u < t1; ++u) a.dlogp[o + u] = a.mask[o + u] ? c : 0.f;
+    }
+  }
 }
 
 // Few tokens: one block does all of it.
@@ -474,14 +608,14 @@ __global__ void __launch_bounds__(1024) pref_small(PreferenceArgs a) {
     double s = 0.0;
     int n = 0;
     pref_share<WAVE>(a, row, 0, a.len, threadIdx.x % WAVE, s, n);
-    s = wave_sum(s);
-    n = (int)wave_sum64(n);
+    s = wave_total(s);
+    n = wave_total(n);
     if (threadIdx.x % WAVE == 0) sum[row] = s, cnt[row] = n;
   }
   __syncthreads();
   double acc[PREF_SUMS] = {}, cw = 0.0, cl = 0.0;
   const int p = threadIdx.x;
-  if (p < (int)a.pairs) pref_pair(a, p, sum[p], cnt[p], sum[p + a.pairs], cnt[p + a.pairs], acc, cw, cl);
+  if (p < (int)a.pairs) pair_out(a, p, pref_pair(a, sum[p], cnt[p], sum[p + a.pairs], cnt[p + a.pairs], acc, cw, cl));
   block_sums(acc, sm);
   if (threadIdx.x == 0) {
     pref_out(a, acc);
@@ -513,18 +647,22 @@ size_t policy_ws_bytes(int64_t seqs, int64_t len) {
 
 void launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t st) {
   if (policy_is_small(a.seqs, a.len)) {
-    policy_small<<<1, 1024, 0, st>>>(a);
+    const int n = (int)(a.seqs * a.len);
+    policy_small<<<1, (int)std::min<int64_t>(1024, cdiv(std::max(n, 1), 256) * 64), 0, st>>>(a);
     return;
   }
   double* sums = (double*)ws;
   int64_t* totals = (int64_t*)((char*)ws + up256(POL_BLOCKS * POL_SUMS * sizeof(double)));
   int* nb = (int*)((char*)totals + up256(POL_COUNT_BLOCKS * 2 * sizeof(int64_t)));
+  const int nblk = (int)std::min<int64_t>(POL_BLOCKS, cdiv(a.seqs * a.len, 1024)), nt = (int)std::min(1024, (nblk + 63) / 64 * 64);
   const int64_t groups = a.len >= 16384 ? a.seqs : cdiv(a.seqs, 16);
   const int ncount = (int)std::min<int64_t>(POL_COUNT_BLOCKS, groups);
-  const int nblk = (int)std::min<int64_t>(POL_BLOCKS, cdiv(a.seqs * a.len, 1024));
   policy_count<<<ncount, 1024, 0, st>>>(a, nb, totals);
-  policy_tokens<<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
-  policy_finish<<<1, 256, 0, st>>>(a, totals, ncount, sums, nblk);
+  if (a.seqs * a.len <= POL_EAGER_TOKENS)
+    policy_tokens<true><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
+  else
+    policy_tokens<false><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
+  policy_finish<<<1, nt, 0, st>>>(a, totals, ncount, sums, nblk);
 }
 
 size_t preference_ws_bytes(int64_t pairs, int64_t len) {
@@ -546,7 +684,14 @@ void launch_preference_loss(const PreferenceArgs& a, void* ws, hipStream_t st) {
   float* coef = (float*)((char*)raw + up256(n * sizeof(double)));
   const int64_t per = cdiv(cdiv(a.len, cps), 4) * 4;
   pref_sums<<<(unsigned)std::min<int64_t>(1 << 20, (int64_t)c), 256, 0, st>>>(a, cps, per, sums, ns);
-  pref_pairs<<<1, 1024, 0, st>>>(a, cps, sums, ns, raw, coef);
+  const int64_t cpr = std::max<int64_t>(1, cdiv(a.len, 4096));
+  if (cps == 1 && a.pairs <= PREF_ROWS_PAIRS && (int64_t)n * cpr < 1 << 20) {
+    pref_rows<<<(unsigned)(n * cpr + 1), 256, 0, st>>>(a, (int)cpr, 4096, sums, ns);
+    return;
+  }
+  // a thread per pair, or a wave per row where chunks are joined
+  const int nt = (int)std::min<int64_t>(1024, cps > 1 ? 2 * a.pairs * 64 : cdiv(a.pairs, 64) * 64);
+  pref_pairs<<<1, nt, 0, st>>>(a, cps, sums, ns, raw, coef);
   if (a.len > 0)
     pref_tokens<<<(unsigned)std::min<int64_t>(1 << 16, cdiv((int64_t)n * a.len, 1024)), 256, 0, st>>>(a, coef);
 }

@@ -60,7 +60,10 @@ __device__ __forceinline__ void tri_origin(const GemmArgs& g, int b, int& m0, in
 // a residual row added, alpha (A B) + beta D.
 enum { EPI_PLAIN = 0, EPI_SWIGLU_BWD = 1, EPI_ROPE = 2, EPI_SWIGLU_FWD = 3, EPI_DELTA = 4, EPI_RESID = 5,
        EPI_AXPBY = GEMM_EPI_AXPBY, EPI_AXPBY_DUP = GEMM_EPI_AXPBY_DUP, EPI_NS_SPLIT = GEMM_EPI_NS_SPLIT,
-       EPI_ROWSTAT = GEMM_EPI_ROWSTAT };
+       EPI_ROWSTAT = GEMM_EPI_ROWSTAT, EPI_ROWSTAT_F32 = GEMM_EPI_ROWSTAT + 1 };
+// Epilogue 9 on fp32 operands: the same kernel on the same bytes, K and the leading dimensions counted in 2-byte
+// units, so that a 16-deep step of a fragment holds 8 consecutive fp32 of which a lane has 4.
+constexpr bool epi_rowstat(int e) { return e == EPI_ROWSTAT || e == EPI_ROWSTAT_F32; }
 
 // Output chunks leave with non-temporal stores and read-once epilogue operands arrive with
 // non-temporal loads: a product streams 10-150 MB of them through the 4 MB L2 of each XCD, which
@@ -549,7 +552,7 @@ gemm_dma_kernel(GemmArgs g) {
   constexpr int RP = C_::RP, CPP = RP * WN / (sizeof(OutT) == 2 ? 8 : 4);  // 16-byte chunks per part
   static_assert(CPP % 64 == 0, "every lane stores the same number of chunks per part");
   // (RAG: a wave outside C issues none)
-  constexpr int EPI_OPS = RAG || EPI == EPI_ROWSTAT ? 0 : FM * (32 / RP) * (CPP / 64);
+  constexpr int EPI_OPS = RAG || epi_rowstat(EPI) ? 0 : FM * (32 / RP) * (CPP / 64);
   static_assert((NS - 2) * (PA + PB) + EPI_OPS < 64, "vmcnt range");
   extern __shared__ __align__(16) unsigned char smem[];
   bf16* S = reinterpret_cast<bf16*>(smem);  // [NS][A tile | B tile]
@@ -685,11 +688,23 @@ gemm_dma_kernel(GemmArgs g) {
 #pragma unroll
           for (int j = 0; j < FN; ++j) bfr[c ^ 1][j] = TB::frag(bs, wn0 + j * 32, (ks + 1) * 16);
         }
+        if constexpr (EPI == EPI_ROWSTAT_F32) {
+          // v_mfma_f32_32x32x2_f32 q pairs k = q and q + 4 of the 8: what the lanes' halves hold
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+          for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int j = 0; j < FN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[c][i], bfr[c][j], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+              for (int j = 0; j < FN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, af[c][i])[q],
+                                                                 __builtin_bit_cast(f32x4, bfr[c][j])[q], acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[c][i], bfr[c][j], acc[i][j], 0, 0, 0);
+        }
         if constexpr (ks + 1 < BKT / 16) {
           if constexpr (FM * FN >= FM + FN) {  // one MFMA ahead of every fragment read
             static_for<FM + FN>([&](auto) {
@@ -712,7 +727,7 @@ gemm_dma_kernel(GemmArgs g) {
     }
     wait_vm_lds<63>();
     block_barrier();
-    if constexpr (EPI == EPI_ROWSTAT) stat_epilogue<BM, BN, WM, WN, C_::RP>(g, acc, stg, m0, n0, wm0, wn0);
+    if constexpr (epi_rowstat(EPI)) stat_epilogue<BM, BN, WM, WN, C_::RP>(g, acc, stg, m0, n0, wm0, wn0);
     else dma_epilogue<BM, BN, WM, WN, OutT, EPI, C_::RP, RAG>(g, acc, stg, m0, n0, wm0, wn0, t - g.tile0);
     if (!next) break;
     t = tn; m0 = m1; n0 = n1; at = atn; bt = btn;
@@ -1072,28 +1087,41 @@ int rowstat_config(int64_t M, int64_t N) {
   return 8 * r256 <= 5 * r128 ? ROWSTAT_256 : ROWSTAT_128;
 }
 
-template <int BM, int BN, int WM, int WN, int NS>
+template <int BM, int BN, int WM, int WN, int NS, int EPI>
 void launch_rowstat(const GemmArgs& g, hipStream_t st) {
   const int nblk = (int)(cdiv(g.M, BM) * cdiv(g.N, BN));
   if (g.M % BM == 0 && g.N % BN == 0 && g.K % BKT == 0)
-    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI_ROWSTAT, false>(g, nblk, st);
+    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI, false>(g, nblk, st);
   else
-    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI_ROWSTAT, true>(g, nblk, st);
+    launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI, true>(g, nblk, st);
 }
 }  // namespace
 
-int gemm_rowstat_panel(int64_t M, int64_t N) { return rowstat_config(M, N) == ROWSTAT_256 ? 128 : 64; }
+int gemm_rowstat_panel(bool bf, int64_t M, int64_t N) { return bf && rowstat_config(M, N) == ROWSTAT_256 ? 128 : 64; }
 
-bool gemm_rowstat_try(const GemmArgs& g0, hipStream_t st) {
+bool gemm_rowstat_try(bool bf, const GemmArgs& g0, hipStream_t st) {
   GemmArgs g = g0;
   g.out_f32 = true;
   g.epi = 0;
   g.ksplit = 1;
+  if (!bf) g.K *= 2, g.lda *= 2, g.ldb *= 2;
   if (!g.a_kmajor || !g.b_kmajor || !dma_operands(g)) return false;
-  switch (rowstat_config(g.M, g.N)) {
-    case ROWSTAT_32: launch_rowstat<32, 256, 32, 64, 3>(g, st); break;
-    case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2>(g, st); break;
-    default: launch_rowstat<256, 256, 64, 128, 2>(g, st); break;
+  const int config = rowstat_config(g.M, g.N);
+  if (!bf) {
+    // bound by its matrix instructions from few rows on (138 of 157 TFLOP/s at M 8192, N 32000, K 768): what counts is
+    // how evenly the tiles fill the CUs; a tile of 64 x 128 takes 0.53 of one of 128 x 128.  128 against 64 rows, us: M
+    // 1000, N 5000, K 1024 137 : 109; M 100, N 49152, K 2048 263 : 220; M 333, N 32001, K 512 123 : 130; M 8192, N
+    // 32000, K 768 2896 : 2980
+    const int64_t n128 = cdiv(g.N, 128), r128 = cdiv(cdiv(g.M, 128) * n128, 256), r64 = cdiv(cdiv(g.M, 64) * n128, 256);
+    if (config == ROWSTAT_32) launch_rowstat<32, 256, 32, 64, 3, EPI_ROWSTAT_F32>(g, st);
+    else if (53 * r64 < 100 * r128) launch_rowstat<64, 128, 32, 64, 2, EPI_ROWSTAT_F32>(g, st);
+    else launch_rowstat<128, 128, 64, 64, 2, EPI_ROWSTAT_F32>(g, st);
+    return true;
+  }
+  switch (config) {
+    case ROWSTAT_32: launch_rowstat<32, 256, 32, 64, 3, EPI_ROWSTAT>(g, st); break;
+    case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2, EPI_ROWSTAT>(g, st); break;
+    default: launch_rowstat<256, 256, 64, 128, 2, EPI_ROWSTAT>(g, st); break;
   }
   return true;
 }

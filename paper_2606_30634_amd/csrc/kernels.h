@@ -167,11 +167,11 @@ inline bool gemm_batched_tiles(int M, int N, int K) { return M % 128 == 0 && N %
 void launch_axpby(bool bf, void* y, const void* x, float alpha, float beta, int rows, int cols, int ld,
                   hipStream_t st);
 constexpr int GEMM_EPI_ROWSTAT = 9;
-// Columns of a panel of epilogue 9 for a product of these sizes, and the product itself (bf16, both operands
-// k-contiguous): false if the kernels do not take the operands (K, lda, ldb multiples of 8, 16-byte
+// Columns of a panel of epilogue 9 for a product of these sizes, and the product itself (bf16 or fp32, both
+// operands k-contiguous): false if the kernels do not take the operands (rows of whole 16 bytes, 16-byte
 // aligned; gemm_mfma.hip)
-int gemm_rowstat_panel(int64_t M, int64_t N);
-bool gemm_rowstat_try(const GemmArgs& g, hipStream_t st);
+int gemm_rowstat_panel(bool bf, int64_t M, int64_t N);
+bool gemm_rowstat_try(bool bf, const GemmArgs& g, hipStream_t st);
 constexpr int64_t GEMM_WS_ELEMS = 16 << 20;  // 64 MiB of fp32 split-K partials per stage
 void launch_gemm(bool bf, const GemmArgs& g, hipStream_t st);
 

@@ -25,7 +25,7 @@ template <typename T> constexpr int VE = 16 / (int)sizeof(T);
 template <typename T, int N>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[N]) {
   typedef T raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-  const raw r = *reinterpret_cast<const raw*>(p);
+  const raw r = __builtin_nontemporal_load(reinterpret_cast<const raw*>(p));
 #pragma unroll
   for (int q = 0; q < N; ++q) v[q] = to_f32(r[q]);
 }
@@ -35,7 +35,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[N]) {
   raw r;
 #pragma unroll
   for (int q = 0; q < N; ++q) r[q] = from_f32<T>(v[q]);
-  *reinterpret_cast<raw*>(p) = r;
+  __builtin_nontemporal_store(r, reinterpret_cast<raw*>(p));
 }
 
 // Running statistics of a part of a row
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T
 // without a target, without a distribution or with zero upstream gradients gets zeros and is not read.
 // zero_to > V: the columns [V, zero_to) get zeros.  dx may be x (same type and rows): a lane writes only
 // what it has read.
-template <typename T> constexpr int BWD_U = 4;
+template <typename T> constexpr int BWD_U = 2;
 template <typename T, typename OutT>
 __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T* x, int64_t ld,
                                                    const int32_t* __restrict__ tg, const float* __restrict__ stats,
@@ -269,7 +269,10 @@ void logprob_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg
   const int per = (int)(cdiv(cdiv(V, ns), 8) * 8);
   const T* z = (const T*)x;
   Part* parts = (Part*)ws;
-  if (V <= 2048)
+  // A wave per row up to 24 KiB of logits where there are rows for the chip's waves, no exchange between
+  // waves then (16384 rows, a wave : a block, us: bf16 V 4096 29 : 46, 8192 49 : 61, 16000 95 : 109; fp32 V 4096 45 : 56,
+  // 6000 67 : 73, 8192 86 : 81; 2048 rows, bf16 V 6000 10.7 : 9.8)
+  if (V <= 2048 || (rows >= 1024 && (int64_t)V * sizeof(T) <= 24576))
     logprob_rows<T, 64, 4><<<(unsigned)std::min(GRID, cdiv(rows * ns, 4)), 256, 0, st>>>(
         rows, V, z, ld, tg, c, ns, per, parts, logp, ent, stats);
   else
@@ -367,23 +370,20 @@ int64_t head_chunk(int64_t rows, int64_t vocab, int64_t bytes) {
   const int64_t r = bytes / (4 * vocab);
   return std::max<int64_t>(1, std::min(rows, r > 128 ? r / 128 * 128 : r));
 }
-constexpr int64_t HEAD_F32_BYTES = 256 << 20;  // fp32 heads; a chunk stays in the last-level cache
-constexpr int64_t HEAD_ODD_BYTES = 32 << 20;   // bf16 heads of unaligned rows
-
+constexpr int64_t HEAD_ODD_BYTES = 32 << 20;  // logits of heads of unaligned rows, a chunk at a time
 constexpr int64_t HEAD_ROWS = 16384;  // rows of one fused product: bounds its parts' memory
 
-size_t fused_bytes(int64_t n, int64_t vocab) {
-  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(n, vocab)) * n * sizeof(Part);
+size_t fused_bytes(bool bf, int64_t n, int64_t vocab) {
+  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab)) * n * sizeof(Part);
 }
 size_t chunk_bytes(int64_t r, int64_t vocab) { return align256((size_t)(r * vocab * 4)) + logprob_ws_bytes(r, vocab); }
 
 }  // namespace
 
 size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab) {
-  const size_t chunked = chunk_bytes(head_chunk(rows, vocab, bf ? HEAD_ODD_BYTES : HEAD_F32_BYTES), vocab);
-  if (!bf) return chunked;
+  const size_t chunked = chunk_bytes(head_chunk(rows, vocab, HEAD_ODD_BYTES), vocab);
   const int64_t first = std::min(rows, HEAD_ROWS), last = (rows - 1) % HEAD_ROWS + 1;
-  return std::max({fused_bytes(first, vocab), fused_bytes(last, vocab), chunked});
+  return std::max({fused_bytes(bf, first, vocab), fused_bytes(bf, last, vocab), chunked});
 }
 
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
@@ -395,18 +395,18 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
   g.lda = (int)ldx; g.a_kmajor = true;
   g.B = w; g.ldb = (int)ldw; g.b_kmajor = true;
   // the rows' statistics in the product's epilogue, a part per panel of columns
-  bool fused = bf;
+  bool fused = true;
   for (int64_t r0 = 0; fused && r0 < rows; r0 += HEAD_ROWS) {
     const int64_t n = std::min(HEAD_ROWS, rows - r0);
     g.M = (int)n;
-    g.A = (const char*)x + r0 * ldx * 2;
+    g.A = (const char*)x + r0 * ldx * (bf ? 2 : 4);
     g.stat_c = inv_temp * LOG2E;
     g.targets = targets + r0;
     g.stat_xt = (float*)ws;
     g.stats = (Part*)((char*)ws + align256((size_t)n * 4));
-    fused = gemm_rowstat_try(g, st);  // takes all chunks or none: they differ in n alone
+    fused = gemm_rowstat_try(bf, g, st);  // takes all chunks or none: they differ in n alone
     if (!fused) break;
-    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(n, vocab));
+    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab));
     float* e = ent ? ent + r0 : nullptr;
     float* q = stats ? stats + 2 * r0 : nullptr;
     if (n >= 256)
@@ -417,7 +417,7 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
                                                  q);
   }
   if (fused) return;
-  const int64_t r = head_chunk(rows, vocab, bf ? HEAD_ODD_BYTES : HEAD_F32_BYTES);
+  const int64_t r = head_chunk(rows, vocab, HEAD_ODD_BYTES);
   float* logits = (float*)ws;
   void* parts = (char*)ws + align256((size_t)(r * vocab * 4));
   g.C = logits; g.ldc = vocab; g.out_f32 = true; g.beta = 0.f;

@@ -193,7 +193,7 @@ int stage_backward(stage_t* s, int32_t slot, const void* dy, void* dx_out,
 /* The last stage under a loss on the log-probabilities of its targets instead of the mean cross-entropy
  * (reward or preference fine-tuning; the losses are policy_loss and preference_loss below).
  * stage_forward_logprob is stage_forward up to the logits, then
- *   logp     [micro_batch, seq_len] fp32, device: log-probability of each target at inv_temperature > 0
+ *   logp     [micro_batch, seq_len] fp32, device: log-probability of each target at inv_temperature in (0, 2^60]
  *            (token_logprob's rules; a target outside [0, vocab) is ignored: 0)
  *   entropy  the same shape, or NULL
  * and leaves the slot pending for stage_backward_logprob, which takes
@@ -311,8 +311,8 @@ int hbm_stream_copy(void* dst, const void* src, size_t bytes, void* hip_stream);
  * their operator refuses.  Results are the same bit for bit from call to call.
  */
 
-/* Log-probability of targets[r] under row r of logits, at inv_temperature s > 0: log p = s (x_t - m) -
- * log S with m the row's largest logit and S = sum_j exp(s (x_j - m)), and the entropy H = -sum p log p.
+/* Log-probability of targets[r] under row r of logits, at inv_temperature s in (0, 2^60]: log p =
+ * s (x_t - m) - log S with m the row's largest logit and S = sum_j exp(s (x_j - m)), and the entropy H = -sum p log p.
  *   logits      [rows, vocab] fp32, or bf16 when logits_bf16; rows ld >= vocab elements apart;
  *               vocab in [1, 2^24], ld <= 2^28
  *   targets     [rows] int32; a row whose target is outside [0, vocab) is ignored: its logits are not

@@ -230,24 +230,27 @@ def token_logprob_workspace_bytes(rows, vocab) -> int:
 
 def token_logprob(rows, vocab, logits, ld, logits_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
                   workspace_bytes, stream) -> None:
-    _call("token_logprob", rows, vocab, logits, ld, int(logits_bf16), targets, inv_temperature, logp, entropy, stats,
-          workspace, workspace_bytes, stream)
+    check("token_logprob", LIB.token_logprob(
+        rows, vocab, logits, ld, logits_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
+        workspace_bytes, stream))
 
 
 def token_logprob_backward(rows, vocab, logits, ld, logits_bf16, targets, stats, entropy, dlogp, dentropy,
                            inv_temperature, dlogits, ld_out, out_bf16, stream) -> None:
-    _call("token_logprob_backward", rows, vocab, logits, ld, int(logits_bf16), targets, stats, entropy, dlogp,
-          dentropy, inv_temperature, dlogits, ld_out, int(out_bf16), stream)
+    check("token_logprob_backward", LIB.token_logprob_backward(
+        rows, vocab, logits, ld, logits_bf16, targets, stats, entropy, dlogp, dentropy, inv_temperature, dlogits,
+        ld_out, out_bf16, stream))
 
 
 def head_logprob_workspace_bytes(rows, vocab, d, is_bf16) -> int:
-    return LIB.head_logprob_workspace_bytes(rows, vocab, d, int(is_bf16))
+    return LIB.head_logprob_workspace_bytes(rows, vocab, d, is_bf16)
 
 
 def head_logprob(rows, vocab, d, x, ldx, w, ldw, is_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
                  workspace_bytes, stream) -> None:
-    _call("head_logprob", rows, vocab, d, x, ldx, w, ldw, int(is_bf16), targets, inv_temperature, logp, entropy,
-          stats, workspace, workspace_bytes, stream)
+    check("head_logprob", LIB.head_logprob(
+        rows, vocab, d, x, ldx, w, ldw, is_bf16, targets, inv_temperature, logp, entropy, stats, workspace,
+        workspace_bytes, stream))
 
 
 def policy_loss_workspace_bytes(seqs, length) -> int:
@@ -256,8 +259,9 @@ def policy_loss_workspace_bytes(seqs, length) -> int:
 
 def policy_loss(seqs, length, logp, old_logp, ref_logp, entropy, advantages, mask, hp: PolicyHParams, loss, dlogp,
                 dentropy, metrics, counts, workspace, workspace_bytes, stream) -> None:
-    _call("policy_loss", seqs, length, logp, old_logp, ref_logp, entropy, advantages, mask, C.byref(hp), loss, dlogp,
-          dentropy, metrics, counts, workspace, workspace_bytes, stream)
+    check("policy_loss", LIB.policy_loss(
+        seqs, length, logp, old_logp, ref_logp, entropy, advantages, mask, C.byref(hp), loss, dlogp, dentropy,
+        metrics, counts, workspace, workspace_bytes, stream))
 
 
 def preference_loss_workspace_bytes(pairs, length) -> int:
@@ -266,8 +270,9 @@ def preference_loss_workspace_bytes(pairs, length) -> int:
 
 def preference_loss(pairs, length, logp, ref_logp, mask, hp: PreferenceHParams, loss, dlogp, pair_loss, rewards,
                     metrics, counts, workspace, workspace_bytes, stream) -> None:
-    _call("preference_loss", pairs, length, logp, ref_logp, mask, C.byref(hp), loss, dlogp, pair_loss, rewards,
-          metrics, counts, workspace, workspace_bytes, stream)
+    check("preference_loss", LIB.preference_loss(
+        pairs, length, logp, ref_logp, mask, C.byref(hp), loss, dlogp, pair_loss, rewards, metrics, counts, workspace,
+        workspace_bytes, stream))
 
 
 def stage_embed_indices(s: int, slot: int, ids, counts, n_unique) -> None:

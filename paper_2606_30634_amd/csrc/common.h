@@ -114,6 +114,10 @@ __device__ __forceinline__ void wait_vm_lds() {
 __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds) {
   asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "{m0}"(lds) : "memory");
 }
+// The same for data that is read once: it leaves the caches first.
+__device__ __forceinline__ void dma16_once(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("global_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(base), "{m0}"(lds) : "memory");
+}
 // The same with 4 bytes per lane (lane l writes lds + 4 l).
 __device__ __forceinline__ void dma4(const void* base, uint32_t voff, uint32_t lds) {
   asm volatile("global_load_lds_dword %0, %1" ::"v"(voff), "s"(base), "{m0}"(lds) : "memory");
@@ -131,6 +135,9 @@ __device__ __forceinline__ u32x4 buffer_range(const void* base, const void* end)
 }
 __device__ __forceinline__ void dma16_range(u32x4 range, uint32_t voff, uint32_t lds) {
   asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(range), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void dma16_range_once(u32x4 range, uint32_t voff, uint32_t lds) {
+  asm volatile("buffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(range), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void dma4_range(u32x4 range, uint32_t voff, uint32_t lds) {
   asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(range), "{m0}"(lds) : "memory");

@@ -60,10 +60,12 @@ __device__ __forceinline__ void tri_origin(const GemmArgs& g, int b, int& m0, in
 // a residual row added, alpha (A B) + beta D.
 enum { EPI_PLAIN = 0, EPI_SWIGLU_BWD = 1, EPI_ROPE = 2, EPI_SWIGLU_FWD = 3, EPI_DELTA = 4, EPI_RESID = 5,
        EPI_AXPBY = GEMM_EPI_AXPBY, EPI_AXPBY_DUP = GEMM_EPI_AXPBY_DUP, EPI_NS_SPLIT = GEMM_EPI_NS_SPLIT,
-       EPI_ROWSTAT = GEMM_EPI_ROWSTAT, EPI_ROWSTAT_F32 = GEMM_EPI_ROWSTAT + 1 };
-// Epilogue 9 on fp32 operands: the same kernel on the same bytes, K and the leading dimensions counted in 2-byte
-// units, so that a 16-deep step of a fragment holds 8 consecutive fp32 of which a lane has 4.
-constexpr bool epi_rowstat(int e) { return e == EPI_ROWSTAT || e == EPI_ROWSTAT_F32; }
+       EPI_ROWSTAT = GEMM_EPI_ROWSTAT, ROWSTAT_F32 = 1, ROWSTAT_ONCE = 2 };
+// Epilogue 9 has two flags on top.  F32: fp32 operands, the same kernel on the same bytes, K and the leading
+// dimensions counted in 2-byte units, so that a 16-deep step of a fragment holds 8 consecutive fp32 of which a
+// lane has 4.  ONCE: B is read once (one row tile) and is loaded past the caches.
+constexpr bool epi_rowstat(int e) { return e >= EPI_ROWSTAT; }
+constexpr bool epi_rowstat_flag(int e, int f) { return epi_rowstat(e) && ((e - EPI_ROWSTAT) & f) != 0; }
 
 // Output chunks leave with non-temporal stores and read-once epilogue operands arrive with
 // non-temporal loads: a product streams 10-150 MB of them through the 4 MB L2 of each XCD, which
@@ -607,6 +609,7 @@ gemm_dma_kernel(GemmArgs g) {
                                           : (int64_t)(g.K - 1) * g.lda + (g.a_padded ? g.lda : g.M));
   const bf16* eb = (const bf16*)g.B + (BKM ? (int64_t)(glu ? 2 * g.glu - 1 : g.N - 1) * g.ldb + g.K
                                            : (int64_t)(g.K - 1) * g.ldb + g.N);
+  constexpr bool ONCE = epi_rowstat_flag(EPI, ROWSTAT_ONCE);
   int kca, kcb, r_;
   static_assert(BKT == 64 && NW % 4 == 0, "one k chunk per thread");
   TA::row_chunk(wave * 64 + lane, r_, kca);
@@ -622,12 +625,18 @@ gemm_dma_kernel(GemmArgs g) {
 #pragma unroll
       for (int q = 0; q < PA; ++q) dma16_range(ra, outa ? BUFFER_OUT : oa[q], ta + q * NW * 1024);
 #pragma unroll
-      for (int q = 0; q < PB; ++q) dma16_range(rb, outb ? BUFFER_OUT : ob[q], tb + q * NW * 1024);
+      for (int q = 0; q < PB; ++q) {
+        if constexpr (ONCE) dma16_range_once(rb, outb ? BUFFER_OUT : ob[q], tb + q * NW * 1024);
+        else dma16_range(rb, outb ? BUFFER_OUT : ob[q], tb + q * NW * 1024);
+      }
     } else {
 #pragma unroll
       for (int q = 0; q < PA; ++q) dma16(as, oa[q], ta + q * NW * 1024);
 #pragma unroll
-      for (int q = 0; q < PB; ++q) dma16(bs, ob[q], tb + q * NW * 1024);
+      for (int q = 0; q < PB; ++q) {
+        if constexpr (ONCE) dma16_once(bs, ob[q], tb + q * NW * 1024);
+        else dma16(bs, ob[q], tb + q * NW * 1024);
+      }
     }
   };
 
@@ -688,7 +697,7 @@ gemm_dma_kernel(GemmArgs g) {
 #pragma unroll
           for (int j = 0; j < FN; ++j) bfr[c ^ 1][j] = TB::frag(bs, wn0 + j * 32, (ks + 1) * 16);
         }
-        if constexpr (EPI == EPI_ROWSTAT_F32) {
+        if constexpr (epi_rowstat_flag(EPI, ROWSTAT_F32)) {
           // v_mfma_f32_32x32x2_f32 q pairs k = q and q + 4 of the 8: what the lanes' halves hold
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -1076,7 +1085,7 @@ bool gemm_mfma_try(const GemmArgs& g0, hipStream_t st) {
 // ------------------------------------------------------------------ row statistics (epilogue 9)
 namespace {
 // Tiles of the statistics product.  Up to 32 rows it streams W: 32 x 256 tiles in 3 stages, two blocks per
-// CU (one row, d 4096, N 128256: 173.5 us, 6.1 TB/s; 32 x 128 in 4 stages 181, 128 x 128 179).  Above, rounds
+// CU (one row, d 4096, N 128256: 173.5 us; 32 x 128 in 4 stages 181, 128 x 128 179).  Above, rounds
 // decide: a round of 256 blocks of 256 x 256 takes 1.5 to 1.75 times one of 512 of 128 x 128.  128 against
 // 256, us: N 32000, K 768: M 256 23 : 30, M 512 38 : 35; N 49152, K 2048: M 256 63 : 58, M 512 105 : 107, M 8192
 // 1609 : 1370; N 128256, K 4096: M 128 198 : 250, M 256 342 : 274; N 4000, K 512: M 2048 20 : 26, M 8192 56 : 49.
@@ -1087,13 +1096,21 @@ int rowstat_config(int64_t M, int64_t N) {
   return 8 * r256 <= 5 * r128 ? ROWSTAT_256 : ROWSTAT_128;
 }
 
-template <int BM, int BN, int WM, int WN, int NS, int EPI>
+template <int BM, int BN, int WM, int WN, int NS, int FLAGS>
 void launch_rowstat(const GemmArgs& g, hipStream_t st) {
   const int nblk = (int)(cdiv(g.M, BM) * cdiv(g.N, BN));
+  constexpr int EPI = EPI_ROWSTAT + FLAGS;
   if (g.M % BM == 0 && g.N % BN == 0 && g.K % BKT == 0)
     launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI, false>(g, nblk, st);
   else
     launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI, true>(g, nblk, st);
+}
+template <int FLAGS>
+void launch_rowstat_32(const GemmArgs& g, hipStream_t st) {
+  // past the caches where W is more than half of the last one (N 128256, K 4096, 1 row: 180 -> 165 us, 6.4 TB/s; N
+  // 49152, K 2048: 52 -> 48; but N 32000, K 768, 49 MB: 18 -> 19.5 with the matrix in use again and again)
+  if ((int64_t)g.N * g.K * 2 > 128 << 20) launch_rowstat<32, 256, 32, 64, 3, FLAGS + ROWSTAT_ONCE>(g, st);
+  else launch_rowstat<32, 256, 32, 64, 3, FLAGS>(g, st);
 }
 }  // namespace
 
@@ -1113,15 +1130,15 @@ bool gemm_rowstat_try(bool bf, const GemmArgs& g0, hipStream_t st) {
     // 1000, N 5000, K 1024 137 : 109; M 100, N 49152, K 2048 263 : 220; M 333, N 32001, K 512 123 : 130; M 8192, N
     // 32000, K 768 2896 : 2980
     const int64_t n128 = cdiv(g.N, 128), r128 = cdiv(cdiv(g.M, 128) * n128, 256), r64 = cdiv(cdiv(g.M, 64) * n128, 256);
-    if (config == ROWSTAT_32) launch_rowstat<32, 256, 32, 64, 3, EPI_ROWSTAT_F32>(g, st);
-    else if (53 * r64 < 100 * r128) launch_rowstat<64, 128, 32, 64, 2, EPI_ROWSTAT_F32>(g, st);
-    else launch_rowstat<128, 128, 64, 64, 2, EPI_ROWSTAT_F32>(g, st);
+    if (config == ROWSTAT_32) launch_rowstat_32<ROWSTAT_F32>(g, st);
+    else if (53 * r64 < 100 * r128) launch_rowstat<64, 128, 32, 64, 2, ROWSTAT_F32>(g, st);
+    else launch_rowstat<128, 128, 64, 64, 2, ROWSTAT_F32>(g, st);
     return true;
   }
   switch (config) {
-    case ROWSTAT_32: launch_rowstat<32, 256, 32, 64, 3, EPI_ROWSTAT>(g, st); break;
-    case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2, EPI_ROWSTAT>(g, st); break;
-    default: launch_rowstat<256, 256, 64, 128, 2, EPI_ROWSTAT>(g, st); break;
+    case ROWSTAT_32: launch_rowstat_32<0>(g, st); break;
+    case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2, 0>(g, st); break;
+    default: launch_rowstat<256, 256, 64, 128, 2, 0>(g, st); break;
   }
   return true;
 }

@@ -92,8 +92,9 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, bool on, floa
   const float xf = (float)x, r = expf(xf);
   const bool rise = adv > 0.f && x > a.log_hi, fall = adv < 0.f && x < a.log_lo, cut = rise || fall;
   const float held = rise ? 1.f + a.clip_high : fall ? 1.f - a.clip_low : r;
-  float d = cut ? 0.f : -r * adv;
-  f[0] -= on ? om * (held * adv) : 0.f;
+  const float ra = adv == 0.f ? 0.f : held * adv;  // no advantage: nothing, also where e^x is past the type
+  float d = cut ? 0.f : -ra;
+  f[0] -= on ? om * ra : 0.f;
   f[3] += on && cut ? om : 0.f;
   f[4] += on ? om * kl_term(xf, r) : 0.f;
   f[5] += on ? om * r : 0.f;

@@ -48,7 +48,7 @@ bool preference_sizes(int64_t pairs, int64_t len) {
 const char* check_rows(int64_t rows, int64_t vocab, const int32_t* targets, float s, const float* logp,
                        const float* entropy, const float* stats) {
   if (!row_sizes(rows, vocab)) return "rows must be in [0, 2^31), vocab in [1, 2^24]";
-  if (!(s > 0.f) || !std::isfinite(s)) return "inv_temperature must be positive and finite";
+  if (!(s > 0.f && s <= 0x1p60f)) return "inv_temperature must be in (0, 2^60]";
   if (rows > 0 && (!targets || !logp)) return "null targets or logp";
   if (off(targets, 4) || off(logp, 4) || off(entropy, 4) || off(stats, 4)) return "arrays must be 4-byte aligned";
   return nullptr;

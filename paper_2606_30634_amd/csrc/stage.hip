@@ -893,8 +893,8 @@ int check_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
 int check_logprob(stage_t* s, const int32_t* targets, float inv_temperature, const float* logp) {
   if (!s->sh.last_stage) return fail(STAGE_EINVAL, "log-probabilities need a last stage");
   if (!targets || !logp) return fail(STAGE_EINVAL, "null targets or logp");
-  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature))
-    return fail(STAGE_EINVAL, "inv_temperature must be positive and finite");
+  if (!(inv_temperature > 0.f && inv_temperature <= 0x1p60f))
+    return fail(STAGE_EINVAL, "inv_temperature must be in (0, 2^60]");
   return STAGE_OK;
 }
 

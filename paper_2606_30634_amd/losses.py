@@ -51,7 +51,7 @@ class PreferenceLoss(NamedTuple):
 
 
 def _require(name, t, dev, dtype, shape):
-    if t.device != dev or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -71,7 +71,8 @@ def _rows(name, t, dev=None):
 def _out(name, t, dev, dtype, shape):
     if t is None:
         return torch.empty(shape, dtype=dtype, device=dev)
-    _require("out." + name, t, dev, dtype, torch.Size(shape))
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        _require("out." + name, t, dev, dtype, torch.Size(shape))
     return t
 
 

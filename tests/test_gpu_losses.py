@@ -293,6 +293,19 @@ def test_policy_loss(b, s, reduction):
         assert all(x is y is None or torch.equal(x, y) for x, y in zip(got, again))
 
 
+def test_policy_loss_of_ratios_past_the_type():
+    """e^x overflows: a clipped token and one with no advantage stay finite, and so does the loss of the
+    others' sequence."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    x, _ = _f32(np.array([[100.0, 0.1, 0.0, 0.0], [100.0, -0.1, 0.0, 0.0]]))
+    adv, _ = _f32(np.array([[2.0, 1.0, 0.0, 0.0], [0.0, 1.0, 0.0, 0.0]]))
+    out = losses.policy_loss(x, torch.zeros_like(x), adv, torch.ones(2, 4, dtype=torch.bool, device="cuda:0"))
+    want = -(1.2 * 2.0 + np.exp(0.1) + np.exp(-0.1)) / 8
+    assert abs(float(out.loss) - want) < 1e-6 and float(out.metrics[0]) == float(out.loss)
+    assert torch.isfinite(out.dlogp).all() and float(out.dlogp[0, 0]) == 0 and float(out.dlogp[1, 0]) == 0
+
+
 def test_policy_loss_at_the_clip():
     """Tokens a rounding away from the clip on either side, and far ratios: the side is that of the exact
     difference of the two log-probabilities."""

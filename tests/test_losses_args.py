@@ -31,7 +31,7 @@ FWD = dict(rows=4, vocab=100, logits=P, ld=100, bf=0, targets=P, s=1.0, logp=Q, 
 @pytest.mark.parametrize("bad", [dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(ld=99),
                                  dict(ld=(1 << 28) + 1), dict(logits=None), dict(logits=P + 2), dict(targets=None),
                                  dict(targets=P + 1), dict(logp=None), dict(ent=Q + 2), dict(stats=Q + 1), dict(s=0.0),
-                                 dict(s=-1.0), dict(s=math.inf), dict(s=math.nan), dict(bf=1, logits=P + 1)])
+                                 dict(s=-1.0), dict(s=math.inf), dict(s=math.nan), dict(s=2.0 ** 61), dict(bf=1, logits=P + 1)])
 def test_token_logprob_refuses(bad):
     _refused(B.token_logprob, *_with(FWD, **bad))
 

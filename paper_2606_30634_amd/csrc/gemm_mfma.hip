@@ -378,13 +378,14 @@ __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[W
   if (c0 >= g.N) return;  // no column of the wave is in C
   const bool edge = c0 + WN > g.N;
   float* stg = stage + wave * RP * EP;
-  const int64_t panel = (int64_t)(c0 / WN) * g.M;
+  const int64_t panel = (int64_t)(c0 / WN) * g.stat_ld;
+  const int rows = (int)min((int64_t)g.M, g.stat_ld);  // packed rows reach up to a whole tile
   const float c = g.stat_c;
   int tgt[NPART];
 #pragma unroll
   for (int p = 0; p < NPART; ++p) {
     const int row = m0 + wm0 + (p / NP) * 32 + RP * (p % NP) + r;
-    tgt[p] = row < g.M ? g.targets[row] : -1;
+    tgt[p] = row < rows ? g.targets[row] : -1;
   }
   static_for<NPART>([&](auto P) {
     constexpr int p = P, i = p / NP, h = p % NP;
@@ -426,7 +427,7 @@ __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[W
       s += __shfl_xor(s, o, 64);
       w += __shfl_xor(w, o, 64);
     }
-    if (k == 0 && row < g.M) g.stats[panel + row] = RowPart{m, s, w};
+    if (k == 0 && row < rows) g.stats[panel + row] = RowPart{m, s, w};
   });
 }
 
@@ -544,6 +545,14 @@ gemm_dma_kernel(GemmArgs g) {
     g.C = (char*)g.C + z * g.sC * (int64_t)sizeof(OutT);
     if (g.D) g.D = (const OutT*)g.D + z * g.sD;
   }
+  if constexpr (epi_rowstat(EPI)) {
+    if (g.live && *g.live < g.M) {  // the rows that count, packed
+      g.A = g.A2;
+      g.lda = g.lda2;
+      g.targets = g.targets2;
+      g.M = (*g.live + BM - 1) / BM * BM;
+    }
+  }
   using C_ = DmaCfg<BM, BN, WM, WN, AK, BKM, BKT, NS>;
   using TA = typename C_::TA;
   using TB = typename C_::TB;
@@ -642,6 +651,7 @@ gemm_dma_kernel(GemmArgs g) {
 
   const int tile_end = g.tile_n > 0 ? g.tile0 + g.tile_n : tiles;
   int t = g.tile0 + blockIdx.x;
+  if (epi_rowstat(EPI) && t >= tile_end) return;  // fewer tiles than the launch was made for
   int m0, n0;
   origin(t, m0, n0);
   const bf16* at = a_tile(m0);
@@ -1116,13 +1126,18 @@ void launch_rowstat_32(const GemmArgs& g, hipStream_t st) {
 
 int gemm_rowstat_panel(bool bf, int64_t M, int64_t N) { return bf && rowstat_config(M, N) == ROWSTAT_256 ? 128 : 64; }
 
-bool gemm_rowstat_try(bool bf, const GemmArgs& g0, hipStream_t st) {
-  GemmArgs g = g0;
+static GemmArgs rowstat_args(bool bf, GemmArgs g) {
   g.out_f32 = true;
   g.epi = 0;
   g.ksplit = 1;
-  if (!bf) g.K *= 2, g.lda *= 2, g.ldb *= 2;
-  if (!g.a_kmajor || !g.b_kmajor || !dma_operands(g)) return false;
+  if (!bf) g.K *= 2, g.lda *= 2, g.ldb *= 2, g.lda2 *= 2;
+  return g;
+}
+
+bool gemm_rowstat_takes(bool bf, const GemmArgs& g) { return g.a_kmajor && g.b_kmajor && dma_operands(rowstat_args(bf, g)); }
+
+void gemm_rowstat(bool bf, const GemmArgs& g0, hipStream_t st) {
+  const GemmArgs g = rowstat_args(bf, g0);
   const int config = rowstat_config(g.M, g.N);
   if (!bf) {
     // bound by its matrix instructions from few rows on (138 of 157 TFLOP/s at M 8192, N 32000, K 768): what counts is
@@ -1133,12 +1148,11 @@ bool gemm_rowstat_try(bool bf, const GemmArgs& g0, hipStream_t st) {
     if (config == ROWSTAT_32) launch_rowstat_32<ROWSTAT_F32>(g, st);
     else if (53 * r64 < 100 * r128) launch_rowstat<64, 128, 32, 64, 2, ROWSTAT_F32>(g, st);
     else launch_rowstat<128, 128, 64, 64, 2, ROWSTAT_F32>(g, st);
-    return true;
+    return;
   }
   switch (config) {
     case ROWSTAT_32: launch_rowstat_32<0>(g, st); break;
     case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2, 0>(g, st); break;
     default: launch_rowstat<256, 256, 64, 128, 2, 0>(g, st); break;
   }
-  return true;
 }

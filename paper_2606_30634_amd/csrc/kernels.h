@@ -146,12 +146,19 @@ struct GemmArgs {
   int sym = 0;
   // epilogue 9 (row statistics): nothing of the product is stored.  Per row and panel of
   // gemm_rowstat_panel() columns, panel p of row m writes its maximum x0 and the sums of 2^t and of
-  // t 2^t, t = stat_c (x - x0), to stats[p M + m], and the row's logit of column targets[m] goes to
+  // t 2^t, t = stat_c (x - x0), to stats[p stat_ld + m], and the row's logit of column targets[m] goes to
   // stat_xt[m] (nothing where targets[m] is outside [0, N)).
   RowPart* stats = nullptr;
   float stat_c = 0.f;
   const int32_t* targets = nullptr;
   float* stat_xt = nullptr;
+  int64_t stat_ld = 0;  // rows of a panel: M, or what it was before packing
+  // live: a count in device memory.  When it is below M, the product is that of the first *live rows of A2
+  // (row stride lda2, zeros up to a multiple of 256 rows) with targets2 instead of A and targets
+  const int32_t* live = nullptr;
+  const void* A2 = nullptr;
+  int lda2 = 0;
+  const int32_t* targets2 = nullptr;
 };
 constexpr int GEMM_EPI_AXPBY = 6;
 // epilogue 7 (AXPBY with duplicated columns): C[r, 2c] = C[r, 2c + 1] = alpha (A B)[r, c] +
@@ -167,11 +174,11 @@ inline bool gemm_batched_tiles(int M, int N, int K) { return M % 128 == 0 && N %
 void launch_axpby(bool bf, void* y, const void* x, float alpha, float beta, int rows, int cols, int ld,
                   hipStream_t st);
 constexpr int GEMM_EPI_ROWSTAT = 9;
-// Columns of a panel of epilogue 9 for a product of these sizes, and the product itself (bf16 or fp32, both
-// operands k-contiguous): false if the kernels do not take the operands (rows of whole 16 bytes, 16-byte
-// aligned; gemm_mfma.hip)
+// Columns of a panel of epilogue 9 for a product of these sizes; whether the kernels take its operands (bf16 or
+// fp32, both k-contiguous, rows of whole 16 bytes, 16-byte aligned); and the product (gemm_mfma.hip)
 int gemm_rowstat_panel(bool bf, int64_t M, int64_t N);
-bool gemm_rowstat_try(bool bf, const GemmArgs& g, hipStream_t st);
+bool gemm_rowstat_takes(bool bf, const GemmArgs& g);
+void gemm_rowstat(bool bf, const GemmArgs& g, hipStream_t st);
 constexpr int64_t GEMM_WS_ELEMS = 16 << 20;  // 64 MiB of fp32 split-K partials per stage
 void launch_gemm(bool bf, const GemmArgs& g, hipStream_t st);
 
@@ -251,7 +258,7 @@ void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, in
                         const float* stats, const float* ent, const float* dlogp, const float* dent, float inv_temp,
                         bool out_bf, void* dlogits, int64_t ldo, int zero_to, hipStream_t st);
 // launch_logprob of the logits x W^T (x [rows, d], W [vocab, d], rows of ldx and ldw elements)
-size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab);
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d);
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
                          int64_t ldw, const int32_t* targets, float inv_temp, float* logp, float* ent, float* stats,
                          void* ws, hipStream_t st);

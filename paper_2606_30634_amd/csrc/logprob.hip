@@ -322,27 +322,77 @@ void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, in
 // ------------------------------------------------------------------ from hidden states
 namespace {
 
-// Joins the panels of every row (parts[p rows + row]): RJ rows per block of 256, 256 / RJ threads on each.
+// Packing: the rows whose target is in the vocabulary, in order.  pos[r] is a row's place among them (-1: it has none),
+// live[0] their number.  One block; a thread takes a run of rows.
+__global__ void __launch_bounds__(1024) pack_rows(int rows, int V, const int32_t* __restrict__ tg, int32_t* __restrict__ pos,
+                                                  int32_t* __restrict__ live) {
+  __shared__ int base[16];
+  const int per = (rows + 1023) / 1024, r0 = threadIdx.x * per, r1 = min(rows, r0 + per);
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  int n = 0;
+  for (int r = r0; r < r1; ++r) n += tg[r] >= 0 && tg[r] < V;
+  int at = n;  // inclusive sum over the wave's lanes, then over the waves
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) {
+    const int v = __shfl_up(at, o, WAVE);
+    if (lane >= o) at += v;
+  }
+  if (lane == WAVE - 1) base[wave] = at;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < 16; ++w) before += w < wave ? base[w] : 0, all += base[w];
+  at += before - n;
+  for (int r = r0; r < r1; ++r) pos[r] = tg[r] >= 0 && tg[r] < V ? at++ : -1;
+  if (threadIdx.x == 0) live[0] = all;
+}
+
+// Copies the rows of x (16-byte chunks) that have a place there, with their targets, and clears the rows after them
+// up to a multiple of 256; nothing to do where every row has one.
+__global__ void __launch_bounds__(256) gather_rows(int rows, int chunks, const u32x4* __restrict__ x, int64_t ldx,
+                                                   const int32_t* __restrict__ tg, const int32_t* __restrict__ pos,
+                                                   const int32_t* __restrict__ live, u32x4* __restrict__ xp,
+                                                   int32_t* __restrict__ tp) {
+  const int n = live[0], r = blockIdx.x * 4 + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+  if (n == rows) return;
+  if (r < rows) {
+    const int p = pos[r];
+    if (p < 0) return;
+    for (int k = lane; k < chunks; k += WAVE) xp[(int64_t)p * chunks + k] = x[r * ldx + k];
+    if (lane == 0) tp[p] = tg[r];
+  } else {
+    const int p = n + r - rows;
+    if (p >= (n + 255) / 256 * 256) return;
+    for (int k = lane; k < chunks; k += WAVE) xp[(int64_t)p * chunks + k] = u32x4{0, 0, 0, 0};
+    if (lane == 0) tp[p] = -1;
+  }
+}
+
+// Joins the panels of every row (parts[p rows + row], or of its place where rows are packed): RJ rows per block of
+// 256, 256 / RJ threads on each.
 template <int RJ>
 __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panels, const int32_t* __restrict__ tg, float c,
                                                   const Part* __restrict__ parts, const float* __restrict__ xt,
+                                                  const int32_t* __restrict__ pos, const int32_t* __restrict__ live,
                                                   float* __restrict__ logp, float* __restrict__ ent,
                                                   float* __restrict__ stats) {
   constexpr int TR = 256 / RJ;  // threads per row
   __shared__ Part sm[4 * RJ];
   const int r = threadIdx.x % RJ, k = threadIdx.x / RJ;
   const int64_t row = (int64_t)blockIdx.x * RJ + r;
+  const int t = row < rows ? tg[row] : -1;
+  const bool on = t >= 0 && t < V;
+  const int64_t at = !on ? 0 : pos && *live < rows ? pos[row] : row;
   Part a = part_empty();
-  if (row < rows) {
+  if (on) {
     int p = k;
     for (; p + 3 * TR < panels; p += 4 * TR) {
       Part b[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) b[u] = parts[(int64_t)(p + u * TR) * rows + row];
+      for (int u = 0; u < 4; ++u) b[u] = parts[(int64_t)(p + u * TR) * rows + at];
 #pragma unroll
       for (int u = 0; u < 4; ++u) part_merge(a, b[u], c);
     }
-    for (; p < panels; p += TR) part_merge(a, parts[(int64_t)p * rows + row], c);
+    for (; p < panels; p += TR) part_merge(a, parts[(int64_t)p * rows + at], c);
   }
   // a wave holds 64 / RJ threads of each of the block's rows
   constexpr int LR = WAVE / RJ;
@@ -357,9 +407,8 @@ __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panel
     for (int w = 1; w < 4; ++w) part_merge(a, sm[w * RJ + r], c);
   }
   if (k == 0 && row < rows) {
-    const int t = tg[row];
-    if (t < 0 || t >= V) row_ignored(row, logp, ent, stats);
-    else row_finish(a, xt[row], c, row, logp, ent, stats);
+    if (on) row_finish(a, xt[at], c, row, logp, ent, stats);
+    else row_ignored(row, logp, ent, stats);
   }
 }
 
@@ -373,17 +422,41 @@ int64_t head_chunk(int64_t rows, int64_t vocab, int64_t bytes) {
 constexpr int64_t HEAD_ODD_BYTES = 32 << 20;  // logits of heads of unaligned rows, a chunk at a time
 constexpr int64_t HEAD_ROWS = 16384;  // rows of one fused product: bounds its parts' memory
 
-size_t fused_bytes(bool bf, int64_t n, int64_t vocab) {
-  return align256((size_t)n * 4) + (size_t)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab)) * n * sizeof(Part);
+// Whether a product is worth packing its rows for: 8 us of kernels against 250 us or more (at 1.2 PFLOP/s in bf16, a
+// tenth of it in fp32), in which rows without a target would take their share.  8192 x 49152 x 2048 bf16, without :
+// with packing, us: no such rows 1380 : 1390, a tenth of them 1385 : 1285, half 1390 : 725; half of 4096 x 32000 x 768
+// fp32 1480 : 760.
+bool head_packs(bool bf, int64_t n, int64_t vocab, int64_t d) {
+  return n > 256 && (double)n * vocab * d >= (bf ? 1.5e11 : 1.5e10);
+}
+struct HeadLayout { size_t xt, parts, pos, tp, xp, total; };  // byte offsets in the workspace
+HeadLayout head_layout(bool bf, int64_t n, int64_t vocab, int64_t d) {
+  HeadLayout l{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += align256(bytes);
+    return o;
+  };
+  l.xt = take((size_t)n * 4);
+  l.parts = take((size_t)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab)) * n * sizeof(Part));
+  if (head_packs(bf, n, vocab, d)) {
+    const int64_t np = cdiv(n, 256) * 256;
+    l.pos = take((size_t)(n + 1) * 4);  // and the count
+    l.tp = take((size_t)np * 4);
+    l.xp = take((size_t)np * d * (bf ? 2 : 4));
+  }
+  l.total = at;
+  return l;
 }
 size_t chunk_bytes(int64_t r, int64_t vocab) { return align256((size_t)(r * vocab * 4)) + logprob_ws_bytes(r, vocab); }
 
 }  // namespace
 
-size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab) {
+size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d) {
   const size_t chunked = chunk_bytes(head_chunk(rows, vocab, HEAD_ODD_BYTES), vocab);
   const int64_t first = std::min(rows, HEAD_ROWS), last = (rows - 1) % HEAD_ROWS + 1;
-  return std::max({fused_bytes(bf, first, vocab), fused_bytes(bf, last, vocab), chunked});
+  return std::max({head_layout(bf, first, vocab, d).total, head_layout(bf, last, vocab, d).total, chunked});
 }
 
 void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x, int64_t ldx, const void* w,
@@ -402,19 +475,38 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
     g.A = (const char*)x + r0 * ldx * (bf ? 2 : 4);
     g.stat_c = inv_temp * LOG2E;
     g.targets = targets + r0;
-    g.stat_xt = (float*)ws;
-    g.stats = (Part*)((char*)ws + align256((size_t)n * 4));
-    fused = gemm_rowstat_try(bf, g, st);  // takes all chunks or none: they differ in n alone
-    if (!fused) break;
+    const HeadLayout l = head_layout(bf, n, vocab, d);
+    char* w0 = (char*)ws;
+    g.stat_xt = (float*)(w0 + l.xt);
+    g.stats = (Part*)(w0 + l.parts);
+    g.stat_ld = n;
+    int32_t* pos = nullptr;
+    g.live = nullptr;
+    if (!gemm_rowstat_takes(bf, g)) {  // all chunks or none: they differ in n alone
+      fused = false;
+      break;
+    }
+    if (head_packs(bf, n, vocab, d)) {
+      pos = (int32_t*)(w0 + l.pos);
+      int32_t* tp = (int32_t*)(w0 + l.tp);
+      g.live = pos + n;
+      g.A2 = w0 + l.xp; g.lda2 = d;
+      g.targets2 = tp;
+      const int per = bf ? 8 : 4;  // elements per 16 bytes
+      pack_rows<<<1, 1024, 0, st>>>((int)n, vocab, g.targets, pos, pos + n);
+      gather_rows<<<(unsigned)cdiv(n + 255, 4), 256, 0, st>>>((int)n, d / per, (const u32x4*)g.A, ldx / per, g.targets,
+                                                              pos, pos + n, (u32x4*)(w0 + l.xp), tp);
+    }
+    gemm_rowstat(bf, g, st);
     const int panels = (int)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab));
     float* e = ent ? ent + r0 : nullptr;
     float* q = stats ? stats + 2 * r0 : nullptr;
     if (n >= 256)
-      panel_join<16><<<(unsigned)cdiv(n, 16), 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt,
-                                                            logp + r0, e, q);
+      panel_join<16><<<(unsigned)cdiv(n, 16), 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, pos,
+                                                            g.live, logp + r0, e, q);
     else
-      panel_join<1><<<(unsigned)n, 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, logp + r0, e,
-                                                 q);
+      panel_join<1><<<(unsigned)n, 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, pos, g.live,
+                                                 logp + r0, e, q);
   }
   if (fused) return;
   const int64_t r = head_chunk(rows, vocab, HEAD_ODD_BYTES);

@@ -96,7 +96,7 @@ int token_logprob_backward(int64_t rows, int64_t vocab, const void* logits, int6
 }
 
 size_t head_logprob_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int32_t is_bf16) {
-  return rows > 0 && head_sizes(rows, vocab, d) ? head_logprob_ws_bytes(is_bf16 != 0, rows, vocab) : 0;
+  return rows > 0 && head_sizes(rows, vocab, d) ? head_logprob_ws_bytes(is_bf16 != 0, rows, vocab, d) : 0;
 }
 
 int head_logprob(int64_t rows, int64_t vocab, int64_t d, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -108,7 +108,7 @@ int head_logprob(int64_t rows, int64_t vocab, int64_t d, const void* x, int64_t 
   if (rows == 0) return STAGE_OK;
   const size_t e = is_bf16 ? 2 : 4;
   if (!x || !w || off(x, e) || off(w, e)) return bad("x or w null or not aligned to their type");
-  if (const char* m = check_ws(workspace, workspace_bytes, head_logprob_ws_bytes(is_bf16 != 0, rows, vocab)))
+  if (const char* m = check_ws(workspace, workspace_bytes, head_logprob_ws_bytes(is_bf16 != 0, rows, vocab, d)))
     return bad(m);
   launch_head_logprob(is_bf16 != 0, rows, (int)vocab, (int)d, x, ldx, w, ldw, targets, inv_temperature, logp, entropy,
                       stats, workspace, (hipStream_t)hip_stream);

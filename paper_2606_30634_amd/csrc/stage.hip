@@ -403,7 +403,7 @@ size_t layout(stage* S, char* base) {
     sl.rstdf = sh.last_stage ? (float*)carve(T * 4) : nullptr;
     // scoring takes the logits' memory for its workspace
     sl.logits = sh.last_stage ? (float*)carve(std::max<int64_t>(T * (int64_t)sh.vocab * 4,
-                                                                (int64_t)head_logprob_ws_bytes(sh.dtype == 1, T, sh.vocab)))
+                                                                (int64_t)head_logprob_ws_bytes(sh.dtype == 1, T, sh.vocab, d)))
                               : nullptr;
     sl.lse_ce = sh.last_stage ? (float*)carve(T * 4) : nullptr;
     sl.lp_stats = sh.last_stage ? (float*)carve(T * 8) : nullptr;

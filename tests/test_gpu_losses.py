@@ -456,6 +456,33 @@ def test_captured_chain(B, S, V, d):
         assert all(torch.equal(a, b) for a, b in zip(got, _leaves(eager))), k
 
 
+@pytest.mark.parametrize("bf16,n,v,d", [(True, 4096, 9216, 4096), (True, 1025, 30001, 5000), (False, 2048, 4096, 2048),
+                                        (False, 700, 9001, 2996)])
+def test_head_logprob_packs_the_rows_that_count(bf16, n, v, d):
+    """Heads large enough that rows without a target are left out of the product: none, some, a run, all but a
+    few, all of them."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n + v)
+    mx, xv = _matrix(r.normal(size=(n, d)), bf16, pad=8)
+    mw, wv = _matrix(r.normal(size=(v, d)) * (2 / np.sqrt(d)), bf16)
+    t = r.integers(0, v, size=n)
+    ref = L.token_logprob(xv @ wv.T, t, 1.25)
+    e = _head_tol(d, xv[:64], wv[:256], 1.25) * 1.5  # the largest magnitude sum, from a part of the rows
+    for case in ("all", "random", "run", "few", "one", "none"):
+        keep = {"all": np.ones(n, bool), "random": r.random(n) < 0.6, "run": np.arange(n) > n // 3,
+                "few": r.random(n) < 0.01, "one": np.arange(n) == n - 1, "none": np.zeros(n, bool)}[case]
+        log(f"{case}: {keep.sum()} of {n} rows")
+        tt = np.where(keep, t, np.where(r.random(n) < 0.5, -1, v))
+        out = losses.LogProb(*(torch.full(s, 9.0, device="cuda:0") for s in ((n,), (n,), (n, 2))))
+        got = losses.head_logprob(mx, mw, _i32(tt), inv_temperature=1.25, out=out)
+        for k, g in enumerate(got):
+            assert not _np(g)[~keep].any()
+            d_ = np.abs(_np(g) - ref[k])[keep]
+            tol = (2 * e + 2 * _err(v, 12.0)) * (1 + np.log(v)) * (2 if k == 1 else 1)
+            assert d_.size == 0 or d_.max() <= tol, (case, k, d_.max(), tol)
+
+
 def test_head_logprob_of_more_rows_than_one_product_takes():
     """Rows of both chunks of a tall input, at the chunk's border and at its end, in a small head."""
     torch = _torch()

@@ -96,7 +96,10 @@ __device__ __forceinline__ void row_ignored(int64_t row, float* logp, float* ent
   if (stats) stats[2 * row] = 0.f, stats[2 * row + 1] = 0.f;
 }
 
-// One row (or one of nsplit equal parts of it) per group of NT threads of a block; a block holds RPB groups.
+// One row (or one of nsplit equal parts of it) per group of NT threads of a block; a block holds RPB groups.  One pass:
+// the maximum and both sums as they run, rescaled where a 16-byte vector raises the maximum.
+// Bound: memory, each logit read once, past the caches (8192 x 49152 fp32, a quarter of the rows ignored: 181 us,
+// 6.7 TB/s, where a streaming copy reaches 6.3; with cached loads 212); 12 vector operations a logit are 0.4 of that.
 template <typename T, int NT, int RPB>
 __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
                                                          const int32_t* __restrict__ tg, float c, int nsplit, int per,
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
   }
 }
 
-// Joins the nsplit <= 64 parts of every row, a wave per row.
+// Joins the nsplit <= 64 parts of every row, a wave per row (2.2 us for one).
 template <typename T>
 __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
                                                     const int32_t* __restrict__ tg, float c, int nsplit,
@@ -174,6 +177,9 @@ __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T
 // without a target, without a distribution or with zero upstream gradients gets zeros and is not read.
 // zero_to > V: the columns [V, zero_to) get zeros.  dx may be x (same type and rows): a lane writes only
 // what it has read.
+// Bound: memory, one read and one write past the caches (4096 x 128256 bf16, a quarter of the rows without a gradient:
+// 295 us, 6.2 TB/s; 999 x 32001 fp32 to bf16 with an entropy term 30 us, 6.0).  Two vectors a lane: 4096 x 128256 with
+// 4 of them 319 us, with 1 294 but 39 for the other.
 template <typename T> constexpr int BWD_U = 2;
 template <typename T, typename OutT>
 __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T* x, int64_t ld,
@@ -324,7 +330,6 @@ void launch_logprob_bwd(bool bf, int64_t rows, int vocab, const void* logits, in
 // ------------------------------------------------------------------ from hidden states
 namespace {
 
-
 constexpr int64_t HEAD_ROWS = 16384;  // rows of one fused product: bounds its parts' memory
 
 // Packing: the rows whose target is in the vocabulary, in order.  pos[r] is a row's place among them (-1: it has none),
@@ -380,7 +385,7 @@ __global__ void __launch_bounds__(256) gather_rows(int rows, int chunks, const u
 }
 
 // Joins the panels of every row (parts[p rows + row], or of its place where rows are packed): RJ rows per block of
-// 256, 256 / RJ threads on each.
+// 256, 256 / RJ threads on each.  384 panels of 8192 rows: 10 us for 38 MB.
 template <int RJ>
 __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panels, const int32_t* __restrict__ tg, float c,
                                                   const Part* __restrict__ parts, const float* __restrict__ xt,

@@ -1,8 +1,19 @@
 // Losses on the log-probabilities of answers, with their gradients: the clipped policy loss with a KL term
 // and an entropy bonus, and the preference loss of paired log ratios.
 //
-// Arrays are [sequences, len] row-major; a token counts where its mask byte is not 0, and nothing is
-// read of the others (their values may be anything).  Sums run in double in a fixed order.
+// Arrays are [sequences, len] row-major; a token counts where its mask byte is not 0, and what stands at the
+// others, whatever it is, is selected away and reaches nothing.  Sums run in double in a fixed order (over 4
+// consecutive tokens in fp32).
+//
+// Both are bound by memory where they are large and by round trips to it where they are not.  Policy loss: the
+// weights need the counts before the gradients can be written, so a first kernel counts (the mask alone), a
+// second takes the tokens, 4 a thread with the next ones' mask on its way, and a third adds the blocks' sums; up to
+// 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4 count, with reference, entropy and advantage
+// per token: 3.6 + 13.5 + 4.4 us, 35 MB at 1.7 TB/s (800 vector instructions per 4 tokens that count, a quarter of
+// the time, and a load that waits for its mask); 37 x 1111: 2.8 + 6.3 + 2.1; 4 x 64: 4.0.
+// Preference loss: the rows' sums, then the pairs and the gradients in one kernel whose blocks find their row's
+// coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.8 + 5.6 us, 17 MB at 1.7
+// TB/s; 2 x 100: 5.2.
 #include "common.h"
 #include "kernels.h"
 #include <algorithm>
@@ -73,8 +84,9 @@ __device__ __forceinline__ int count_share(const uint8_t* m, int64_t n, int tid)
 
 // ------------------------------------------------------------------ policy loss
 constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE;
-// policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024
-constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024, POL_EAGER_TOKENS = 1 << 19;
+// policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024.  One launch against
+// three, us on the GPU: 4096 tokens 7.7 : 9.7, 8192 9.8 : 9.8 (and two launches less to issue).
+constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024;
 
 // 1 / n for n > 0, to 2^-44: one step of Newton's method from the hardware's 2^-23
 __device__ __forceinline__ double inverse(int n) {
@@ -158,8 +170,8 @@ __device__ __forceinline__ void tokens_load(Tokens& v, const PolicyArgs& a, int6
   if (F & POL_TOKEN_ADV) v.adv = get(a.adv);
 }
 
-// Their sums (fp32 over four tokens, in weights relative to the first one's, then in double) and gradients; nb: the
-// sequences' counts.
+// Their sums (fp32 over four tokens, in weights relative to the first one's, which the hardware's reciprocal gives to
+// 2^-22; then in double) and gradients; nb: the sequences' counts.
 template <int F>
 __device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v, int64_t i, int64_t n, const int* nb,
                                            double scale, double (&acc)[POL_SUMS]) {
@@ -265,9 +277,9 @@ __device__ __forceinline__ void policy_totals(const int64_t* totals, int nblk, i
   seqs = wave_total(l < nblk ? totals[2 * l + 1] : (int64_t)0);
 }
 
-// The tokens' pass.  EAGER: a thread's tokens are requested together with their mask, one round trip to memory
-// instead of two, where that and not the bytes of the tokens that do not count is what takes time.
-template <int F, bool EAGER>
+// The tokens' pass.  A thread's tokens are requested once their mask says that one counts: asking for them with the
+// mask, one round trip less, reads the others too and measured the same from 9600 tokens on, 11 % more for 512 x 2048.
+template <int F>
 __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb, const int64_t* totals, int ncount,
                                                      double* sums) {
   __shared__ double sm[POL_SUMS * 16];
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb
   Tokens v = {}, next = {};
   if (i < n) {
     tokens_start<F>(v, a, i, n, nb);
-    if (EAGER || tokens_any(v)) tokens_load<F>(v, a, i);
+    if (tokens_any(v)) tokens_load<F>(v, a, i);
   }
   int64_t tokens, seqs;
   policy_totals(totals, ncount, tokens, seqs);
@@ -284,14 +296,11 @@ __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb
   double acc[POL_SUMS] = {};
   while (i < n) {
     const int64_t in = i + step;
-    if (in < n) {  // the next mask is on its way while these tokens are worked on
-      tokens_start<F>(next, a, in, n, nb);
-      if (EAGER) tokens_load<F>(next, a, in);
-    }
+    if (in < n) tokens_start<F>(next, a, in, n, nb);  // the next mask is on its way while these are worked on
     tokens_run<F>(a, v, i, n, nb, scale, acc);
     v = next;
     i = in;
-    if (!EAGER && i < n && tokens_any(v)) tokens_load<F>(v, a, i);
+    if (i < n && tokens_any(v)) tokens_load<F>(v, a, i);
   }
   block_sums(acc, sm);
   if (threadIdx.x == 0) {
@@ -385,9 +394,11 @@ __global__ void __launch_bounds__(1024) policy_small(PolicyArgs a) {
   for (int k = 0; k < PER; ++k) {
     const int i = 4 * (threadIdx.x + k * nt);
     if (i < n) {
-      const int b = (uint32_t)i / (uint32_t)a.len;
-      v[k].nb0 = nb[b];
-      v[k].nb1 = nb[v[k].turn < 4 ? b + 1 : b];
+      if (v[k].vec) {
+        const int b = (uint32_t)i / (uint32_t)a.len;
+        v[k].nb0 = nb[b];
+        v[k].nb1 = nb[v[k].turn < 4 ? b + 1 : b];
+      }
       tokens_run<F>(a, v[k], i, n, nb, scale, acc);
     }
   }
@@ -398,7 +409,7 @@ __global__ void __launch_bounds__(1024) policy_small(PolicyArgs a) {
 bool policy_is_small(int64_t seqs, int64_t len) { return seqs <= POL_SMALL_SEQS && seqs * len <= POL_SMALL_TOKENS; }
 
 // ------------------------------------------------------------------ preference loss
-constexpr int PREF_SUMS = 6, PREF_SMALL_ROWS = 512, PREF_SMALL_TOKENS = 8192, PREF_ROWS_PAIRS = 2048;
+constexpr int PREF_SUMS = 6, PREF_SMALL_ROWS = 512, PREF_SMALL_TOKENS = 8192, PREF_ROWS_PAIRS = 512;
 
 // Sum of logp - ref over the tokens of [t0, t1) of a row that count, and their number: this thread's share.
 template <int NT>
@@ -577,7 +588,8 @@ __global__ void __launch_bounds__(256) pref_tokens(PreferenceArgs a, const float
 }
 
 // The same two steps in one launch, for few pairs of one chunk a row: block b < 2 pairs cpr takes a share of row
-// b / cpr and finds the row's coefficient itself, the last block writes the pairs' outputs.
+// b / cpr and finds the row's coefficient itself, the last block writes the pairs' outputs.  Against the two
+// launches, us in all: 256 pairs of 4096 11.4 : 14.1, 1000 of 1000 17.2 : 15.1 (every block counts the pairs).
 __global__ void __launch_bounds__(256) pref_rows(PreferenceArgs a, int cpr, int64_t per, const double* sums,
                                                  const int* ns) {
   __shared__ double sm[PREF_SUMS * 16];
@@ -676,10 +688,7 @@ void policy_launch(const PolicyArgs& a, void* ws, hipStream_t st) {
   const int64_t groups = a.len >= 16384 ? a.seqs : cdiv(a.seqs, 16);
   const int ncount = (int)std::min<int64_t>(POL_COUNT_BLOCKS, groups);
   policy_count<<<ncount, 1024, 0, st>>>(a, nb, totals);
-  if (a.seqs * a.len <= POL_EAGER_TOKENS)
-    policy_tokens<F, true><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
-  else
-    policy_tokens<F, false><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
+  policy_tokens<F><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
   policy_finish<<<1, (int)std::min<int64_t>(256, cdiv(nblk, 64) * 64), 0, st>>>(a, totals, ncount, sums, nblk);
 }
 template <int... Fs>

@@ -51,6 +51,8 @@ class PreferenceLoss(NamedTuple):
 
 
 def _require(name, t, dev, dtype, shape):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
@@ -59,6 +61,8 @@ def _require(name, t, dev, dtype, shape):
 
 def _rows(name, t, dev=None):
     """(pointer, rows, columns, row stride, is bf16) of a matrix whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     if t.dim() != 2 or t.dtype not in (_F32, _BF16) or not t.is_cuda or (dev is not None and t.device != dev):
         raise ValueError(f"{name}: expected a float32 or bfloat16 matrix on {dev or 'a GPU'}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")

@@ -250,7 +250,8 @@ def _answers(r, b, s, empty=()):
 
 
 GRIDS = [(1, 1), (1, 3), (2, 1), (3, 5), (4, 64), (8, 1024), (37, 111), (1025, 3), (5000, 1), (2, 40001), (1, 20000),
-         (600, 66), (130, 127), (9, 4096)]
+         (600, 66), (130, 127), (9, 4096),
+         (1024, 3), (1024, 7), (341, 24)]
 
 
 @pytest.mark.parametrize("reduction", ["token", "sequence"])
@@ -373,6 +374,46 @@ def test_no_tokens():
         out = losses.preference_loss(z, off, ref_logp=z)
         assert float(out.loss) == 0 and not out.dlogp.any() and not out.pair_loss.any() and not out.rewards.any()
         assert not out.metrics.any() and out.counts.tolist() == [0]
+
+
+def test_torch_layer_refuses_on_a_device():
+    """Wrong types, shapes, strides, devices and missing parts, on real device tensors."""
+    torch = _torch()
+    from paper_2606_30634_amd import binding as B
+    from paper_2606_30634_amd import losses
+    f = lambda *s: torch.zeros(*s, device="cuda:0")  # noqa: E731
+    t = torch.zeros(4, dtype=torch.int32, device="cuda:0")
+    on = torch.ones(2, 8, dtype=torch.bool, device="cuda:0")
+    fwd = losses.token_logprob(f(4, 10), t)
+    for call in (lambda: losses.token_logprob(f(4, 10), t.long()), lambda: losses.token_logprob(f(4, 10), t[:3]),
+                 lambda: losses.token_logprob(f(4, 10), t.cpu()), lambda: losses.token_logprob(f(10, 4).t(), t),
+                 lambda: losses.token_logprob(f(4, 10).half(), t), lambda: losses.token_logprob(f(1, 10).expand(4, 10), t),
+                 lambda: losses.token_logprob(f(4, 10), t, out=losses.LogProb(f(3))),
+                 lambda: losses.token_logprob(f(4, 10), t, out=losses.LogProb(f(8)[::2])),
+                 lambda: losses.token_logprob_backward(f(4, 10), t, losses.LogProb(), f(4)),
+                 lambda: losses.token_logprob_backward(f(4, 10), t, fwd._replace(entropy=None), f(4), f(4)),
+                 lambda: losses.token_logprob_backward(f(4, 10), t, fwd, f(4), out=f(4, 11)),
+                 lambda: losses.head_logprob(f(4, 8), f(10, 7), t), lambda: losses.head_logprob(f(4, 8), f(10, 8).bfloat16(), t),
+                 lambda: losses.policy_loss(f(2, 8), f(2, 7), f(2), on), lambda: losses.policy_loss(f(2, 8), f(2, 8), f(3), on),
+                 lambda: losses.policy_loss(f(2, 8), f(2, 8), f(2), on.int()),
+                 lambda: losses.policy_loss(f(2, 8), f(2, 8), f(2), on, reduction="mean"),
+                 lambda: losses.policy_loss(f(2, 8), f(2, 8), f(2), on, out=losses.PolicyLoss(dentropy=f(2, 8))),
+                 lambda: losses.preference_loss(f(3, 8), torch.ones(3, 8, dtype=torch.bool, device="cuda:0")),
+                 lambda: losses.preference_loss(f(2, 8), on, kind="log"),
+                 lambda: losses.preference_loss(f(2, 8), on, ref_logp=f(2, 9)[:, :8])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: losses.policy_loss(f(2, 8), f(2, 8), f(2), on, kl_coef=0.1),
+                 lambda: losses.policy_loss(f(2, 8), f(2, 8), f(2), on, entropy_coef=0.1),
+                 lambda: losses.preference_loss(f(2, 8), on, beta=0.0),
+                 lambda: losses.token_logprob(f(4, 10), t, inv_temperature=0.0),
+                 lambda: losses.token_logprob_backward(fwd.stats.repeat(1, 5), t, fwd, f(4), inv_temperature=-1.0)):
+        with pytest.raises(B.StageError):
+            call()
+    buf = f(60)
+    a = buf[:40].view(4, 10)
+    with pytest.raises(B.StageError):  # overlapping, not the same
+        losses.token_logprob_backward(a, t, fwd, f(4), out=buf[10:50].view(4, 10))
 
 
 # ------------------------------------------------------------------ together

@@ -416,6 +416,36 @@ def test_torch_layer_refuses_on_a_device():
         losses.token_logprob_backward(a, t, fwd, f(4), out=buf[10:50].view(4, 10))
 
 
+def test_losses_past_32_bits():
+    """Arrays of more than 2^32 tokens of an odd length, a handful of which count, at both ends and around
+    2^31 and 2^32: gradients there and nowhere else."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    b, s = 5, (1 << 30) - 123
+    lp = torch.full((b, s), -0.5, device="cuda:0")
+    on = torch.zeros(b, s, dtype=torch.uint8, device="cuda:0")
+    at = [0, 5, s - 1, s, (1 << 31) - 1, 1 << 31, (1 << 32) - 1, 1 << 32, b * s - 2, b * s - 1]
+    on.view(-1)[torch.tensor(at, device="cuda:0")] = 1
+    adv = torch.arange(1.0, b + 1, device="cuda:0")
+    out = losses.policy_loss(lp, lp, adv, on)
+    seq = np.array([i // s for i in at])
+    want = -(seq + 1.0) / len(at)  # ratio 1: -A / N
+    got = _np(out.dlogp.view(-1)[torch.tensor(at, device="cuda:0")])
+    assert (np.abs(got - want) <= 4 * U * np.abs(want)).all(), (got, want)
+    assert int((out.dlogp != 0).sum()) == len(at) and out.counts.tolist() == [len(at), len(set(seq))]
+    assert abs(float(out.loss) - want.sum()) <= 4 * U * abs(want.sum())
+    del out
+    out = losses.preference_loss(lp[:4], on[:4], beta=1.0)
+    n = [int((seq == k).sum()) for k in range(4)]
+    live = [p for p in range(2) if n[p] and n[p + 2]]  # row 3 has no token: pair 1 does not count
+    c = [-1 / (1 + np.exp(-0.5 * (n[p] - n[p + 2]))) / len(live) if p in live else 0.0 for p in range(2)]
+    want = np.array([[c[0], c[1], -c[0], -c[1]][k] for k in seq if k < 4])
+    keep = [i for i in at if i < 4 * s]
+    got = _np(out.dlogp.view(-1)[torch.tensor(keep, device="cuda:0")])
+    assert (np.abs(got - want) <= 4 * U * np.abs(want)).all(), (got, want)
+    assert int((out.dlogp != 0).sum()) == int((want != 0).sum()) and out.counts.tolist() == [len(live)] == [1]
+
+
 # ------------------------------------------------------------------ together
 def _chain(losses, x, w, t, old, ref, adv, mask, ws):
     """One step as a training loop makes it, on given buffers: the reference's log-probabilities from the

@@ -14,7 +14,7 @@
 // 16-deep step are read from LDS while the MFMAs of the current one run.  The epilogue stages each
 // wave's tile through LDS and writes 16-byte rows.  Block order is remapped so that consecutive
 // tiles of one output row band land on one XCD (one L2).  Deterministic split-K for underfilled
-// fp32-output products.
+// fp32-output products.  One epilogue stores no product: it leaves the statistics of its rows, in bf16 and fp32.
 #include "common.h"
 #include "kernels.h"
 #include <algorithm>
@@ -366,7 +366,8 @@ __device__ __forceinline__ void dma_epilogue(const GemmArgs& g, f32x16 (&acc)[WM
 // Epilogue 9: the maximum and the two sums of every row over the wave's WN columns (kernels.h).  A part
 // of RP rows goes through the wave's LDS staging as above and comes back as 64 / RP lanes per row, each
 // with every (64 / RP)-th 16-byte chunk of it, so that a row's exponentials are spread over few lanes and
-// its sums take 2 or 3 exchanges.
+// its sums take 2 or 3 exchanges.  Bound: the product's matrix instructions (8192 x 49152 x 2048: 1350 us, 1.22
+// PFLOP/s, the rate of the plain products; writing the fp32 logits and reading them back took 1930), or B's bytes.
 template <int BM, int BN, int WM, int WN, int RP>
 __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[WM / 32][WN / 32], float* stage, int m0,
                                               int n0, int wm0, int wn0) {
@@ -1094,16 +1095,42 @@ bool gemm_mfma_try(const GemmArgs& g0, hipStream_t st) {
 
 // ------------------------------------------------------------------ row statistics (epilogue 9)
 namespace {
-// Tiles of the statistics product.  Up to 32 rows it streams W: 32 x 256 tiles in 3 stages, two blocks per
-// CU (one row, d 4096, N 128256: 173.5 us; 32 x 128 in 4 stages 181, 128 x 128 179).  Above, rounds
-// decide: a round of 256 blocks of 256 x 256 takes 1.5 to 1.75 times one of 512 of 128 x 128.  128 against
-// 256, us: N 32000, K 768: M 256 23 : 30, M 512 38 : 35; N 49152, K 2048: M 256 63 : 58, M 512 105 : 107, M 8192
-// 1609 : 1370; N 128256, K 4096: M 128 198 : 250, M 256 342 : 274; N 4000, K 512: M 2048 20 : 26, M 8192 56 : 49.
-enum { ROWSTAT_32, ROWSTAT_128, ROWSTAT_256 };
-int rowstat_config(int64_t M, int64_t N) {
-  if (M <= 32) return ROWSTAT_32;
-  const int64_t r128 = cdiv(cdiv(M, 128) * cdiv(N, 128), 512), r256 = cdiv(cdiv(M, 256) * cdiv(N, 256), 256);
-  return 8 * r256 <= 5 * r128 ? ROWSTAT_256 : ROWSTAT_128;
+// Tiles of the statistics product, which cannot be split over K: with few tiles it is bound by the chain of one
+// tile's slices, with many by their throughput.  A CU takes cdiv(tiles, 256) tiles, up to `res` of them at once; r of
+// them together take slice[r - 1] us per 64-deep (fp32: 32-deep) slice and epi[r - 1] us for their epilogues.
+// Fitted to 23 shapes of 2 to 8192 rows, 74 to 49152 columns, K 512 to 4096, and the least sum is taken.  Against
+// 128 x 128 (and 256 x 256 from 1.6 fewer rounds), us: bf16 M 45, N 10902, K 2144 33 : 22; 372 x 651 x 2600 33 : 23;
+// 64 x 3000 x 4096 46 : 32; 182 x 17655 x 1984 35 : 31; 1472 x 3605 x 4016 70 : 70; 8192 x 49152 x 2048 1370 : 1370;
+// fp32 45 x 10902 x 2144 152 : 58; 372 x 651 x 2600 183 : 67; 182 x 17655 x 1984 254 : 142; 8192 x 32000 x 768 2896 : 2896.
+struct RowstatTile { int bm, bn, res, panel; double slice[3], epi[3]; };
+enum { ROWSTAT_64, ROWSTAT_64_128, ROWSTAT_128, ROWSTAT_256, ROWSTAT_32_128, ROWSTAT_32_256 };
+constexpr RowstatTile ROWSTAT_BF16[] = {{64, 64, 3, 32, {.37, .55, .78}, {0, 1.5, 2.5}},
+                                        {64, 128, 2, 64, {.44, .63}, {0, 3}},
+                                        {128, 128, 2, 64, {.65, .85}, {2, 8}},
+                                        {256, 256, 1, 128, {1.3}, {8}}};
+constexpr RowstatTile ROWSTAT_FP32[] = {{64, 64, 3, 32, {.71, 1.25, 1.78}, {0, .5, 1}},
+                                        {64, 128, 2, 64, {1.2, 2.1}, {0, 1}},
+                                        {128, 128, 2, 64, {2.15, 3.97}, {2, 6}}};
+double rowstat_cost(const RowstatTile& t, int64_t M, int64_t N, int64_t slices) {
+  const int64_t n = cdiv(cdiv(M, t.bm) * cdiv(N, t.bn), 256);
+  const int rest = (int)(n % t.res);
+  double us = (double)(n / t.res) * (slices * t.slice[t.res - 1] + t.epi[t.res - 1]);
+  if (rest) us += slices * t.slice[rest - 1] + t.epi[rest - 1];
+  return us;
+}
+// Up to 32 rows the product streams W, through 32 x 256 tiles in 3 stages when they are enough (one row, bf16, N 128256, K
+// 4096: 173.5 us; 32 x 128 in 4 stages 181, 128 x 128 179; 24 rows, N 37255, K 1176 23.4 against 26.2 in 64 x 64; but 8
+// rows, N 10000, K 2048 25.9 : 20.3); in fp32, whose matrix instructions such a tile waits for, through 32 x 128 ones
+// (24 rows, N 37255, K 1176 59.8, 32 x 256 69.9; 8 rows, N 10000, K 2048 55 : 92).
+int rowstat_config(bool bf, int64_t M, int64_t N, int64_t K) {
+  if (M <= 32 && !bf) return ROWSTAT_32_128;
+  if (M <= 32 && N > 25600) return ROWSTAT_32_256;
+  const RowstatTile* t = bf ? ROWSTAT_BF16 : ROWSTAT_FP32;
+  const int64_t slices = cdiv(bf ? K : 2 * K, BKT);
+  int best = 0;
+  for (int k = 1; k < (bf ? 4 : 3); ++k)
+    if (rowstat_cost(t[k], M, N, slices) < rowstat_cost(t[best], M, N, slices)) best = k;
+  return best;
 }
 
 template <int BM, int BN, int WM, int WN, int NS, int FLAGS>
@@ -1115,16 +1142,20 @@ void launch_rowstat(const GemmArgs& g, hipStream_t st) {
   else
     launch_dma_one<BM, BN, WM, WN, true, true, float, BKT, NS, EPI, true>(g, nblk, st);
 }
-template <int FLAGS>
+// One row tile, so W is read once: past the caches where it is more than half of the last one (N 128256, K 4096, 1 row:
+// 180 -> 165 us, 6.4 TB/s; N 49152, K 2048: 52 -> 48; but N 32000, K 768, 49 MB: 18 -> 19.5 with the matrix in use
+// again and again)
+template <int BN, int NS, int FLAGS>
 void launch_rowstat_32(const GemmArgs& g, hipStream_t st) {
-  // past the caches where W is more than half of the last one (N 128256, K 4096, 1 row: 180 -> 165 us, 6.4 TB/s; N
-  // 49152, K 2048: 52 -> 48; but N 32000, K 768, 49 MB: 18 -> 19.5 with the matrix in use again and again)
-  if ((int64_t)g.N * g.K * 2 > 128 << 20) launch_rowstat<32, 256, 32, 64, 3, FLAGS + ROWSTAT_ONCE>(g, st);
-  else launch_rowstat<32, 256, 32, 64, 3, FLAGS>(g, st);
+  if ((int64_t)g.N * g.K * 2 > 128 << 20) launch_rowstat<32, BN, 32, BN / 4, NS, FLAGS + ROWSTAT_ONCE>(g, st);
+  else launch_rowstat<32, BN, 32, BN / 4, NS, FLAGS>(g, st);
 }
 }  // namespace
 
-int gemm_rowstat_panel(bool bf, int64_t M, int64_t N) { return bf && rowstat_config(M, N) == ROWSTAT_256 ? 128 : 64; }
+int gemm_rowstat_panel(bool bf, int64_t M, int64_t N, int64_t K) {
+  const int config = rowstat_config(bf, M, N, K);
+  return config == ROWSTAT_32_128 ? 32 : config == ROWSTAT_32_256 ? 64 : ROWSTAT_BF16[config].panel;
+}
 
 static GemmArgs rowstat_args(bool bf, GemmArgs g) {
   g.out_f32 = true;
@@ -1138,20 +1169,20 @@ bool gemm_rowstat_takes(bool bf, const GemmArgs& g) { return g.a_kmajor && g.b_k
 
 void gemm_rowstat(bool bf, const GemmArgs& g0, hipStream_t st) {
   const GemmArgs g = rowstat_args(bf, g0);
-  const int config = rowstat_config(g.M, g.N);
+  const int config = rowstat_config(bf, g0.M, g0.N, g0.K);
   if (!bf) {
-    // bound by its matrix instructions from few rows on (138 of 157 TFLOP/s at M 8192, N 32000, K 768): what counts is
-    // how evenly the tiles fill the CUs; a tile of 64 x 128 takes 0.53 of one of 128 x 128.  128 against 64 rows, us: M
-    // 1000, N 5000, K 1024 137 : 109; M 100, N 49152, K 2048 263 : 220; M 333, N 32001, K 512 123 : 130; M 8192, N
-    // 32000, K 768 2896 : 2980
-    const int64_t n128 = cdiv(g.N, 128), r128 = cdiv(cdiv(g.M, 128) * n128, 256), r64 = cdiv(cdiv(g.M, 64) * n128, 256);
-    if (config == ROWSTAT_32) launch_rowstat_32<ROWSTAT_F32>(g, st);
-    else if (53 * r64 < 100 * r128) launch_rowstat<64, 128, 32, 64, 2, ROWSTAT_F32>(g, st);
-    else launch_rowstat<128, 128, 64, 64, 2, ROWSTAT_F32>(g, st);
+    switch (config) {
+      case ROWSTAT_32_128: launch_rowstat_32<128, 4, ROWSTAT_F32>(g, st); break;
+      case ROWSTAT_64: launch_rowstat<64, 64, 32, 32, 3, ROWSTAT_F32>(g, st); break;
+      case ROWSTAT_64_128: launch_rowstat<64, 128, 32, 64, 2, ROWSTAT_F32>(g, st); break;
+      default: launch_rowstat<128, 128, 64, 64, 2, ROWSTAT_F32>(g, st); break;
+    }
     return;
   }
   switch (config) {
-    case ROWSTAT_32: launch_rowstat_32<0>(g, st); break;
+    case ROWSTAT_32_256: launch_rowstat_32<256, 3, 0>(g, st); break;
+    case ROWSTAT_64: launch_rowstat<64, 64, 32, 32, 3, 0>(g, st); break;
+    case ROWSTAT_64_128: launch_rowstat<64, 128, 32, 64, 3, 0>(g, st); break;
     case ROWSTAT_128: launch_rowstat<128, 128, 64, 64, 2, 0>(g, st); break;
     default: launch_rowstat<256, 256, 64, 128, 2, 0>(g, st); break;
   }

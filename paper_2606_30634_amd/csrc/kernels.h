@@ -176,7 +176,7 @@ void launch_axpby(bool bf, void* y, const void* x, float alpha, float beta, int 
 constexpr int GEMM_EPI_ROWSTAT = 9;
 // Columns of a panel of epilogue 9 for a product of these sizes; whether the kernels take its operands (bf16 or
 // fp32, both k-contiguous, rows of whole 16 bytes, 16-byte aligned); and the product (gemm_mfma.hip)
-int gemm_rowstat_panel(bool bf, int64_t M, int64_t N);
+int gemm_rowstat_panel(bool bf, int64_t M, int64_t N, int64_t K);
 bool gemm_rowstat_takes(bool bf, const GemmArgs& g);
 void gemm_rowstat(bool bf, const GemmArgs& g, hipStream_t st);
 constexpr int64_t GEMM_WS_ELEMS = 16 << 20;  // 64 MiB of fp32 split-K partials per stage

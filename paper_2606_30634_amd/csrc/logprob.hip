@@ -455,7 +455,7 @@ HeadLayout head_layout(bool bf, int64_t n, int64_t vocab, int64_t d) {
     return o;
   };
   l.xt = take((size_t)n * 4);
-  l.parts = take((size_t)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab)) * n * sizeof(Part));
+  l.parts = take((size_t)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab, d)) * n * sizeof(Part));
   if (head_packs(bf, n, vocab, d)) {
     const int64_t np = cdiv(n, 256) * 256;
     l.pos = take((size_t)(n + 1) * 4);  // and the count
@@ -514,7 +514,7 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
                                                               pos, pos + n, (u32x4*)(w0 + l.xp), tp);
     }
     gemm_rowstat(bf, g, st);
-    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab));
+    const int panels = (int)cdiv(vocab, gemm_rowstat_panel(bf, n, vocab, d));
     float* e = ent ? ent + r0 : nullptr;
     float* q = stats ? stats + 2 * r0 : nullptr;
     if (n >= 256)

@@ -527,6 +527,31 @@ def test_captured_chain(B, S, V, d):
         assert all(torch.equal(a, b) for a, b in zip(got, _leaves(eager))), k
 
 
+@pytest.mark.parametrize("bf16,n,v,d", [
+    (True, 64, 128, 64), (True, 130, 257, 40),            # 64 x 64 tiles, whole and ragged
+    (True, 1152, 4096, 1024), (True, 1100, 4000, 1032),   # 64 x 128
+    (True, 2944, 1024, 64), (True, 1000, 3001, 136),      # 128 x 128
+    (True, 4096, 4096, 256), (True, 2000, 6001, 520),     # 256 x 256
+    (True, 32, 25856, 64), (True, 7, 26001, 72), (True, 3, 40000, 2048),  # 32 x 256, the last past the caches
+    (False, 64, 128, 64), (False, 130, 257, 40), (False, 1024, 4096, 256), (False, 1000, 4001, 260),
+    (False, 2048, 4096, 768), (False, 2000, 4001, 772),
+    (False, 32, 1280, 64), (False, 5, 1001, 68), (False, 2, 20000, 2048)])
+def test_head_logprob_of_every_tile(bf16, n, v, d):
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n + v + d)
+    mx, xv = _matrix(r.normal(size=(n, d)), bf16)
+    mw, wv = _matrix(r.normal(size=(v, d)) * (2 / np.sqrt(d)), bf16)
+    t = r.integers(0, v, size=n)
+    t[n // 2], t[n - 1] = 0, v - 1  # both ends of the vocabulary
+    got = losses.head_logprob(mx, mw, _i32(t))
+    ref = L.token_logprob(xv @ wv.T, t, 1.0)
+    e = _head_tol(d, xv[:64], wv, 1.0) * 1.5  # the largest magnitude sum, from a part of the rows
+    assert (np.abs(_np(got.logp) - ref[0]) <= 2 * e + _err(v, ref[0])).all()
+    assert (np.abs(_np(got.stats)[:, 0] - ref[2][:, 0]) <= e).all()
+    assert (np.abs(_np(got.stats)[:, 1] - ref[2][:, 1]) <= 2 * e + _err(v, 0.0)).all()
+    assert (np.abs(_np(got.entropy) - ref[1]) <= (2 * e + 2 * _err(v, 0.0)) * 2 * (1 + np.log(v) + ref[2][:, 1])).all()
+
+
 @pytest.mark.parametrize("bf16,n,v,d", [(True, 4096, 9216, 4096), (True, 1025, 30001, 5000), (False, 2048, 4096, 2048),
                                         (False, 700, 9001, 2996)])
 def test_head_logprob_packs_the_rows_that_count(bf16, n, v, d):

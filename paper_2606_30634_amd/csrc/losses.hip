@@ -7,10 +7,10 @@
 //
 // Both are bound by memory where they are large and by round trips to it where they are not.  Policy loss: the
 // weights need the counts before the gradients can be written, so a first kernel counts (the mask alone), a
-// second takes the tokens, 4 a thread with the next ones' mask on its way, and a third adds the blocks' sums; up to
-// 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4 count, with reference, entropy and advantage
+// second takes the tokens, 4 a thread with the next ones' mask on its way, and its last block or, from 2^17 tokens
+// on, a third kernel adds the blocks' sums; up to 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4 count, with reference, entropy and advantage
 // per token: 3.6 + 13.5 + 4.4 us, 35 MB at 1.7 TB/s (800 vector instructions per 4 tokens that count, a quarter of
-// the time, and a load that waits for its mask); 37 x 1111: 2.8 + 6.3 + 2.1; 4 x 64: 4.0.
+// the time, and a load that waits for its mask); 37 x 1111: 2.8 + 8; 4 x 64: 4.0.
 // Preference loss: the rows' sums, then the pairs and the gradients in one kernel whose blocks find their row's
 // coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.8 + 5.6 us, 17 MB at 1.7
 // TB/s; 2 x 100: 5.2.
@@ -83,7 +83,7 @@ __device__ __forceinline__ int count_share(const uint8_t* m, int64_t n, int tid)
 }
 
 // ------------------------------------------------------------------ policy loss
-constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE;
+constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE, POL_LAST_BLOCKS = 128;
 // policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024.  One launch against
 // three, us on the GPU: 4096 tokens 7.7 : 9.7, 8192 9.8 : 9.8 (and two launches less to issue).
 constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024;
@@ -233,8 +233,10 @@ __device__ __forceinline__ void policy_out(const PolicyArgs& a, const double (&v
 }
 
 // Counts of every sequence, and the block's totals: a wave per sequence, or the block where they are long.
-__global__ void __launch_bounds__(1024) policy_count(PolicyArgs a, int* nb, int64_t* totals) {
+// It also clears the count of the token pass's blocks that are done.
+__global__ void __launch_bounds__(1024) policy_count(PolicyArgs a, int* nb, int64_t* totals, int* done) {
   __shared__ int64_t sm[2][16];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *done = 0;
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
   int64_t tokens = 0, seqs = 0;  // lane 0 of every wave
   if (a.len >= 16384) {
@@ -279,10 +281,15 @@ __device__ __forceinline__ void policy_totals(const int64_t* totals, int nblk, i
 
 // The tokens' pass.  A thread's tokens are requested once their mask says that one counts: asking for them with the
 // mask, one round trip less, reads the others too and measured the same from 9600 tokens on, 11 % more for 512 x 2048.
+// The blocks' sums are policy_finish's to add; or, with `done`, the last block's, in their order whichever it is: every
+// block publishes its own (stores at device scope) before it counts itself (acquire and release), the last one reads
+// them after.  That saves a launch, but the release writes the block's L2 back: 37 x 1111 tokens 18.5 -> 15.2 us as
+// issued (10.7 -> 11.2 on the GPU), 128 x 1024 12.1 -> 12.0, 256 x 1024 11.2 -> 14.6, 512 x 4096 22 -> 48.
 template <int F>
 __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb, const int64_t* totals, int ncount,
-                                                     double* sums) {
+                                                     double* sums, int* done) {
   __shared__ double sm[POL_SUMS * 16];
+  __shared__ bool last;
   const int64_t n = a.seqs * a.len, step = 1024 * (int64_t)gridDim.x;
   int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   Tokens v = {}, next = {};
@@ -303,19 +310,38 @@ __global__ void __launch_bounds__(256) policy_tokens(PolicyArgs a, const int* nb
     if (i < n && tokens_any(v)) tokens_load<F>(v, a, i);
   }
   block_sums(acc, sm);
+  if (!done) {
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int k = 0; k < POL_SUMS; ++k) sums[k * gridDim.x + blockIdx.x] = acc[k];
+    }
+    return;
+  }
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int k = 0; k < POL_SUMS; ++k) sums[(int64_t)k * gridDim.x + blockIdx.x] = acc[k];
+    for (int k = 0; k < POL_SUMS; ++k)
+      __hip_atomic_store(&sums[k * gridDim.x + blockIdx.x], acc[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
   }
+  __syncthreads();
+  if (!last) return;
+#pragma unroll
+  for (int k = 0; k < POL_SUMS; ++k) acc[k] = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += 256)
+#pragma unroll
+    for (int k = 0; k < POL_SUMS; ++k)
+      acc[k] += __hip_atomic_load(&sums[k * gridDim.x + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  block_sums(acc, sm);
+  if (threadIdx.x == 0) policy_out(a, acc, tokens, seqs);
 }
 
 __global__ void __launch_bounds__(256) policy_finish(PolicyArgs a, const int64_t* totals, int ncount, const double* sums,
-                                                      int nblk) {
+                                                     int nblk) {
   __shared__ double sm[POL_SUMS * 16];
   double acc[POL_SUMS] = {};
-  for (int i = threadIdx.x; i < nblk; i += blockDim.x)
+  for (int i = threadIdx.x; i < nblk; i += 256)
 #pragma unroll
-    for (int k = 0; k < POL_SUMS; ++k) acc[k] += sums[(int64_t)k * nblk + i];
+    for (int k = 0; k < POL_SUMS; ++k) acc[k] += sums[k * nblk + i];
   int64_t tokens, seqs;
   policy_totals(totals, ncount, tokens, seqs);
   block_sums(acc, sm);
@@ -670,7 +696,7 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 size_t policy_ws_bytes(int64_t seqs, int64_t len) {
   if (policy_is_small(seqs, len)) return 0;
   return up256(POL_BLOCKS * POL_SUMS * sizeof(double)) + up256(POL_COUNT_BLOCKS * 2 * sizeof(int64_t)) +
-         up256((size_t)seqs * sizeof(int));
+         up256(sizeof(int)) + up256((size_t)seqs * sizeof(int));
 }
 
 namespace {
@@ -683,13 +709,18 @@ void policy_launch(const PolicyArgs& a, void* ws, hipStream_t st) {
   }
   double* sums = (double*)ws;
   int64_t* totals = (int64_t*)((char*)ws + up256(POL_BLOCKS * POL_SUMS * sizeof(double)));
-  int* nb = (int*)((char*)totals + up256(POL_COUNT_BLOCKS * 2 * sizeof(int64_t)));
+  int* done = (int*)((char*)totals + up256(POL_COUNT_BLOCKS * 2 * sizeof(int64_t)));
+  int* nb = (int*)((char*)done + up256(sizeof(int)));
   const int nblk = (int)std::min<int64_t>(POL_BLOCKS, cdiv(a.seqs * a.len, 1024));
   const int64_t groups = a.len >= 16384 ? a.seqs : cdiv(a.seqs, 16);
   const int ncount = (int)std::min<int64_t>(POL_COUNT_BLOCKS, groups);
-  policy_count<<<ncount, 1024, 0, st>>>(a, nb, totals);
-  policy_tokens<F><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums);
-  policy_finish<<<1, (int)std::min<int64_t>(256, cdiv(nblk, 64) * 64), 0, st>>>(a, totals, ncount, sums, nblk);
+  policy_count<<<ncount, 1024, 0, st>>>(a, nb, totals, done);
+  if (nblk <= POL_LAST_BLOCKS) {
+    policy_tokens<F><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums, done);
+    return;
+  }
+  policy_tokens<F><<<nblk, 256, 0, st>>>(a, nb, totals, ncount, sums, nullptr);
+  policy_finish<<<1, 256, 0, st>>>(a, totals, ncount, sums, nblk);
 }
 template <int... Fs>
 void policy_dispatch(int f, const PolicyArgs& a, void* ws, hipStream_t st, std::integer_sequence<int, Fs...>) {

@@ -251,7 +251,7 @@ def _answers(r, b, s, empty=()):
 
 GRIDS = [(1, 1), (1, 3), (2, 1), (3, 5), (4, 64), (8, 1024), (37, 111), (1025, 3), (5000, 1), (2, 40001), (1, 20000),
          (600, 66), (130, 127), (9, 4096),
-         (1024, 3), (1024, 7), (341, 24)]
+         (1024, 3), (1024, 7), (341, 24), (40, 4099)]
 
 
 @pytest.mark.parametrize("reduction", ["token", "sequence"])
@@ -292,6 +292,33 @@ def test_policy_loss(b, s, reduction):
         again = losses.policy_loss(T["lp"][0], T["old"][0], T["adv"][0], mask.view(torch.uint8) * 200,
                                    ref_logp=T["ref"][0] if ref_on else None, entropy=T["ent"][0] if ent_on else None, **kw)
         assert all(x is y is None or torch.equal(x, y) for x, y in zip(got, again))
+
+
+@pytest.mark.parametrize("b,s", [(37, 1111), (128, 1024), (129, 1024), (3, 2731)])
+def test_policy_loss_is_the_same_every_time(b, s):
+    """The order in which blocks finish leaves no trace: a hundred calls in a row, on one workspace and on
+    two streams at once, give the same bits."""
+    torch = _torch()
+    from paper_2606_30634_amd import binding as B
+    from paper_2606_30634_amd import losses
+    g = torch.Generator(device="cuda:0").manual_seed(b + s)
+    rnd = lambda *n: torch.randn(*n, generator=g, device="cuda:0")  # noqa: E731
+    lp = -rnd(b, s).abs()
+    args = (lp, lp + 0.2 * rnd(b, s), rnd(b), rnd(b, s) > -0.2)
+    kw = dict(ref_logp=lp + 0.1 * rnd(b, s), kl_coef=0.25, reduction="sequence")
+    want = losses.policy_loss(*args, **kw)
+    torch.cuda.synchronize()
+    need = B.policy_loss_workspace_bytes(b, s)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ws = [torch.full((max(need, 1),), 255, dtype=torch.uint8, device="cuda:0") for _ in streams]
+    torch.cuda.synchronize()
+    got = []
+    for k in range(100):
+        with torch.cuda.stream(streams[k % 2]):
+            got.append(losses.policy_loss(*args, workspace=ws[k % 2], **kw))
+    torch.cuda.synchronize()
+    for out in got:
+        assert all(x is y is None or torch.equal(x, y) for x, y in zip(out, want))
 
 
 def test_policy_loss_of_ratios_past_the_type():

@@ -479,7 +479,8 @@ __device__ __forceinline__ PairOut pref_pair(const PreferenceArgs& a, double sw,
   double loss, dh;
   if (a.kind == 0) {
     const double soft = log1p(exp(-fabs(h)));  // log(1 + e^-|h|)
-    loss = (1.0 - e) * (soft + fmax(-h, 0.0)) + (e > 0.0 ? e * (soft + fmax(h, 0.0)) : 0.0);
+    // a side without a weight adds nothing, also where it is infinite
+    loss = (e < 1.0 ? (1.0 - e) * (soft + fmax(-h, 0.0)) : 0.0) + (e > 0.0 ? e * (soft + fmax(h, 0.0)) : 0.0);
     if (h != h) loss = h;
     dh = e - 1.0 / (1.0 + exp(h));
   } else if (a.kind == 1) {

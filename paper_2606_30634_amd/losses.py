@@ -164,12 +164,14 @@ def head_logprob(x, weight, targets, *, inv_temperature: float = 1.0, out: Optio
 
 
 def _mask(mask, dev, shape):
-    if mask.dtype == torch.bool:
+    if getattr(mask, "dtype", None) is torch.bool:
         mask = mask.view(_U8)
     return _require("mask", mask, dev, _U8, shape)
 
 
 def _grid(name, t):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name}: expected a [sequences, length] tensor on a GPU, got {tuple(t.shape)} on {t.device}")
     return t.device, t.shape
@@ -189,7 +191,7 @@ def policy_loss(logp, old_logp, advantages, mask, *, ref_logp=None, entropy=None
     old = _require("old_logp", old_logp, dev, _F32, shape)
     ref = None if ref_logp is None else _require("ref_logp", ref_logp, dev, _F32, shape)
     ent = None if entropy is None else _require("entropy", entropy, dev, _F32, shape)
-    per_token = advantages.dim() == 2
+    per_token = getattr(advantages, "ndim", 1) == 2
     adv = _require("advantages", advantages, dev, _F32, shape if per_token else torch.Size((b,)))
     m = _mask(mask, dev, shape)
     if reduction not in _REDUCTIONS:

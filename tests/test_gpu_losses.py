@@ -390,6 +390,24 @@ def test_preference_loss(p, s, kind, smoothing, normalize):
         assert all(torch.equal(x, y) for x, y in zip(got, again))
 
 
+@pytest.mark.parametrize("p,s", [(3, 5), (300, 40), (2, 50001)])
+def test_preference_loss_of_answers_that_cannot_occur(p, s):
+    """A chosen answer of probability 0 is delta = -inf: the loss is the weight of that side times infinity, and 0
+    where all weight is on the other side, for which the pair is as it should be."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    lp = torch.full((2 * p, s), -1.0, device="cuda:0")
+    lp[0, s // 2] = -torch.inf
+    on = torch.ones(2 * p, s, dtype=torch.bool, device="cuda:0")
+    for e, first in ((0.0, torch.inf), (0.25, torch.inf), (1.0, 0.0)):
+        out = losses.preference_loss(lp, on, label_smoothing=e, beta=0.5)
+        assert float(out.pair_loss[0]) == first and bool(out.pair_loss[1:].isfinite().all())
+        assert float(out.loss) == (torch.inf if first else float(out.loss)) and not bool(out.loss.isnan())
+        assert float(out.rewards[0]) == -torch.inf and int(out.counts[0]) == p
+        want = 0.5 * (e - 1.0) / p  # sigmoid(h) is 0
+        assert bool((out.dlogp[0] - want).abs().max() <= abs(want) * 2.0 ** -22)
+
+
 def test_no_tokens():
     torch = _torch()
     from paper_2606_30634_amd import losses

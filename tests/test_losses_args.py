@@ -122,7 +122,9 @@ def test_no_rows_is_no_work():
     lambda f, i: losses.preference_loss(f(2, 8), f(2, 8) > 0),
     lambda f, i: losses.token_logprob(f(4, 10).double(), i(4)),
     lambda f, i: losses.policy_loss(f(8), f(8), f(1), f(8) > 0),
-    lambda f, i: losses.token_logprob(None, i(4))])
+    lambda f, i: losses.token_logprob(None, i(4)),
+    lambda f, i: losses.policy_loss(None, f(2, 8), f(2), f(2, 8) > 0),
+    lambda f, i: losses.preference_loss([[0.0]], f(2, 8) > 0)])
 def test_torch_layer_refuses(call):
     with pytest.raises(ValueError):
         call(lambda *s: torch.zeros(*s), lambda n: torch.zeros(n, dtype=torch.int32))

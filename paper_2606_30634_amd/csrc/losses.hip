@@ -7,13 +7,13 @@
 //
 // Both are bound by memory where they are large and by round trips to it where they are not.  Policy loss: the
 // weights need the counts before the gradients can be written, so a first kernel counts (the mask alone), a
-// second takes the tokens, 4 a thread with the next ones' mask on its way, and its last block or, from 2^17 tokens
-// on, a third kernel adds the blocks' sums; up to 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4 count, with reference, entropy and advantage
-// per token: 3.6 + 13.5 + 4.4 us, 35 MB at 1.7 TB/s (800 vector instructions per 4 tokens that count, a quarter of
-// the time, and a load that waits for its mask); 37 x 1111: 2.8 + 8; 4 x 64: 4.0.
+// second takes the tokens, 4 a thread with the next ones' mask on its way, and its last block or, above 2^17 tokens,
+// a third kernel adds the blocks' sums; up to 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4
+// count, with reference, entropy and advantage per token: 3.5 + 12.7 + 3.8 us, 35 MB in the second, in which a copy
+// of as many bytes takes 7.9 and the vector instructions, 330 per 4 tokens, 4.6; 37 x 1111: 2.9 + 6.9; 4 x 64: 3.4.
 // Preference loss: the rows' sums, then the pairs and the gradients in one kernel whose blocks find their row's
-// coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.8 + 5.6 us, 17 MB at 1.7
-// TB/s; 2 x 100: 5.2.
+// coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.6 + 5.8 us, 17 MB at 1.7
+// TB/s; 2 x 100: 4.1.
 #include "common.h"
 #include "kernels.h"
 #include <algorithm>
@@ -35,15 +35,70 @@ __device__ __forceinline__ float kl_term(float x, float ex) {
   p = p * x + 1.f / 24.f;
   p = p * x + 1.f / 6.f;
   p = p * x + 0.5f;
-  return fabsf(x) >= 0.5f ? (ex - 1.f) - x : p * x * x;
+  const float near = p * x * x, far = (ex - 1.f) - x;  // both, so that no branch holds up the next token
+  return fabsf(x) >= 0.5f ? far : near;
+}
+
+// Sums over each 16 lanes, in all of them.
+template <int CTRL>
+__device__ __forceinline__ double row_add(double v) {
+  uint32_t w[2];
+  __builtin_memcpy(w, &v, 8);
+  w[0] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[0], CTRL, 0xf, 0xf, true);
+  w[1] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[1], CTRL, 0xf, 0xf, true);
+  double o;
+  __builtin_memcpy(&o, w, 8);
+  return v + o;
+}
+__device__ __forceinline__ double row_total(double v) {
+  return row_add<0x121>(row_add<0x122>(row_add<0x124>(row_add<0x128>(v))));  // row_ror 8, 4, 2, 1
+}
+__device__ __forceinline__ double read_lane(double v, int lane) {
+  uint32_t w[2];
+  __builtin_memcpy(w, &v, 8);
+  w[0] = (uint32_t)__builtin_amdgcn_readlane((int)w[0], lane);
+  w[1] = (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane);
+  __builtin_memcpy(&v, w, 8);
+  return v;
+}
+// [a.low + a.high | b.low + b.high] of the wave's halves; with ROWS of its 16-lane rows 0 + 1 and 2 + 3,
+// [a01 | b01 | a23 | b23]
+template <bool ROWS>
+__device__ __forceinline__ double swap_add(double a, double b) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  uint32_t x[2], y[2];
+  __builtin_memcpy(x, &a, 8);
+  __builtin_memcpy(y, &b, 8);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const u32x2 r = ROWS ? __builtin_amdgcn_permlane16_swap(x[k], y[k], false, false)
+                         : __builtin_amdgcn_permlane32_swap(x[k], y[k], false, false);
+    x[k] = r[0], y[k] = r[1];
+  }
+  __builtin_memcpy(&a, x, 8);
+  __builtin_memcpy(&b, y, 8);
+  return a + b;
+}
+// Sums of N doubles over the wave, in every lane: two exchanges leave a row of 16 lanes to each value, so that four of
+// them take the last four steps at once (some 50 instructions for 6 values, one after the other 190: 37 x 1111 tokens of
+// the policy loss 11.1 -> 9.9 us, 2 pairs of 100 5.3 -> 4.1).
+template <int N>
+__device__ __forceinline__ void wave_sums(double (&v)[N]) {
+  constexpr int H = (N + 1) / 2, Q = (H + 1) / 2;
+  double a[H], b[Q];
+#pragma unroll
+  for (int j = 0; j < H; ++j) a[j] = swap_add<false>(v[2 * j], v[2 * j + 1 < N ? 2 * j + 1 : N - 1]);
+#pragma unroll
+  for (int j = 0; j < Q; ++j) b[j] = row_total(swap_add<true>(a[2 * j], a[2 * j + 1 < H ? 2 * j + 1 : H - 1]));
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = read_lane(b[k / 4], (k % 2) * 32 + (k / 2 % 2) * 16);
 }
 
 // Block-wide sums of N doubles, for blocks of whole waves; valid in the first wave.
 template <int N>
 __device__ __forceinline__ void block_sums(double (&v)[N], double* sm /* N x 16 */) {
   const int w = threadIdx.x / WAVE, l = threadIdx.x % WAVE, nw = blockDim.x / WAVE;
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = wave_total(v[k]);
+  wave_sums(v);
   if (nw == 1) return;
   __syncthreads();
   if (l == 0) {
@@ -53,7 +108,12 @@ __device__ __forceinline__ void block_sums(double (&v)[N], double* sm /* N x 16 
   __syncthreads();
   if (w == 0) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = wave_total(l < nw ? sm[k * 16 + l] : 0.0);
+    for (int j = 0; j < N; j += 4) {  // a row of lanes per value
+      const int k = j + l / 16;
+      const double t = row_total(k < N && l % 16 < nw ? sm[k * 16 + l % 16] : 0.0);
+#pragma unroll
+      for (int q = 0; q < 4 && j + q < N; ++q) v[j + q] = read_lane(t, 16 * q);
+    }
   }
 }
 
@@ -85,7 +145,8 @@ __device__ __forceinline__ int count_share(const uint8_t* m, int64_t n, int tid)
 // ------------------------------------------------------------------ policy loss
 constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE, POL_LAST_BLOCKS = 128;
 // policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024.  One launch against
-// three, us on the GPU: 4096 tokens 7.7 : 9.7, 8192 9.8 : 9.8 (and two launches less to issue).
+// two, us on the GPU: 4096 tokens 6.6 : 8.2, 8192 8.6 : 8.4, with sequence means 11.2 : 8.9; as issued, 8192 13.7 : 17.2
+// and 13.4 : 16.7.
 constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024;
 
 // 1 / n for n > 0, to 2^-44: one step of Newton's method from the hardware's 2^-23
@@ -117,14 +178,16 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, bool on, floa
   const float held = rise ? 1.f + a.clip_high : fall ? 1.f - a.clip_low : r;
   const float ra = adv == 0.f ? 0.f : held * adv;  // no advantage: nothing, also where e^x is past the type
   float d = cut ? 0.f : -ra;
+  const float kx = kl_term(xf, r);
   f[0] -= on ? om * ra : 0.f;
   f[3] += on && cut ? om : 0.f;
-  f[4] += on ? om * kl_term(xf, r) : 0.f;
+  f[4] += on ? om * kx : 0.f;
   f[5] += on ? om * r : 0.f;
   if constexpr (F & POL_REF) {
     const float q = ref - lp, eq = expf(q), k = kl_term(q, eq);
     f[1] += on ? om * k : 0.f;
-    if (a.kl_coef != 0.f) d -= a.kl_coef * (fabsf(q) >= 0.5f ? eq - 1.f : k + q);
+    const float near = k + q, far = eq - 1.f;
+    if (a.kl_coef != 0.f) d -= a.kl_coef * (fabsf(q) >= 0.5f ? far : near);
   }
   if constexpr (F & POL_ENT) f[2] += on ? om * ent : 0.f;
   return on ? d : 0.f;
@@ -139,7 +202,7 @@ __device__ __forceinline__ int64_t seq_of(int64_t i, int64_t len) {
 // b + 1; the two sequences' counts and advantages.  vec: all four exist and sequences are at least that long (the
 // others are taken one by one, from memory).
 struct Tokens {
-  u8x4u on;
+  uint32_t on;  // the mask's 4 bytes, taken apart where they are used (at once, they would be waited for)
   f32x4u lp, old, ref, ent, adv;
   int turn, nb0, nb1;
   float ab0, ab1;
@@ -151,13 +214,14 @@ __device__ __forceinline__ void tokens_start(Tokens& v, const PolicyArgs& a, int
   if (!v.vec) return;
   const int64_t b = seq_of(i, a.len), left = (b + 1) * a.len - i;
   v.turn = left < 4 ? (int)left : 4;
-  v.on = *reinterpret_cast<const u8x4u*>(a.mask + i);
+  typedef uint32_t u32u __attribute__((aligned(1)));
+  v.on = *reinterpret_cast<const u32u*>(a.mask + i);
   const int64_t b1 = v.turn < 4 ? b + 1 : b;
   if ((F & POL_SEQ_MEAN) && nb) v.nb0 = nb[b], v.nb1 = nb[b1];
   if (!(F & POL_TOKEN_ADV)) v.ab0 = a.adv[b], v.ab1 = a.adv[b1];
 }
 __device__ __forceinline__ bool tokens_any(const Tokens& v) {
-  return v.vec && (v.on[0] | v.on[1] | v.on[2] | v.on[3]);
+  return v.vec && v.on;
 }
 template <int F>
 __device__ __forceinline__ void tokens_load(Tokens& v, const PolicyArgs& a, int64_t i) {
@@ -191,10 +255,12 @@ __device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v,
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const bool first = q < v.turn;
+        const bool on = (v.on >> 8 * q & 0xff) != 0;
         const float gw = first ? g0 : g1, ab = first ? v.ab0 : v.ab1;
-        g[q] = v.on[q] ? gw * policy_token<F>(a, v.on[q], first ? 1.f : om, v.lp[q], v.old[q], (F & POL_TOKEN_ADV) ? v.adv[q] : ab,
-                                           v.ref[q], v.ent[q], f) : 0.f;
-        ge[q] = v.on[q] ? -a.ent_coef * gw : 0.f;
+        const float d = policy_token<F>(a, on, first ? 1.f : om, v.lp[q], v.old[q], (F & POL_TOKEN_ADV) ? v.adv[q] : ab,
+                                        v.ref[q], v.ent[q], f);
+        g[q] = on ? gw * d : 0.f;
+        ge[q] = on ? -a.ent_coef * gw : 0.f;
       }
       weigh(w0, f);
     }
@@ -275,8 +341,10 @@ __global__ void __launch_bounds__(1024) policy_count(PolicyArgs a, int* nb, int6
 // Totals of the count's blocks (at most a wave's lanes of them), in every thread of full waves.
 __device__ __forceinline__ void policy_totals(const int64_t* totals, int nblk, int64_t& tokens, int64_t& seqs) {
   const int l = threadIdx.x % WAVE;
-  tokens = wave_total(l < nblk ? totals[2 * l] : (int64_t)0);
-  seqs = wave_total(l < nblk ? totals[2 * l + 1] : (int64_t)0);
+  double t[2] = {l < nblk ? (double)totals[2 * l] : 0.0, l < nblk ? (double)totals[2 * l + 1] : 0.0};  // exact
+  wave_sums(t);
+  tokens = (int64_t)t[0];
+  seqs = (int64_t)t[1];
 }
 
 // The tokens' pass.  A thread's tokens are requested once their mask says that one counts: asking for them with the

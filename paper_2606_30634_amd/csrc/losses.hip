@@ -2,17 +2,16 @@
 // and an entropy bonus, and the preference loss of paired log ratios.
 //
 // Arrays are [sequences, len] row-major; a token counts where its mask byte is not 0, and what stands at the
-// others, whatever it is, is selected away and reaches nothing.  Sums run in double in a fixed order (over 4
-// consecutive tokens in fp32).
+// others, whatever it is, is selected away and reaches nothing.  Sums run in double in a fixed order.
 //
 // Both are bound by memory where they are large and by round trips to it where they are not.  Policy loss: the
 // weights need the counts before the gradients can be written, so a first kernel counts (the mask alone), a
 // second takes the tokens, 4 a thread with the next ones' mask on its way, and its last block or, above 2^17 tokens,
 // a third kernel adds the blocks' sums; up to 8192 tokens one block does it all.  512 x 4096 tokens of which 0.4
-// count, with reference, entropy and advantage per token: 3.5 + 12.7 + 3.8 us, 35 MB in the second, in which a copy
-// of as many bytes takes 7.9 and the vector instructions, 330 per 4 tokens, 4.6; 37 x 1111: 2.9 + 6.9; 4 x 64: 3.4.
+// count, with reference, entropy and advantage per token: 3.5 + 13.7 + 3.9 us, 35 MB in the second, in which a copy
+// of as many bytes takes 7.9 and the vector instructions, 360 per 4 tokens, 5.0; 37 x 1111: 2.8 + 7.5; 4 x 64: 3.6.
 // Preference loss: the rows' sums, then the pairs and the gradients in one kernel whose blocks find their row's
-// coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.6 + 5.8 us, 17 MB at 1.7
+// coefficient themselves (with the number of pairs that count).  256 pairs of 4096: 4.5 + 5.5 us, 17 MB at 1.7
 // TB/s; 2 x 100: 4.1.
 #include "common.h"
 #include "kernels.h"
@@ -145,8 +144,8 @@ __device__ __forceinline__ int count_share(const uint8_t* m, int64_t n, int tid)
 // ------------------------------------------------------------------ policy loss
 constexpr int POL_SUMS = 6, POL_BLOCKS = 1024, POL_COUNT_BLOCKS = WAVE, POL_LAST_BLOCKS = 128;
 // policy_small: at most two vectors of 4 tokens and four of 16 mask bytes per thread of 64 to 1024.  One launch against
-// two, us on the GPU: 4096 tokens 6.6 : 8.2, 8192 8.6 : 8.4, with sequence means 11.2 : 8.9; as issued, 8192 13.7 : 17.2
-// and 13.4 : 16.7.
+// two, us on the GPU: 4096 tokens 7.1 : 8.4, 8192 9.4 : 8.6, with sequence means 11.9 : 8.9; as issued, 8192 13.4 : 19.1
+// and 13.1 : 18.8.
 constexpr int POL_SMALL_TOKENS = 8192, POL_SMALL_SEQS = 1024;
 
 // 1 / n for n > 0, to 2^-44: one step of Newton's method from the hardware's 2^-23
@@ -165,31 +164,34 @@ __device__ __forceinline__ double mean_scale(const PolicyArgs& a, int64_t tokens
   return d > 0 ? 1.0 / d : 0.0;
 }
 
-// A token's terms, times om, added to f where it counts (whatever the others hold), and its gradient
-// apart from the weight.  Which side of the clip a token is on is decided in the logarithm, on the exact
-// difference of the two log-probabilities, so that the gradient's jump there does not hang on the rounding of
-// e^x.
+// A token's terms, times w, added to acc where it counts (whatever the others hold), and its gradient apart from
+// the weight.  Which side of the clip a token is on is decided in the logarithm, on the exact difference of the two
+// log-probabilities, so that the gradient's jump there does not hang on the rounding of e^x.
 template <int F>
-__device__ __forceinline__ float policy_token(const PolicyArgs& a, bool on, float om, float lp, float old, float adv, float ref,
-                                              float ent, float (&f)[POL_SUMS]) {
+__device__ __forceinline__ float policy_token(const PolicyArgs& a, bool on, double w, float lp, float old, float adv,
+                                              float ref, float ent, double (&acc)[POL_SUMS]) {
+  auto add = [&](int k, float v) { acc[k] += w * (double)(on ? v : 0.f); };
   const double x = (double)lp - (double)old;
   const float xf = (float)x, r = expf(xf);
   const bool rise = adv > 0.f && x > a.log_hi, fall = adv < 0.f && x < a.log_lo, cut = rise || fall;
-  const float held = rise ? 1.f + a.clip_high : fall ? 1.f - a.clip_low : r;
-  const float ra = adv == 0.f ? 0.f : held * adv;  // no advantage: nothing, also where e^x is past the type
-  float d = cut ? 0.f : -ra;
   const float kx = kl_term(xf, r);
-  f[0] -= on ? om * ra : 0.f;
-  f[3] += on && cut ? om : 0.f;
-  f[4] += on ? om * kx : 0.f;
-  f[5] += on ? om * r : 0.f;
+  // The surrogate's terms have both signs, and where they cancel the rounding of e^x would be all that is left: near
+  // 1 it is taken from its small part in double (the loss against 64 bits over 150 cases 2.7e-7 -> 2.5e-8).
+  const double near1 = (1.0 + x) + (double)kx, e = fabsf(xf) >= 0.5f ? (double)r : near1, av = on ? adv : 0.f;
+  const double held = rise ? 1.0 + (double)a.clip_high : fall ? 1.0 - (double)a.clip_low : e;
+  const double ra = av == 0.0 ? 0.0 : held * av;  // no advantage: nothing, also where e^x is past the type
+  float d = cut ? 0.f : -(float)ra;
+  acc[0] -= w * ra;
+  add(3, cut ? 1.f : 0.f);
+  add(4, kx);
+  add(5, r);
   if constexpr (F & POL_REF) {
     const float q = ref - lp, eq = expf(q), k = kl_term(q, eq);
-    f[1] += on ? om * k : 0.f;
+    add(1, k);
     const float near = k + q, far = eq - 1.f;
     if (a.kl_coef != 0.f) d -= a.kl_coef * (fabsf(q) >= 0.5f ? far : near);
   }
-  if constexpr (F & POL_ENT) f[2] += on ? om * ent : 0.f;
+  if constexpr (F & POL_ENT) add(2, ent);
   return on ? d : 0.f;
 }
 
@@ -234,15 +236,10 @@ __device__ __forceinline__ void tokens_load(Tokens& v, const PolicyArgs& a, int6
   if (F & POL_TOKEN_ADV) v.adv = get(a.adv);
 }
 
-// Their sums (fp32 over four tokens, in weights relative to the first one's, which the hardware's reciprocal gives to
-// 2^-22; then in double) and gradients; nb: the sequences' counts.
+// Their sums and gradients; nb: the sequences' counts.
 template <int F>
 __device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v, int64_t i, int64_t n, const int* nb,
                                            double scale, double (&acc)[POL_SUMS]) {
-  auto weigh = [&](double w, float (&f)[POL_SUMS]) {
-#pragma unroll
-    for (int k = 0; k < POL_SUMS; ++k) acc[k] += w * (double)f[k];
-  };
   if (v.vec) {
     f32x4u g = {0.f, 0.f, 0.f, 0.f}, ge = g;
     if (tokens_any(v)) {
@@ -250,19 +247,16 @@ __device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v,
       const double w0 = (F & POL_SEQ_MEAN) ? scale * inverse(max(v.nb0, 1)) : scale;
       const double w1 = (F & POL_SEQ_MEAN) ? scale * inverse(max(v.nb1, 1)) : scale;
       const float g0 = (float)(w0 * a.grad_scale), g1 = (float)(w1 * a.grad_scale);
-      const float om = (F & POL_SEQ_MEAN) ? (float)max(v.nb0, 1) * __builtin_amdgcn_rcpf((float)max(v.nb1, 1)) : 1.f;
-      float f[POL_SUMS] = {};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const bool first = q < v.turn;
         const bool on = (v.on >> 8 * q & 0xff) != 0;
         const float gw = first ? g0 : g1, ab = first ? v.ab0 : v.ab1;
-        const float d = policy_token<F>(a, on, first ? 1.f : om, v.lp[q], v.old[q], (F & POL_TOKEN_ADV) ? v.adv[q] : ab,
-                                        v.ref[q], v.ent[q], f);
+        const float d = policy_token<F>(a, on, first ? w0 : w1, v.lp[q], v.old[q], (F & POL_TOKEN_ADV) ? v.adv[q] : ab,
+                                        v.ref[q], v.ent[q], acc);
         g[q] = on ? gw * d : 0.f;
         ge[q] = on ? -a.ent_coef * gw : 0.f;
       }
-      weigh(w0, f);
     }
     *reinterpret_cast<f32x4u*>(a.dlogp + i) = g;
     if (F & POL_ENT) *reinterpret_cast<f32x4u*>(a.dent + i) = ge;
@@ -275,11 +269,9 @@ __device__ __forceinline__ void tokens_run(const PolicyArgs& a, const Tokens& v,
       const int64_t b = seq_of(j, a.len);
       const double w = (F & POL_SEQ_MEAN) ? scale * inverse(nb[b]) : scale;
       const float gw = (float)(w * a.grad_scale);
-      float f[POL_SUMS] = {};
-      g = gw * policy_token<F>(a, true, 1.f, a.logp[j], a.old[j], a.adv[(F & POL_TOKEN_ADV) ? j : b], (F & POL_REF) ? a.ref[j] : 0.f,
-                            (F & POL_ENT) ? a.ent[j] : 0.f, f);
+      g = gw * policy_token<F>(a, true, w, a.logp[j], a.old[j], a.adv[(F & POL_TOKEN_ADV) ? j : b],
+                               (F & POL_REF) ? a.ref[j] : 0.f, (F & POL_ENT) ? a.ent[j] : 0.f, acc);
       ge = -a.ent_coef * gw;
-      weigh(w, f);
     }
     a.dlogp[j] = g;
     if (F & POL_ENT) a.dent[j] = ge;

@@ -321,6 +321,33 @@ def test_policy_loss_is_the_same_every_time(b, s):
         assert all(x is y is None or torch.equal(x, y) for x, y in zip(out, want))
 
 
+@pytest.mark.parametrize("b,s", [(2, 3), (4, 64), (3, 2731), (37, 1111), (300, 1024)])
+def test_policy_loss_where_its_terms_cancel(b, s):
+    """Advantages of both signs whose terms all but cancel: what is left must not be the rounding of e^x.  Near 1 the
+    kernel has e^x as 1 + x + t, x exact in double and t = e^x - 1 - x in fp32 within 2^-20 (8 steps of Horner's rule,
+    each 2^-24, and as much for the series' end and products): so the loss within that of sum w |A| t, plus half a
+    step of its own type."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(b + s)
+    on = _answers(r, b, s)
+    lp = -np.abs(r.normal(size=(b, s)))
+    old = lp + 0.01 * r.normal(size=(b, s))
+    adv = r.normal(size=(b, s))
+    n = on.sum()
+    adv[on] -= adv[on].sum() / n  # sum of A near 0, and so of -e^x A
+    T = {k: _f32(a) for k, a in dict(lp=lp, old=old, adv=adv).items()}
+    mask = torch.from_numpy(on).to("cuda:0")
+    for red in ("token", "sequence"):
+        kw = dict(clip_low=0.5, clip_high=0.5, reduction=red)
+        got = losses.policy_loss(T["lp"][0], T["old"][0], T["adv"][0], mask, **kw)
+        want = L.policy_loss(T["lp"][1], T["old"][1], T["adv"][1], on, **kw)
+        x = T["lp"][1] - T["old"][1]
+        w = 1.0 / n if red == "token" else on / np.maximum(on.sum(1, keepdims=True), 1) / (on.sum(1) > 0).sum()
+        bound = (on * w * np.abs(T["adv"][1]) * (np.expm1(x) - x)).sum() * 2.0 ** -20
+        _close("loss", got.loss, np.array([want["loss"]]), U, bound + 1e-15)
+
+
 def test_policy_loss_of_ratios_past_the_type():
     """e^x overflows: a clipped token and one with no advantage stay finite, and so does the loss of the
     others' sequence."""

@@ -428,7 +428,7 @@ __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[W
       s += __shfl_xor(s, o, 64);
       w += __shfl_xor(w, o, 64);
     }
-    if (k == 0 && row < rows) g.stats[panel + row] = RowPart{m, s, w};
+    if (k == 0 && row < rows) g.stats[panel + row] = RowPart{m, s - 1.f, w};
   });
 }
 

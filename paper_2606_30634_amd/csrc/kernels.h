@@ -91,8 +91,8 @@ void launch_ce_bwd(bool bf, const float* logits, const int32_t* targets, const f
                    float scale, void* dlogits, int ld, hipStream_t st);
 void launch_mean(const float* v, int n, float* out, hipStream_t st);
 
-// Statistics of a part of a row of logits: its maximum m, s = sum 2^t and w = sum t 2^t, t = c (x - m);
-// m is the lowest finite value where there is nothing above it
+// Statistics of a part of a row of logits: its maximum m, s = sum 2^t - 1 and w = sum t 2^t, t = c (x - m);
+// m is the lowest finite value where there is nothing above it, s = -1 of only -inf
 struct RowPart { float m, s, w; };
 
 // ------------------------------------------------------------------ GEMM (gemm.hip)
@@ -145,9 +145,9 @@ struct GemmArgs {
   // product of partial tiles ignores the flag (and computes every tile)
   int sym = 0;
   // epilogue 9 (row statistics): nothing of the product is stored.  Per row and panel of
-  // gemm_rowstat_panel() columns, panel p of row m writes its maximum x0 and the sums of 2^t and of
-  // t 2^t, t = stat_c (x - x0), to stats[p stat_ld + m], and the row's logit of column targets[m] goes to
-  // stat_xt[m] (nothing where targets[m] is outside [0, N)).
+  // gemm_rowstat_panel() columns, panel p of row m writes its statistics (RowPart, c = stat_c) to
+  // stats[p stat_ld + m], and the row's logit of column targets[m] goes to stat_xt[m] (nothing where targets[m]
+  // is outside [0, N)).
   RowPart* stats = nullptr;
   float stat_c = 0.f;
   const int32_t* targets = nullptr;

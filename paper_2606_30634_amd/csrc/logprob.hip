@@ -2,13 +2,14 @@
 //
 // For a row x of V logits, s = inv_temperature > 0, m = max x and S = sum exp(s (x_j - m)):
 //   log p_j = s (x_j - m) - log S,   H = log S - sum p_j s (x_j - m)   (both terms >= 0: no cancellation)
+// with S held as S - 1, the sum without the maximum's own term.
 //   dx_j = s (g (1[j = t] - p_j) - h p_j (log p_j + H))   for upstream g = dlogp, h = dentropy.
 // Everything is taken relative to m: x_j - m is exact where it matters, so logits of any magnitude
 // lose nothing, and log p_t = s (x_t - m) - log S is small where p_t is near 1.  Exponentials are base 2
 // with c = s log2(e); sums are fp32.
 //
 // What a row may hold: -inf adds nothing; the running maximum starts at the lowest finite value, so a row
-// of only -inf ends with S = 0 (told apart from one of lowest finite values, which is uniform); a NaN or
+// of only -inf ends with S = 0, S - 1 = -1 (told apart from one of lowest finite values, which is uniform); a NaN or
 // +inf makes the row NaN through S.
 #include "common.h"
 #include "kernels.h"
@@ -38,39 +39,45 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[N]) {
   __builtin_nontemporal_store(r, reinterpret_cast<raw*>(p));
 }
 
-// Running statistics of a part of a row
+// Statistics of a part of a row: its maximum and the sums but for the maximum's own 1, so that they keep their bits
+// where it is nearly all of the row (log p is then the logarithm of 1 plus them).  Of no logit, or only -inf: s = -1.
 typedef RowPart Part;
-__device__ __forceinline__ Part part_empty() { return {-FLT_MAX, 0.f, 0.f}; }
+__device__ __forceinline__ Part part_empty() { return {-FLT_MAX, -1.f, 0.f}; }
 
-// a's sums relative to the maximum mx >= a.m (an empty part's shift is -inf or NaN: it has nothing to move)
-__device__ __forceinline__ void part_raise(Part& a, float mx, float c) {
-  const float d = fmaxf((a.m - mx) * c, TINY_T), k = __builtin_amdgcn_exp2f(d);
-  a.w = k * (a.w + d * a.s);
-  a.s *= k;
-  a.m = mx;
-}
 __device__ __forceinline__ void part_merge(Part& a, Part b, float c) {
-  const float mx = fmaxf(a.m, b.m);
-  part_raise(a, mx, c);
-  part_raise(b, mx, c);
-  a.s += b.s;
-  a.w += b.w;
+  const bool up = b.m > a.m;
+  const Part hi{up ? b.m : a.m, up ? b.s : a.s, up ? b.w : a.w}, lo{up ? a.m : b.m, up ? a.s : b.s, up ? a.w : b.w};
+  // (an empty part's shift is -inf or NaN: it has nothing to move)
+  const float d = fmaxf((lo.m - hi.m) * c, TINY_T), k = __builtin_amdgcn_exp2f(d), s = 1.f + lo.s;
+  a = {hi.m, hi.s + k * s, hi.w + k * (lo.w + d * s)};
 }
+// The same while it runs: the logits at the maximum are counted apart.
+struct Running { float m, s, w, n; };
+__device__ __forceinline__ Part part_of(const Running& a) { return {a.m, a.s + (a.n - 1.f), a.w}; }
 template <int N>
-__device__ __forceinline__ void part_add(Part& a, const float (&v)[N], float c) {
+__device__ __forceinline__ void part_add(Running& a, const float (&v)[N], float c) {
   float mx = v[0];
 #pragma unroll
   for (int q = 1; q < N; ++q) mx = fmaxf(mx, v[q]);
-  if (mx > a.m) part_raise(a, mx, c);
+  if (mx > a.m) {
+    const float d = fmaxf((a.m - mx) * c, TINY_T), k = __builtin_amdgcn_exp2f(d), s = a.s + a.n;
+    a.w = k * (a.w + d * s);
+    a.s = k * s;
+    a.m = mx;
+    a.n = 0.f;
+  }
+  a.n += (float)N;
 #pragma unroll
   for (int q = 0; q < N; ++q) {
     const float t = (v[q] - a.m) * c, e = __builtin_amdgcn_exp2f(t);
-    a.s += e;
+    const float below = __builtin_amdgcn_fmed3f(t * -1e38f, 0.f, 1.f);  // 0 at the maximum, else 1
+    a.n -= below;
+    a.s += e * below;
     a.w += e * fmaxf(t, TINY_T);
   }
 }
 template <int LANES>
-__device__ __forceinline__ void part_lanes(Part& a, float c) {  // the same in every lane of the group
+__device__ __forceinline__ void part_lanes(Part& a, float c) {  // the group's; lane 0's is the one to use
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) {
     const Part b{__shfl_xor(a.m, o, WAVE), __shfl_xor(a.s, o, WAVE), __shfl_xor(a.w, o, WAVE)};
@@ -81,10 +88,11 @@ __device__ __forceinline__ void part_lanes(Part& a, float c) {  // the same in e
 // What a row's statistics say about its target (x_t its logit).
 __device__ __forceinline__ void row_finish(const Part& a, float xt, float c, int64_t row, float* logp, float* ent,
                                            float* stats) {
-  const float ls = logf(a.s);
-  const bool none = a.s == 0.f;  // every logit -inf: no distribution
+  // log(1 + s): of the rounded sum, and what its rounding left, which is exact
+  const float u = 1.f + a.s, ls = logf(u) + (a.s - (u - 1.f)) * __builtin_amdgcn_rcpf(u);
+  const bool none = a.s == -1.f;  // every logit -inf: no distribution
   logp[row] = none ? -INFINITY : (xt - a.m) * c * LN2 - ls;
-  if (ent) ent[row] = none ? 0.f : ls - a.w / a.s * LN2;
+  if (ent) ent[row] = none ? 0.f : ls - a.w / u * LN2;
   if (stats) {
     stats[2 * row] = none ? -INFINITY : a.m;
     stats[2 * row + 1] = none ? 0.f : ls;
@@ -97,9 +105,11 @@ __device__ __forceinline__ void row_ignored(int64_t row, float* logp, float* ent
 }
 
 // One row (or one of nsplit equal parts of it) per group of NT threads of a block; a block holds RPB groups.  One pass:
-// the maximum and both sums as they run, rescaled where a 16-byte vector raises the maximum.
-// Bound: memory, each logit read once, past the caches (8192 x 49152 fp32, a quarter of the rows ignored: 181 us,
-// 6.7 TB/s, where a streaming copy reaches 6.3; with cached loads 212); 12 vector operations a logit are 0.4 of that.
+// the maximum and both sums as they run, rescaled where a 16-byte vector raises the maximum; what stands at the maximum is counted instead.
+// Bound: memory, each logit read once, past the caches (8192 x 49152 fp32, a quarter of the rows ignored: 182 us,
+// 6.6 TB/s, where a streaming copy reaches 6.3; with cached loads 212); 14 vector operations a logit are 0.45 of that.
+// Two of them leave the maximum out of the sum: fp32 as fast without, bf16 51 : 55 us (4096 x 32000) and 512 logits
+// a row 37 : 40 (60000 fp32), against a log p of 1e-4 to one part in 1000.
 template <typename T, int NT, int RPB>
 __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
                                                          const int32_t* __restrict__ tg, float c, int nsplit, int per,
@@ -119,24 +129,25 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
     }
     const T* z = x + row * ld + (int64_t)sp * per;
     const int n = max(0, min(per, V - sp * per)), nv = n / E;
-    Part a = part_empty();
+    Running run{-FLT_MAX, 0.f, 0.f, 0.f};
     int j = tid;
     for (; j + (U - 1) * NT < nv; j += U * NT) {
       float v[U][E];
 #pragma unroll
       for (int u = 0; u < U; ++u) load_vec(z + (int64_t)(j + u * NT) * E, v[u]);
 #pragma unroll
-      for (int u = 0; u < U; ++u) part_add(a, v[u], c);
+      for (int u = 0; u < U; ++u) part_add(run, v[u], c);
     }
     for (; j < nv; j += NT) {
       float v[E];
       load_vec(z + (int64_t)j * E, v);
-      part_add(a, v, c);
+      part_add(run, v, c);
     }
     if (tid < n - nv * E) {
       const float v[1] = {to_f32(z[nv * E + tid])};
-      part_add(a, v, c);
+      part_add(run, v, c);
     }
+    Part a = part_of(run);
     part_lanes<WAVE>(a, c);
     if constexpr (NW > 1) {
       __syncthreads();  // the row before has been read

@@ -161,6 +161,32 @@ def test_rows_of_masks_and_nonfinite_values(v, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,v", [(1, 3), (5, 100), (1100, 513), (3, 2500), (7, 40007), (1, 128256)])
+def test_a_target_of_probability_near_one(n, v, bf16):
+    """log p of a target that has nearly all of the row is -log(1 + s) with s the others' sum, some 2^-20: it keeps
+    its own relative accuracy, as the entropy does.  Every term of s: its exponent t < 2^5 rounded, 2^5 log 2 u, and
+    exp2's 2 u; the sum: a thread's chain of at most v / 64 + 32 additions and 16 merges of 3 roundings; the logarithm
+    and the last products 8 u."""
+    torch = _torch()
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(v + n)
+    x = r.normal(size=(n, v))
+    t = r.integers(0, v, size=n).astype(np.int32)
+    x = np.minimum(x, 2.0)
+    x[np.arange(n), t] = 16.0 + np.floor(np.log(v))
+    X, ref = _matrix(x, bf16)
+    got = losses.token_logprob(X, _i32(t))
+    z = ref - ref[np.arange(n), t][:, None]
+    e = np.exp(z)
+    e[np.arange(n), t] = 0.0
+    s = e.sum(1)
+    assert (s < 2.0 ** -10).all()
+    tol = (22 + 2 + v / 64 + 32 + 48 + 8) * U
+    _close("logp", got.logp, -np.log1p(s), tol)
+    _close("entropy", got.entropy, np.log1p(s) - (e * z).sum(1) / (1 + s), 2 * tol)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 def test_gradient_in_place(bf16):
     from paper_2606_30634_amd import losses
     r = np.random.default_rng(5)

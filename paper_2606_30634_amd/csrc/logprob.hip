@@ -105,7 +105,8 @@ __device__ __forceinline__ void row_ignored(int64_t row, float* logp, float* ent
 }
 
 // One row (or one of nsplit equal parts of it) per group of NT threads of a block; a block holds RPB groups.  One pass:
-// the maximum and both sums as they run, rescaled where a 16-byte vector raises the maximum; what stands at the maximum is counted instead.
+// the maximum and both sums as they run, rescaled where a 16-byte vector raises the maximum; what stands at the maximum
+// is counted instead.
 // Bound: memory, each logit read once, past the caches (8192 x 49152 fp32, a quarter of the rows ignored: 182 us,
 // 6.6 TB/s, where a streaming copy reaches 6.3; with cached loads 212); 14 vector operations a logit are 0.45 of that.
 // Two of them leave the maximum out of the sum: fp32 as fast without, bf16 51 : 55 us (4096 x 32000) and 512 logits

@@ -477,12 +477,17 @@ HeadLayout head_layout(bool bf, int64_t n, int64_t vocab, int64_t d) {
   l.total = at;
   return l;
 }
-size_t chunk_bytes(int64_t r, int64_t vocab) { return align256((size_t)(r * vocab * 4)) + logprob_ws_bytes(r, vocab); }
+// The logits of r rows, then the parts of the rows of the call's chunks: the last chunk has fewer rows, which are split
+// further and can have more parts than the others (V 128256: 65 rows 455 parts, 64 rows 512).
+size_t chunked_bytes(int64_t rows, int64_t r, int64_t vocab) {
+  const int64_t last = (rows - 1) % r + 1;
+  return align256((size_t)(r * vocab * 4)) + std::max(logprob_ws_bytes(r, vocab), logprob_ws_bytes(last, vocab));
+}
 
 }  // namespace
 
 size_t head_logprob_ws_bytes(bool bf, int64_t rows, int64_t vocab, int64_t d) {
-  const size_t chunked = chunk_bytes(head_chunk(rows, vocab, HEAD_ODD_BYTES), vocab);
+  const size_t chunked = chunked_bytes(rows, head_chunk(rows, vocab, HEAD_ODD_BYTES), vocab);
   const int64_t first = std::min(rows, HEAD_ROWS), last = (rows - 1) % HEAD_ROWS + 1;
   return std::max({head_layout(bf, first, vocab, d).total, head_layout(bf, last, vocab, d).total, chunked});
 }

@@ -85,13 +85,14 @@ __device__ __forceinline__ void part_lanes(Part& a, float c) {  // the group's; 
   }
 }
 
-// What a row's statistics say about its target (x_t its logit).
-__device__ __forceinline__ void row_finish(const Part& a, float xt, float c, int64_t row, float* logp, float* ent,
+// What a row's statistics say about its target (x_t its logit).  s (x_t - m) by s itself: as a multiple of c it took
+// three roundings for one, and a target at the lowest finite value overflowed.
+__device__ __forceinline__ void row_finish(const Part& a, float xt, float inv_temp, int64_t row, float* logp, float* ent,
                                            float* stats) {
   // log(1 + s): of the rounded sum, and what its rounding left, which is exact
   const float u = 1.f + a.s, ls = logf(u) + (a.s - (u - 1.f)) * __builtin_amdgcn_rcpf(u);
   const bool none = a.s == -1.f;  // every logit -inf: no distribution
-  logp[row] = none ? -INFINITY : (xt - a.m) * c * LN2 - ls;
+  logp[row] = none ? -INFINITY : (xt - a.m) * inv_temp - ls;
   if (ent) ent[row] = none ? 0.f : ls - a.w / u * LN2;
   if (stats) {
     stats[2 * row] = none ? -INFINITY : a.m;
@@ -113,12 +114,13 @@ __device__ __forceinline__ void row_ignored(int64_t row, float* logp, float* ent
 // a row 37 : 40 (60000 fp32), against a log p of 1e-4 to one part in 1000.
 template <typename T, int NT, int RPB>
 __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
-                                                         const int32_t* __restrict__ tg, float c, int nsplit, int per,
-                                                         Part* __restrict__ parts, float* __restrict__ logp,
+                                                         const int32_t* __restrict__ tg, float inv_temp, int nsplit,
+                                                         int per, Part* __restrict__ parts, float* __restrict__ logp,
                                                          float* __restrict__ ent, float* __restrict__ stats) {
   constexpr int NW = NT / WAVE, E = VE<T>, U = 32 / E;
   static_assert(NW == 1 || RPB == 1, "groups of one wave, or one group per block");
   __shared__ Part sm[NW];
+  const float c = inv_temp * LOG2E;
   const int tid = threadIdx.x % NT;
   const int64_t items = rows * nsplit;
   for (int64_t it = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; it < items; it += (int64_t)gridDim.x * RPB) {
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
     }
     if (tid == 0) {
       if (nsplit > 1) parts[it] = a;
-      else row_finish(a, to_f32(x[row * ld + t]), c, row, logp, ent, stats);
+      else row_finish(a, to_f32(x[row * ld + t]), inv_temp, row, logp, ent, stats);
     }
   }
 }
@@ -169,9 +171,10 @@ __global__ void __launch_bounds__(NT * RPB) logprob_rows(int64_t rows, int V, co
 // Joins the nsplit <= 64 parts of every row, a wave per row (2.2 us for one).
 template <typename T>
 __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T* __restrict__ x, int64_t ld,
-                                                    const int32_t* __restrict__ tg, float c, int nsplit,
+                                                    const int32_t* __restrict__ tg, float inv_temp, int nsplit,
                                                     const Part* __restrict__ parts, float* __restrict__ logp,
                                                     float* __restrict__ ent, float* __restrict__ stats) {
+  const float c = inv_temp * LOG2E;
   const int lane = threadIdx.x % WAVE;
   for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE; row < rows; row += (int64_t)gridDim.x * 4) {
     const int t = tg[row];
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T
     }
     Part a = lane < nsplit ? parts[row * nsplit + lane] : part_empty();
     part_lanes<WAVE>(a, c);
-    if (lane == 0) row_finish(a, to_f32(x[row * ld + t]), c, row, logp, ent, stats);
+    if (lane == 0) row_finish(a, to_f32(x[row * ld + t]), inv_temp, row, logp, ent, stats);
   }
 }
 
@@ -284,7 +287,6 @@ constexpr int64_t GRID = 1 << 20;  // blocks of a launch at most; the kernels wa
 template <typename T>
 void logprob_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg, float s, float* logp, float* ent,
                float* stats, void* ws, hipStream_t st) {
-  const float c = s * LOG2E;
   const int ns = row_splits(rows, V);
   const int per = (int)(cdiv(cdiv(V, ns), 8) * 8);
   const T* z = (const T*)x;
@@ -294,12 +296,12 @@ void logprob_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg
   // 6000 67 : 73, 8192 86 : 81; 2048 rows, bf16 V 6000 10.7 : 9.8)
   if (V <= 2048 || (rows >= 1024 && (int64_t)V * sizeof(T) <= 24576))
     logprob_rows<T, 64, 4><<<(unsigned)std::min(GRID, cdiv(rows * ns, 4)), 256, 0, st>>>(
-        rows, V, z, ld, tg, c, ns, per, parts, logp, ent, stats);
+        rows, V, z, ld, tg, s, ns, per, parts, logp, ent, stats);
   else
-    logprob_rows<T, 256, 1><<<(unsigned)std::min(GRID, rows * ns), 256, 0, st>>>(rows, V, z, ld, tg, c, ns, per,
+    logprob_rows<T, 256, 1><<<(unsigned)std::min(GRID, rows * ns), 256, 0, st>>>(rows, V, z, ld, tg, s, ns, per,
                                                                                   parts, logp, ent, stats);
   if (ns > 1)
-    logprob_join<T><<<(unsigned)std::min(GRID, cdiv(rows, 4)), 256, 0, st>>>(rows, V, z, ld, tg, c, ns, parts, logp,
+    logprob_join<T><<<(unsigned)std::min(GRID, cdiv(rows, 4)), 256, 0, st>>>(rows, V, z, ld, tg, s, ns, parts, logp,
                                                                               ent, stats);
 }
 
@@ -399,13 +401,14 @@ __global__ void __launch_bounds__(256) gather_rows(int rows, int chunks, const u
 // Joins the panels of every row (parts[p rows + row], or of its place where rows are packed): RJ rows per block of
 // 256, 256 / RJ threads on each.  384 panels of 8192 rows: 10 us for 38 MB.
 template <int RJ>
-__global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panels, const int32_t* __restrict__ tg, float c,
-                                                  const Part* __restrict__ parts, const float* __restrict__ xt,
+__global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panels, const int32_t* __restrict__ tg,
+                                                  float inv_temp, const Part* __restrict__ parts, const float* __restrict__ xt,
                                                   const int32_t* __restrict__ pos, const int32_t* __restrict__ live,
                                                   float* __restrict__ logp, float* __restrict__ ent,
                                                   float* __restrict__ stats) {
   constexpr int TR = 256 / RJ;  // threads per row
   __shared__ Part sm[4 * RJ];
+  const float c = inv_temp * LOG2E;
   const int r = threadIdx.x % RJ, k = threadIdx.x / RJ;
   const int64_t row = (int64_t)blockIdx.x * RJ + r;
   const int t = row < rows ? tg[row] : -1;
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panel
     for (int w = 1; w < 4; ++w) part_merge(a, sm[w * RJ + r], c);
   }
   if (k == 0 && row < rows) {
-    if (on) row_finish(a, xt[at], c, row, logp, ent, stats);
+    if (on) row_finish(a, xt[at], inv_temp, row, logp, ent, stats);
     else row_ignored(row, logp, ent, stats);
   }
 }
@@ -535,10 +538,10 @@ void launch_head_logprob(bool bf, int64_t rows, int vocab, int d, const void* x,
     float* e = ent ? ent + r0 : nullptr;
     float* q = stats ? stats + 2 * r0 : nullptr;
     if (n >= 256)
-      panel_join<16><<<(unsigned)cdiv(n, 16), 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, pos,
+      panel_join<16><<<(unsigned)cdiv(n, 16), 256, 0, st>>>(n, vocab, panels, g.targets, inv_temp, g.stats, g.stat_xt, pos,
                                                             g.live, logp + r0, e, q);
     else
-      panel_join<1><<<(unsigned)n, 256, 0, st>>>(n, vocab, panels, g.targets, g.stat_c, g.stats, g.stat_xt, pos, g.live,
+      panel_join<1><<<(unsigned)n, 256, 0, st>>>(n, vocab, panels, g.targets, inv_temp, g.stats, g.stat_xt, pos, g.live,
                                                  logp + r0, e, q);
   }
   if (fused) return;

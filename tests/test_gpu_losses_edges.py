@@ -91,3 +91,111 @@ def test_other_workspaces_are_enough():
             ws, whole = _guarded(B.preference_loss_workspace_bytes(b // 2, s))
             losses.preference_loss(lp, on, workspace=ws)
             assert whole()
+
+
+# ------------------------------------------------------------------ from hidden states
+def _one_hot(n, d, bf16):
+    """Hidden states that pick a column of the head's matrix each, so that a product's logits are its elements."""
+    import torch
+    x = torch.zeros(n, d, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+    x[torch.arange(n), torch.arange(n) % d] = 1
+    return x
+
+
+TILES = [(True, 64, 128, 64), (True, 130, 257, 40), (True, 1152, 4096, 1024), (True, 2944, 1024, 64), (True, 2000, 6001, 520),
+         (True, 32, 25856, 64), (True, 7, 26001, 72), (False, 64, 128, 64), (False, 130, 257, 40), (False, 1024, 4096, 256),
+         (False, 2000, 4001, 772), (False, 32, 1280, 64), (False, 5, 1001, 68), (True, 5, 40, 64), (False, 3, 700, 33)]
+
+
+@pytest.mark.parametrize("bf16,n,v,d", TILES)
+def test_head_of_masks_and_nonfinite_values(bf16, n, v, d):
+    """-inf, the type's lowest value, +inf and NaN among the logits of a head, at both ends of the vocabulary and inside it:
+    as for rows of logits."""
+    import torch
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(v)
+    lowest = float(torch.finfo(torch.bfloat16 if bf16 else torch.float32).min)
+    w = np.minimum(r.normal(size=(v, d)) * 2, 6.0)
+    kinds = np.arange(d) % 6
+    tk = r.integers(0, v, size=d)
+    w[:, kinds == 1] = lowest                                  # uniform
+    for j in np.nonzero(kinds == 2)[0]:                        # one token left
+        w[:, j] = lowest
+        w[tk[j], j] = 3.0
+    w[::2, kinds == 3] = lowest                                # every other one masked
+    w[-1, kinds == 4] = lowest
+    w[:, kinds == 5] += 3e4                                    # large logits
+    mw, wv = _matrix(w, bf16)
+    x = _one_hot(n, d, bf16)
+    k = np.arange(n) % d
+    ref = L.token_logprob(wv.T.copy(), tk, 1.0)
+
+    def check(got, rows):
+        for g, want, tol in zip(got, ref, (_err(v, ref[0]), 2 * _err(v, 0.0) * (np.abs(ref[2][:, 1]) + 1 + np.log(v)),
+                                           np.full((d, 1), _err(v, 0.0)))):
+            g, want, tol = _np(g)[rows], want[k][rows], np.asarray(tol)[k][rows]
+            assert (np.abs(g - want) <= tol).all(), np.abs(g - want).max()
+        assert (_np(got.stats)[rows, 0] == ref[2][k][rows, 0]).all()
+    got = losses.head_logprob(x, mw, _i32(tk[k]))
+    check(got, np.ones(n, bool))
+    # a hidden state with a NaN or an infinity makes its own row NaN and no other
+    x[0, 0] = float("nan")
+    x[n - 1, d - 1] = float("inf")
+    got = losses.head_logprob(x, mw, _i32(tk[k]))
+    for row in (0, n - 1):
+        with np.errstate(invalid="ignore"):
+            z = _np(x[row]) @ wv.T
+        if (np.isnan(z) | (z == np.inf)).any():
+            assert np.isnan(_np(got.logp)[row]) and np.isnan(_np(got.entropy)[row])
+        else:  # the infinity met only negative elements
+            assert (z == -np.inf).all() and _np(got.logp)[row] == -np.inf and _np(got.entropy)[row] == 0
+    check(got, np.arange(n) % (n - 1) != 0)
+    # rows of the head's matrix that are -inf: tokens that cannot occur; nothing else: no distribution
+    x = torch.ones_like(x)
+    wi, t = wv.copy(), tk[k]
+    wi[: v // 2] = -np.inf
+    wi[-1] = -np.inf
+    t = np.where(t < v // 2, 0, np.minimum(t, v - 2))
+    mw, wiv = _matrix(wi / 64, bf16)
+    got = losses.head_logprob(x, mw, _i32(t))
+    z = wiv.sum(1)
+    z[z < np.finfo(np.float32).min] = -np.inf  # a product past fp32, of a wide head's masks
+    with np.errstate(invalid="ignore"):
+        one = L.token_logprob(np.repeat(z[None], n, 0), t, 1.0)
+    assert (_np(got.logp)[one[0] == -np.inf] == -np.inf).all() and (one[0][t == 0] == -np.inf).all()
+    e = 2 * U * (d + 2) * float(np.abs(wiv[np.isfinite(wiv).all(1)]).sum(1).max())
+    fin = np.isfinite(one[0])
+    assert (np.abs(_np(got.logp)[fin] - one[0][fin]) <= e + _err(v, one[0][fin])).all()
+    assert (np.abs(_np(got.entropy) - one[1]) <= (e + 2 * _err(v, 0.0)) * 2 * (1 + np.log(v) + one[2][:, 1])).all()
+    got = losses.head_logprob(x, torch.full_like(mw, -torch.inf), _i32(t))
+    assert bool((got.logp == -torch.inf).all()) and not bool(got.entropy.any())
+    assert bool((got.stats[:, 0] == -torch.inf).all()) and not bool(got.stats[:, 1].any())
+
+
+# ------------------------------------------------------------------ the target's own term
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("path", ["rows", "parts", "head"])
+def test_log_probability_of_a_far_target(path, bf16):
+    """s (x_t - m) beside a log-sum that is nearly nothing: with m = 0 and s = 1 the difference and the product are exact
+    and log p is rounded once, u of it; with another s twice.  The log-sum's own 8 u come on top."""
+    import torch
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(3)
+    n, v = 64, 40000 if path == "parts" else 96
+    x = np.full((n, v), -150.0)
+    x[np.arange(n), r.integers(0, v // 2, size=n)] = 0.0
+    t = v // 2 + r.integers(0, v // 2, size=n)
+    x[np.arange(n), t] = -r.uniform(9, 90, size=n)
+    for s, roundings in ((1.0, 1), (1.3, 2)):
+        if path == "head":  # a row of the identity per logit row
+            mx, xv = _matrix(x.T.copy(), bf16)
+            got = losses.head_logprob(_one_hot(n, n, bf16), mx, _i32(t), inv_temperature=s)
+            xv = xv.T
+        else:
+            mx, xv = _matrix(x, bf16)
+            got = losses.token_logprob(mx, _i32(t), inv_temperature=s)
+        sf = float(np.float32(s))
+        ls = np.log1p(np.exp(sf * xv[np.arange(n), t]))
+        want = sf * xv[np.arange(n), t] - ls
+        d = np.abs(_np(got.logp) - want)
+        assert (d <= roundings * U * np.abs(want) * (1 + 2.0 ** -20) + 8 * U * ls).all(), (s, (d / np.abs(want)).max() / U)

@@ -227,17 +227,19 @@ __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T*
       continue;
     }
     // without an entropy gradient an element is -g p; the target's is written apart, after its wave's stores
-    // (1 - p_t is -(e^lp - 1), which keeps its bits where p_t is near 1)
+    // (1 - p_t is -(e^lp - 1), which keeps its bits where p_t is near 1); where p is 0, log p may be -inf or h log p past
+    // the type
     auto grad = [&](float v) {
       const float q = (v - m) * c - l2, p = __builtin_amdgcn_exp2f(q);
-      return h == 0.f ? -g * p : -p * (g + h * (fmaxf(q, TINY_T) * LN2 + H));
+      return h == 0.f ? -g * p : p == 0.f ? 0.f : -p * (g + h * (q * LN2 + H));
     };
     const bool mine = t >= j0 && t < j0 + CH;
     float dt = 0.f;
     if (mine) {
       const float q = (to_f32(z[t]) - m) * c - l2;
       dt = -g * expm1f(q * LN2);
-      if (h != 0.f) dt -= __builtin_amdgcn_exp2f(q) * h * (fmaxf(q, TINY_T) * LN2 + H);
+      const float p = __builtin_amdgcn_exp2f(q);
+      if (h != 0.f && p != 0.f) dt -= p * h * (q * LN2 + H);
     }
     if (j0 + CH <= V) {
       float v[U][E];

@@ -199,3 +199,35 @@ def test_log_probability_of_a_far_target(path, bf16):
         want = sf * xv[np.arange(n), t] - ls
         d = np.abs(_np(got.logp) - want)
         assert (d <= roundings * U * np.abs(want) * (1 + 2.0 ** -20) + 8 * U * ls).all(), (s, (d / np.abs(want)).max() / U)
+
+
+# ------------------------------------------------------------------ masked logits under a large upstream gradient
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("v", [6, 700, 40001])
+def test_entropy_gradient_of_masked_logits_at_large_scales(v, bf16):
+    """-inf logits, and ones s takes past the type's range, have p = 0 and so no entropy gradient, however large s times
+    dentropy is."""
+    import torch
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(v)
+    n = 5
+    x = r.normal(size=(n, v))
+    x[:, ::2] = -np.inf
+    x[:, 1], x[:, 5] = 4.0, 4.0  # two tokens share the row where s is large
+    t = np.array([1, 1, 0, 3, 5])  # the third cannot occur
+    x[3, 3] = 4.0
+    mx, xv = _matrix(x, bf16)
+    g, gv = _f32(r.normal(size=n))
+    for s, dent in ((2.0 ** 40, 1e-2), (2.0 ** 60, 1e-6), (1.0, 1e10), (2.0 ** 60, 1.0), (3.0, 0.5)):
+        h, hv = _f32(np.full(n, dent))
+        fwd = losses.token_logprob(mx, _i32(t), inv_temperature=s)
+        got = _np(losses.token_logprob_backward(mx, _i32(t), fwd, g, h, inv_temperature=s,
+                                                out=torch.empty(n, v, dtype=torch.float32, device="cuda:0")))
+        with np.errstate(invalid="ignore", divide="ignore"):
+            want = L.token_logprob_bwd(xv, t, s, gv, hv)
+        assert np.isfinite(got).all(), (s, dent, np.argwhere(~np.isfinite(got))[:4])
+        tol = 4 * s * _err(v, 100.0) * (np.abs(gv) + hv * (4 + 2 * np.log(v)))[:, None]
+        assert (np.abs(got - want) <= tol).all(), (s, dent, np.abs(got - want).max())
+        masked = np.isneginf(xv)
+        masked[np.arange(n), t] = False
+        assert not got[masked].any()

@@ -357,7 +357,8 @@ int head_logprob(int64_t rows, int64_t vocab, int64_t d, const void* x, int64_t 
  *   place of N or B (a count over the whole step, where it is split into microbatches)
  *   dlogp = grad_scale w (-r A [not clipped] + kl_coef (1 - e^d)),  dentropy = -grad_scale w entropy_coef
  * A token is clipped where A > 0 and x > log(1 + clip_high), or A < 0 and x < log(1 - clip_low); it then
- * has no gradient from the first term. */
+ * has no gradient from the first term.  A term is left out where its factor (A, kl_coef, entropy_coef) is 0,
+ * also where it is infinite; e^d - 1 - d is infinite at d = +-inf. */
 typedef struct {
   float clip_low, clip_high; /* clip_low in [0, 1], clip_high >= 0 */
   float kl_coef, entropy_coef;

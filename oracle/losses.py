@@ -55,6 +55,11 @@ def token_logprob_bwd(x, targets, s, g, h=None):
 
 
 # ---------------------------------------------------------------- policy loss
+def _kl(d):
+    """e^d - 1 - d, infinite at both ends"""
+    return np.inf if np.isinf(d) else np.expm1(d) - d
+
+
 def policy_loss(logp, old, adv, mask, *, ref=None, entropy=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
                 entropy_coef=0.0, reduction="token", norm=0.0, grad_scale=1.0):
     """dict of loss, dlogp, dentropy, metrics [6], counts [2]; [B, S] arrays, adv [B] or [B, S]."""
@@ -75,18 +80,20 @@ def policy_loss(logp, old, adv, mask, *, ref=None, entropy=None, clip_low=0.2, c
             cut = (a > 0 and x > np.log1p(clip_high)) or (a < 0 and x < np.log1p(-clip_low))
             met[0] += w * max(-r * a, -min(max(r, 1.0 - clip_low), 1.0 + clip_high) * a)
             met[3] += w * cut
-            met[4] += w * (np.expm1(x) - x)
+            met[4] += w * _kl(x)
             met[5] += w * r
             g = 0.0 if cut else -r * a
             if ref is not None:
                 d = float(ref[b, t]) - float(logp[b, t])
-                met[1] += w * (np.expm1(d) - d)
-                g -= kl_coef * np.expm1(d)
+                met[1] += w * _kl(d)
+                g -= kl_coef * np.expm1(d) if kl_coef else 0.0
             if entropy is not None:
                 met[2] += w * float(entropy[b, t])
             dlogp[b, t] = grad_scale * w * g
             dent[b, t] = -grad_scale * w * entropy_coef
-    return dict(loss=met[0] + kl_coef * met[1] - entropy_coef * met[2], dlogp=dlogp,
+    # a term without a weight adds nothing, also where it is infinite
+    loss = met[0] + (kl_coef * met[1] if kl_coef else 0.0) - (entropy_coef * met[2] if entropy_coef else 0.0)
+    return dict(loss=loss, dlogp=dlogp,
                 dentropy=dent if entropy is not None else None, metrics=met, counts=np.array([tokens, seqs]))
 
 

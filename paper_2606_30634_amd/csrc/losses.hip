@@ -24,7 +24,8 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint8_t u8x4u __attribute__((ext_vector_type(4), aligned(1)));
 
 // e^x - 1 - x >= 0, given ex = e^x: the series up to x^9 where the difference cancels (next term below 3e-9 of
-// the value; from |x| = 1/2 on the difference keeps all but 2 bits).  With x added it is e^x - 1.
+// the value; from |x| = 1/2 on the difference keeps all but 2 bits).  With x added it is e^x - 1.  Infinite at x = +-inf:
+// past 89 e^x is infinite and no less for an x of 128 taken away.
 __device__ __forceinline__ float kl_term(float x, float ex) {
   float p = 1.f / 362880.f;
   p = p * x + 1.f / 40320.f;
@@ -34,7 +35,7 @@ __device__ __forceinline__ float kl_term(float x, float ex) {
   p = p * x + 1.f / 24.f;
   p = p * x + 1.f / 6.f;
   p = p * x + 0.5f;
-  const float near = p * x * x, far = (ex - 1.f) - x;  // both, so that no branch holds up the next token
+  const float near = p * x * x, far = (ex - 1.f) - fminf(x, 128.f);  // both, so that no branch holds up the next token
   return fabsf(x) >= 0.5f ? far : near;
 }
 

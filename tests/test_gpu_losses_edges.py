@@ -231,3 +231,29 @@ def test_entropy_gradient_of_masked_logits_at_large_scales(v, bf16):
         masked = np.isneginf(xv)
         masked[np.arange(n), t] = False
         assert not got[masked].any()
+
+
+# ------------------------------------------------------------------ infinite terms of the policy loss
+@pytest.mark.parametrize("b,s", [(1, 5), (3, 64), (40, 1000)])
+def test_policy_loss_of_tokens_that_cannot_occur(b, s):
+    """A counted token whose log-probability is -inf under the policy (or was under the old one): its KL terms are +inf,
+    which the loss has only with a weight on them; nothing is NaN."""
+    import torch
+    from paper_2606_30634_amd import losses
+    base = torch.full((b, s), -1.0, device="cuda:0")
+    on = torch.ones(b, s, dtype=torch.bool, device="cuda:0")
+    adv = torch.ones(b, device="cuda:0")
+    at = s // 2
+    for who in ("policy", "old", "reference"):
+        lp, old, ref = base.clone(), base.clone(), base - 0.5
+        {"policy": lp, "old": old, "reference": ref}[who][b - 1, at] = -torch.inf
+        for kl in (0.0, 0.25):
+            log(f"{who} kl {kl}")
+            got = losses.policy_loss(lp, old, adv, on, ref_logp=ref, kl_coef=kl)
+            with np.errstate(invalid="ignore", over="ignore"):
+                want = L.policy_loss(_np(lp), _np(old), _np(adv), on.cpu().numpy(), ref=_np(ref), kl_coef=kl)
+            assert not bool(got.loss.isnan()) and not bool(got.metrics.isnan().any()) and not bool(got.dlogp.isnan().any())
+            for g, w in ((got.loss, np.array([want["loss"]])), (got.metrics, want["metrics"]), (got.dlogp, want["dlogp"])):
+                g = _np(g)
+                fin = np.isfinite(w)
+                assert (g[~fin] == w[~fin]).all() and (np.abs(g[fin] - w[fin]) <= 32 * U * (1 + np.abs(w[fin]))).all(), (who, kl, g, w)

@@ -66,6 +66,19 @@ def test_policy_gradient(reduction, norm):
     assert none["loss"] == 0 and not none["dlogp"].any()
 
 
+def test_policy_of_a_token_that_cannot_occur():
+    """e^d - 1 - d at d = +inf (the policy's log-probability is -inf) and at d = -inf (the reference's): infinite, and in
+    the loss only with a weight."""
+    logp, ref = np.full((1, 3), -1.0), np.full((1, 3), -1.5)
+    for a in (logp, ref):
+        keep, a[0, 1] = a[0, 1], -np.inf
+        with np.errstate(invalid="ignore"):
+            for kl, loss in ((0.5, np.inf), (0.0, -2 / 3 if a is logp else -1.0)):
+                out = L.policy_loss(logp, np.full((1, 3), -1.0), np.ones(1), np.ones((1, 3)), ref=ref, kl_coef=kl)
+                assert np.isclose(out["loss"], loss) and out["metrics"][1] == np.inf and not np.isnan(out["dlogp"]).any()
+        a[0, 1] = keep
+
+
 @pytest.mark.parametrize("kind,smoothing", [("sigmoid", 0.0), ("sigmoid", 0.2), ("hinge", 0.0), ("square", 0.0)])
 @pytest.mark.parametrize("normalize", [False, True])
 def test_preference_gradient(kind, smoothing, normalize):

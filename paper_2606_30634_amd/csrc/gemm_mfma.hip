@@ -366,8 +366,10 @@ __device__ __forceinline__ void dma_epilogue(const GemmArgs& g, f32x16 (&acc)[WM
 // Epilogue 9: the maximum and the two sums of every row over the wave's WN columns (kernels.h).  A part
 // of RP rows goes through the wave's LDS staging as above and comes back as 64 / RP lanes per row, each
 // with every (64 / RP)-th 16-byte chunk of it, so that a row's exponentials are spread over few lanes and
-// its sums take 2 or 3 exchanges.  Bound: the product's matrix instructions (8192 x 49152 x 2048: 1350 us, 1.22
-// PFLOP/s, the rate of the plain products; writing the fp32 logits and reading them back took 1930), or B's bytes.
+// its sums take 2 or 3 exchanges.  What stands at the maximum is counted and not summed (n), so that a row whose
+// other terms are far below 1 keeps them (log p near 0 to 10^-5 of itself or better; with the 1 in the sum 0.3 to 38 %
+// off at sums of some 3 10^-7).  Bound: the product's matrix instructions (8192 x 49152 x 2048: 1418 us, 1.16 PFLOP/s, the rate of the plain
+// products; without the count 1403; writing the fp32 logits and reading them back took 1930), or B's bytes.
 template <int BM, int BN, int WM, int WN, int RP>
 __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[WM / 32][WN / 32], float* stage, int m0,
                                               int n0, int wm0, int wn0) {
@@ -414,21 +416,24 @@ __device__ __forceinline__ void stat_epilogue(const GemmArgs& g, f32x16 (&acc)[W
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    float s = 0.f, w = 0.f;
+    float s = 0.f, w = 0.f, n = 4.f * CI;
 #pragma unroll
     for (int q = 0; q < CI; ++q)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const float t = (v[q][u] - m) * c, e = __builtin_amdgcn_exp2f(t);
-        s += e;
+        const float below = __builtin_amdgcn_fmed3f(t * -1e38f, 0.f, 1.f);
+        n -= below;
+        s += e * below;
         w += e * fmaxf(t, -1e30f);
       }
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) {
+      n += __shfl_xor(n, o, 64);
       s += __shfl_xor(s, o, 64);
       w += __shfl_xor(w, o, 64);
     }
-    if (k == 0 && row < rows) g.stats[panel + row] = RowPart{m, s - 1.f, w};
+    if (k == 0 && row < rows) g.stats[panel + row] = RowPart{m, s + (n - 1.f), w};
   });
 }
 

@@ -108,6 +108,55 @@ TILES = [(True, 64, 128, 64), (True, 130, 257, 40), (True, 1152, 4096, 1024), (T
 
 
 @pytest.mark.parametrize("bf16,n,v,d", TILES)
+def test_head_target_of_probability_near_one(bf16, n, v, d):
+    """log p of a target that has nearly all of its row is -log(1 + s), s the others' sum of some 2^-20, to s's own
+    relative accuracy.  The logits are exact.  A term of s: its exponent t < 2^5 rounded, 2^5 log 2 u, and exp2's 2 u; the
+    sum: at most 32 additions of a lane and 4 of lanes, then merges of 3 roundings, at most v / 512 + 16 of them (panels of
+    32 columns or more, 16 threads or more on a row, 4 steps in a wave, 3 across, and those of rows in parts); the logarithm
+    and the last products 8 u."""
+    import torch
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n + v + d)
+    w = np.minimum(r.normal(size=(v, d)), 2.0)
+    tk = r.integers(0, v, size=d)
+    w[tk, np.arange(d)] = 16.0 + np.floor(np.log(v))
+    mw, wv = _matrix(w, bf16)
+    k = np.arange(n) % d
+    got = losses.head_logprob(_one_hot(n, d, bf16), mw, _i32(tk[k]))
+    z = wv - wv[tk, np.arange(d)][None]
+    e = np.exp(z)
+    e[tk, np.arange(d)] = 0.0
+    s = e.sum(0)
+    assert (s < 2.0 ** -10).all()
+    tol = (22 + 2 + 36 + 3 * (v / 512 + 16) + 8) * U
+    for name, g, want, rel in (("logp", got.logp, -np.log1p(s), tol),
+                               ("entropy", got.entropy, np.log1p(s) - (e * z).sum(0) / (1 + s), 2 * tol)):
+        d_ = np.abs(_np(g) - want[k]) / np.abs(want[k])
+        assert d_.max() <= rel, (name, d_.max(), rel)
+    assert torch.equal(got.stats[:, 0].double().cpu(), torch.from_numpy(wv[tk, np.arange(d)][k]))
+
+
+@pytest.mark.parametrize("bf16,n,v,d", TILES)
+def test_head_of_several_largest_logits(bf16, n, v, d):
+    """Rows whose largest logit stands in 1, 2, 3 or 5 places, in one panel or in several: exact counts, log p = -log 5
+    and the like, beside logits so low that they add nothing."""
+    from paper_2606_30634_amd import losses
+    r = np.random.default_rng(n)
+    w = np.full((v, d), -200.0)
+    c = np.array([1, 2, 3, 5])[np.arange(d) % 4]
+    tk = np.zeros(d, np.int64)
+    for j in range(d):
+        first = int(r.integers(0, v - 5))
+        at = first + np.arange(c[j]) if j % 8 < 4 else r.choice(v, size=c[j], replace=False)
+        w[at, j], tk[j] = 7.0, at[-1]
+    mw, _ = _matrix(w, bf16)
+    k = np.arange(n) % d
+    got = losses.head_logprob(_one_hot(n, d, bf16), mw, _i32(tk[k]))
+    want = np.log(c[k].astype(float))
+    assert (np.abs(_np(got.logp) + want) <= 4 * U * want).all() and (np.abs(_np(got.entropy) - want) <= 4 * U * want).all()
+
+
+@pytest.mark.parametrize("bf16,n,v,d", TILES)
 def test_head_of_masks_and_nonfinite_values(bf16, n, v, d):
     """-inf, the type's lowest value, +inf and NaN among the logits of a head, at both ends of the vocabulary and inside it:
     as for rows of logits."""

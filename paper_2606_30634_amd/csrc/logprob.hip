@@ -448,9 +448,10 @@ __global__ void __launch_bounds__(256) panel_join(int64_t rows, int V, int panel
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Rows of fp32 logits held at once where they go through memory: within `bytes`, whole 128s if more than that
+// Rows of fp32 logits held at once where they go through memory: within `bytes`, whole 128s if more than that; at most
+// 2^20, since the product's row tiles of 64 are its grid's second dimension, which takes 65536
 int64_t head_chunk(int64_t rows, int64_t vocab, int64_t bytes) {
-  const int64_t r = bytes / (4 * vocab);
+  const int64_t r = std::min<int64_t>(bytes / (4 * vocab), 1 << 20);
   return std::max<int64_t>(1, std::min(rows, r > 128 ? r / 128 * 128 : r));
 }
 constexpr int64_t HEAD_ODD_BYTES = 32 << 20;  // logits of heads of unaligned rows, a chunk at a time

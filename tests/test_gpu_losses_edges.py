@@ -306,3 +306,19 @@ def test_policy_loss_of_tokens_that_cannot_occur(b, s):
                 g = _np(g)
                 fin = np.isfinite(w)
                 assert (g[~fin] == w[~fin]).all() and (np.abs(g[fin] - w[fin]) <= 32 * U * (1 + np.abs(w[fin]))).all(), (who, kl, g, w)
+
+
+# ------------------------------------------------------------------ many rows
+@pytest.mark.parametrize("v", [1, 2])
+def test_head_of_millions_of_unaligned_rows(v):
+    """Rows of one or two tokens, a chunk of them far longer than it is wide."""
+    import torch
+    from paper_2606_30634_amd import losses
+    n = 9_000_001
+    x = torch.linspace(-4, 4, n, device="cuda:0").bfloat16().view(n, 1)
+    w = torch.tensor([[1.0], [-0.5]], device="cuda:0").bfloat16()[:v].contiguous()
+    t = torch.arange(n, device="cuda:0", dtype=torch.int32) % v
+    got = losses.head_logprob(x, w, t)
+    z = x.double() @ w.double().t()
+    want = torch.log_softmax(z, 1).gather(1, t.long().view(n, 1)).view(n)
+    assert float((got.logp.double() - want).abs().max()) <= 64 * U * 7

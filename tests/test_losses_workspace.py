@@ -11,7 +11,7 @@ def _up(n, to=256):
 
 
 def _chunk(rows, vocab):
-    r = HELD // (4 * vocab)
+    r = min(HELD // (4 * vocab), 1 << 20)
     return max(1, min(rows, r // 128 * 128 if r > 128 else r))
 
 
@@ -26,3 +26,9 @@ def test_head_workspace_covers_every_chunk(vocab, bf16):
         for n in {r, (rows - 1) % r + 1}:
             need = _up(r * vocab * 4) + B.token_logprob_workspace_bytes(n, vocab)
             assert have >= need, (rows, n, have, need)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3])
+def test_head_chunk_fits_a_grid(vocab):
+    """Chunks of a head of a token or two: their tiles of 64 rows within the 65536 of a grid's second dimension."""
+    assert B.head_logprob_workspace_bytes(9_000_001, vocab, 1, 1) <= _up(65536 * 64 * vocab * 4)

@@ -539,11 +539,13 @@ __device__ __forceinline__ PairOut pref_pair(const PreferenceArgs& a, double sw,
   const double delta = sw - sl, h = a.beta * delta - a.margin, e = a.smoothing;
   double loss, dh;
   if (a.kind == 0) {
-    const double soft = log1p(exp(-fabs(h)));  // log(1 + e^-|h|)
+    const double x = exp(-fabs(h)), soft = log1p(x);  // log(1 + e^-|h|)
     // a side without a weight adds nothing, also where it is infinite
     loss = (e < 1.0 ? (1.0 - e) * (soft + fmax(-h, 0.0)) : 0.0) + (e > 0.0 ? e * (soft + fmax(h, 0.0)) : 0.0);
     if (h != h) loss = h;
-    dh = e - 1.0 / (1.0 + exp(h));
+    // -(1 - e) sigmoid(-h) + e sigmoid(h), of which e - sigmoid(-h) would leave nothing at e = 1 and h far below 0
+    const double near = 1.0 / (1.0 + x), far = x * near;  // sigmoid(|h|), sigmoid(-|h|)
+    dh = h >= 0.0 ? e * near - (1.0 - e) * far : e * far - (1.0 - e) * near;
   } else if (a.kind == 1) {
     loss = fmax(1.0 - h, 0.0);
     if (h != h) loss = h;

@@ -322,3 +322,23 @@ def test_head_of_millions_of_unaligned_rows(v):
     z = x.double() @ w.double().t()
     want = torch.log_softmax(z, 1).gather(1, t.long().view(n, 1)).view(n)
     assert float((got.logp.double() - want).abs().max()) <= 64 * U * 7
+
+
+# ------------------------------------------------------------------ small gradients of the preference loss
+@pytest.mark.parametrize("pairs,s", [(40, 3), (300, 2), (600, 20), (40, 5000)])
+@pytest.mark.parametrize("smoothing", [0.0, 1.0])
+def test_preference_gradient_of_pairs_far_apart(pairs, s, smoothing):
+    """With all weight on one side the gradient of a pair that is far on it is beta sigmoid(-|h|), 10^-17 of the others'
+    and as exact relatively: a rounding of the double and one of the result, 2 u with the scale's."""
+    import torch
+    from paper_2606_30634_amd import losses
+    h = np.linspace(-40, 40, pairs)
+    lp = np.zeros((2 * pairs, s))
+    lp[:pairs, 0] = h
+    t, v = _f32(lp)
+    on = torch.ones(2 * pairs, s, dtype=torch.bool, device="cuda:0")
+    got = losses.preference_loss(t, on, beta=1.0, label_smoothing=smoothing)
+    want = L.preference_loss(v, np.ones((2 * pairs, s), bool), beta=1.0, label_smoothing=smoothing)
+    for name in ("dlogp", "pair_loss"):
+        d = np.abs(_np(getattr(got, name)) - want[name])
+        assert (d <= 2 * U * np.abs(want[name])).all(), (name, (d / np.abs(want[name])).max() / U)

@@ -1118,13 +1118,15 @@ bool gemm_mfma_try(const GemmArgs& g0, hipStream_t st) {
 
 // ------------------------------------------------------------------ row statistics (epilogue 9)
 namespace {
-// Tiles of the statistics product, which cannot be split over K: with few tiles it is bound by the chain of one
-// tile's slices, with many by their throughput.  A CU takes cdiv(tiles, 256) tiles, up to `res` of them at once; r of
+// Tiles of the statistics product, which is not split over K: with few tiles it is bound by the chain of one
+// tile's slices, with many by their throughput.  A CU takes cdiv(tiles, 256) tiles, `res` of them to a round; r of
 // them together take slice[r - 1] us per 64-deep (fp32: 32-deep) slice and epi[r - 1] us for their epilogues.
-// Fitted to 23 shapes of 2 to 8192 rows, 74 to 49152 columns, K 512 to 4096, and the least sum is taken.  Against
-// 128 x 128 (and 256 x 256 from 1.6 fewer rounds), us: bf16 M 45, N 10902, K 2144 33 : 22; 372 x 651 x 2600 33 : 23;
-// 64 x 3000 x 4096 46 : 32; 182 x 17655 x 1984 35 : 31; 1472 x 3605 x 4016 70 : 70; 8192 x 49152 x 2048 1370 : 1370;
-// fp32 45 x 10902 x 2144 152 : 58; 372 x 651 x 2600 183 : 67; 182 x 17655 x 1984 254 : 142; 8192 x 32000 x 768 2896 : 2896.
+// Fitted to 23 shapes of 2 to 8192 rows, 74 to 49152 columns, K 512 to 4096, and the least sum is taken.  128 x 128
+// against the tile taken, us: bf16 M 45, N 10902, K 2144 33 : 22; 372 x 651 x 2600 32 : 23; 64 x 3000 x 4096 45 : 31;
+// 182 x 17655 x 1984 34 : 30; 1472 x 3605 x 4016 70 : 72; 8192 x 49152 x 2048 1656 : 1401; fp32 45 x 10902 x 2144 157 : 59;
+// 372 x 651 x 2600 190 : 69; 182 x 17655 x 1984 259 : 142; 333 x 32001 x 512 117 : 118; 8192 x 32000 x 768 3042 : 3042.
+// A round is as many tiles as a CU holds, but for 64 x 128 in fp32: a CU holds 3, which gain nothing on rounds of 2 and 1
+// (2.91 us a slice; 1.99 + 1.14).  Counted as 3, 43 shapes whose tile that changes took 0.5 % longer.
 struct RowstatTile { int bm, bn, res, panel; double slice[3], epi[3]; };
 enum { ROWSTAT_64, ROWSTAT_64_128, ROWSTAT_128, ROWSTAT_256, ROWSTAT_32_128, ROWSTAT_32_256 };
 constexpr RowstatTile ROWSTAT_BF16[] = {{64, 64, 3, 32, {.37, .55, .78}, {0, 1.5, 2.5}},
@@ -1142,9 +1144,9 @@ double rowstat_cost(const RowstatTile& t, int64_t M, int64_t N, int64_t slices) 
   return us;
 }
 // Up to 32 rows the product streams W, through 32 x 256 tiles in 3 stages when they are enough (one row, bf16, N 128256, K
-// 4096: 173.5 us; 32 x 128 in 4 stages 181, 128 x 128 179; 24 rows, N 37255, K 1176 23.4 against 26.2 in 64 x 64; but 8
-// rows, N 10000, K 2048 25.9 : 20.3); in fp32, whose matrix instructions such a tile waits for, through 32 x 128 ones
-// (24 rows, N 37255, K 1176 59.8, 32 x 256 69.9; 8 rows, N 10000, K 2048 55 : 92).
+// 4096: 180 us; 64 x 64 188, 128 x 128 191; 24 rows, N 37255, K 1176 22.8 against 25.5 in 64 x 64; but 8 rows, N 10000, K
+// 2048 25.5 : 19.7); in fp32, whose matrix instructions such a tile waits for, through 32 x 128 ones (24 rows, N 37255, K
+// 1176 67, 64 x 64 73; 8 rows, N 10000, K 2048 55 in either).
 int rowstat_config(bool bf, int64_t M, int64_t N, int64_t K) {
   if (M <= 32 && !bf) return ROWSTAT_32_128;
   if (M <= 32 && N > 25600) return ROWSTAT_32_256;

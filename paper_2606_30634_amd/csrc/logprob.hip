@@ -195,14 +195,14 @@ __global__ void __launch_bounds__(256) logprob_join(int64_t rows, int V, const T
 // Bound: memory, one read and one write past the caches (4096 x 128256 bf16, a quarter of the rows without a gradient:
 // 295 us, 6.2 TB/s; 999 x 32001 fp32 to bf16 with an entropy term 30 us, 6.0).  Two vectors a lane: 4096 x 128256 with
 // 4 of them 319 us, with 1 294 but 39 for the other.
-template <typename T> constexpr int BWD_U = 2;
+constexpr int BWD_U = 2;
 template <typename T, typename OutT>
 __global__ void __launch_bounds__(256) logprob_bwd(int64_t rows, int V, const T* x, int64_t ld,
                                                    const int32_t* __restrict__ tg, const float* __restrict__ stats,
                                                    const float* __restrict__ ent, const float* __restrict__ dlogp,
                                                    const float* __restrict__ dent, float s, OutT* dx, int64_t ldo,
                                                    int zero_to) {
-  constexpr int U = BWD_U<T>, E = VE<T>, CH = U * E * WAVE;
+  constexpr int U = BWD_U, E = VE<T>, CH = U * E * WAVE;
   const int lane = threadIdx.x % WAVE, W = max(V, zero_to);
   const int64_t per_row = (W + CH - 1) / CH, items = rows * per_row;
   const int64_t w0 = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -311,7 +311,7 @@ template <typename T, typename OutT>
 void logprob_bwd_t(int64_t rows, int V, const void* x, int64_t ld, const int32_t* tg, const float* stats,
                    const float* ent, const float* dlogp, const float* dent, float s, void* dx, int64_t ldo,
                    int zero_to, hipStream_t st) {
-  const int64_t waves = rows * cdiv(std::max(V, zero_to), BWD_U<T> * VE<T> * WAVE);
+  const int64_t waves = rows * cdiv(std::max(V, zero_to), BWD_U * VE<T> * WAVE);
   logprob_bwd<T, OutT><<<(unsigned)std::min(GRID, cdiv(waves, 4)), 256, 0, st>>>(
       rows, V, (const T*)x, ld, tg, stats, ent, dlogp, dent, s, (OutT*)dx, ldo, zero_to);
 }
@@ -454,12 +454,14 @@ int64_t head_chunk(int64_t rows, int64_t vocab, int64_t bytes) {
   const int64_t r = std::min<int64_t>(bytes / (4 * vocab), 1 << 20);
   return std::max<int64_t>(1, std::min(rows, r > 128 ? r / 128 * 128 : r));
 }
-constexpr int64_t HEAD_ODD_BYTES = 32 << 20;  // logits of heads of unaligned rows, a chunk at a time
+// Logits of heads of unaligned rows, a chunk at a time: the products' kernels for such rows, whose rate bounds it (1024 x
+// 32000 x 769: fp32 617 us, 82 TFLOP/s; bf16 881 us on the vector units; 768 instead, 403 and 62)
+constexpr int64_t HEAD_ODD_BYTES = 32 << 20;
 
 // Whether a product is worth packing its rows for: 8 us of kernels against 250 us or more (at 1.2 PFLOP/s in bf16, a
-// tenth of it in fp32), in which rows without a target would take their share.  8192 x 49152 x 2048 bf16, without :
-// with packing, us: no such rows 1380 : 1390, a tenth of them 1385 : 1285, half 1390 : 725; half of 4096 x 32000 x 768
-// fp32 1480 : 760.
+// tenth of it in fp32), in which rows without a target would take their share.  With no such rows, a tenth, half of
+// them, us: 8192 x 49152 x 2048 bf16 1405, 1299, 712 (without packing some 1395 each), 4096 x 32000 x 768 fp32 1558, 1411,
+// 831; 333 x 32001 x 512 fp32, below this, 118 each.
 bool head_packs(bool bf, int64_t n, int64_t vocab, int64_t d) {
   return n > 256 && (double)n * vocab * d >= (bf ? 1.5e11 : 1.5e10);
 }

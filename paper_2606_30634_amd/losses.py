@@ -8,7 +8,10 @@ happens here; every step runs in the library's kernels.
 
 A function writes into the tensors of `out` where given (fields that are None are allocated where the
 operator needs them) and returns its outputs.  `workspace`, a uint8 tensor of at least the matching
-workspace_bytes of the binding, is allocated per call where not given."""
+workspace_bytes of the binding, is allocated per call where not given.
+
+Nothing here records for autograd: outputs are detached whatever the inputs ask for, and a gradient is one of the
+functions above (head_logprob has none)."""
 from __future__ import annotations
 
 from typing import NamedTuple, Optional

@@ -415,6 +415,64 @@ int preference_loss(int64_t pairs, int64_t len, const float* logp, const float* 
                     const preference_hparams_t* hp, float* loss, float* dlogp, float* pair_loss, float* rewards,
                     float* metrics, int64_t* counts, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Key ranges of packed documents.  documents [batch, length] int32: a document is a run of equal ids >= 0; ids
+ * below 0 are padding.  Query i sees the keys [key_start[i], key_end[i]) of its row: from the first token of
+ * its document to itself; with prefix [batch, length] uint8 (or NULL), the tokens from a document's first one on
+ * whose flag is not 0 see that whole run of them.  Padding sees nothing (0, 0).  batch in [0, 2^24], length in [0, 2^30]. */
+int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents, const uint8_t* prefix,
+                         int32_t* key_start, int32_t* key_end, void* hip_stream);
+
+/* Softmax attention over a range of keys per query, forward and backward, of grouped query heads (query head h
+ * reads key/value head h / (heads / kv_heads)).  Query i of a sequence has position q_start + i and sees
+ * keys [key_start[i], key_end[i]) (what lies outside [0, keys) is cut off), or, with key_start NULL, the
+ * keys at or before its position.  With x = scale q.k the score of key j is
+ *   cap tanh(x / cap) - slopes[h] |position - j|   (softcap 0: x; slopes NULL: no second term).
+ * A query that sees no key has o = 0, lse = -inf and no gradient; what a query does not see has no
+ * influence on it, whatever it holds.  Products of bf16 accumulate in fp32; in bf16 the backward takes
+ * the probabilities and their gradients rounded to bf16, the forward to 16 bits and more. */
+typedef struct {
+  int64_t batch, queries, keys;        /* [0, 2^24], [0, 2^30], [0, 2^30]                   */
+  int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim 32, 64 or 128    */
+  int32_t is_bf16;                     /* q, k, v, o and the gradients: bf16, else fp32     */
+  int64_t q_strides[3], k_strides[3], v_strides[3]; /* elements between sequences, rows and heads; a head's
+                                          elements are contiguous, strides and pointers whole 16 bytes  */
+  const int32_t *key_start, *key_end;  /* [batch, queries] device arrays, or both NULL      */
+  const int32_t* q_start;              /* [batch] device array; NULL: keys - queries        */
+  const float* slopes;                 /* [heads] device array or NULL                      */
+  float scale;                         /* > 0                                               */
+  float softcap;                       /* 0 (none) or > 0                                   */
+} attention_params_t;
+
+/*   q             [batch, queries, heads, head_dim];  k, v [batch, keys, kv_heads, head_dim], as strided
+ *   o             [batch, queries, heads, head_dim], contiguous
+ *   o_f32         the same in fp32 before its rounding, for the backward of a bf16 attention, or NULL
+ *   lse           [batch, heads, queries] fp32: log of the sum of exp(score)
+ *   workspace     attention_workspace_bytes(), 256-byte aligned (NULL where that is 0) */
+size_t attention_workspace_bytes(const attention_params_t* p);
+int attention_forward(const attention_params_t* p, const void* q, const void* k, const void* v, void* o, float* o_f32,
+                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients in q, k and v, from what the forward read and wrote (o_f32 or o: the former where it was kept) and
+ * the gradient dout in o.  No atomics: the same inputs give the same bits.  dq, dk and dv may be the heads of one
+ * packed row (equal row strides). */
+typedef struct {
+  int64_t dout_strides[3], dq_strides[3], dk_strides[3], dv_strides[3];
+  void *dq, *dk, *dv;
+} attention_grads_t;
+size_t attention_backward_workspace_bytes(const attention_params_t* p);
+int attention_backward(const attention_params_t* p, const void* q, const void* k, const void* v, const void* o,
+                       const float* o_f32, const float* lse, const void* dout, const attention_grads_t* g,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Dropout added to a residual: out = residual + keep x / (1 - p') over [rows, cols] with p' = t / 65536, t = p
+ * 65536 rounded, p in [0, 1 - 2^-16].  Element e = row cols + col is kept when its 16-bit number is >= t:
+ * bits 16 (e mod 2) .. of word (e mod 8) / 2 of Philox4x32-10 of the counter (e / 8, offset) under the key
+ * seed.  The mask depends on nothing else, so the backward is the same call on the gradient with residual
+ * NULL (nothing is added).  fp32 or bf16 (all three), rows ldx, ldr and ldo >= cols elements apart; out
+ * may be x or residual itself.  Dropped elements of x may hold anything. */
+int dropout_add(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual, int64_t ldr, void* out,
+                int64_t ldo, int32_t is_bf16, double p, uint64_t seed, uint64_t offset, void* hip_stream);
+
 /* Ascending unique token ids of the microbatch in `slot` and their counts (after its backward
  * on a first stage).  ids, counts: device int32 arrays of >= micro_batch*seq_len entries;
  * n_unique: device int32. */

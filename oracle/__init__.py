@@ -13,6 +13,7 @@ Contents
   model   stage forward / backward (stack of blocks, embedding, head)
   update  Alg. 1 of §2 with AdamW and the Error-Feedback correction of §3.2 / App. A.4
   losses  log-probabilities of tokens, the policy and preference losses on them
+  attention  attention over key ranges, the ranges of packed documents, counter-based dropout
   run()   the training loop: fwd/bwd at x_t, then the delayed update, for T iterations
 """
 from __future__ import annotations
@@ -21,7 +22,7 @@ from typing import Callable, Dict, List, Optional
 
 import numpy as np
 
-from . import losses, model, ops, update  # noqa: F401
+from . import attention, losses, model, ops, update  # noqa: F401
 from .update import HParams, OptState, iteration_update
 
 

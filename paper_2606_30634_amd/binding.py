@@ -22,7 +22,8 @@ EXPORTS = ["stage_required_bytes", "stage_init", "stage_num_tensors", "stage_ten
            "grad_norm_flat_noalloc", "token_logprob_workspace_bytes", "token_logprob", "token_logprob_backward",
            "head_logprob_workspace_bytes", "head_logprob", "policy_loss_workspace_bytes", "policy_loss",
            "preference_loss_workspace_bytes", "preference_loss", "stage_forward_logprob", "stage_backward_logprob",
-           "stage_score_logprob"]
+           "stage_score_logprob", "attention_key_ranges", "attention_workspace_bytes", "attention_forward",
+           "attention_backward_workspace_bytes", "attention_backward", "dropout_add"]
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_UPDATE, PROF_NORM, PROF_OTHER, PROF_NS = range(7)
 
 
@@ -52,6 +53,22 @@ class PreferenceHParams(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("beta", "label_smoothing", "margin")] + [
         (n, C.c_int32) for n in ("kind", "length_normalize")] + [
         (n, C.c_double) for n in ("norm", "grad_scale")]
+
+
+_STRIDES = C.c_int64 * 3
+
+
+class AttentionParams(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch", "queries", "keys")] + [
+        (n, C.c_int32) for n in ("heads", "kv_heads", "head_dim", "is_bf16")] + [
+        (n, _STRIDES) for n in ("q_strides", "k_strides", "v_strides")] + [
+        (n, C.c_void_p) for n in ("key_start", "key_end", "q_start", "slopes")] + [
+        (n, C.c_float) for n in ("scale", "softcap")]
+
+
+class AttentionGrads(C.Structure):
+    _fields_ = [(n, _STRIDES) for n in ("dout_strides", "dq_strides", "dk_strides", "dv_strides")] + [
+        (n, C.c_void_p) for n in ("dq", "dk", "dv")]
 
 
 class StageError(RuntimeError):
@@ -109,6 +126,13 @@ def _load():
         "preference_loss_workspace_bytes": (sz, [i64, i64]),
         "preference_loss": (C.c_int, [i64, i64, vp, vp, vp, C.POINTER(PreferenceHParams), vp, vp, vp, vp, vp, vp,
                                       vp, sz, vp]),
+        "attention_key_ranges": (C.c_int, [i64, i64, vp, vp, vp, vp, vp]),
+        "attention_workspace_bytes": (sz, [C.POINTER(AttentionParams)]),
+        "attention_forward": (C.c_int, [C.POINTER(AttentionParams), vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "attention_backward_workspace_bytes": (sz, [C.POINTER(AttentionParams)]),
+        "attention_backward": (C.c_int, [C.POINTER(AttentionParams), vp, vp, vp, vp, vp, vp, vp,
+                                         C.POINTER(AttentionGrads), vp, sz, vp]),
+        "dropout_add": (C.c_int, [i64, i64, vp, i64, vp, i64, vp, i64, i32, C.c_double, C.c_uint64, C.c_uint64, vp]),
         "stage_last_error": (C.c_char_p, []),
         "stage_destroy": (None, [vp]),
     }
@@ -273,6 +297,33 @@ def preference_loss(pairs, length, logp, ref_logp, mask, hp: PreferenceHParams, 
     check("preference_loss", LIB.preference_loss(
         pairs, length, logp, ref_logp, mask, C.byref(hp), loss, dlogp, pair_loss, rewards, metrics, counts, workspace,
         workspace_bytes, stream))
+
+
+def attention_key_ranges(batch, length, documents, prefix, key_start, key_end, stream) -> None:
+    check("attention_key_ranges", LIB.attention_key_ranges(batch, length, documents, prefix, key_start, key_end, stream))
+
+
+def attention_workspace_bytes(params: AttentionParams) -> int:
+    return LIB.attention_workspace_bytes(C.byref(params))
+
+
+def attention_forward(params: AttentionParams, q, k, v, o, o_f32, lse, workspace, workspace_bytes, stream) -> None:
+    check("attention_forward", LIB.attention_forward(
+        C.byref(params), q, k, v, o, o_f32, lse, workspace, workspace_bytes, stream))
+
+
+def attention_backward_workspace_bytes(params: AttentionParams) -> int:
+    return LIB.attention_backward_workspace_bytes(C.byref(params))
+
+
+def attention_backward(params: AttentionParams, q, k, v, o, o_f32, lse, dout, grads: AttentionGrads, workspace,
+                       workspace_bytes, stream) -> None:
+    check("attention_backward", LIB.attention_backward(
+        C.byref(params), q, k, v, o, o_f32, lse, dout, C.byref(grads), workspace, workspace_bytes, stream))
+
+
+def dropout_add(rows, cols, x, ldx, residual, ldr, out, ldo, is_bf16, p, seed, offset, stream) -> None:
+    check("dropout_add", LIB.dropout_add(rows, cols, x, ldx, residual, ldr, out, ldo, is_bf16, p, seed, offset, stream))
 
 
 def stage_embed_indices(s: int, slot: int, ids, counts, n_unique) -> None:

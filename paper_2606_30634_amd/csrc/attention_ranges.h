@@ -1,0 +1,86 @@
+// What the kernels of attention over key ranges share (attention_ranges.hip and attention_ranges_mfma.hip).
+#pragma once
+#include "common.h"
+#include "kernels.h"
+
+namespace {
+
+__device__ __forceinline__ int64_t position(const RangeArgs& a, int b, int i) {
+  return (int64_t)(a.q_start ? a.q_start[b] : a.Sk - a.Sq) + i;
+}
+
+// The keys that query i of sequence b sees; none is (0, 0)
+__device__ __forceinline__ int2 seen_keys(const RangeArgs& a, int b, int i) {
+  int lo = 0, hi;
+  if (a.key_start) {
+    lo = max(a.key_start[(int64_t)b * a.Sq + i], 0);
+    hi = min(a.key_end[(int64_t)b * a.Sq + i], a.Sk);
+  } else {
+    hi = (int)min((int64_t)a.Sk, max((int64_t)0, position(a, b, i) + 1));
+  }
+  return lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+}
+__device__ __forceinline__ bool sees(const int2& s, int key) { return (uint32_t)(key - s.x) < (uint32_t)(s.y - s.x); }
+
+// What a score is taken relative to in a row of this maximum or lse: a row of only -inf has weights of 0
+__device__ __forceinline__ float weight_base(float m) { return m == -INFINITY ? 0.f : m; }
+
+// tanh(y) and its derivative 1 - tanh(y)^2.  Up to |y| = 1/2 the odd polynomial y + y^3 P(y^2) with P the
+// minimax fit of degree 3 (relative error 2^-26); beyond it 1 - u with u = 2 e / (1 + e), e = exp(-2 |y|),
+// whose derivative u (2 - u) keeps its relative accuracy where tanh rounds to 1.
+constexpr float TANH_SMALL = 0.5f;
+constexpr float TANH_C[4] = {-0.3333314359f, 0.1332587898f, -0.0530454814f, 0.0172414685f};
+__device__ __forceinline__ float tanh_ratio(float z) {  // tanh(y) / y, z = y^2
+  float p = __builtin_fmaf(z, TANH_C[3], TANH_C[2]);
+  p = __builtin_fmaf(z, p, TANH_C[1]);
+  p = __builtin_fmaf(z, p, TANH_C[0]);
+  return __builtin_fmaf(z, p, 1.0f);
+}
+__device__ __forceinline__ float tanh_and_slope(float y, float& slope) {
+  if (fabsf(y) < TANH_SMALL) {
+    const float t = y * tanh_ratio(y * y);
+    slope = __builtin_fmaf(-t, t, 1.0f);
+    return t;
+  }
+  const float e = __builtin_amdgcn_exp2f(fabsf(y) * -2.8853900817779268f);
+  const float u = 2.0f * e * __builtin_amdgcn_rcpf(1.0f + e);
+  slope = u * (2.0f - u);
+  return copysignf(1.0f - u, y);
+}
+
+template <typename T>
+__device__ __forceinline__ const T* rows_of(const HeadRows& r, int b, int h) {
+  return (const T*)r.p + b * r.batch + h * r.head;
+}
+template <typename T>
+__device__ __forceinline__ T* rows_out(const HeadRows& r, int b, int h) {
+  return (T*)r.p + b * r.batch + h * r.head;
+}
+
+// A wave's minimum and maximum over all its lanes
+__device__ __forceinline__ int wave_min_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, WAVE));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// The keys [lo, hi) that some query of a wave sees (none: 0, 0), and those [all_lo, all_hi) that all of them see
+// (none: all_lo > all_hi).  valid: the lane's query exists.
+struct WaveKeys {
+  int lo, hi, all_lo, all_hi;
+  __device__ WaveKeys(const int2& s, bool valid) {
+    const bool some = valid && s.x < s.y;
+    hi = wave_max_i(some ? s.y : 0);
+    lo = hi > 0 ? wave_min_i(some ? s.x : INT32_MAX) : 0;
+    all_lo = wave_max_i(some ? s.x : valid ? INT32_MAX : 0);
+    all_hi = wave_min_i(some ? s.y : valid ? 0 : INT32_MAX);
+  }
+  __device__ bool whole(int k0, int k1) const { return all_lo <= k0 && k1 <= all_hi; }  // all see [k0, k1)
+};
+
+}  // namespace

@@ -1,0 +1,559 @@
+// Grouped-query attention over a range of keys per query, its scores capped by a tanh and lowered by the
+// distance between query and key, forward and backward; and the key ranges of packed documents.
+//
+//   x_ij = scale q_i.k_j;  s_ij = cap tanh(x_ij / cap) - slope_h |pos_i - j|;  query i sees keys [lo_i, hi_i)
+//   P_ij = exp(s_ij - lse_i), lse_i = log sum_j exp(s_ij) over the keys it sees;  o = P v
+//   delta_i = dO_i.o_i;  dP = dO v^T;  dS = P (dP - delta) (1 - tanh^2);  dq = scale dS k
+//   dk = scale dS^T q and dv = P^T dO, summed over the query heads of a key/value head
+// A query that sees no key has o = 0, lse = -inf and no gradient.
+//
+// These kernels take fp32 (and bf16 of head dimension 32) on the fp32 matrix cores, tiled as in attention.hip:
+// a block owns 32 rows of one side, its waves take every fourth tile of 32 rows of the other.  Tiles start at
+// the first key (query) that a row of the block sees and end with the last; a tile that every row sees whole
+// skips the mask.
+#include "attention_ranges.h"
+#include "attention_rows.h"
+#include <algorithm>
+
+namespace {
+
+// Score of x = scale q.k at distance `far` (x itself without cap and slopes)
+struct Score {
+  float cap, inv_cap, slope;
+  bool capped, biased;
+  __device__ Score(const RangeArgs& a, int h) {
+    cap = a.cap;
+    capped = a.cap > 0.f;
+    inv_cap = capped ? 1.0f / a.cap : 0.f;
+    biased = a.slopes != nullptr;
+    slope = biased ? a.slopes[h] : 0.f;
+  }
+  __device__ float operator()(float x, float far, float& grad) const {
+    grad = 1.f;
+    if (capped) x = cap * tanh_and_slope(x * inv_cap, grad);
+    if (biased) x = __builtin_fmaf(-slope, fabsf(far), x);
+    return x;
+  }
+};
+
+__device__ __forceinline__ int acc_row(int e) { return 8 * (e / 4) + 4 * (threadIdx.x % 64 / 32) + e % 4; }
+
+// One block per (32 queries, query head, sequence, share of their keys)
+template <typename T, int HD>
+__global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a) {
+  __shared__ float red[NW * WAVE_LDS<HD>];
+  const int nt = (a.Sq + TR - 1) / TR;
+  int64_t id = blockIdx.x;
+  const int split = id % a.nsplit;
+  id /= a.nsplit;
+  const int q0 = (nt - 1 - (int)(id % nt)) * TR;
+  id /= nt;
+  const int h = id % a.Hq, b = (int)(id / a.Hq), kvh = h / (a.Hq / a.Hkv);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = q0 + lane % 32, qc = min(q, a.Sq - 1);
+  float* mine = red + wave * WAVE_LDS<HD>;
+  const T* kp = rows_of<T>(a.k, b, kvh);
+  const T* vp = rows_of<T>(a.v, b, kvh);
+  const int2 mask = seen_keys(a, b, qc);
+  const WaveKeys wk(mask, q < a.Sq);
+  const int64_t pos = position(a, b, qc);
+  const Score score(a, h);
+  // this share's keys: tiles of 32 from the first key seen on
+  const int tiles = wk.hi > wk.lo ? (wk.hi - wk.lo + TR - 1) / TR : 0;
+  const int t0 = (int)((int64_t)tiles * split / a.nsplit), t1 = (int)((int64_t)tiles * (split + 1) / a.nsplit);
+  RowFrag<HD> qf;
+  qf.load(rows_of<T>(a.q, b, h), qc, a.q.row);
+#pragma unroll
+  for (int i = 0; i < HD / 8; ++i) qf.v[i] *= a.scale;
+  f32x16 o[HD / 32];
+#pragma unroll
+  for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  auto tile = [&](int k0, auto edge) {
+    RowFrag<HD> kf;
+    kf.load(kp, min(k0 + lane % 32, wk.hi - 1), a.k.row);
+    f32x16 s = rows_product<HD>(kf, qf);  // rows: keys; column: this lane's query
+    const float base_far = (float)(pos - k0);
+    float mt = -INFINITY, g;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = score(s[e], base_far - (float)acc_row(e), g);
+      if (edge && !sees(mask, k0 + acc_row(e))) s[e] = -INFINITY;
+      mt = fmaxf(mt, s[e]);
+    }
+    const float mn = fmaxf(m, pair_max(mt));
+    const float base = weight_base(mn);
+    const float corr = expf(m - base);
+    float rs = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = expf(s[e] - base);
+      rs += s[e];
+    }
+    l = l * corr + pair_sum(rs);
+    m = mn;
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; ++dt) o[dt] *= corr;
+    if constexpr (edge) {
+      kf.load(vp, min(k0 + lane % 32, wk.hi - 1), a.v.row);
+      if (!kf.finite()) {  // 0 times what a query does not see could be a NaN
+        cols_product_seen<HD>(o, vp, k0, a.v.row, s, mine, [&](int r) { return sees(mask, k0 + r); });
+        return;
+      }
+    }
+    cols_product<HD>(o, vp, k0, wk.hi - 1, a.v.row, s);
+  };
+  for (int t = t0 + wave; t < t1; t += NW) {
+    const int k0 = wk.lo + t * TR;
+    if (wk.whole(k0, k0 + TR)) tile(k0, std::false_type{});
+    else tile(k0, std::true_type{});
+  }
+  if (lane < TR) {
+    mine[lane] = m;
+    mine[TR + lane] = l;
+  }
+  __syncthreads();
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, red[w * WAVE_LDS<HD> + lane % 32]);
+  const float base = weight_base(M);
+#pragma unroll
+  for (int w = 0; w < NW; ++w)
+    L += expf(red[w * WAVE_LDS<HD> + lane % 32] - base) * red[w * WAVE_LDS<HD> + TR + lane % 32];
+  __syncthreads();
+  const float wt = expf(m - base);
+  put_partial<HD>(red, o, a.nsplit > 1 ? wt : L == 0.f ? 0.f : wt / L);
+  __syncthreads();
+  const int64_t row0 = ((int64_t)b * a.Sq * a.Hq + h);  // row of query i: row0 + i Hq
+  if (a.nsplit > 1) {
+    const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
+    store_rows<HD>(red, 1.0f, a.part + (n * split + row0) * HD, a.Hq * HD, q0, a.Sq, nullptr, nullptr);
+    if (wave == 0 && lane < TR && q < a.Sq) a.part_ml[n * split + row0 + (int64_t)q * a.Hq] = make_float2(M, L);
+    return;
+  }
+  store_rows<HD>(red, 1.0f, (T*)a.o + row0 * HD, a.Hq * HD, q0, a.Sq, nullptr, nullptr,
+                 a.o32 ? a.o32 + row0 * HD : nullptr);
+  if (wave == 0 && lane < TR && q < a.Sq) a.lse[((int64_t)b * a.Hq + h) * a.Sq + q] = base + logf(L);
+}
+
+// The shares of a row joined: HD / 4 lanes per row (b, i, h)
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_join(RangeArgs a) {
+  constexpr int LR = HD / 4;
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq, r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;
+  const int c = (threadIdx.x % LR) * 4;
+  if (r >= n) return;
+  float M = -INFINITY, L = 0.f;
+  for (int s = 0; s < a.nsplit; ++s) M = fmaxf(M, a.part_ml[n * s + r].x);
+  const float base = weight_base(M);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float2 ml = a.part_ml[n * s + r];
+    const float w = expf(ml.x - base);
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    L += w * ml.y;
+    o += w * ld4(a.part + (n * s + r) * HD + c);
+  }
+  o *= L == 0.f ? 0.f : 1.0f / L;
+  st4((T*)a.o + r * HD + c, o);
+  if (a.o32) st4(a.o32 + r * HD + c, o);
+  if (c == 0) {
+    const int64_t row = r / a.Hq, b = row / a.Sq;
+    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = base + logf(L);
+  }
+}
+
+// delta_i = dO_i.o_i per (sequence, head, query): HD / 4 lanes per row; and the keys each query sees
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_prep(RangeArgs a) {
+  constexpr int LR = HD / 4;
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;  // (b, i, h)
+  const int c = (threadIdx.x % LR) * 4;
+  const bool in = r < (int64_t)a.B * a.Sq * a.Hq;
+  const int64_t row = r / a.Hq;
+  const int h = (int)(r % a.Hq), b = (int)(row / a.Sq), i = (int)(row % a.Sq);
+  float s = 0.f;
+  if (in) {
+    const f32x4 d = ld4(rows_of<T>(a.dout, b, h) + (int64_t)i * a.dout.row + c);
+    const f32x4 o = a.o32 ? ld4(a.o32 + r * HD + c) : ld4((const T*)a.o + r * HD + c);
+    s = (o[0] * d[0] + o[1] * d[1]) + (o[2] * d[2] + o[3] * d[3]);
+  }
+#pragma unroll
+  for (int k = 1; k < LR; k <<= 1) s += __shfl_xor(s, k, WAVE);
+  if (!in || c) return;
+  a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
+  if (h == 0) a.seen[row] = seen_keys(a, b, i);
+}
+
+// [x, y): the first and last query that see a key of tile t of `width` keys, one block per (tile, sequence)
+__global__ void __launch_bounds__(256) range_plan(RangeArgs a, int width, int ntile) {
+  __shared__ int first[4], last[4];
+  const int t = blockIdx.x % ntile, b = blockIdx.x / ntile;
+  const int k0 = t * width, k1 = min(k0 + width, a.Sk);
+  int lo = INT32_MAX, hi = 0;
+  for (int i = threadIdx.x; i < a.Sq; i += 256) {
+    const int2 s = seen_keys(a, b, i);
+    if (max(s.x, k0) < min(s.y, k1)) {
+      lo = min(lo, i);
+      hi = i + 1;
+    }
+  }
+  lo = wave_min_i(lo);
+  hi = wave_max_i(hi);
+  if (threadIdx.x % 64 == 0) {
+    first[threadIdx.x / 64] = lo;
+    last[threadIdx.x / 64] = hi;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      lo = min(lo, first[w]);
+      hi = max(hi, last[w]);
+    }
+    a.sees[blockIdx.x] = lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+  }
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int b, float* red) {
+  const int kvh = h / (a.Hq / a.Hkv), q0 = qb * TR;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = q0 + lane % 32, qc = min(q, a.Sq - 1);
+  const T* kp = rows_of<T>(a.k, b, kvh);
+  const T* vp = rows_of<T>(a.v, b, kvh);
+  const int2 mask = a.seen[(int64_t)b * a.Sq + qc];
+  const WaveKeys wk(mask, q < a.Sq);
+  const int64_t pos = position(a, b, qc);
+  const Score score(a, h);
+  RowFrag<HD> qf, df;
+  qf.load(rows_of<T>(a.q, b, h), qc, a.q.row);
+  df.load(rows_of<T>(a.dout, b, h), qc, a.dout.row);
+#pragma unroll
+  for (int i = 0; i < HD / 8; ++i) qf.v[i] *= a.scale;
+  const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + qc;
+  const float lse = weight_base(a.lse[sidx]), dl = a.delta[sidx];
+  f32x16 dq[HD / 32];
+#pragma unroll
+  for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dq[dt][e] = 0.f;
+  auto tile = [&](int k0, auto edge) {
+    const int kr = min(k0 + lane % 32, wk.hi - 1);
+    RowFrag<HD> f;
+    f.load(kp, kr, a.k.row);
+    const bool plain = !edge || f.finite();
+    f32x16 s = rows_product<HD>(f, qf);
+    f.load(vp, kr, a.v.row);
+    const f32x16 dp = rows_product<HD>(f, df);
+    const float base_far = (float)(pos - k0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float g;
+      const float x = score(s[e], base_far - (float)acc_row(e), g);
+      s[e] = !edge || sees(mask, k0 + acc_row(e)) ? expf(x - lse) * (dp[e] - dl) * g : 0.f;
+    }
+    if (plain) cols_product<HD>(dq, kp, k0, wk.hi - 1, a.k.row, s);
+    else cols_product_seen<HD>(dq, kp, k0, a.k.row, s, red + wave * WAVE_LDS<HD>, [&](int r) { return sees(mask, k0 + r); });
+  };
+  for (int k0 = wk.lo + wave * TR; k0 < wk.hi; k0 += NW * TR) {
+    if (wk.whole(k0, k0 + TR)) tile(k0, std::false_type{});
+    else tile(k0, std::true_type{});
+  }
+  put_partial<HD>(red, dq, 1.0f);
+  __syncthreads();
+  store_rows<HD>(red, a.scale, rows_out<T>(a.dq, b, h), a.dq.row, q0, a.Sq, a.rope_cos, a.rope_sin);
+}
+
+// dk and dv of 32 keys of key/value head kvh, summed over its query heads
+template <typename T, int HD>
+__device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, int b, float* red) {
+  const int k0 = kb * TR, group = a.Hq / a.Hkv;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, key = k0 + lane % 32, kc = min(key, a.Sk - 1);
+  RowFrag<HD> kf, vf;
+  kf.load(rows_of<T>(a.k, b, kvh), kc, a.k.row);
+  vf.load(rows_of<T>(a.v, b, kvh), kc, a.v.row);
+#pragma unroll
+  for (int i = 0; i < HD / 8; ++i) kf.v[i] *= a.scale;
+  f32x16 dk[HD / 32], dv[HD / 32];
+#pragma unroll
+  for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { dk[dt][e] = 0.f; dv[dt][e] = 0.f; }
+  const int2 by = a.sees[(int64_t)b * ((a.Sk + TR - 1) / TR) + kb];
+  const int nt = (by.y - by.x + TR - 1) / TR;
+  const int2* seen = a.seen + (int64_t)b * a.Sq;
+  for (int64_t it = wave; it < (int64_t)group * nt; it += NW) {
+    const int h = kvh * group + (int)(it / nt), q0 = by.x + (int)(it % nt) * TR, ql = by.y - 1;
+    const T* qp = rows_of<T>(a.q, b, h);
+    const T* dp_ = rows_of<T>(a.dout, b, h);
+    const int64_t sb = ((int64_t)b * a.Hq + h) * a.Sq;
+    const int qr = min(q0 + lane % 32, ql);
+    const Score score(a, h);
+    const int2 mine = seen[qr];
+    // every key of the block is seen by every query of the tile
+    const bool whole = q0 + TR <= by.y && __all(mine.x <= k0 && k0 + TR <= mine.y);
+    RowFrag<HD> f;
+    f.load(qp, qr, a.q.row);
+    const bool plain_q = whole || f.finite();
+    f32x16 p = rows_product<HD>(f, kf);  // rows: queries; column: this lane's key
+    f.load(dp_, qr, a.dout.row);
+    const bool plain_d = whole || f.finite();
+    f32x16 ds = rows_product<HD>(f, vf);
+    const float base_far = (float)(position(a, b, q0) - key);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int q = q0 + acc_row(e), qc = min(q, ql);
+      const bool on = q <= ql && sees(seen[qc], key);
+      float g;
+      const float x = score(p[e], base_far + (float)acc_row(e), g);
+      p[e] = on ? expf(x - weight_base(a.lse[sb + qc])) : 0.f;
+      ds[e] = on ? p[e] * (ds[e] - a.delta[sb + qc]) * g : 0.f;
+    }
+    auto on = [&](int r) { return q0 + r <= ql && sees(seen[min(q0 + r, ql)], key); };
+    float* tmp = red + wave * WAVE_LDS<HD>;
+    if (plain_d) cols_product<HD>(dv, dp_, q0, ql, a.dout.row, p);
+    else cols_product_seen<HD>(dv, dp_, q0, a.dout.row, p, tmp, on);
+    if (plain_q) cols_product<HD>(dk, qp, q0, ql, a.q.row, ds);
+    else cols_product_seen<HD>(dk, qp, q0, a.q.row, ds, tmp, on);
+  }
+  put_partial<HD>(red, dk, 1.0f);
+  __syncthreads();
+  store_rows<HD>(red, a.scale, rows_out<T>(a.dk, b, kvh), a.dk.row, k0, a.Sk, a.rope_cos, a.rope_sin);
+  __syncthreads();
+  put_partial<HD>(red, dv, 1.0f);
+  __syncthreads();
+  store_rows<HD>(red, 1.0f, rows_out<T>(a.dv, b, kvh), a.dv.row, k0, a.Sk, nullptr, nullptr);
+}
+
+// dk/dv blocks and dq blocks in one launch
+template <typename T, int HD>
+__global__ void __launch_bounds__(NW * 64, bwd_waves(HD)) range_bwd(RangeArgs a) {
+  __shared__ float red[NW * WAVE_LDS<HD>];
+  const int nk = (a.Sk + TR - 1) / TR, nq = (a.Sq + TR - 1) / TR;
+  const int64_t nkv = (int64_t)nk * a.Hkv * a.B;
+  int64_t id = blockIdx.x;
+  if (id < nkv) {
+    const int kb = id % nk;
+    id /= nk;
+    range_dkv<T, HD>(a, kb, (int)(id % a.Hkv), (int)(id / a.Hkv), red);
+  } else {
+    id -= nkv;
+    const int qb = nq - 1 - (int)(id % nq);
+    id /= nq;
+    range_dq<T, HD>(a, qb, (int)(id % a.Hq), (int)(id / a.Hq), red);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ key ranges
+// A block takes RT tokens of a row, PT consecutive ones per thread.  The last position at or before a token
+// where a document starts, and where a token is no prefix token, are running maxima over the row; the next
+// position where a prefix ends is a running minimum from its end.  What lies outside the block's tokens is
+// searched for, outwards from them and no further than the document goes.
+constexpr int RT = 2048, RTH = 256, PT = RT / RTH;
+
+// the value of the threads before this one (MAX) or after it (MIN) combined: exclusive scans over the block
+__device__ __forceinline__ int scan_before(int v, int none, int* lds) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, WAVE);
+    if (lane >= o) v = max(v, u);
+  }
+  if (lane == 63) lds[wave] = v;
+  int r = __shfl_up(v, 1, WAVE);
+  if (lane == 0) r = none;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) r = max(r, lds[w]);
+  __syncthreads();
+  return r;
+}
+__device__ __forceinline__ int scan_after(int v, int none, int* lds) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_down(v, o, WAVE);
+    if (lane + o < 64) v = min(v, u);
+  }
+  if (lane == 0) lds[wave] = v;
+  int r = __shfl_down(v, 1, WAVE);
+  if (lane == 63) r = none;
+  __syncthreads();
+  for (int w = wave + 1; w < RTH / 64; ++w) r = min(r, lds[w]);
+  __syncthreads();
+  return r;
+}
+__device__ __forceinline__ int block_max_i(int v, int* lds) {
+  v = wave_max_i(v);
+  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < RTH / 64; ++w) v = max(v, lds[w]);
+  __syncthreads();
+  return v;
+}
+
+__global__ void __launch_bounds__(RTH) key_ranges(int S, int nb, const int32_t* __restrict__ ids,
+                                                  const uint8_t* __restrict__ flags, int32_t* __restrict__ start,
+                                                  int32_t* __restrict__ end) {
+  __shared__ int lds[RTH / 64];
+  const int64_t row = blockIdx.x / nb;
+  const int c0 = (int)(blockIdx.x % nb) * RT, c1 = min(c0 + RT, S);
+  ids += row * S;
+  if (flags) flags += row * S;
+  start += row * S;
+  end += row * S;
+  auto begins = [&](int i) { return i == 0 || ids[i] != ids[i - 1]; };
+  // the first token's document: where it starts, and whether a token of it before c0 is no prefix token
+  int doc = c0, plain = -1;
+  if (!begins(c0)) {
+    int hi = c0;  // tokens [.., hi) still to be looked at
+    doc = 0;
+    while (hi > 0) {
+      const int lo = max(0, hi - RT);
+      int b = -1, p = -1;
+      for (int i = lo + (int)threadIdx.x; i < hi; i += RTH) {
+        if (begins(i)) b = i;
+        if (flags && flags[i] == 0) p = i;
+      }
+      b = block_max_i(b, lds);
+      if (flags && plain < 0) plain = block_max_i(p, lds);
+      if (b >= 0) {
+        doc = b;
+        break;
+      }
+      hi = lo;
+    }
+  }
+  int id[PT], fl[PT];
+  const int i0 = c0 + (int)threadIdx.x * PT;
+  int before = i0 > 0 && i0 < c1 ? ids[i0 - 1] : 0;
+#pragma unroll
+  for (int j = 0; j < PT; ++j) {
+    const bool in = i0 + j < c1;
+    id[j] = in ? ids[i0 + j] : 0;
+    fl[j] = in && flags ? flags[i0 + j] : 0;
+  }
+  int b = -1, p = -1;
+  bool bg[PT];
+#pragma unroll
+  for (int j = 0; j < PT; ++j) {
+    bg[j] = i0 + j < c1 && (i0 + j == 0 || id[j] != (j ? id[j - 1] : before));
+    if (bg[j]) b = i0 + j;
+    if (i0 + j < c1 && !fl[j]) p = i0 + j;
+  }
+  int cur = max(doc, scan_before(b, -1, lds)), lastp = -1, stop = 0;
+  int stops[PT];
+  if (flags) {
+    lastp = max(plain, scan_before(p, -1, lds));
+    // where a prefix that runs over the block's end stops
+    stop = c1;
+    while (stop < S) {
+      const int hi = min(S, stop + RT);
+      int f = INT32_MAX;
+      for (int i = hi - 1 - (int)threadIdx.x; i >= stop; i -= RTH)
+        if (begins(i) || flags[i] == 0) f = i;
+      f = -block_max_i(-f, lds);
+      if (f != INT32_MAX) {
+        stop = f;
+        break;
+      }
+      stop = hi;
+    }
+    int s = INT32_MAX;
+#pragma unroll
+    for (int j = PT - 1; j >= 0; --j)
+      if (i0 + j < c1 && (bg[j] || !fl[j])) s = i0 + j;
+    int nx = min(stop, scan_after(s, INT32_MAX, lds));
+#pragma unroll
+    for (int j = PT - 1; j >= 0; --j) {
+      stops[j] = nx;
+      if (i0 + j < c1 && (bg[j] || !fl[j])) nx = i0 + j;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < PT; ++j) {
+    const int i = i0 + j;
+    if (i >= c1) break;
+    if (bg[j]) cur = i;
+    if (flags && !fl[j]) lastp = i;
+    const bool live = id[j] >= 0;
+    start[i] = live ? cur : 0;
+    end[i] = live ? (flags && lastp < cur ? stops[j] : i + 1) : 0;
+  }
+}
+
+template <typename T, typename F>
+void dispatch_hd(int hd, F&& run) {
+  if (hd == 32) run(T{}, std::integral_constant<int, 32>{});
+  else if (hd == 64) run(T{}, std::integral_constant<int, 64>{});
+  else run(T{}, std::integral_constant<int, 128>{});
+}
+template <typename F>
+void dispatch(bool bf, int hd, F&& run) {
+  if (bf) dispatch_hd<bf16>(hd, run);
+  else dispatch_hd<float>(hd, run);
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Shares of a forward item's keys: towards 512 items, two per compute unit, of at least 256 keys
+int fwd_splits(const RangeArgs& a) {
+  const int64_t items = cdiv(a.Sq, TR) * a.Hq * a.B;
+  if (items == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, 512 / items, a.Sk / 256}));
+}
+
+}  // namespace
+
+size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a) {
+  const int64_t ns = fwd_splits(a), n = (int64_t)a.B * a.Sq * a.Hq;
+  return ns > 1 ? up256(ns * n * a.hd * 4) + up256(ns * n * 8) : 0;
+}
+
+void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
+  a.nsplit = fwd_splits(a);
+  if (a.nsplit > 1) {
+    a.part = (float*)ws;
+    a.part_ml = (float2*)((char*)ws + up256(a.nsplit * n * a.hd * 4));
+  }
+  dispatch(bf, a.hd, [&](auto t, auto hd) {
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
+    if (a.nsplit > 1) range_join<T, HD><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
+  });
+}
+
+size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
+  return up256((int64_t)a.B * a.Hq * a.Sq * 4) + up256((int64_t)a.B * a.Sq * 8) + up256(a.B * cdiv(a.Sk, TR) * 8);
+}
+
+void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
+  char* p = (char*)ws;
+  auto take = [&](int64_t bytes) {
+    char* r = p;
+    p += up256(bytes);
+    return r;
+  };
+  a.delta = (float*)take((int64_t)a.B * a.Hq * a.Sq * 4);
+  a.seen = (int2*)take((int64_t)a.B * a.Sq * 8);
+  a.sees = (int2*)take(a.B * cdiv(a.Sk, TR) * 8);
+  const int ntile = (int)cdiv(a.Sk, TR);
+  if (a.Sk > 0) range_plan<<<(unsigned)((int64_t)ntile * a.B), 256, 0, st>>>(a, TR, ntile);
+  dispatch(bf, a.hd, [&](auto t, auto hd) {
+    using T = decltype(t);
+    constexpr int HD = decltype(hd)::value;
+    if (a.Sq > 0)
+      range_prep<T, HD><<<(unsigned)cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256), 256, 0, st>>>(a);
+    const int64_t blocks = cdiv(a.Sk, TR) * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
+    range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
+  });
+}
+
+void launch_key_ranges(int64_t B, int S, const int32_t* ids, const uint8_t* flags, int32_t* start, int32_t* end,
+                       hipStream_t st) {
+  const int nb = (int)cdiv(S, RT);
+  key_ranges<<<(unsigned)(B * nb), RTH, 0, st>>>(S, nb, ids, flags, start, end);
+}

@@ -212,6 +212,55 @@ void launch_attention_fwd(bool bf, const AttnArgs& a, hipStream_t st);
 void launch_attention_delta(bool bf, const AttnArgs& a, hipStream_t st);
 void launch_attention_bwd(bool bf, const AttnArgs& a, hipStream_t st);
 
+// ------------------------------------------------------------------ attention over key ranges (attention_ranges.hip)
+// Rows of a head: head h of row i of sequence b starts at element b batch + i row + h head of p
+struct HeadRows {
+  void* p;
+  int64_t batch, head;
+  int row;
+};
+// Query i of sequence b sees the keys [key_start, key_end) of [b, i] within [0, Sk), or those at or before its
+// position q_start[b] + i (q_start null: Sk - Sq) when key_start is null.  With x = scale q.k its score is
+// cap tanh(x / cap) (cap 0: x) - slopes[h] |position - j| (slopes null: no such term).
+struct RangeArgs {
+  int B, Sq, Sk, Hq, Hkv, hd;
+  HeadRows q, k, v;
+  void* o;     // [B, Sq, Hq, hd]
+  float* o32;  // the same in fp32; may be null
+  float* lse;  // [B, Hq, Sq]
+  const int32_t *key_start, *key_end, *q_start;
+  const float* slopes;
+  float scale, cap;
+  // backward
+  HeadRows dout, dq, dk, dv;
+  const float *rope_cos, *rope_sin;  // as in AttnArgs
+  // workspace, laid out by the launchers
+  float* delta;      // [B, Hq, Sq]
+  int2* seen;        // [B, Sq]: the keys each query sees (x = y = 0: none)
+  int2* sees;        // [B, key tiles]: the queries that see any key of a tile lie in [x, y)
+  float* part;       // partial sums of split items
+  float2* part_ml;   // and their maxima and sums
+  int nsplit;
+};
+size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a);
+void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st);
+size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a);
+void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st);
+// key_start, key_end [B, S] of packed documents ids [B, S] (flags: prefix tokens, may be null)
+void launch_key_ranges(int64_t B, int S, const int32_t* ids, const uint8_t* flags, int32_t* start, int32_t* end,
+                       hipStream_t st);
+
+// ------------------------------------------------------------------ dropout (dropout.hip)
+// out = resid + keep(e) x 65536 / (65536 - threshold) over [rows, cols], e = row cols + col; resid may be null
+struct DropoutArgs {
+  int64_t rows, cols, ldx, ldr, ldo;
+  const void *x, *resid;
+  void* out;
+  uint32_t threshold;
+  uint64_t seed, offset;
+};
+void launch_dropout(bool bf, const DropoutArgs& a, hipStream_t st);
+
 // ------------------------------------------------------------------ Muon (muon.hip)
 // One weight matrix of delayed Muon: W [rows, cols] row-major at element offset `off` of the flat
 // parameter vectors; x[0], x[1] its fp32 Newton-Schulz iterates in wide orientation (the

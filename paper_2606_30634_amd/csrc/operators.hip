@@ -1,5 +1,5 @@
-// C entries of the stateless log-probability and loss operators: argument checks, then the launchers of
-// logprob.hip and losses.hip.
+// C entries of the stateless operators: argument checks, then the launchers of logprob.hip, losses.hip,
+// attention_ranges.hip and dropout.hip.
 #include <cmath>
 
 #include "../../include/asyncstage.h"
@@ -52,6 +52,72 @@ const char* check_rows(int64_t rows, int64_t vocab, const int32_t* targets, floa
   if (rows > 0 && (!targets || !logp)) return "null targets or logp";
   if (off(targets, 4) || off(logp, 4) || off(entropy, 4) || off(stats, 4)) return "arrays must be 4-byte aligned";
   return nullptr;
+}
+
+// nullptr, or what is wrong with the sizes, ranges and numbers of an attention call
+const char* check_attention(const attention_params_t* p, RangeArgs& a) {
+  constexpr int64_t most = (int64_t)1 << 30;
+  if (!p) return "null attention parameters";
+  if (p->batch < 0 || p->batch > (1 << 24) || p->queries < 0 || p->queries > most || p->keys < 0 || p->keys > most)
+    return "batch must be in [0, 2^24], queries and keys in [0, 2^30]";
+  if (p->kv_heads < 1 || p->heads < p->kv_heads || p->heads > 4096 || p->heads % p->kv_heads)
+    return "kv_heads must be at least 1 and divide heads (at most 4096)";
+  if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 32, 64 or 128";
+  if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return "scale must be positive and finite";
+  if (!(p->softcap >= 0.f) || !std::isfinite(p->softcap) || !std::isfinite(1.f / p->softcap) != (p->softcap == 0.f))
+    return "softcap must be 0 (none) or positive and finite, with a finite reciprocal";
+  if ((p->key_start != nullptr) != (p->key_end != nullptr)) return "key_start and key_end come together";
+  if (off(p->key_start, 4) || off(p->key_end, 4) || off(p->q_start, 4) || off(p->slopes, 4))
+    return "arrays must be 4-byte aligned";
+  const int64_t blocks = ((p->queries + 31) / 32 + 1) * p->heads + ((p->keys + 31) / 32 + 1) * p->kv_heads;
+  if (p->batch * blocks >= ((int64_t)1 << 25) || p->batch * p->queries * p->heads >= ((int64_t)1 << 33))
+    return "batch x (queries heads + keys kv_heads) is too large for a launch";
+  a = RangeArgs{};
+  a.B = (int)p->batch; a.Sq = (int)p->queries; a.Sk = (int)p->keys;
+  a.Hq = p->heads; a.Hkv = p->kv_heads; a.hd = p->head_dim;
+  a.key_start = p->key_start; a.key_end = p->key_end; a.q_start = p->q_start; a.slopes = p->slopes;
+  a.scale = p->scale; a.cap = p->softcap;
+  return nullptr;
+}
+
+// nullptr, or what is wrong with rows [batch, rows, heads, head_dim] at p with strides s (elements)
+const char* check_rows_of(const void* p, const int64_t* s, int64_t rows, bool bf, HeadRows& out) {
+  const int64_t per = bf ? 8 : 4, most = (int64_t)1 << 40;
+  if (rows > 0 && !p) return "null rows";
+  if (off(p, 16)) return "rows must be 16-byte aligned";
+  for (int k = 0; k < 3; ++k)
+    if (s[k] < 0 || s[k] > most || s[k] % per) return "strides must be whole 16 bytes, none negative, at most 2^40";
+  if (s[1] > (1 << 24)) return "a row stride must be at most 2^24 elements";
+  out = HeadRows{const_cast<void*>(p), s[0], s[2], (int)s[1]};
+  return nullptr;
+}
+// what a kernel writes must not meet itself: sorted by stride, each dimension steps over the ones within it
+bool apart(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t hd) {
+  int64_t st[3] = {s[0], s[1], s[2]}, n[3] = {batch, rows, heads};
+  int64_t within = hd;
+  bool used[3] = {};
+  for (int k = 0; k < 3; ++k) {
+    int best = -1;
+    for (int j = 0; j < 3; ++j)
+      if (!used[j] && n[j] > 1 && (best < 0 || st[j] < st[best])) best = j;
+    if (best < 0) break;
+    used[best] = true;
+    if (st[best] < within) return false;
+    within += st[best] * (n[best] - 1);
+  }
+  return true;
+}
+// gradients x and y (heads of `w` elements in all, strides sx and sy) are different heads of the same packed rows
+bool packed_apart(const void* x, const int64_t* sx, int64_t wx, const void* y, const int64_t* sy, int64_t wy, size_t esz) {
+  if (sx[0] != sy[0] || sx[1] != sy[1]) return false;
+  if ((uintptr_t)y < (uintptr_t)x) return packed_apart(y, sy, wy, x, sx, wx, esz);
+  const int64_t at = ((const char*)y - (const char*)x) / (int64_t)esz;  // both multiples of 16 bytes
+  return wx <= at && at + wy <= sx[1];
+}
+// bytes that rows span
+size_t extent(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t hd, size_t esz) {
+  if (batch == 0 || rows == 0) return 0;
+  return ((batch - 1) * s[0] + (rows - 1) * s[1] + (heads - 1) * s[2] + hd) * esz;
 }
 
 }  // namespace
@@ -192,6 +258,132 @@ int preference_loss(int64_t pairs, int64_t len, const float* logp, const float* 
   a.norm = hp->norm; a.grad_scale = hp->grad_scale;
   a.loss = loss; a.dlogp = dlogp; a.pair_loss = pair_loss; a.rewards = rewards; a.metrics = metrics; a.counts = counts;
   launch_preference_loss(a, workspace, (hipStream_t)hip_stream);
+  return launched();
+}
+
+int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents, const uint8_t* prefix,
+                         int32_t* key_start, int32_t* key_end, void* hip_stream) {
+  if (batch < 0 || length < 0 || length > ((int64_t)1 << 30) || batch > ((int64_t)1 << 24) ||
+      batch * ((length + 2047) / 2048) >= ((int64_t)1 << 31))
+    return bad("batch must be in [0, 2^24], length in [0, 2^30], batch length / 2048 below 2^31");
+  if (batch * length == 0) return STAGE_OK;
+  if (!documents || !key_start || !key_end) return bad("null documents, key_start or key_end");
+  if (off(documents, 4) || off(key_start, 4) || off(key_end, 4)) return bad("arrays must be 4-byte aligned");
+  const size_t n = (size_t)(batch * length);
+  for (const int32_t* o : {key_start, key_end})
+    if (meet(documents, 4 * n, o, 4 * n) || meet(prefix, n, o, 4 * n)) return bad("the ranges may not overlap an input");
+  if (meet(key_start, 4 * n, key_end, 4 * n)) return bad("key_start and key_end overlap");
+  launch_key_ranges(batch, (int)length, documents, prefix, key_start, key_end, (hipStream_t)hip_stream);
+  return launched();
+}
+
+size_t attention_workspace_bytes(const attention_params_t* p) {
+  RangeArgs a;
+  if (check_attention(p, a) || a.B == 0 || a.Sq == 0) return 0;
+  return range_fwd_ws_bytes(p->is_bf16 != 0, a);
+}
+
+int attention_forward(const attention_params_t* p, const void* q, const void* k, const void* v, void* o, float* o_f32,
+                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  RangeArgs a;
+  if (const char* m = check_attention(p, a)) return bad(m);
+  const bool bf = p->is_bf16 != 0;
+  const size_t esz = bf ? 2 : 4;
+  if (const char* m = check_rows_of(q, p->q_strides, a.B * p->queries, bf, a.q)) return bad(m);
+  if (const char* m = check_rows_of(k, p->k_strides, a.B * p->keys, bf, a.k)) return bad(m);
+  if (const char* m = check_rows_of(v, p->v_strides, a.B * p->keys, bf, a.v)) return bad(m);
+  if (a.B == 0 || a.Sq == 0) return STAGE_OK;
+  if (!o || !lse) return bad("null o or lse");
+  if (off(o, 16) || off(o_f32, 16) || off(lse, 4)) return bad("o and o_f32 must be 16-byte aligned, lse to its type");
+  if (o_f32 && !bf) return bad("o_f32 belongs to bf16: an fp32 o is the output itself");
+  const size_t n = (size_t)(p->batch * p->queries * a.Hq), eq = extent(p->q_strides, a.B, a.Sq, a.Hq, a.hd, esz),
+               ek = extent(p->k_strides, a.B, a.Sk, a.Hkv, a.hd, esz), ev = extent(p->v_strides, a.B, a.Sk, a.Hkv, a.hd, esz);
+  struct { const void* p; size_t n; } outs[3] = {{o, n * a.hd * esz}, {o_f32, n * a.hd * 4}, {lse, n * 4}};
+  for (int i = 0; i < 3; ++i) {
+    if (meet(q, eq, outs[i].p, outs[i].n) || meet(k, ek, outs[i].p, outs[i].n) || meet(v, ev, outs[i].p, outs[i].n))
+      return bad("an output may not overlap q, k or v");
+    for (int j = 0; j < i; ++j)
+      if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n)) return bad("the outputs overlap");
+  }
+  if (const char* m = check_ws(workspace, workspace_bytes, range_fwd_ws_bytes(bf, a))) return bad(m);
+  a.o = o; a.o32 = o_f32; a.lse = lse;
+  launch_range_fwd(bf, a, workspace, (hipStream_t)hip_stream);
+  return launched();
+}
+
+size_t attention_backward_workspace_bytes(const attention_params_t* p) {
+  RangeArgs a;
+  if (check_attention(p, a) || a.B == 0) return 0;
+  return range_bwd_ws_bytes(p->is_bf16 != 0, a);
+}
+
+int attention_backward(const attention_params_t* p, const void* q, const void* k, const void* v, const void* o,
+                       const float* o_f32, const float* lse, const void* dout, const attention_grads_t* g,
+                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  RangeArgs a;
+  if (const char* m = check_attention(p, a)) return bad(m);
+  if (!g) return bad("null gradients");
+  const bool bf = p->is_bf16 != 0;
+  const size_t esz = bf ? 2 : 4;
+  const int64_t nq = a.B * p->queries, nk = a.B * p->keys;
+  if (const char* m = check_rows_of(q, p->q_strides, nq, bf, a.q)) return bad(m);
+  if (const char* m = check_rows_of(k, p->k_strides, nk, bf, a.k)) return bad(m);
+  if (const char* m = check_rows_of(v, p->v_strides, nk, bf, a.v)) return bad(m);
+  if (const char* m = check_rows_of(dout, g->dout_strides, nq, bf, a.dout)) return bad(m);
+  if (const char* m = check_rows_of(g->dq, g->dq_strides, nq, bf, a.dq)) return bad(m);
+  if (const char* m = check_rows_of(g->dk, g->dk_strides, nk, bf, a.dk)) return bad(m);
+  if (const char* m = check_rows_of(g->dv, g->dv_strides, nk, bf, a.dv)) return bad(m);
+  if (nq + nk == 0) return STAGE_OK;
+  if (nq > 0 && (!lse || !(o || o_f32))) return bad("null lse or o");
+  if (off(o, 16) || off(o_f32, 16) || off(lse, 4)) return bad("o and o_f32 must be 16-byte aligned, lse to its type");
+  if (!apart(g->dq_strides, a.B, a.Sq, a.Hq, a.hd) || !apart(g->dk_strides, a.B, a.Sk, a.Hkv, a.hd) ||
+      !apart(g->dv_strides, a.B, a.Sk, a.Hkv, a.hd))
+    return bad("the rows of a gradient overlap");
+  const size_t n = (size_t)nq * a.Hq;
+  struct { const void* p; size_t n; } ins[7] = {{q, extent(p->q_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
+                                                {k, extent(p->k_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
+                                                {v, extent(p->v_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
+                                                {dout, extent(g->dout_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
+                                                {o, n * a.hd * esz}, {o_f32, n * a.hd * 4}, {lse, n * 4}},
+                                      outs[3] = {{g->dq, extent(g->dq_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
+                                                 {g->dk, extent(g->dk_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
+                                                 {g->dv, extent(g->dv_strides, a.B, a.Sk, a.Hkv, a.hd, esz)}};
+  for (auto& x : outs)
+    for (auto& y : ins)
+      if (meet(x.p, x.n, y.p, y.n)) return bad("a gradient may not overlap an input");
+  // the three may be interleaved, as the heads of one packed row are
+  const int64_t* st[3] = {g->dq_strides, g->dk_strides, g->dv_strides};
+  int64_t wide[3];
+  for (int i = 0; i < 3; ++i) wide[i] = ((i ? a.Hkv : a.Hq) - 1) * st[i][2] + a.hd;
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < i; ++j)
+      if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n) &&
+          !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz))
+        return bad("the gradients overlap");
+  if (const char* m = check_ws(workspace, workspace_bytes, range_bwd_ws_bytes(bf, a))) return bad(m);
+  a.o = const_cast<void*>(o); a.o32 = const_cast<float*>(o_f32); a.lse = const_cast<float*>(lse);
+  launch_range_bwd(bf, a, workspace, (hipStream_t)hip_stream);
+  return launched();
+}
+
+int dropout_add(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual, int64_t ldr, void* out,
+                int64_t ldo, int32_t is_bf16, double p, uint64_t seed, uint64_t offset, void* hip_stream) {
+  constexpr int64_t most = (int64_t)1 << 40;
+  if (rows < 0 || cols < 0 || rows > most || cols > most || (cols > 0 && rows > most / cols))
+    return bad("rows and cols must not be negative, rows cols at most 2^40");
+  if (!(p >= 0.0 && p <= 65535.0 / 65536.0)) return bad("p must be in [0, 1 - 2^-16]");
+  if (rows * cols == 0) return STAGE_OK;
+  if (ldx < cols || ldo < cols || (residual && ldr < cols) || ldx > most || ldo > most || ldr > most)
+    return bad("ldx, ldr and ldo must be in [cols, 2^40]");
+  const size_t e = is_bf16 ? 2 : 4;
+  if (!x || !out || off(x, e) || off(residual, e) || off(out, e)) return bad("x or out null or not aligned to their type");
+  auto span = [&](int64_t ld) { return (size_t)((rows - 1) * ld + cols) * e; };
+  if ((x != out || ldx != ldo) && meet(x, span(ldx), out, span(ldo))) return bad("out may be x itself but not overlap it otherwise");
+  if ((residual != out || ldr != ldo) && meet(residual, span(ldr), out, span(ldo)))
+    return bad("out may be the residual itself but not overlap it otherwise");
+  if (rows * cols > (int64_t)256 * 8 * 0x7fffffff) return bad("rows cols is too large for a launch");
+  launch_dropout(is_bf16 != 0, DropoutArgs{rows, cols, ldx, ldr, ldo, x, residual, out,
+                                           (uint32_t)std::nearbyint(65536.0 * p), seed, offset}, (hipStream_t)hip_stream);
   return launched();
 }
 

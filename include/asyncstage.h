@@ -428,8 +428,8 @@ int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents
  * keys at or before its position.  With x = scale q.k the score of key j is
  *   cap tanh(x / cap) - slopes[h] |position - j|   (softcap 0: x; slopes NULL: no second term).
  * A query that sees no key has o = 0, lse = -inf and no gradient; what a query does not see has no
- * influence on it, whatever it holds.  Products of bf16 accumulate in fp32; in bf16 the backward takes
- * the probabilities and their gradients rounded to bf16, the forward to 16 bits and more. */
+ * influence on it, whatever it holds.  Products of bf16 accumulate in fp32; their operands P and dS
+ * are rounded to bf16, but where o_f32 is kept the forward takes P in two bf16 parts (16 bits). */
 typedef struct {
   int64_t batch, queries, keys;        /* [0, 2^24], [0, 2^30], [0, 2^30]                   */
   int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim 32, 64 or 128    */
@@ -452,17 +452,18 @@ size_t attention_workspace_bytes(const attention_params_t* p);
 int attention_forward(const attention_params_t* p, const void* q, const void* k, const void* v, void* o, float* o_f32,
                       float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Gradients in q, k and v, from what the forward read and wrote (o_f32 or o: the former where it was kept) and
- * the gradient dout in o.  No atomics: the same inputs give the same bits.  dq, dk and dv may be the heads of one
+/* Gradients in q, k and v, from what the forward read and wrote (o, or better the o_f32 that it kept) and the
+ * gradient dout in o.  No atomics: the same inputs give the same bits.  dq, dk and dv may be the heads of one
  * packed row (equal row strides). */
 typedef struct {
-  int64_t dout_strides[3], dq_strides[3], dk_strides[3], dv_strides[3];
+  int64_t o_strides[3], dout_strides[3], dq_strides[3], dk_strides[3], dv_strides[3];
   void *dq, *dk, *dv;
+  int32_t o_is_f32;   /* o is in fp32, whatever the type of the rest */
 } attention_grads_t;
 size_t attention_backward_workspace_bytes(const attention_params_t* p);
 int attention_backward(const attention_params_t* p, const void* q, const void* k, const void* v, const void* o,
-                       const float* o_f32, const float* lse, const void* dout, const attention_grads_t* g,
-                       void* workspace, size_t workspace_bytes, void* hip_stream);
+                       const float* lse, const void* dout, const attention_grads_t* g, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
 
 /* Dropout added to a residual: out = residual + keep x / (1 - p') over [rows, cols] with p' = t / 65536, t = p
  * 65536 rounded, p in [0, 1 - 2^-16].  Element e = row cols + col is kept when its 16-bit number is >= t:

@@ -111,15 +111,15 @@ def attention_backward(q, k, v, forward: Attention, dout, *, key_start=None, key
     dout [B, Sq, H, hd] in o.  out: the three, of the inputs' shapes and type, any strides as in attention()."""
     params, pq, pk, pv, dev = _params(q, k, v, key_start, key_end, q_start, scale, softcap, slopes)
     b, nq, h, _ = q.shape
-    o = None if forward.o is None else _require("forward.o", forward.o, dev, q.dtype, q.shape)
-    o32 = None if forward.o_f32 is None else _require("forward.o_f32", forward.o_f32, dev, _F32, q.shape)
+    wide = forward.o_f32 is not None
+    po, so = _heads("forward.o_f32", forward.o_f32, dev, _F32, q.shape) if wide else _heads("forward.o", forward.o, dev, q.dtype, q.shape)
     lse = _require("forward.lse", forward.lse, dev, _F32, torch.Size((b, h, nq)))
     pd, sd = _heads("dout", dout, dev, q.dtype, q.shape)
     if out is None:
         out = tuple(torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
     dq, dk, dv = out
     (gq, tq), (gk, tk), (gv, tv) = (_heads("out", g, dev, q.dtype, t.shape) for g, t in ((dq, q), (dk, k), (dv, v)))
-    grads = B.AttentionGrads(sd, tq, tk, tv, gq, gk, gv)
+    grads = B.AttentionGrads(so, sd, tq, tk, tv, gq, gk, gv, wide)
     ws, nb = _workspace(workspace, B.attention_backward_workspace_bytes(params), dev)
-    _launch(dev, B.attention_backward, params, pq, pk, pv, o, o32, lse, pd, grads, _ptr(ws), nb)
+    _launch(dev, B.attention_backward, params, pq, pk, pv, po, lse, pd, grads, _ptr(ws), nb)
     return dq, dk, dv

@@ -67,8 +67,8 @@ class AttentionParams(C.Structure):
 
 
 class AttentionGrads(C.Structure):
-    _fields_ = [(n, _STRIDES) for n in ("dout_strides", "dq_strides", "dk_strides", "dv_strides")] + [
-        (n, C.c_void_p) for n in ("dq", "dk", "dv")]
+    _fields_ = [(n, _STRIDES) for n in ("o_strides", "dout_strides", "dq_strides", "dk_strides", "dv_strides")] + [
+        (n, C.c_void_p) for n in ("dq", "dk", "dv")] + [("o_is_f32", C.c_int32)]
 
 
 class StageError(RuntimeError):
@@ -130,7 +130,7 @@ def _load():
         "attention_workspace_bytes": (sz, [C.POINTER(AttentionParams)]),
         "attention_forward": (C.c_int, [C.POINTER(AttentionParams), vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "attention_backward_workspace_bytes": (sz, [C.POINTER(AttentionParams)]),
-        "attention_backward": (C.c_int, [C.POINTER(AttentionParams), vp, vp, vp, vp, vp, vp, vp,
+        "attention_backward": (C.c_int, [C.POINTER(AttentionParams), vp, vp, vp, vp, vp, vp,
                                          C.POINTER(AttentionGrads), vp, sz, vp]),
         "dropout_add": (C.c_int, [i64, i64, vp, i64, vp, i64, vp, i64, i32, C.c_double, C.c_uint64, C.c_uint64, vp]),
         "stage_last_error": (C.c_char_p, []),
@@ -316,10 +316,10 @@ def attention_backward_workspace_bytes(params: AttentionParams) -> int:
     return LIB.attention_backward_workspace_bytes(C.byref(params))
 
 
-def attention_backward(params: AttentionParams, q, k, v, o, o_f32, lse, dout, grads: AttentionGrads, workspace,
+def attention_backward(params: AttentionParams, q, k, v, o, lse, dout, grads: AttentionGrads, workspace,
                        workspace_bytes, stream) -> None:
     check("attention_backward", LIB.attention_backward(
-        C.byref(params), q, k, v, o, o_f32, lse, dout, C.byref(grads), workspace, workspace_bytes, stream))
+        C.byref(params), q, k, v, o, lse, dout, C.byref(grads), workspace, workspace_bytes, stream))
 
 
 def dropout_add(rows, cols, x, ldx, residual, ldr, out, ldo, is_bf16, p, seed, offset, stream) -> None:

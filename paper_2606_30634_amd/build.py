@@ -18,7 +18,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wno-unused-res
 # Per-file additions.  The attention kernels keep their fp32 accumulators in arch VGPRs (MFMA
 # VGPR form): their softmax and rescale touch every accumulator with VALU instructions, which the
 # AGPR form turns into accumulator-register copies.
-FILE_FLAGS = {"attention_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+_MFMA_VGPR = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+FILE_FLAGS = {"attention_mfma.hip": _MFMA_VGPR, "attention_ranges_mfma.hip": _MFMA_VGPR}
 
 
 def _compile(src: str) -> str:

@@ -489,25 +489,6 @@ __device__ __forceinline__ void bwd_dkv_block(const AttnArgs& a, int bx, int spl
 // iteration takes the score tiles of the newest stage and the products of the one before while the next
 // arrives.  Two sequences of 4096, 32 heads on 8: 697 -> 575 us (all products of a stage, then its
 // softmax, then the products before).
-//
-// acc += A B with the accumulator kept in accumulator registers (this file's builtin MFMAs keep theirs
-// in vector registers, which 128 more would overflow).  The compiler does not know the instruction, so
-// its distances are kept here: in the loop operands come from LDS reads (waited for) or vector
-// instructions several MFMAs back, and one accumulator's products are 16 MFMAs apart; COPIED (outside
-// the loop, where the compiler moves accumulators between registers) waits between such a move and the
-// product; and acc_settled() stands between the last products and any other read.
-template <bool COPIED>
-__device__ __forceinline__ void mfma_acc(f32x16& acc, const bf16x8& a, const bf16x8& b) {
-  if constexpr (COPIED) asm volatile("s_nop 4\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
-  else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
-}
-__device__ __forceinline__ void acc_settled(f32x16 (&x)[4], f32x16 (&y)[4]) {
-  asm volatile("s_nop 15\n\ts_nop 15"
-               : "+a"(x[0]), "+a"(x[1]), "+a"(x[2]), "+a"(x[3]), "+a"(y[0]), "+a"(y[1]), "+a"(y[2]), "+a"(y[3]));
-}
-// keeps the computation of two values ahead of this point of the schedule
-__device__ __forceinline__ void pin(float& x, float& y) { asm volatile("" : "+v"(x), "+v"(y)); }
-
 struct Dkv128 {
   static constexpr int HD = 128, KS = 8, DT = 4, NS = 3;
   static constexpr int TSZ = KB * HD, SSZ = 2 * TSZ + 4 * KB;  // bf16 elements: Q, dO, lse and delta rows

@@ -22,6 +22,12 @@ __device__ __forceinline__ int2 seen_keys(const RangeArgs& a, int b, int i) {
 }
 __device__ __forceinline__ bool sees(const int2& s, int key) { return (uint32_t)(key - s.x) < (uint32_t)(s.y - s.x); }
 
+// The same from the arrays that the backward lays out
+__device__ __forceinline__ int2 seen_keys_kept(const RangeArgs& a, int64_t row) {
+  const int lo = a.seen_lo[row];
+  return make_int2(lo, lo + a.seen_len[row]);
+}
+
 // What a score is taken relative to in a row of this maximum or lse: a row of only -inf has weights of 0
 __device__ __forceinline__ float weight_base(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -57,17 +63,21 @@ __device__ __forceinline__ T* rows_out(const HeadRows& r, int b, int h) {
   return (T*)r.p + b * r.batch + h * r.head;
 }
 
-// A wave's minimum and maximum over all its lanes
-__device__ __forceinline__ int wave_min_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, WAVE));
-  return __builtin_amdgcn_readfirstlane(v);
+// A wave's minimum and maximum over all its lanes, by data-parallel moves (as wave_total)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_same(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xf, false); }
+template <typename F>
+__device__ __forceinline__ int wave_fold(int v, F&& f) {
+  v = f(v, dpp_or_same<0x111, 0xf>(v));
+  v = f(v, dpp_or_same<0x112, 0xf>(v));
+  v = f(v, dpp_or_same<0x114, 0xf>(v));
+  v = f(v, dpp_or_same<0x118, 0xf>(v));
+  v = f(v, dpp_or_same<0x142, 0xa>(v));
+  v = f(v, dpp_or_same<0x143, 0xc>(v));
+  return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
-  return __builtin_amdgcn_readfirstlane(v);
-}
+__device__ __forceinline__ int wave_min_i(int v) { return wave_fold(v, [](int x, int y) { return min(x, y); }); }
+__device__ __forceinline__ int wave_max_i(int v) { return wave_fold(v, [](int x, int y) { return max(x, y); }); }
 
 // The keys [lo, hi) that some query of a wave sees (none: 0, 0), and those [all_lo, all_hi) that all of them see
 // (none: all_lo > all_hi).  valid: the lane's query exists.

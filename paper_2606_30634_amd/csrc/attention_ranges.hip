@@ -15,6 +15,13 @@
 #include "attention_rows.h"
 #include <algorithm>
 
+// attention_ranges_mfma.hip: bf16 of head dimensions 64 and 128
+int64_t range_mfma_items(const RangeArgs& a);
+void range_mfma_fwd(const RangeArgs& a, hipStream_t st);
+int range_mfma_keys();  // keys of a dK/dV block
+int range_mfma_dkv_splits(const RangeArgs& a);
+void range_mfma_bwd(const RangeArgs& a, hipStream_t st);
+
 namespace {
 
 // Score of x = scale q.k at distance `far` (x itself without cap and slopes)
@@ -137,8 +144,9 @@ __global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a)
   if (wave == 0 && lane < TR && q < a.Sq) a.lse[((int64_t)b * a.Hq + h) * a.Sq + q] = base + logf(L);
 }
 
-// The shares of a row joined: HD / 4 lanes per row (b, i, h)
-template <typename T, int HD>
+// The shares of a row joined: HD / 4 lanes per row (b, i, h).  LOG2: their maxima are in log2 units (the bf16
+// kernels').
+template <typename T, int HD, bool LOG2>
 __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   constexpr int LR = HD / 4;
   const int64_t n = (int64_t)a.B * a.Sq * a.Hq, r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;
@@ -150,8 +158,7 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < a.nsplit; ++s) {
     const float2 ml = a.part_ml[n * s + r];
-    const float w = expf(ml.x - base);
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    const float w = LOG2 ? exp2f(ml.x - base) : expf(ml.x - base);
     L += w * ml.y;
     o += w * ld4(a.part + (n * s + r) * HD + c);
   }
@@ -160,7 +167,7 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   if (a.o32) st4(a.o32 + r * HD + c, o);
   if (c == 0) {
     const int64_t row = r / a.Hq, b = row / a.Sq;
-    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = base + logf(L);
+    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2 ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
   }
 }
 
@@ -176,14 +183,21 @@ __global__ void __launch_bounds__(256) range_prep(RangeArgs a) {
   float s = 0.f;
   if (in) {
     const f32x4 d = ld4(rows_of<T>(a.dout, b, h) + (int64_t)i * a.dout.row + c);
-    const f32x4 o = a.o32 ? ld4(a.o32 + r * HD + c) : ld4((const T*)a.o + r * HD + c);
+    const int64_t at = b * a.ob + i * a.orow + h * a.oh + c;
+    const f32x4 o = a.o32 ? ld4(a.o32 + at) : ld4((const T*)a.o + at);
     s = (o[0] * d[0] + o[1] * d[1]) + (o[2] * d[2] + o[3] * d[3]);
   }
 #pragma unroll
   for (int k = 1; k < LR; k <<= 1) s += __shfl_xor(s, k, WAVE);
   if (!in || c) return;
   a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
-  if (h == 0) a.seen[row] = seen_keys(a, b, i);
+  const float lse = a.lse[((int64_t)b * a.Hq + h) * a.Sq + i];
+  a.nlse2[((int64_t)b * a.Hq + h) * a.Sq + i] = -1.4426950408889634f * weight_base(lse);
+  if (h == 0) {
+    const int2 k = seen_keys(a, b, i);
+    a.seen_lo[row] = k.x;
+    a.seen_len[row] = k.y - k.x;
+  }
 }
 
 // [x, y): the first and last query that see a key of tile t of `width` keys, one block per (tile, sequence)
@@ -222,7 +236,7 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int 
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = q0 + lane % 32, qc = min(q, a.Sq - 1);
   const T* kp = rows_of<T>(a.k, b, kvh);
   const T* vp = rows_of<T>(a.v, b, kvh);
-  const int2 mask = a.seen[(int64_t)b * a.Sq + qc];
+  const int2 mask = seen_keys_kept(a, (int64_t)b * a.Sq + qc);
   const WaveKeys wk(mask, q < a.Sq);
   const int64_t pos = position(a, b, qc);
   const Score score(a, h);
@@ -282,7 +296,7 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, i
     for (int e = 0; e < 16; ++e) { dk[dt][e] = 0.f; dv[dt][e] = 0.f; }
   const int2 by = a.sees[(int64_t)b * ((a.Sk + TR - 1) / TR) + kb];
   const int nt = (by.y - by.x + TR - 1) / TR;
-  const int2* seen = a.seen + (int64_t)b * a.Sq;
+  const int64_t row0 = (int64_t)b * a.Sq;
   for (int64_t it = wave; it < (int64_t)group * nt; it += NW) {
     const int h = kvh * group + (int)(it / nt), q0 = by.x + (int)(it % nt) * TR, ql = by.y - 1;
     const T* qp = rows_of<T>(a.q, b, h);
@@ -290,7 +304,7 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, i
     const int64_t sb = ((int64_t)b * a.Hq + h) * a.Sq;
     const int qr = min(q0 + lane % 32, ql);
     const Score score(a, h);
-    const int2 mine = seen[qr];
+    const int2 mine = seen_keys_kept(a, row0 + qr);
     // every key of the block is seen by every query of the tile
     const bool whole = q0 + TR <= by.y && __all(mine.x <= k0 && k0 + TR <= mine.y);
     RowFrag<HD> f;
@@ -304,13 +318,13 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, i
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int q = q0 + acc_row(e), qc = min(q, ql);
-      const bool on = q <= ql && sees(seen[qc], key);
+      const bool on = q <= ql && sees(seen_keys_kept(a, row0 + qc), key);
       float g;
       const float x = score(p[e], base_far + (float)acc_row(e), g);
       p[e] = on ? expf(x - weight_base(a.lse[sb + qc])) : 0.f;
       ds[e] = on ? p[e] * (ds[e] - a.delta[sb + qc]) * g : 0.f;
     }
-    auto on = [&](int r) { return q0 + r <= ql && sees(seen[min(q0 + r, ql)], key); };
+    auto on = [&](int r) { return q0 + r <= ql && sees(seen_keys_kept(a, row0 + min(q0 + r, ql)), key); };
     float* tmp = red + wave * WAVE_LDS<HD>;
     if (plain_d) cols_product<HD>(dv, dp_, q0, ql, a.dout.row, p);
     else cols_product_seen<HD>(dv, dp_, q0, a.dout.row, p, tmp, on);
@@ -497,23 +511,27 @@ void dispatch(bool bf, int hd, F&& run) {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Shares of a forward item's keys: towards 512 items, two per compute unit, of at least 256 keys
-int fwd_splits(const RangeArgs& a) {
-  const int64_t items = cdiv(a.Sq, TR) * a.Hq * a.B;
+bool mfma(bool bf, int hd) { return bf && hd != 32; }
+
+// Shares of a forward item's keys: towards 512 items, two per compute unit, of at least 256 keys (two tiles on the
+// bf16 matrix cores)
+int fwd_splits(bool bf, const RangeArgs& a) {
+  const bool mm = mfma(bf, a.hd);
+  const int64_t items = mm ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
   if (items == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({64, 512 / items, a.Sk / 256}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({256, 512 / items, a.Sk / (mm ? 128 : 256)}));
 }
 
 }  // namespace
 
 size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a) {
-  const int64_t ns = fwd_splits(a), n = (int64_t)a.B * a.Sq * a.Hq;
+  const int64_t ns = fwd_splits(bf, a), n = (int64_t)a.B * a.Sq * a.Hq;
   return ns > 1 ? up256(ns * n * a.hd * 4) + up256(ns * n * 8) : 0;
 }
 
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
-  a.nsplit = fwd_splits(a);
+  a.nsplit = fwd_splits(bf, a);
   if (a.nsplit > 1) {
     a.part = (float*)ws;
     a.part_ml = (float2*)((char*)ws + up256(a.nsplit * n * a.hd * 4));
@@ -521,34 +539,53 @@ void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
-    if (a.nsplit > 1) range_join<T, HD><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2 && HD != 32) range_mfma_fwd(a, st);
+    else range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
+    if (a.nsplit > 1) range_join<T, HD, sizeof(T) == 2 && HD != 32><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
   });
 }
 
+namespace {
+
+// The backward's workspace at p (null: its size alone)
+size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
+  size_t n = 0;
+  auto take = [&](int64_t bytes) {
+    char* r = p + n;
+    n += up256(bytes);
+    return r;
+  };
+  const bool mm = mfma(bf, a.hd);
+  const int64_t rows = (int64_t)a.B * a.Sq;
+  a.delta = (float*)take(rows * a.Hq * 4);
+  a.nlse2 = (float*)take(rows * a.Hq * 4);
+  a.seen_lo = (int32_t*)take(rows * 4);
+  a.seen_len = (int32_t*)take(rows * 4);
+  a.sees = (int2*)take(a.B * cdiv(a.Sk, mm ? range_mfma_keys() : TR) * 8);
+  a.nsplit = mm ? range_mfma_dkv_splits(a) : 1;
+  a.part = a.nsplit > 1 ? (float*)take(2 * (int64_t)a.nsplit * a.B * a.Sk * a.Hkv * a.hd * 4) : nullptr;
+  return n;
+}
+
+}  // namespace
+
 size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
-  return up256((int64_t)a.B * a.Hq * a.Sq * 4) + up256((int64_t)a.B * a.Sq * 8) + up256(a.B * cdiv(a.Sk, TR) * 8);
+  RangeArgs t = a;
+  return bwd_layout(bf, t, nullptr);
 }
 
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
-  char* p = (char*)ws;
-  auto take = [&](int64_t bytes) {
-    char* r = p;
-    p += up256(bytes);
-    return r;
-  };
-  a.delta = (float*)take((int64_t)a.B * a.Hq * a.Sq * 4);
-  a.seen = (int2*)take((int64_t)a.B * a.Sq * 8);
-  a.sees = (int2*)take(a.B * cdiv(a.Sk, TR) * 8);
-  const int ntile = (int)cdiv(a.Sk, TR);
-  if (a.Sk > 0) range_plan<<<(unsigned)((int64_t)ntile * a.B), 256, 0, st>>>(a, TR, ntile);
+  bwd_layout(bf, a, (char*)ws);
+  const int width = mfma(bf, a.hd) ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
+  if (a.Sk > 0) range_plan<<<(unsigned)((int64_t)ntile * a.B), 256, 0, st>>>(a, width, ntile);
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     if (a.Sq > 0)
       range_prep<T, HD><<<(unsigned)cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256), 256, 0, st>>>(a);
     const int64_t blocks = cdiv(a.Sk, TR) * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
-    range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2 && HD != 32) range_mfma_bwd(a, st);
+    else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
   });
 }
 

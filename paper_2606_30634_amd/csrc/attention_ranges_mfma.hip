@@ -1,0 +1,1156 @@
+// Attention over key ranges (the formulas are in attention_ranges.hip) for bf16 of head dimensions 64 and 128, on
+// the bf16 matrix cores, with the tiles, operand layouts and rings of attention_mfma.hip.
+//
+// What differs from the causal kernels there: tiles start at the first key that a query of the block sees and end
+// with the last, so nothing else is loaded; every lane owns one query (one key in dK/dV) and keeps its range, and
+// only tiles that some row does not see whole are masked; rows come from strided tensors; a forward block
+// may hold the query heads of one key/value head (`pack` rows per query) and a share of the keys.
+// A block whose result is not finite (a value that one of its rows does not see may be an infinity or a NaN, and 0
+// times it is a NaN) computes the rows in question again, key by key over what they see.
+#include "attention_ranges.h"
+#include "attention_tiles.h"
+#include <algorithm>
+
+namespace {
+
+// Scores in log2 units from the products x = q.k of a 32 x 32 accumulator: c (x scale), or c cap tanh(x scale / cap)
+struct CapScale {
+  float sl2;    // scale log2(e)
+  float y_of;   // scale / cap
+  float out;    // cap log2(e)
+  float small;  // |x| up to which |y| <= TANH_SMALL
+  __device__ explicit CapScale(const RangeArgs& a) {
+    sl2 = a.scale * LOG2E;
+    y_of = a.cap > 0.f ? a.scale / a.cap : 0.f;
+    out = a.cap * LOG2E;
+    small = TANH_SMALL / y_of;
+  }
+};
+
+// tanh(scale x / cap) of a wave's products.  One branch for the wave: where no |y| passes TANH_SMALL (scores within
+// half the cap, most tiles) the polynomial alone.
+template <int N>
+__device__ __forceinline__ void tanh_scores(f32x16 (&s)[N], const CapScale& c) {
+  float big = 0.f;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) big = fmaxf(big, fabsf(s[t][e]));
+  if (__all(big <= c.small)) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = s[t][e] * c.y_of;
+        s[t][e] = y * tanh_ratio(y * y);
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float g;
+        s[t][e] = tanh_and_slope(s[t][e] * c.y_of, g);
+      }
+  }
+}
+
+// One score of the row-by-row path, in log2 units, and the derivative of its cap
+__device__ __forceinline__ float score2(float x, const RangeArgs& a, const CapScale& c, float slope2, float far, float& g) {
+  g = 1.f;
+  x = a.cap > 0.f ? c.out * tanh_and_slope(x * c.y_of, g) : x * c.sl2;
+  return a.slopes ? __builtin_fmaf(-slope2, fabsf(far), x) : x;
+}
+
+// x.y of two rows of a head
+template <int HD>
+__device__ __forceinline__ float row_dot(const bf16* x, const bf16* y) {
+  float s = 0.f;
+  for (int c = 0; c < HD; c += 8) {
+    const bf16x8 u = *reinterpret_cast<const bf16x8*>(x + c), v = *reinterpret_cast<const bf16x8*>(y + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (float)u[j] * (float)v[j];
+  }
+  return s;
+}
+
+// ------------------------------------------------------------------------------------------ forward
+// Rows of a forward block: row r of unit (sequence b, heads h0 .. h0 + pack - 1) is query r / pack of head
+// h0 + r mod pack.
+struct Rows {
+  int pack, n, h0, b;
+  __device__ int query(int r) const { return pack == 1 ? r : r / pack; }
+  __device__ int head(int r) const { return pack == 1 ? h0 : h0 + r % pack; }
+};
+
+// o of one row again, touching only what it sees: a key per lane for the weights, columns per lane for the sum
+template <int HD>
+__device__ __forceinline__ void row_again(const RangeArgs& a, const Rows& rows, int r, float base, float inv, int k_lo,
+                                                    int k_hi, float* part) {
+  const int lane = threadIdx.x % 64, i = rows.query(r), h = rows.head(r), kvh = h / (a.Hq / a.Hkv);
+  const bf16* q = rows_of<bf16>(a.q, rows.b, h) + (int64_t)i * a.q.row;
+  const bf16* k = rows_of<bf16>(a.k, rows.b, kvh);
+  const bf16* v = rows_of<bf16>(a.v, rows.b, kvh);
+  const CapScale c(a);
+  const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
+  const int64_t pos = position(a, rows.b, i);
+  float o[HD / 64];
+#pragma unroll
+  for (int d = 0; d < HD / 64; ++d) o[d] = 0.f;
+  for (int j0 = k_lo; j0 < k_hi; j0 += 64) {
+    const int n = min(64, k_hi - j0), j = j0 + min(lane, n - 1);
+    float g;
+    const float p = fast_exp2(score2(row_dot<HD>(q, k + (int64_t)j * a.k.row), a, c, slope2, (float)(pos - j), g) - base);
+    for (int t = 0; t < n; ++t) {
+      const float w = __shfl(p, t, 64);
+#pragma unroll
+      for (int d = 0; d < HD / 64; ++d) o[d] += w * (float)v[(int64_t)(j0 + t) * a.v.row + 64 * d + lane];
+    }
+  }
+  const int64_t row = ((int64_t)rows.b * a.Sq + i) * a.Hq + h;
+#pragma unroll
+  for (int d = 0; d < HD / 64; ++d) {
+    if (part) part[row * HD + 64 * d + lane] = o[d];
+    else {
+      ((bf16*)a.o)[row * HD + 64 * d + lane] = (bf16)(o[d] * inv);
+      if (a.o32) a.o32[row * HD + 64 * d + lane] = o[d] * inv;
+    }
+  }
+}
+
+// HILO: P enters the P V product as its hi / lo bf16 pair, for an o that is kept in fp32 (as in flash_fwd)
+template <int HD, bool HILO, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) {
+  using L = Lds<HD>;
+  using TT = DmaRowTile<HD>;
+  constexpr int KS = HD / 16, DT = HD / 32, NS = L::NS;
+  extern __shared__ __align__(16) unsigned char smem[];
+  bf16* ring = reinterpret_cast<bf16*>(smem);  // [NS][K tile | V tile], swizzled
+  Rows rows;
+  rows.pack = pack;
+  rows.n = a.Sq * pack;
+  const int nb = (rows.n + QB - 1) / QB, heads = a.Hq / pack;
+  int unit, idx;  // unit: (sequence, query head or key/value head); last query blocks first
+  xcd_item(blockIdx.x, nb * a.nsplit * heads * a.B, nb * a.nsplit, unit, idx);
+  const int rb = nb - 1 - idx / a.nsplit, split = idx % a.nsplit;
+  rows.h0 = unit % heads * pack;
+  rows.b = unit / heads;
+  const int b = rows.b, kvh = rows.h0 / (a.Hq / a.Hkv);
+  const bf16* kbase = rows_of<bf16>(a.k, b, kvh);
+  const bf16* vbase = rows_of<bf16>(a.v, b, kvh);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+  const int r0 = rb * QB + wave * 32, myr = r0 + col;
+  const bool valid = myr < rows.n;
+  const int i = rows.query(min(myr, rows.n - 1)), h = rows.head(min(myr, rows.n - 1));
+  const int2 mask = seen_keys(a, b, i);
+  const WaveKeys wk(mask, valid);
+  // the block's keys, and this share's tiles of them
+  int blo, bhi;
+  {
+    const int x = rb * QB + lane, y = x + 64;
+    const int2 sx = x < rows.n ? seen_keys(a, b, rows.query(x)) : make_int2(0, 0);
+    const int2 sy = y < rows.n ? seen_keys(a, b, rows.query(y)) : make_int2(0, 0);
+    bhi = wave_max_i(max(sx.y, sy.y));
+    blo = wave_min_i(min(sx.y > 0 ? sx.x : INT32_MAX, sy.y > 0 ? sy.x : INT32_MAX));
+    if (bhi == 0) blo = 0;
+  }
+  const int ntile = (bhi - blo + KB - 1) / KB;
+  const int t0 = __builtin_amdgcn_readfirstlane((int)((int64_t)ntile * split / a.nsplit));
+  const int t1 = __builtin_amdgcn_readfirstlane((int)((int64_t)ntile * (split + 1) / a.nsplit));
+  auto issue = [&](int t) {
+    bf16* st = ring + (t % NS) * 2 * L::TSZ;
+    TT::issue(kbase, a.k.row, blo + t * KB, bhi, lds_addr(st));
+    TT::issue(vbase, a.v.row, blo + t * KB, bhi, lds_addr(st + L::TSZ));
+  };
+  bf16x8 qf[KS];
+  {
+    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (valid) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+      else for (int j = 0; j < 8; ++j) qf[ks][j] = (bf16)0.f;
+    }
+  }
+  const CapScale cs(a);
+  float slope2 = 0.f, pos_far = 0.f;
+  int64_t pos = 0;
+  if constexpr (BIAS) {
+    slope2 = a.slopes[h] * LOG2E;
+    pos = position(a, b, i);
+  }
+  wait_vm_lds<0>();  // the register loads, before the ring's (as in flash_fwd)
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (t0 + s < t1) issue(t0 + s);
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m = -INFINITY, lsum = 0.f;
+
+  for (int kt = t0; kt < t1; ++kt) {
+    ring_wait<NS, 2 * TT::PER>(kt + 1 < t1);
+    block_barrier();
+    if (kt + NS - 1 < t1) issue(kt + NS - 1);
+    const bf16* Ks = ring + (kt % NS) * 2 * L::TSZ;
+    const bf16* Vs = Ks + L::TSZ;
+    const int key0 = blo + kt * KB;
+    if (key0 < wk.hi && key0 + KB > wk.lo) {
+      f32x16 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+      bf16x8 fk[2][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) fk[0][t] = frag_rows<HD>(Ks, t * 32, 0);
+      static_for<KS>([&](auto KSI) {
+        constexpr int ks = KSI, c = ks & 1;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (ks + 1 < KS) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) fk[c ^ 1][t] = frag_rows<HD>(Ks, t * 32, (ks + 1) * 16);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], s[t], 0, 0, 0);
+        if constexpr (ks + 1 < KS) {
+          static_for<2>([&](auto) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
+          });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (CAP) tanh_scores(s, cs);
+      const float to_log2 = CAP ? cs.out : cs.sl2;  // of s
+      if constexpr (BIAS) {
+        pos_far = (float)(pos - key0 - 4 * half);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float far = fabsf(pos_far - (float)(t * 32 + 8 * (e / 4) + e % 4));
+            s[t][e] = __builtin_fmaf(-slope2, far, s[t][e] * to_log2);
+          }
+      }
+      if (!wk.whole(key0, key0 + KB)) {
+        const uint32_t first = (uint32_t)(key0 + 4 * half - mask.x), len = (uint32_t)(mask.y - mask.x);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (first + (uint32_t)(t * 32 + 8 * (e / 4) + e % 4) >= len) s[t][e] = -INFINITY;
+      }
+      float bm = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bm = fmaxf(bm, s[t][e]);
+      bm = pair_max(bm);
+      if constexpr (!BIAS) bm *= to_log2;  // with it s is in log2 units already
+      // the lazy maximum of flash_fwd; a row that sees nothing yet has base 0 and weights of 0
+      const bool move = bm > m + 8.0f;
+      const float mn = move ? bm : m;
+      const float corr = (m == -INFINITY) ? 0.f : fast_exp2(m - mn);
+      const float base = weight_base(mn);
+      float rs = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = fast_exp2(BIAS ? s[t][e] - base : __builtin_fmaf(s[t][e], to_log2, -base));
+          s[t][e] = p;
+          rs += p;
+        }
+      rs = pair_sum(rs);
+      lsum = lsum * corr + rs;
+      m = mn;
+      if (__any(move)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= corr;
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        if constexpr (HILO) {
+          bf16x8 ph, pl, vfr[DT];
+          if (kk % 2) acc_rows_to_b_split<8>(s[kk / 2], ph, pl);
+          else acc_rows_to_b_split<0>(s[kk / 2], ph, pl);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) vfr[dt] = frag_cols<HD>(Vs, dt * 32, kk * 16);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[dt], ph, o[dt], 0, 0, 0);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[dt], pl, o[dt], 0, 0, 0);
+        } else {
+          const bf16x8 pf = (kk % 2) ? acc_rows_to_b<8>(s[kk / 2]) : acc_rows_to_b<0>(s[kk / 2]);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Vs, dt * 32, kk * 16), pf, o[dt], 0, 0, 0);
+        }
+      }
+    }
+  }
+  block_barrier();  // every wave is done with the last tile: the ring becomes the output staging
+  const float inv = a.nsplit > 1 ? 1.0f : lsum == 0.f ? 0.f : 1.0f / lsum;
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
+  if (half == 0 && valid) {
+    if (a.nsplit > 1) a.part_ml[n * split + ((int64_t)b * a.Sq + i) * a.Hq + h] = make_float2(m, lsum);
+    else a.lse[((int64_t)b * a.Hq + h) * a.Sq + i] = (weight_base(m) + log2f(lsum)) * 0.6931471805599453f;
+  }
+  float z = 0.f;  // stays 0 as long as every value is finite
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z = __builtin_fmaf(o[dt][e], 0.f, z);
+  float* stage = reinterpret_cast<float*>(smem);
+  stage_rows_from_t<HD>(stage, o, 1.0f);
+  // the rows leave scaled: the factor of row r is in lane r mod 32 of wave r / 32
+  float* scales = stage + QB * (HD + 4);
+  if (half == 0) scales[wave * 32 + col] = inv;
+  __syncthreads();
+  float* part = a.nsplit > 1 ? a.part + n * split * HD : nullptr;
+  for (int c = threadIdx.x; c < QB * HD / 8; c += NT) {
+    const int r = rb * QB + c / (HD / 8), d = (c % (HD / 8)) * 8;
+    if (r >= rows.n) continue;
+    const float* sr = stage + c / (HD / 8) * (HD + 4) + d;
+    const float f = scales[c / (HD / 8)];
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(sr) * f, hi = *reinterpret_cast<const f32x4*>(sr + 4) * f;
+    const int64_t at = (((int64_t)b * a.Sq + rows.query(r)) * a.Hq + rows.head(r)) * HD + d;
+    float* f32 = part ? part : HILO ? a.o32 : nullptr;
+    if (f32) {
+      *reinterpret_cast<f32x4*>(f32 + at) = lo;
+      *reinterpret_cast<f32x4*>(f32 + at + 4) = hi;
+    }
+    if (!part) {
+      bf16x8 ov;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { ov[q] = (bf16)lo[q]; ov[q + 4] = (bf16)hi[q]; }
+      *reinterpret_cast<bf16x8*>((bf16*)a.o + at) = ov;
+    }
+  }
+  uint64_t bad = __ballot(valid && !(z == 0.f));
+  if (__syncthreads_or(bad != 0)) {  // behind every wave's stores of these rows
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    while (bad) {
+      const int c = __builtin_ctzll(bad);
+      bad &= bad - 1;
+      row_again<HD>(a, rows, r0 + c, weight_base(__shfl(m, c, 64)), __shfl(inv, c, 64),
+                    max(__shfl(mask.x, c, 64), blo + t0 * KB), min(__shfl(mask.y, c, 64), blo + t1 * KB), part);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ backward
+// P and dS of one pair, from dp = dO.v and s = q.k, or with CAP its tanh_scores
+struct Pair { float p, ds; };
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ Pair grad_pair(float s, float dp, float nlse2, float delta, const CapScale& c, float slope2,
+                                          float far) {
+  float x = __builtin_fmaf(s, CAP ? c.out : c.sl2, nlse2);
+  if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far), x);
+  const float p = fast_exp2(x), ds = p * (dp - delta);
+  return Pair{p, CAP ? ds * __builtin_fmaf(-s, s, 1.0f) : ds};
+}
+
+template <int N>
+__device__ __forceinline__ bool all_finite(const f32x16 (&x)[N]) {
+  float z = 0.f;  // stays 0 as long as every value is finite
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z = __builtin_fmaf(x[t][e], 0.f, z);
+  return z == 0.f;
+}
+
+// x rotated back by the angle of row `row` (as store_rows_from_t): lane l holds elements l, l + 64, ..
+template <int HD>
+__device__ __forceinline__ void unrotate(float (&x)[HD / 64], const RangeArgs& a, int row) {
+  constexpr int HH = HD / 2;
+  const int lane = threadIdx.x % 64;
+  if (!a.rope_cos) return;
+  const int64_t t = (int64_t)row * HH + lane % HH;
+  const float cs = a.rope_cos[t], sn = a.rope_sin[t];
+  if constexpr (HD == 128) {
+    const float u = x[0], v = x[1];
+    x[0] = u * cs + v * sn;
+    x[1] = v * cs - u * sn;
+  } else {
+    const float other = __shfl_xor(x[0], 32, 64);
+    x[0] = lane < HH ? x[0] * cs + other * sn : x[0] * cs - other * sn;
+  }
+}
+
+// dq of query i again, touching only the keys it sees
+template <int HD>
+__device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, int i) {
+  const int lane = threadIdx.x % 64, kvh = h / (a.Hq / a.Hkv);
+  const int2 keys = seen_keys_kept(a, (int64_t)b * a.Sq + i);
+  const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row;
+  const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row;
+  const bf16* k = rows_of<bf16>(a.k, b, kvh);
+  const bf16* v = rows_of<bf16>(a.v, b, kvh);
+  const CapScale c(a);
+  const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
+  const int64_t pos = position(a, b, i), sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
+  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
+  float acc[HD / 64];
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) acc[x] = 0.f;
+  for (int j0 = keys.x; j0 < keys.y; j0 += 64) {
+    const int n = min(64, keys.y - j0), j = j0 + min(lane, n - 1);
+    float g;
+    const float p = fast_exp2(score2(row_dot<HD>(q, k + (int64_t)j * a.k.row), a, c, slope2, (float)(pos - j), g) + nl);
+    const float ds = p * (row_dot<HD>(d, v + (int64_t)j * a.v.row) - dl) * g;
+    for (int t = 0; t < n; ++t) {
+      const float w = __shfl(ds, t, 64);
+#pragma unroll
+      for (int x = 0; x < HD / 64; ++x) acc[x] += w * (float)k[(int64_t)(j0 + t) * a.k.row + 64 * x + lane];
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) acc[x] *= a.scale;
+  unrotate<HD>(acc, a, i);
+  bf16* out = rows_out<bf16>(a.dq, b, h) + (int64_t)i * a.dq.row;
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) out[64 * x + lane] = (bf16)acc[x];
+}
+
+// What a dK/dV item covers: keys of block kb, 64-query tiles of the queries [by.x, by.y) that see one of them, of
+// every query head of the group: iterations [it0, nit) of tiles x group (its share of nsplit)
+struct KeyItem {
+  int kb, kvh, b, split, tiles, it0, nit, qlo, qhi;
+  __device__ KeyItem(const RangeArgs& a, int kb_, int split_, int kvh_, int b_) : kb(kb_), kvh(kvh_), b(b_), split(split_) {
+    const int2 by = a.sees[(int64_t)b * ((a.Sk + QB - 1) / QB) + kb];
+    qlo = __builtin_amdgcn_readfirstlane(by.x);
+    qhi = __builtin_amdgcn_readfirstlane(by.y);
+    tiles = (qhi - qlo + KB - 1) / KB;
+    const int64_t all = (int64_t)(a.Hq / a.Hkv) * tiles;
+    it0 = __builtin_amdgcn_readfirstlane((int)(all * split / a.nsplit));
+    nit = __builtin_amdgcn_readfirstlane((int)(all * (split + 1) / a.nsplit));
+  }
+};
+
+// Where partial sums of split items lie: dk (0) or dv (1) of `split`, rows of Hkv HD
+template <int HD>
+__device__ __forceinline__ float* dkv_part(const RangeArgs& a, int split, int which, int b, int kvh) {
+  return a.part + (((int64_t)split * 2 + which) * a.B + b) * a.Sk * a.Hkv * HD + kvh * HD;
+}
+
+// dk and dv of one key again over the item's iterations, touching only the queries that see it
+template <int HD>
+__device__ __forceinline__ void dkv_row_again(const RangeArgs& a, const KeyItem& it_, int key) {
+  const int lane = threadIdx.x % 64, group = a.Hq / a.Hkv, b = it_.b;
+  const bf16* k = rows_of<bf16>(a.k, b, it_.kvh) + (int64_t)key * a.k.row;
+  const bf16* v = rows_of<bf16>(a.v, b, it_.kvh) + (int64_t)key * a.v.row;
+  const CapScale c(a);
+  float dk[HD / 64], dv[HD / 64];
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) dk[x] = dv[x] = 0.f;
+  for (int it = it_.it0; it < it_.nit; ++it) {
+    const int h = it_.kvh * group + it / it_.tiles, q0 = it_.qlo + it % it_.tiles * KB;
+    const int i = min(q0 + lane, it_.qhi - 1);
+    const bool on = q0 + lane < it_.qhi && sees(seen_keys_kept(a, (int64_t)b * a.Sq + i), key);
+    const bf16* q = rows_of<bf16>(a.q, b, h);
+    const bf16* d = rows_of<bf16>(a.dout, b, h);
+    const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
+    const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
+    float g;
+    const float p = fast_exp2(score2(row_dot<HD>(q + (int64_t)i * a.q.row, k), a, c, slope2, (float)(position(a, b, i) - key), g) +
+                              a.nlse2[sidx]);
+    const float ds = p * (row_dot<HD>(d + (int64_t)i * a.dout.row, v) - a.delta[sidx]) * g;
+    for (uint64_t left = __ballot(on); left; left &= left - 1) {
+      const int t = __builtin_ctzll(left);
+      const float wp = __shfl(p, t, 64), wd = __shfl(ds, t, 64);
+#pragma unroll
+      for (int x = 0; x < HD / 64; ++x) {
+        dv[x] += wp * (float)d[(int64_t)(q0 + t) * a.dout.row + 64 * x + lane];
+        dk[x] += wd * (float)q[(int64_t)(q0 + t) * a.q.row + 64 * x + lane];
+      }
+    }
+  }
+  if (a.nsplit > 1) {
+    const int64_t row = (int64_t)key * a.Hkv * HD;
+#pragma unroll
+    for (int x = 0; x < HD / 64; ++x) {
+      dkv_part<HD>(a, it_.split, 0, b, it_.kvh)[row + 64 * x + lane] = dk[x];
+      dkv_part<HD>(a, it_.split, 1, b, it_.kvh)[row + 64 * x + lane] = dv[x];
+    }
+    return;
+  }
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) dk[x] *= a.scale;
+  unrotate<HD>(dk, a, key);
+#pragma unroll
+  for (int x = 0; x < HD / 64; ++x) {
+    (rows_out<bf16>(a.dk, b, it_.kvh) + (int64_t)key * a.dk.row)[64 * x + lane] = (bf16)dk[x];
+    (rows_out<bf16>(a.dv, b, it_.kvh) + (int64_t)key * a.dv.row)[64 * x + lane] = (bf16)dv[x];
+  }
+}
+
+// The item's dk and dv leave, and the keys whose sums are not finite are computed again
+template <int HD>
+__device__ __forceinline__ void dkv_store(const RangeArgs& a, const KeyItem& item, const f32x16 (&dk)[HD / 32],
+                                          const f32x16 (&dv)[HD / 32], float* stage) {
+  const int wave = threadIdx.x / 64, key0 = item.kb * QB + wave * 32;
+  uint64_t bad = __ballot(key0 + (int)(threadIdx.x % 32) < a.Sk && !(all_finite(dk) && all_finite(dv)));
+  if (a.nsplit > 1) {
+    store_partial_from_t<HD>(stage, dk, dkv_part<HD>(a, item.split, 0, item.b, item.kvh), a.Hkv * HD, item.kb * QB, a.Sk);
+    store_partial_from_t<HD>(stage, dv, dkv_part<HD>(a, item.split, 1, item.b, item.kvh), a.Hkv * HD, item.kb * QB, a.Sk);
+  } else {
+    store_rows_from_t<HD>(stage, dk, a.scale, rows_out<bf16>(a.dk, item.b, item.kvh), a.dk.row, item.kb * QB, a.Sk,
+                          a.rope_cos, a.rope_sin);
+    store_rows_from_t<HD>(stage, dv, 1.0f, rows_out<bf16>(a.dv, item.b, item.kvh), a.dv.row, item.kb * QB, a.Sk);
+  }
+  if (__syncthreads_or(bad != 0)) {  // behind every wave's stores of these rows
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    for (; bad; bad &= bad - 1) dkv_row_again<HD>(a, item, key0 + __builtin_ctzll(bad));
+  }
+}
+
+template <int HD, bool CAP, bool BIAS>
+__device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h, int b, unsigned char* __restrict__ smem) {
+  using L = Lds<HD>;
+  using TT = DmaRowTile<HD>;
+  constexpr int KS = HD / 16, DT = HD / 32, NS = L::NS;
+  bf16* ring = reinterpret_cast<bf16*>(smem);  // [NS][K tile | V tile], swizzled
+  const int kvh = h / (a.Hq / a.Hkv);
+  const bf16* kbase = rows_of<bf16>(a.k, b, kvh);
+  const bf16* vbase = rows_of<bf16>(a.v, b, kvh);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+  const int myq = qb * QB + wave * 32 + col, i = min(myq, a.Sq - 1);
+  const bool valid = myq < a.Sq;
+  const int64_t row0 = (int64_t)b * a.Sq;
+  const int2 mask = seen_keys_kept(a, row0 + i);
+  const WaveKeys wk(mask, valid);
+  int blo, bhi;  // the block's keys
+  {
+    const int x = qb * QB + lane, y = x + 64;
+    const int2 sx = x < a.Sq ? seen_keys_kept(a, row0 + x) : make_int2(0, 0);
+    const int2 sy = y < a.Sq ? seen_keys_kept(a, row0 + y) : make_int2(0, 0);
+    bhi = wave_max_i(max(sx.y, sy.y));
+    blo = wave_min_i(min(sx.y > 0 ? sx.x : INT32_MAX, sy.y > 0 ? sy.x : INT32_MAX));
+    if (bhi == 0) blo = 0;
+  }
+  const int ntile = (bhi - blo + KB - 1) / KB;
+  auto issue = [&](int t) {
+    bf16* st = ring + (t % NS) * 2 * L::TSZ;
+    TT::issue(kbase, a.k.row, blo + t * KB, bhi, lds_addr(st));
+    TT::issue(vbase, a.v.row, blo + t * KB, bhi, lds_addr(st + L::TSZ));
+  };
+  bf16x8 qf[KS], df[KS];
+  {
+    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
+    const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+      df[ks] = *reinterpret_cast<const bf16x8*>(d + ks * 16);
+    }
+  }
+  const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
+  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
+  const CapScale cs(a);
+  float slope2 = 0.f;
+  int64_t pos = 0;
+  if constexpr (BIAS) {
+    slope2 = a.slopes[h] * LOG2E;
+    pos = position(a, b, i);
+  }
+  wait_vm_lds<0>();  // register loads done before the ring starts
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < ntile) issue(s);
+  f32x16 dq[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dq[dt][e] = 0.f;
+  for (int kt = 0; kt < ntile; ++kt) {
+    ring_wait<NS, 2 * TT::PER>(kt + 1 < ntile);
+    block_barrier();
+    if (kt + NS - 1 < ntile) issue(kt + NS - 1);
+    const bf16* Ks = ring + (kt % NS) * 2 * L::TSZ;
+    const bf16* Vs = Ks + L::TSZ;
+    const int key0 = blo + kt * KB;
+    if (key0 < wk.hi && key0 + KB > wk.lo) {
+      // as in attention_mfma.hip: S and dP of both 32-key sub-tiles, then the softmax and the dQ products of each
+      f32x16 s[2], dp[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { s[t][e] = 0.f; dp[t][e] = 0.f; }
+      if constexpr (HD == 128) {
+        bf16x8 fk[2][2], fv[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          fk[0][t] = frag_rows<HD>(Ks, t * 32, 0);
+          fv[0][t] = frag_rows<HD>(Vs, t * 32, 0);
+        }
+        static_for<KS>([&](auto KSI) {
+          constexpr int ks = KSI, c = ks & 1;
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (ks + 1 < KS) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              fk[c ^ 1][t] = frag_rows<HD>(Ks, t * 32, (ks + 1) * 16);
+              fv[c ^ 1][t] = frag_rows<HD>(Vs, t * 32, (ks + 1) * 16);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], s[t], 0, 0, 0);
+            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[c][t], df[ks], dp[t], 0, 0, 0);
+          }
+          if constexpr (ks + 1 < KS) {
+            static_for<4>([&](auto) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
+              __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
+            });
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ks, t * 32, ks * 16), qf[ks], s[t], 0, 0, 0);
+            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Vs, t * 32, ks * 16), df[ks], dp[t], 0, 0, 0);
+          }
+      }
+      if constexpr (CAP) tanh_scores(s, cs);
+      const float base_far = BIAS ? (float)(pos - key0 - 4 * half) : 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        constexpr int NC = 2 * DT, RA = 3;
+        bf16x8 fc[RA + 1];
+        if constexpr (HD == 128) {
+          static_for<RA>([&](auto QI) {
+            constexpr int q = QI;
+            fc[q] = frag_cols<HD>(Ks, (q % DT) * 32, t * 32 + (q / DT) * 16);
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          dp[t][e] = grad_pair<CAP, BIAS>(s[t][e], dp[t][e], nl, dl, cs, slope2, base_far - (float)(t * 32 + 8 * (e / 4) + e % 4)).ds;
+        if (!wk.whole(key0 + t * 32, key0 + t * 32 + 32)) {
+          const uint32_t first = (uint32_t)(key0 + t * 32 + 4 * half - mask.x), len = (uint32_t)(mask.y - mask.x);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (first + (uint32_t)(8 * (e / 4) + e % 4) >= len) dp[t][e] = 0.f;
+        }
+        if constexpr (HD == 128) {
+          const bf16x8 b0 = acc_rows_to_b<0>(dp[t]), b1 = acc_rows_to_b<8>(dp[t]);
+          static_for<NC>([&](auto QI) {
+            constexpr int q = QI, g2 = q / DT, dt = q % DT;
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (q + RA < NC)
+              fc[(q + RA) % (RA + 1)] = frag_cols<HD>(Ks, ((q + RA) % DT) * 32, t * 32 + ((q + RA) / DT) * 16);
+            dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[q % (RA + 1)], g2 ? b1 : b0, dq[dt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        } else {
+#pragma unroll
+          for (int g2 = 0; g2 < 2; ++g2) {
+            const bf16x8 bop = g2 ? acc_rows_to_b<8>(dp[t]) : acc_rows_to_b<0>(dp[t]);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+              dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Ks, dt * 32, t * 32 + g2 * 16), bop, dq[dt], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+  block_barrier();  // every wave is done with the last tile: the ring becomes the output staging
+  uint64_t bad = __ballot(valid && !all_finite(dq));
+  store_rows_from_t<HD>(reinterpret_cast<float*>(smem), dq, a.scale, rows_out<bf16>(a.dq, b, h), a.dq.row, qb * QB, a.Sq,
+                        a.rope_cos, a.rope_sin);
+  if (__syncthreads_or(bad != 0)) {
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    for (; bad; bad &= bad - 1) dq_row_again<HD>(a, b, h, qb * QB + wave * 32 + __builtin_ctzll(bad));
+  }
+}
+
+// A stage of streamed query rows: Q and dO tiles, then nlse2, delta, seen_lo and seen_len of the rows
+template <int HD>
+struct QueryStage {
+  static constexpr int TSZ = KB * HD, SZ = 2 * TSZ + 8 * KB;  // bf16 elements
+  static constexpr size_t bytes(int stages) { return std::max((size_t)stages * SZ * 2, Lds<HD>::out_bytes); }
+};
+
+// dK and dV of head dimension 64
+template <int HD, bool CAP, bool BIAS>
+__device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyItem& item, unsigned char* __restrict__ smem) {
+  using TT = DmaRowTile<HD>;
+  using Q = QueryStage<HD>;
+  constexpr int KS = HD / 16, DT = HD / 32, NS = ring_stages<HD>();
+  bf16* ring = reinterpret_cast<bf16*>(smem);
+  const int group = a.Hq / a.Hkv, b = item.b;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+  const int k0 = item.kb * QB + wave * 32, mykey = k0 + col, kc = min(mykey, a.Sk - 1);
+  const int wu = __builtin_amdgcn_readfirstlane(wave);
+  // each wave loads one row vector per stage
+  auto issue = [&](int it) {
+    const int h = item.kvh * group + it / item.tiles, q0 = item.qlo + it % item.tiles * KB;
+    bf16* st = ring + (it % NS) * Q::SZ;
+    TT::issue(rows_of<bf16>(a.q, b, h), a.q.row, q0, item.qhi, lds_addr(st));
+    TT::issue(rows_of<bf16>(a.dout, b, h), a.dout.row, q0, item.qhi, lds_addr(st + Q::TSZ));
+    const void* v = wu == 0 ? (const void*)(a.nlse2 + ((int64_t)b * a.Hq + h) * a.Sq)
+                  : wu == 1 ? (const void*)(a.delta + ((int64_t)b * a.Hq + h) * a.Sq)
+                  : wu == 2 ? (const void*)(a.seen_lo + (int64_t)b * a.Sq) : (const void*)(a.seen_len + (int64_t)b * a.Sq);
+    dma4(v, 4u * (uint32_t)min(q0 + lane, item.qhi - 1), lds_addr(st + 2 * Q::TSZ) + (uint32_t)wu * KB * 4u);
+  };
+  bf16x8 kf[KS], vf[KS];
+  {
+    const bf16* k = rows_of<bf16>(a.k, b, item.kvh) + (int64_t)kc * a.k.row + 8 * half;
+    const bf16* v = rows_of<bf16>(a.v, b, item.kvh) + (int64_t)kc * a.v.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[ks] = *reinterpret_cast<const bf16x8*>(k + ks * 16);
+      vf[ks] = *reinterpret_cast<const bf16x8*>(v + ks * 16);
+    }
+  }
+  wait_vm_lds<0>();
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (item.it0 + s < item.nit) issue(item.it0 + s);
+  const CapScale cs(a);
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { dk[dt][e] = 0.f; dv[dt][e] = 0.f; }
+  for (int it = item.it0; it < item.nit; ++it) {
+    ring_wait<NS, 2 * TT::PER + 1>(it + 1 < item.nit);
+    block_barrier();
+    if (it + NS - 1 < item.nit) issue(it + NS - 1);
+    const bf16* Qs = ring + (it % NS) * Q::SZ;
+    const bf16* Ds = Qs + Q::TSZ;
+    const float* Ls = reinterpret_cast<const float*>(Qs + 2 * Q::TSZ);
+    const int q0 = item.qlo + it % item.tiles * KB;
+    float slope2 = 0.f;
+    int64_t far0 = 0;
+    if constexpr (BIAS) {
+      slope2 = a.slopes[item.kvh * group + it / item.tiles] * LOG2E;
+      far0 = position(a, b, q0) - mykey + 4 * half;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s[1], dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { s[0][e] = 0.f; dp[e] = 0.f; }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Qs, t * 32, ks * 16), kf[ks], s[0], 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ds, t * 32, ks * 16), vf[ks], dp, 0, 0, 0);
+      }
+      if constexpr (CAP) tanh_scores(s, cs);
+      const float base_far = (float)far0;
+      const int left = item.qhi - q0 - t * 32 - 4 * half;  // accumulator rows of this lane that exist
+#pragma unroll
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const float* r = Ls + t * 32 + 8 * e4 + 4 * half;
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(r), d4 = *reinterpret_cast<const f32x4*>(r + KB);
+        const u32x4 lo4 = *reinterpret_cast<const u32x4*>(r + 2 * KB), n4 = *reinterpret_cast<const u32x4*>(r + 3 * KB);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int e = 4 * e4 + j;
+          const Pair w = grad_pair<CAP, BIAS>(s[0][e], dp[e], l4[j], d4[j], cs, slope2, base_far + (float)(t * 32 + 8 * e4 + j));
+          const bool on = (uint32_t)mykey - lo4[j] < n4[j] && 8 * e4 + j < left;
+          s[0][e] = on ? w.p : 0.f;
+          dp[e] = on ? w.ds : 0.f;
+        }
+      }
+#pragma unroll
+      for (int g2 = 0; g2 < 2; ++g2) {
+        const bf16x8 pb = g2 ? acc_rows_to_b<8>(s[0]) : acc_rows_to_b<0>(s[0]);
+        const bf16x8 sb = g2 ? acc_rows_to_b<8>(dp) : acc_rows_to_b<0>(dp);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Ds, dt * 32, t * 32 + g2 * 16), pb, dv[dt], 0, 0, 0);
+          dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Qs, dt * 32, t * 32 + g2 * 16), sb, dk[dt], 0, 0, 0);
+        }
+      }
+    }
+  }
+  block_barrier();
+  dkv_store<HD>(a, item, dk, dv, reinterpret_cast<float*>(smem));
+}
+
+// dK and dV of head dimension 128, pipelined over 32-query tiles as flash_bwd_dkv128
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const KeyItem& item, unsigned char* __restrict__ smem) {
+  constexpr int HD = 128, KS = 8, DT = 4, NS = 3;
+  using TT = DmaRowTile<HD>;
+  using Q = QueryStage<HD>;
+  bf16* ring = reinterpret_cast<bf16*>(smem);
+  const int group = a.Hq / a.Hkv, b = item.b;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+  const int mykey = item.kb * QB + wave * 32 + col, kc = min(mykey, a.Sk - 1);
+  const int wu = __builtin_amdgcn_readfirstlane(wave);
+  // The tile being loaded (head h, queries q0 .. of 64), its stage slot, and the ranges of its rows.  Rows past
+  // the last query that sees a key arrive as zeros, and see none.
+  struct Fetch {
+    int h, q0, slot;
+    u32x4 q, d, r;
+    uint32_t lds;
+  } f;
+  auto ranges = [&] {
+    const bf16 *qh = rows_of<bf16>(a.q, b, f.h), *dh = rows_of<bf16>(a.dout, b, f.h);
+    f.q = buffer_range(qh + (int64_t)f.q0 * a.q.row, qh + (int64_t)(item.qhi - 1) * a.q.row + HD);
+    f.d = buffer_range(dh + (int64_t)f.q0 * a.dout.row, dh + (int64_t)(item.qhi - 1) * a.dout.row + HD);
+    const int64_t rows = wu < 2 ? ((int64_t)b * a.Hq + f.h) * a.Sq : (int64_t)b * a.Sq;
+    const float* v = (wu == 0 ? a.nlse2 : wu == 1 ? a.delta : wu == 2 ? (const float*)a.seen_lo : (const float*)a.seen_len) + rows;
+    f.r = buffer_range(v + f.q0, v + item.qhi);
+    f.lds = lds_addr(ring + f.slot * Q::SZ) + (uint32_t)wu * 1024u;
+  };
+  auto next_tile = [&] {  // past the item's last tile it wraps: loaded again, into a stage nobody reads
+    f.q0 += KB;
+    if (f.q0 >= item.qhi) {
+      f.q0 = item.qlo;
+      f.h = f.h + 1 < (item.kvh + 1) * group ? f.h + 1 : item.kvh * group;
+    }
+    f.slot = f.slot + 1 < NS ? f.slot + 1 : 0;
+    ranges();
+  };
+  // load k of the 2 PER + 1 of a stage
+  auto fetch = [&](auto K_) {
+    constexpr int k = K_;
+    if constexpr (k < TT::PER) TT::issue_range(f.q, k, a.q.row, f.lds);
+    else if constexpr (k < 2 * TT::PER) TT::issue_range(f.d, k - TT::PER, a.dout.row, f.lds + Q::TSZ * 2);
+    else dma4_range(f.r, 4u * (uint32_t)lane, lds_addr(ring + f.slot * Q::SZ + 2 * Q::TSZ) + (uint32_t)wu * KB * 4u);
+  };
+  static_assert(2 * TT::PER + 1 <= 2 * KS, "a load per group of the two steps");
+  bf16x8 kf[KS], vf[KS];
+  {
+    const bf16* k = rows_of<bf16>(a.k, b, item.kvh) + (int64_t)kc * a.k.row + 8 * half;
+    const bf16* v = rows_of<bf16>(a.v, b, item.kvh) + (int64_t)kc * a.v.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[ks] = *reinterpret_cast<const bf16x8*>(k + ks * 16);
+      vf[ks] = *reinterpret_cast<const bf16x8*>(v + ks * 16);
+    }
+  }
+  wait_vm_lds<0>();
+  const CapScale cs(a);
+  const int64_t first = BIAS ? position(a, b, 0) - mykey + 4 * half : 0;
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { dk[dt][e] = 0.f; dv[dt][e] = 0.f; }
+  f32x16 s[2], dp[2];         // S and dP of the two tiles of a stage; after the softmax P and dS
+  bf16x8 pb[2][2], sb[2][2];  // P and dS as operands, two 16-query halves each
+
+  // One step, as there: the loads of a stage (FE), S and dP of tile T of the stage at `rows` (SC), the softmax of
+  // the other tile, whose first query is sq0 and head's slope slope2, with the row vectors at `stats` (SM; with CAP on its tanh_scores), and dV and dK
+  // of tile T of the stage at `cols` (PV).
+  auto step = [&](auto T_, auto SC_, auto SM_, auto PV_, auto FE_, const bf16* rows, const bf16* stats, int sq0,
+                  float slope2, const bf16* cols) {
+    constexpr int T = T_, U = T ^ 1;
+    constexpr bool SC = SC_, SM = SM_, PV = PV_, FE = FE_;
+    const bf16 *Qr = rows, *Dr = rows + Q::TSZ, *Qc = cols, *Dc = cols + Q::TSZ;
+    const float* Ls = reinterpret_cast<const float*>(stats + 2 * Q::TSZ) + U * 32 + 4 * half;
+    const float base_far = BIAS && SM ? (float)(first + sq0) : 0.f;
+    auto cfrag = [&](auto QI) {
+      constexpr int q = QI;
+      return frag_cols<HD>(q % 2 ? Qc : Dc, ((q / 2) % DT) * 32, T * 32 + (q / 8) * 16);
+    };
+    bf16x8 fq[2], fd[2], fc[4];
+    f32x4 l4[2], d4[2];
+    u32x4 lo4[2], n4[2];
+    auto stat = [&](auto I) {
+      constexpr int n = I;
+      l4[n % 2] = *reinterpret_cast<const f32x4*>(Ls + 8 * n);
+      d4[n % 2] = *reinterpret_cast<const f32x4*>(Ls + KB + 8 * n);
+      lo4[n % 2] = *reinterpret_cast<const u32x4*>(Ls + 2 * KB + 8 * n);
+      n4[n % 2] = *reinterpret_cast<const u32x4*>(Ls + 3 * KB + 8 * n);
+    };
+    if constexpr (SM) stat(std::integral_constant<int, 0>{});
+    if constexpr (SC) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { s[T][e] = 0.f; dp[T][e] = 0.f; }
+      fq[0] = frag_rows<HD>(Qr, T * 32, 0);
+      fd[0] = frag_rows<HD>(Dr, T * 32, 0);
+    }
+    if constexpr (PV) {
+      fc[0] = cfrag(std::integral_constant<int, 0>{});
+      fc[1] = cfrag(std::integral_constant<int, 1>{});
+    }
+    static_for<KS>([&](auto G) {
+      constexpr int g = G, c = g & 1;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (FE && T * KS + g < 2 * TT::PER + 1) fetch(std::integral_constant<int, T * KS + g>{});
+      if constexpr (SC && g + 1 < KS) {
+        fq[c ^ 1] = frag_rows<HD>(Qr, T * 32, (g + 1) * 16);
+        fd[c ^ 1] = frag_rows<HD>(Dr, T * 32, (g + 1) * 16);
+      }
+      if constexpr (PV && g + 1 < KS) {
+        fc[2 * (c ^ 1)] = cfrag(std::integral_constant<int, (2 * g + 2) % 16>{});
+        fc[2 * (c ^ 1) + 1] = cfrag(std::integral_constant<int, (2 * g + 3) % 16>{});
+      }
+      if constexpr (SM && g % 2 == 1 && g + 1 < KS) stat(std::integral_constant<int, (g + 1) / 2>{});
+      // four MFMAs, each followed by a quarter of the vector work
+      constexpr int e0 = 2 * g, e1 = e0 + 1, lb = g / 2 % 2;
+      float x0, x1, y0, y1;
+      if constexpr (SC) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[c], kf[g], s[T], 0, 0, 0);
+      if constexpr (SM) {
+        x0 = __builtin_fmaf(s[U][e0], CAP ? cs.out : cs.sl2, l4[lb][e0 % 4]);
+        x1 = __builtin_fmaf(s[U][e1], CAP ? cs.out : cs.sl2, l4[lb][e1 % 4]);
+        if constexpr (BIAS) {
+          x0 = __builtin_fmaf(-slope2, fabsf(base_far + (float)(8 * (e0 / 4) + e0 % 4)), x0);
+          x1 = __builtin_fmaf(-slope2, fabsf(base_far + (float)(8 * (e1 / 4) + e1 % 4)), x1);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (PV) mfma_acc<!SC>(dv[g % DT], fc[2 * c], pb[T][g / DT]);
+      if constexpr (SM) {
+        x0 = fast_exp2(x0);
+        x1 = fast_exp2(x1);
+        pin(x0, x1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (SC) dp[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[c], vf[g], dp[T], 0, 0, 0);
+      if constexpr (SM) {
+        y0 = dp[U][e0] - d4[lb][e0 % 4];
+        y1 = dp[U][e1] - d4[lb][e1 % 4];
+        if constexpr (CAP) {
+          y0 *= __builtin_fmaf(-s[U][e0], s[U][e0], 1.0f);
+          y1 *= __builtin_fmaf(-s[U][e1], s[U][e1], 1.0f);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (PV) mfma_acc<!SC>(dk[g % DT], fc[2 * c + 1], sb[T][g / DT]);
+      if constexpr (SM) {
+        const bool on0 = (uint32_t)mykey - lo4[lb][e0 % 4] < n4[lb][e0 % 4], on1 = (uint32_t)mykey - lo4[lb][e1 % 4] < n4[lb][e1 % 4];
+        s[U][e0] = on0 ? x0 : 0.f;
+        s[U][e1] = on1 ? x1 : 0.f;
+        dp[U][e0] = on0 ? x0 * y0 : 0.f;
+        dp[U][e1] = on1 ? x1 * y1 : 0.f;
+        if constexpr (g == 3) { pb[U][0] = acc_rows_to_b<0>(s[U]); sb[U][0] = acc_rows_to_b<0>(dp[U]); }
+        if constexpr (g == 7) { pb[U][1] = acc_rows_to_b<8>(s[U]); sb[U][1] = acc_rows_to_b<8>(dp[U]); }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  constexpr std::integral_constant<int, 0> t0{};
+  constexpr std::integral_constant<int, 1> t1{};
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  auto soft = [&](auto T_, auto SC_, auto PV_, auto FE_, const bf16* rows, const bf16* stats, int sq0, float slope2, const bf16* cols) {
+    if constexpr (CAP) {
+      f32x16(&u)[1] = reinterpret_cast<f32x16(&)[1]>(s[T_ ^ 1]);
+      tanh_scores(u, cs);
+    }
+    step(T_, SC_, std::true_type{}, PV_, FE_, rows, stats, sq0, slope2, cols);
+  };
+  auto arrive = [&] {
+    wait_vm_lds<0>();
+    block_barrier();  // every thread's loads of the stage are in; every wave is done with the last iteration
+  };
+  auto slope_of = [&](int h) { return BIAS ? a.slopes[h] * LOG2E : 0.f; };
+  if (item.it0 < item.nit) {
+    f.h = item.kvh * group + item.it0 / item.tiles;
+    f.q0 = item.qlo + item.it0 % item.tiles * KB;
+    f.slot = 0;
+    ranges();
+    static_for<2 * TT::PER + 1>(fetch);
+    const bf16 *cur = ring, *prev;
+    int qc = f.q0, qp;  // first queries of the stages cur and prev, and the slopes of their heads
+    float mc = slope_of(f.h), mp;
+    auto turn = [&] {   // the stage just loaded becomes cur
+      prev = cur;
+      qp = qc;
+      mp = mc;
+      cur = ring + f.slot * Q::SZ;
+      qc = f.q0;
+      mc = slope_of(f.h);
+    };
+    arrive();
+    next_tile();
+    step(t0, yes, no, no, yes, cur, cur, 0, 0.f, cur);
+    soft(t1, yes, no, yes, cur, cur, qc, mc, cur);
+    for (int it = item.it0 + 1; it < item.nit; ++it) {
+      turn();
+      arrive();
+      next_tile();  // into the stage before prev
+      soft(t0, yes, yes, yes, cur, prev, qp + 32, mp, prev);
+      soft(t1, yes, yes, yes, cur, cur, qc, mc, prev);
+      acc_settled(dk, dv);  // register copies the compiler may place at the loop's end
+    }
+    acc_settled(dk, dv);
+    soft(t0, no, yes, no, cur, cur, qc + 32, mc, cur);
+    step(t1, no, no, yes, no, cur, cur, 0, 0.f, cur);
+    acc_settled(dk, dv);
+    wait_vm_lds<0>();  // the last, unread loads: the ring becomes the output staging
+  }
+  block_barrier();
+  dkv_store<HD>(a, item, dk, dv, reinterpret_cast<float*>(smem));
+}
+
+template <bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) range_flash_dq128(RangeArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int nqb = (a.Sq + QB - 1) / QB;
+  int unit, idx;  // unit: (sequence, query head)
+  xcd_item(blockIdx.x, nqb * a.Hq * a.B, nqb, unit, idx);
+  range_dq_block<128, CAP, BIAS>(a, nqb - 1 - idx, unit % a.Hq, unit / a.Hq, smem);
+}
+
+template <bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT) range_flash_dkv128(RangeArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int nkb = (a.Sk + QB - 1) / QB;
+  int unit, idx;  // unit: (sequence, key/value head)
+  xcd_item(blockIdx.x, nkb * a.nsplit * a.Hkv * a.B, nkb * a.nsplit, unit, idx);
+  const KeyItem item(a, idx / a.nsplit, idx % a.nsplit, unit % a.Hkv, unit / a.Hkv);
+  range_dkv128_block<CAP, BIAS>(a, item, smem);
+}
+
+// dQ and dK/dV items of head dimension 64 in one launch: a unit is one (sequence, key/value head)
+template <bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) range_flash_bwd64(RangeArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int nkb = (a.Sk + QB - 1) / QB, nqb = (a.Sq + QB - 1) / QB, group = a.Hq / a.Hkv;
+  const int per_unit = nkb * a.nsplit + nqb * group;
+  int unit, idx;
+  xcd_item(blockIdx.x, per_unit * a.Hkv * a.B, per_unit, unit, idx);
+  const int kvh = unit % a.Hkv, b = unit / a.Hkv;
+  if (idx < nkb * a.nsplit) {
+    const KeyItem item(a, idx / a.nsplit, idx % a.nsplit, kvh, b);
+    range_dkv_block<64, CAP, BIAS>(a, item, smem);
+  } else {
+    idx -= nkb * a.nsplit;
+    range_dq_block<64, CAP, BIAS>(a, nqb - 1 - idx / group, kvh * group + idx % group, b, smem);
+  }
+}
+
+// dk and dv of split items: the partial sums added in order, 8 columns per thread
+template <int HD>
+__global__ void __launch_bounds__(256) range_dkv_join(RangeArgs a) {
+  constexpr int HH = HD / 2;
+  const int kvd = a.Hkv * HD;
+  const int64_t n = (int64_t)a.B * a.Sk * kvd, c = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (c >= 2 * n) return;
+  const bool isv = c >= n;
+  const int64_t e = isv ? c - n : c, row = e / kvd;
+  const int kvh = (int)(e % kvd) / HD, d = (int)(e % HD), b = (int)(row / a.Sk), key = (int)(row % a.Sk);
+  auto sum = [&](int64_t o, float* v) {  // elements o .. o + 7 of every share
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = 0.f;
+    for (int s = 0; s < a.nsplit; ++s) {
+      const float* p = a.part + 2 * n * s + o;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { v[q] += lo[q]; v[q + 4] += hi[q]; }
+    }
+  };
+  float v[8];
+  sum(c, v);
+  if (!isv) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= a.scale;
+    if (a.rope_cos) {
+      const bool first = d < HH;
+      float p[8];
+      sum(first ? c + HH : c - HH, p);
+      const int64_t t = (int64_t)key * HH + d % HH;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float y = p[q] * a.scale, cs = a.rope_cos[t + q], sn = a.rope_sin[t + q];
+        v[q] = first ? v[q] * cs + y * sn : v[q] * cs - y * sn;
+      }
+    }
+  }
+  bf16x8 ov;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) ov[q] = (bf16)v[q];
+  const HeadRows& out = isv ? a.dv : a.dk;
+  *reinterpret_cast<bf16x8*>(rows_out<bf16>(out, b, kvh) + (int64_t)key * out.row + d) = ov;
+}
+
+template <int HD>
+constexpr size_t range_fwd_lds() {
+  const size_t out = (size_t)QB * (HD + 4) * 4 + QB * 4;
+  return std::max(Lds<HD>::NS * Lds<HD>::kv_stage, out);
+}
+
+template <typename K>
+void set_lds(K kernel, size_t bytes) {
+  (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <int HD, bool HILO, bool CAP, bool BIAS>
+void fwd_launch(const RangeArgs& a, int pack, unsigned blocks, hipStream_t st) {
+  static const bool once = (set_lds(range_flash_fwd<HD, HILO, CAP, BIAS>, range_fwd_lds<HD>()), true);
+  (void)once;
+  range_flash_fwd<HD, HILO, CAP, BIAS><<<blocks, NT, range_fwd_lds<HD>(), st>>>(a, pack);
+}
+
+// f(std::bool_constant<x>, std::bool_constant<y>, std::bool_constant<z>)
+template <typename F>
+void with_flags(bool x, bool y, bool z, F&& f) {
+  auto third = [&](auto X, auto Y) { if (z) f(X, Y, std::true_type{}); else f(X, Y, std::false_type{}); };
+  auto second = [&](auto X) { if (y) third(X, std::true_type{}); else third(X, std::false_type{}); };
+  if (x) second(std::true_type{}); else second(std::false_type{});
+}
+
+}  // namespace
+
+// The query heads of a key/value head share a block's rows where that makes fewer blocks (few queries)
+int range_mfma_pack(const RangeArgs& a) {
+  const int group = a.Hq / a.Hkv;
+  return cdiv((int64_t)a.Sq * group, QB) < group * cdiv(a.Sq, QB) ? group : 1;
+}
+
+int64_t range_mfma_items(const RangeArgs& a) {
+  const int pack = range_mfma_pack(a);
+  return cdiv((int64_t)a.Sq * pack, QB) * (a.Hq / pack) * a.B;
+}
+
+void range_mfma_fwd(const RangeArgs& a, hipStream_t st) {
+  const unsigned blocks = (unsigned)(range_mfma_items(a) * a.nsplit);
+  const int pack = range_mfma_pack(a);
+  with_flags(a.o32 != nullptr, a.cap > 0.f, a.slopes != nullptr, [&](auto hilo, auto cap, auto bias) {
+    if (a.hd == 64) fwd_launch<64, hilo.value, cap.value, bias.value>(a, pack, blocks, st);
+    else fwd_launch<128, hilo.value, cap.value, bias.value>(a, pack, blocks, st);
+  });
+}
+
+int range_mfma_keys() { return QB; }
+
+// As attention_dkv_splits: few key blocks are split over their queries' tiles, the longest by the causal count
+int range_mfma_dkv_splits(const RangeArgs& a) {
+  const int64_t items = cdiv(a.Sk, QB) * a.Hkv * a.B, tiles = (int64_t)(a.Hq / a.Hkv) * cdiv(a.Sq, KB);
+  if (items == 0) return 1;
+  const int64_t most = a.hd == 64 || tiles >= 140 || (tiles >= 48 && 256 % items == 0) ? 512 : 256;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({8, cdiv(most, items), tiles / 8}));
+}
+
+void range_mfma_bwd(const RangeArgs& a, hipStream_t st) {
+  const int64_t nkb = cdiv(a.Sk, QB) * a.nsplit * a.Hkv * a.B, nqb = cdiv(a.Sq, QB) * a.Hq * a.B;
+  with_flags(a.cap > 0.f, a.slopes != nullptr, false, [&](auto cap, auto bias, auto) {
+    constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
+    if (a.hd == 64) {
+      constexpr size_t lds = std::max(Lds<64>::dq_bytes(), QueryStage<64>::bytes(ring_stages<64>()));
+      static const bool once = (set_lds(range_flash_bwd64<CAP, BIAS>, lds), true);
+      (void)once;
+      range_flash_bwd64<CAP, BIAS><<<(unsigned)(nkb + nqb), NT, lds, st>>>(a);
+    } else {
+      constexpr size_t lds_kv = QueryStage<128>::bytes(3), lds_q = Lds<128>::dq_bytes();
+      static const bool once = (set_lds(range_flash_dq128<CAP, BIAS>, lds_q), set_lds(range_flash_dkv128<CAP, BIAS>, lds_kv), true);
+      (void)once;
+      if (nqb) range_flash_dq128<CAP, BIAS><<<(unsigned)nqb, NT, lds_q, st>>>(a);
+      if (nkb) range_flash_dkv128<CAP, BIAS><<<(unsigned)nkb, NT, lds_kv, st>>>(a);
+    }
+  });
+  if (a.nsplit > 1) {
+    const unsigned blocks = (unsigned)cdiv(2 * (int64_t)a.B * a.Sk * a.Hkv * a.hd / 8, 256);
+    if (a.hd == 64) range_dkv_join<64><<<blocks, 256, 0, st>>>(a);
+    else range_dkv_join<128><<<blocks, 256, 0, st>>>(a);
+  }
+}

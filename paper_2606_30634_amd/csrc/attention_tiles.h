@@ -268,4 +268,22 @@ struct Lds {
   static constexpr size_t dkv_bytes() { return mx(NS * qd_stage, out_bytes); }
 };
 
+// acc += A B with the accumulator kept in accumulator registers (this file's builtin MFMAs keep theirs
+// in vector registers, which 128 more would overflow).  The compiler does not know the instruction, so
+// its distances are kept here: in the loop operands come from LDS reads (waited for) or vector
+// instructions several MFMAs back, and one accumulator's products are 16 MFMAs apart; COPIED (outside
+// the loop, where the compiler moves accumulators between registers) waits between such a move and the
+// product; and acc_settled() stands between the last products and any other read.
+template <bool COPIED>
+__device__ __forceinline__ void mfma_acc(f32x16& acc, const bf16x8& a, const bf16x8& b) {
+  if constexpr (COPIED) asm volatile("s_nop 4\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void acc_settled(f32x16 (&x)[4], f32x16 (&y)[4]) {
+  asm volatile("s_nop 15\n\ts_nop 15"
+               : "+a"(x[0]), "+a"(x[1]), "+a"(x[2]), "+a"(x[3]), "+a"(y[0]), "+a"(y[1]), "+a"(y[2]), "+a"(y[3]));
+}
+// keeps the computation of two values ahead of this point of the schedule
+__device__ __forceinline__ void pin(float& x, float& y) { asm volatile("" : "+v"(x), "+v"(y)); }
+
 }  // namespace

@@ -231,12 +231,14 @@ struct RangeArgs {
   const int32_t *key_start, *key_end, *q_start;
   const float* slopes;
   float scale, cap;
-  // backward
+  // backward; o (o32 where not null) is read at element b ob + i orow + h oh
   HeadRows dout, dq, dk, dv;
+  int64_t ob, orow, oh;
   const float *rope_cos, *rope_sin;  // as in AttnArgs
   // workspace, laid out by the launchers
   float* delta;      // [B, Hq, Sq]
-  int2* seen;        // [B, Sq]: the keys each query sees (x = y = 0: none)
+  float* nlse2;      // [B, Hq, Sq]: -lse in log2 units, 0 where it is not finite
+  int32_t *seen_lo, *seen_len;  // [B, Sq]: the keys each query sees are seen_lo .. + seen_len - 1
   int2* sees;        // [B, key tiles]: the queries that see any key of a tile lie in [x, y)
   float* part;       // partial sums of split items
   float2* part_ml;   // and their maxima and sums

@@ -318,8 +318,8 @@ size_t attention_backward_workspace_bytes(const attention_params_t* p) {
 }
 
 int attention_backward(const attention_params_t* p, const void* q, const void* k, const void* v, const void* o,
-                       const float* o_f32, const float* lse, const void* dout, const attention_grads_t* g,
-                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+                       const float* lse, const void* dout, const attention_grads_t* g, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
   RangeArgs a;
   if (const char* m = check_attention(p, a)) return bad(m);
   if (!g) return bad("null gradients");
@@ -334,17 +334,19 @@ int attention_backward(const attention_params_t* p, const void* q, const void* k
   if (const char* m = check_rows_of(g->dk, g->dk_strides, nk, bf, a.dk)) return bad(m);
   if (const char* m = check_rows_of(g->dv, g->dv_strides, nk, bf, a.dv)) return bad(m);
   if (nq + nk == 0) return STAGE_OK;
-  if (nq > 0 && (!lse || !(o || o_f32))) return bad("null lse or o");
-  if (off(o, 16) || off(o_f32, 16) || off(lse, 4)) return bad("o and o_f32 must be 16-byte aligned, lse to its type");
+  HeadRows orows{};
+  if (const char* m = check_rows_of(o, g->o_strides, nq, bf && !g->o_is_f32, orows)) return bad(m);
+  if (nq > 0 && !lse) return bad("null lse");
+  if (off(lse, 4)) return bad("lse must be aligned to its type");
   if (!apart(g->dq_strides, a.B, a.Sq, a.Hq, a.hd) || !apart(g->dk_strides, a.B, a.Sk, a.Hkv, a.hd) ||
       !apart(g->dv_strides, a.B, a.Sk, a.Hkv, a.hd))
     return bad("the rows of a gradient overlap");
   const size_t n = (size_t)nq * a.Hq;
-  struct { const void* p; size_t n; } ins[7] = {{q, extent(p->q_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
+  struct { const void* p; size_t n; } ins[6] = {{q, extent(p->q_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
                                                 {k, extent(p->k_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
                                                 {v, extent(p->v_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
                                                 {dout, extent(g->dout_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
-                                                {o, n * a.hd * esz}, {o_f32, n * a.hd * 4}, {lse, n * 4}},
+                                                {o, extent(g->o_strides, a.B, a.Sq, a.Hq, a.hd, g->o_is_f32 ? 4 : esz)}, {lse, n * 4}},
                                       outs[3] = {{g->dq, extent(g->dq_strides, a.B, a.Sq, a.Hq, a.hd, esz)},
                                                  {g->dk, extent(g->dk_strides, a.B, a.Sk, a.Hkv, a.hd, esz)},
                                                  {g->dv, extent(g->dv_strides, a.B, a.Sk, a.Hkv, a.hd, esz)}};
@@ -361,7 +363,9 @@ int attention_backward(const attention_params_t* p, const void* q, const void* k
           !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz))
         return bad("the gradients overlap");
   if (const char* m = check_ws(workspace, workspace_bytes, range_bwd_ws_bytes(bf, a))) return bad(m);
-  a.o = const_cast<void*>(o); a.o32 = const_cast<float*>(o_f32); a.lse = const_cast<float*>(lse);
+  (g->o_is_f32 ? (void*&)a.o32 : a.o) = const_cast<void*>(o);
+  a.ob = orows.batch; a.orow = orows.row; a.oh = orows.head;
+  a.lse = const_cast<float*>(lse);
   launch_range_bwd(bf, a, workspace, (hipStream_t)hip_stream);
   return launched();
 }

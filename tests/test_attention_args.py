@@ -43,7 +43,7 @@ FWD = dict(q=P, k=P, v=P, o=Q, o32=None, lse=R, ws=1 << 42, nb=1 << 40, stream=N
 def test_params_refused(bad):
     _refused(B.attention_forward, _params(**bad), *FWD.values())
     g = _grads()
-    _refused(B.attention_backward, _params(**bad), P, P, P, P, None, P, P, g, 1 << 42, 1 << 40, None)
+    _refused(B.attention_backward, _params(**bad), P, P, P, P, P, P, g, 1 << 42, 1 << 40, None)
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(k=None), dict(v=None), dict(q=P + 8), dict(v=P + 4), dict(o=None), dict(o=Q + 2),
@@ -64,18 +64,18 @@ def test_forward_refuses_o_f32_of_fp32_and_small_workspaces():
 
 
 def _grads(**kw):
-    d = dict(dos=(1280, 256, 64), dqs=(1280, 256, 64), dks=(1152, 128, 64), dvs=(1152, 128, 64), dq=Q, dk=R, dv=R + (1 << 30))
+    d = dict(os=(1280, 256, 64), dos=(1280, 256, 64), dqs=(1280, 256, 64), dks=(1152, 128, 64), dvs=(1152, 128, 64), dq=Q, dk=R, dv=R + (1 << 30), wide=0)
     d.update(kw)
-    for n in ("dos", "dqs", "dks", "dvs"):
+    for n in ("os", "dos", "dqs", "dks", "dvs"):
         d[n] = S3(*d[n])
     return B.AttentionGrads(*d.values())
 
 
-BWD = dict(q=P, k=P, v=P, o=P, o32=None, lse=P, dout=P, g=None, ws=1 << 42, nb=1 << 40, stream=None)
+BWD = dict(q=P, k=P, v=P, o=P, lse=P, dout=P, g=None, ws=1 << 42, nb=1 << 40, stream=None)
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(o=None), dict(lse=None), dict(lse=P + 2), dict(dout=None), dict(dout=P + 8),
-                                 dict(ws=None), dict(nb=64), dict(ws=(1 << 42) + 16), dict(o=P + 8), dict(o32=P + 8),
+                                 dict(ws=None), dict(nb=64), dict(ws=(1 << 42) + 16), dict(o=P + 8), dict(g=dict(os=(1280, 252, 64))), dict(g=dict(os=(1280, 2, 64), wide=1)),
                                  dict(g=dict(dq=None)), dict(g=dict(dk=None)), dict(g=dict(dv=R + 4)), dict(g=dict(dq=P)),
                                  dict(g=dict(dk=P + 256)), dict(g=dict(dk=Q)), dict(g=dict(dv=R)), dict(g=dict(dv=R + 128)),
                                  dict(g=dict(dqs=(1280, 0, 64))), dict(g=dict(dks=(1152, 64, 64))), dict(g=dict(dvs=(0, 128, 64))),

@@ -429,7 +429,7 @@ int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents
  *   cap tanh(x / cap) - slopes[h] |position - j|   (softcap 0: x; slopes NULL: no second term).
  * A query that sees no key has o = 0, lse = -inf and no gradient; what a query does not see has no
  * influence on it, whatever it holds.  Products of bf16 accumulate in fp32; their operands P and dS
- * are rounded to bf16, but where o_f32 is kept the forward takes P in two bf16 parts (16 bits). */
+ * are rounded to bf16, but where o_f32 is kept the forward takes P in three bf16 parts (24 bits). */
 typedef struct {
   int64_t batch, queries, keys;        /* [0, 2^24], [0, 2^30], [0, 2^30]                   */
   int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim 32, 64 or 128    */

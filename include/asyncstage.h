@@ -297,6 +297,28 @@ int grad_norm_flat_noalloc(int64_t n, const void* g, int32_t g_is_bf16, float cl
  * flight per thread - the practical HBM ceiling the update pass's bandwidth is reported against. */
 int hbm_stream_copy(void* dst, const void* src, size_t bytes, void* hip_stream);
 
+/* A variant of the stage's blocks, beside the plain causal ones: attention scores capped by a tanh and lowered by
+ * distance, rows that pack several documents (attention_key_ranges, attention_forward below say what each
+ * is), and dropout on the outputs of a block's two branches before they join the residual stream (dropout_add). */
+typedef struct {
+  float softcap;         /* 0: none                                                                  */
+  const float* slopes;   /* [n_heads] device array or NULL; kept, owned by the caller                */
+  double dropout;        /* p of both branches; a forward without a backward (stage_score_logprob) has none */
+  uint64_t seed, offset; /* dropout_add's: block i of the n-th forward from here takes the offsets
+                            offset + 2 (n_blocks n + i) (attention) and the next one (feed-forward)  */
+  int32_t documents;     /* not 0: every forward takes the documents of its slot                     */
+} stage_variant_t;
+/* Sets (v NULL: takes back) the variant for the forwards from here on and their backwards; no slot may hold a
+ * pending microbatch (STAGE_ESTATE).  workspace: device memory of stage_variant_bytes(), 256-byte aligned, kept
+ * until the variant is replaced.  To continue a run, pass the offset its next forward would have taken. */
+size_t stage_variant_bytes(stage_t* s, const stage_variant_t* v);
+int stage_set_variant(stage_t* s, const stage_variant_t* v, void* workspace, size_t workspace_bytes);
+/* The documents [micro_batch, seq_len] int32 packed in the slot's rows, and their prefixes (uint8 or NULL), for
+ * its forwards until they are set again: attention_key_ranges on the stage stream, read by then.  RoPE positions
+ * run along the row (only their differences count); targets of padding are the caller's (outside the
+ * vocabulary: ignored).  A forward of a slot whose documents were never set is refused (STAGE_ESTATE). */
+int stage_set_documents(stage_t* s, int32_t slot, const int32_t* documents, const uint8_t* prefix);
+
 /* ---------------------------------------------------------------------------------------------
  * Log-probabilities and the losses on them: fine-tuning by rewards or preferences on the stage that
  * otherwise trains on next-token cross-entropy.  A last stage runs them in its own paths

@@ -23,7 +23,8 @@ EXPORTS = ["stage_required_bytes", "stage_init", "stage_num_tensors", "stage_ten
            "head_logprob_workspace_bytes", "head_logprob", "policy_loss_workspace_bytes", "policy_loss",
            "preference_loss_workspace_bytes", "preference_loss", "stage_forward_logprob", "stage_backward_logprob",
            "stage_score_logprob", "attention_key_ranges", "attention_workspace_bytes", "attention_forward",
-           "attention_backward_workspace_bytes", "attention_backward", "dropout_add"]
+           "attention_backward_workspace_bytes", "attention_backward", "dropout_add",
+           "stage_variant_bytes", "stage_set_variant", "stage_set_documents"]
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_UPDATE, PROF_NORM, PROF_OTHER, PROF_NS = range(7)
 
 
@@ -53,6 +54,11 @@ class PreferenceHParams(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("beta", "label_smoothing", "margin")] + [
         (n, C.c_int32) for n in ("kind", "length_normalize")] + [
         (n, C.c_double) for n in ("norm", "grad_scale")]
+
+
+class StageVariant(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("slopes", C.c_void_p), ("dropout", C.c_double), ("seed", C.c_uint64),
+                ("offset", C.c_uint64), ("documents", C.c_int32)]
 
 
 _STRIDES = C.c_int64 * 3
@@ -98,6 +104,9 @@ def _load():
         "stage_forward_logprob": (C.c_int, [vp, i32, i64, vp, vp, vp, C.c_float, vp, vp]),
         "stage_backward_logprob": (C.c_int, [vp, i32, vp, vp, vp, i32]),
         "stage_score_logprob": (C.c_int, [vp, i32, i64, vp, vp, vp, C.c_float, vp, vp]),
+        "stage_variant_bytes": (sz, [vp, C.POINTER(StageVariant)]),
+        "stage_set_variant": (C.c_int, [vp, C.POINTER(StageVariant), vp, sz]),
+        "stage_set_documents": (C.c_int, [vp, i32, vp, vp]),
         "delayed_update": (C.c_int, [vp, i64, C.POINTER(UpdateHParams)]),
         "delayed_update_flat": (C.c_int, [i64, vp, vp, i32, vp, vp, vp, vp, i32, i64,
                                           C.POINTER(UpdateHParams), vp, vp]),
@@ -213,6 +222,18 @@ def stage_backward_logprob(s: int, slot: int, dlogp, dentropy=None, dx_out=None,
 def stage_score_logprob(s: int, slot: int, step: int, tokens, x_in, targets, inv_temperature: float, logp,
                         entropy=None) -> None:
     _call("stage_score_logprob", s, slot, step, tokens, x_in, targets, inv_temperature, logp, entropy)
+
+
+def stage_variant_bytes(s: int, variant: StageVariant) -> int:
+    return LIB.stage_variant_bytes(s, C.byref(variant))
+
+
+def stage_set_variant(s: int, variant, workspace=None, workspace_bytes: int = 0) -> None:
+    _call("stage_set_variant", s, None if variant is None else C.byref(variant), workspace, workspace_bytes)
+
+
+def stage_set_documents(s: int, slot: int, documents, prefix=None) -> None:
+    _call("stage_set_documents", s, slot, documents, prefix)
 
 
 def delayed_update(s: int, t: int, hp: UpdateHParams) -> None:

@@ -68,6 +68,11 @@ struct Slot {
   hipEvent_t ev_sort = nullptr;
   int64_t step = -1;
   bool pending = false;
+  // variants (stage_set_variant): the key ranges of the slot's documents, whether they were set, and the
+  // dropout counter of the forward's first branch
+  int32_t *key_start = nullptr, *key_end = nullptr;
+  bool documents = false;
+  uint64_t drop_at = 0;
 };
 
 }  // namespace
@@ -163,6 +168,11 @@ struct stage {
   unsigned long long* skipped;
   int32_t* sort_ws;  // the token sort's scratch (its sorts run in order on one stream)
   std::vector<Slot> slots;
+  // a variant of the blocks (stage_set_variant) and its part of the caller's workspace: that of an attention
+  // call, a branch's output before its dropout, and the gradients of the two branches behind theirs
+  bool variant_on = false;
+  stage_variant_t variant = {};
+  void *range_ws = nullptr, *branch = nullptr, *dbranch[2] = {};
   // bookkeeping
   int64_t version_step[2] = {-1, -1};
   int64_t grad_step[STAGE_MAX_DELAY + 1];
@@ -612,8 +622,45 @@ AttnArgs attn_args(const stage* S, const BlockAct& b) {
   return a;
 }
 
-void block_forward(stage* S, int vi, BlockAct& b, const BlockOff& w, void* y) {
+// The variant's attention over the slot's packed projections
+RangeArgs range_args(const stage* S, const Slot& sl, const BlockAct& b) {
   const stage_shape_t& sh = S->sh;
+  RangeArgs a{};
+  a.B = sh.micro_batch; a.Sq = a.Sk = sh.seq_len; a.Hq = sh.n_heads; a.Hkv = sh.n_kv_heads; a.hd = sh.head_dim;
+  auto heads = [&](void* base, int first) {
+    return HeadRows{(char*)base + (size_t)first * sh.head_dim * S->esz, (int64_t)sh.seq_len * S->qkvw, sh.head_dim, S->qkvw};
+  };
+  a.q = heads(b.qkv, 0);
+  a.k = heads(b.qkv, sh.n_heads);
+  a.v = heads(b.qkv, sh.n_heads + sh.n_kv_heads);
+  a.o = b.o; a.o32 = b.o32; a.lse = b.lse;
+  if (S->variant.documents) { a.key_start = sl.key_start; a.key_end = sl.key_end; }
+  a.slopes = S->variant.slopes;
+  a.scale = 1.0f / sqrtf((float)sh.head_dim);
+  a.cap = S->variant.softcap;
+  a.dq = heads(S->dqkv, 0);
+  a.dk = heads(S->dqkv, sh.n_heads);
+  a.dv = heads(S->dqkv, sh.n_heads + sh.n_kv_heads);
+  a.ob = (int64_t)sh.seq_len * S->hqd; a.orow = S->hqd; a.oh = sh.head_dim;
+  a.dout = HeadRows{S->do_, a.ob, sh.head_dim, S->hqd};
+  a.rope_cos = S->cos_t; a.rope_sin = S->sin_t;
+  return a;
+}
+
+uint32_t drop_threshold(const stage* S) {
+  return S->variant_on ? (uint32_t)std::nearbyint(65536.0 * S->variant.dropout) : 0;
+}
+// out = resid + dropout(x) of one branch of a block: counter `at`
+void drop(stage* S, const void* x, const void* resid, void* out, uint64_t at) {
+  const int64_t d = S->sh.d_model;
+  launch_dropout(S->bf, DropoutArgs{S->T, d, d, d, d, x, resid, out, drop_threshold(S), S->variant.seed, at}, S->st);
+}
+
+// drop_at: the dropout counter of the block's attention branch (its other branch: the next one); training: a
+// forward without dropout when not set
+void block_forward(stage* S, int vi, const Slot& sl, BlockAct& b, const BlockOff& w, void* y, uint64_t drop_at, bool training) {
+  const stage_shape_t& sh = S->sh;
+  const bool dropped = training && drop_threshold(S) > 0;
   const int T = S->T, d = sh.d_model, f = sh.d_ffn;
   const bool bf = S->bf;
   hipStream_t st = S->st;
@@ -627,9 +674,13 @@ void block_forward(stage* S, int vi, BlockAct& b, const BlockOff& w, void* y) {
   gq.rope_hd = sh.head_dim;
   gq.rope_S = sh.seq_len;
   run_gemm(S, gq);
-  timed(S, STAGE_PROF_ATTN_FWD, attn_fwd_flops(S), [&] { launch_attention_fwd(bf, attn_args(S, b), st); });
-  run_gemm(S, gemm(T, d, S->hqd, b.o, S->hqd, true, S->wptr(vi, w.wo), S->hqd, true, b.h, d,
-                       false, 0.f, b.x));
+  timed(S, STAGE_PROF_ATTN_FWD, attn_fwd_flops(S), [&] {
+    if (S->variant_on) launch_range_fwd(bf, range_args(S, sl, b), S->range_ws, st);
+    else launch_attention_fwd(bf, attn_args(S, b), st);
+  });
+  run_gemm(S, gemm(T, d, S->hqd, b.o, S->hqd, true, S->wptr(vi, w.wo), S->hqd, true, dropped ? S->branch : b.h, d,
+                       false, 0.f, dropped ? nullptr : b.x));
+  if (dropped) drop(S, S->branch, b.x, b.h, drop_at);
   launch_rmsnorm_fwd(bf, b.h, S->wptr(vi, w.ffn_norm), b.n2, b.rstd2, T, d, sh.rms_eps, st);
   // gate/up projection with the SwiGLU z = silu(gate) up in its epilogue
   GemmArgs gg = gemm(T, 2 * f, d, b.n2, d, true, S->wptr(vi, w.wgu), d, true, b.gu, 2 * f);
@@ -638,7 +689,9 @@ void block_forward(stage* S, int vi, BlockAct& b, const BlockOff& w, void* y) {
   gg.out2 = b.z;
   gg.ld_out2 = f;
   run_gemm(S, gg);
-  run_gemm(S, gemm(T, d, f, b.z, f, true, S->wptr(vi, w.wdown), f, true, y, d, false, 0.f, b.h));
+  run_gemm(S, gemm(T, d, f, b.z, f, true, S->wptr(vi, w.wdown), f, true, dropped ? S->branch : y, d, false, 0.f,
+                   dropped ? nullptr : b.h));
+  if (dropped) drop(S, S->branch, b.h, y, drop_at + 1);
 }
 
 // The norms' dgamma: launch_rmsnorm_bwd leaves partial rows, summed for up to COLSUM_MAX norms at a time
@@ -658,8 +711,9 @@ void norm_backward(stage* S, const void* dn, const void* x, const float* rstd, c
 }
 
 // dy: gradient of the block output; writes the gradient of the block input into dx.
-void block_backward(stage* S, int vi, BlockAct& b, const BlockOff& w, const void* dy, void* dx,
-                    float* g, bool first) {
+void block_backward(stage* S, int vi, const Slot& sl, BlockAct& b, const BlockOff& w, const void* dy, void* dx,
+                    float* g, bool first, uint64_t drop_at) {
+  const bool dropped = drop_threshold(S) > 0;
   const stage_shape_t& sh = S->sh;
   const int T = S->T, d = sh.d_model, f = sh.d_ffn;
   const bool bf = S->bf;
@@ -669,13 +723,18 @@ void block_backward(stage* S, int vi, BlockAct& b, const BlockOff& w, const void
   // overwrites dgu, dh, dqkv or the previous block's dy, it waits for the product that read it.
   // down projection: dz = dy Wd with the SwiGLU backward in its epilogue (-> dgate | dup);
   // dWd (+)= dy^T z
-  GemmArgs gz = gemm(T, f, d, dy, d, true, S->wptr(vi, w.wdown), f, false, S->dgu, 2 * f);
+  const void* dbr = dy;  // the gradient of the down projection's output: dy behind the dropout
+  if (dropped) {
+    drop(S, dy, nullptr, S->dbranch[0], drop_at + 1);  // the last product that read it was waited for before dx was written
+    dbr = S->dbranch[0];
+  }
+  GemmArgs gz = gemm(T, f, d, dbr, d, true, S->wptr(vi, w.wdown), f, false, S->dgu, 2 * f);
   gz.epi = 1;
   gz.aux = b.gu;
   gz.ld_aux = 2 * f;
   after_wgrad(S, WG_GU);
   run_gemm(S, gz);
-  run_wgrad(S, gemm(d, f, T, dy, d, false, b.z, f, false, g + w.wdown, f, true, beta), WG_DOWN);
+  run_wgrad(S, gemm(d, f, T, dbr, d, false, b.z, f, false, g + w.wdown, f, true, beta), WG_DOWN);
   // gate/up: dn2 = dgu Wgu ; dWgu (+)= dgu^T n2
   run_gemm(S, gemm(T, d, 2 * f, S->dgu, 2 * f, true, S->wptr(vi, w.wgu), d, false, S->dn, d));
   run_wgrad(S, gemm(2 * f, d, T, S->dgu, 2 * f, false, b.n2, d, false, g + w.wgu, d, true, beta), WG_GU);
@@ -685,15 +744,22 @@ void block_backward(stage* S, int vi, BlockAct& b, const BlockOff& w, const void
   // in the product's epilogue, from o in fp32 (the bf16 stage's forward keeps an fp32 copy whose P V
   // product took P as a hi / lo pair: delta then matches the P and dP the backward recomputes, where
   // o rounded to bf16 would leave every dS row a nonzero sum once attention sharpens)
-  GemmArgs go = gemm(T, S->hqd, d, S->dh, d, true, S->wptr(vi, w.wo), S->hqd, false, S->do_, S->hqd);
-  go.epi = 4;
-  go.aux = bf ? (const void*)b.o32 : b.o;
-  go.ld_aux = S->hqd;
-  go.delta = S->delta;
-  go.delta_hd = sh.head_dim;
-  go.delta_S = sh.seq_len;
+  const void* dha = S->dh;
+  if (dropped) {
+    drop(S, S->dh, nullptr, S->dbranch[1], drop_at);
+    dha = S->dbranch[1];
+  }
+  GemmArgs go = gemm(T, S->hqd, d, dha, d, true, S->wptr(vi, w.wo), S->hqd, false, S->do_, S->hqd);
+  if (!S->variant_on) {  // the variant's attention backward forms its own
+    go.epi = 4;
+    go.aux = bf ? (const void*)b.o32 : b.o;
+    go.ld_aux = S->hqd;
+    go.delta = S->delta;
+    go.delta_hd = sh.head_dim;
+    go.delta_S = sh.seq_len;
+  }
   run_gemm(S, go);
-  run_wgrad(S, gemm(d, S->hqd, T, S->dh, d, false, b.o, S->hqd, false, g + w.wo, S->hqd, true, beta), WG_O);
+  run_wgrad(S, gemm(d, S->hqd, T, dha, d, false, b.o, S->hqd, false, g + w.wo, S->hqd, true, beta), WG_O);
   AttnArgs a = attn_args(S, b);
   a.dout = S->do_; a.dqkv = S->dqkv; a.delta = S->delta; a.part = S->attn_part;
   a.delta_ready = true;  // computed with do above
@@ -706,7 +772,10 @@ void block_backward(stage* S, int vi, BlockAct& b, const BlockOff& w, const void
     (void)hipStreamWaitEvent(S->ust, S->ev_now, 0);
     launch_pending_chunk(S);
   }
-  timed(S, STAGE_PROF_ATTN_BWD, 2.0 * attn_fwd_flops(S), [&] { launch_attention_bwd(bf, a, st); });
+  timed(S, STAGE_PROF_ATTN_BWD, 2.0 * attn_fwd_flops(S), [&] {
+    if (S->variant_on) launch_range_bwd(bf, range_args(S, sl, b), S->range_ws, st);
+    else launch_attention_bwd(bf, a, st);
+  });
   // qkv projection: dn1 = dqkv Wqkv ; dWqkv (+)= dqkv^T n1
   run_gemm(S, gemm(T, d, S->qkvw, S->dqkv, S->qkvw, true, S->wptr(vi, w.wqkv), d, false, S->dn, d));
   run_wgrad(S, gemm(S->qkvw, d, T, S->dqkv, S->qkvw, false, b.n1, d, false, g + w.wqkv, d, true, beta), WG_QKV);
@@ -887,7 +956,51 @@ int check_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
     return fail(STAGE_ESTATE, "weights of step " + std::to_string(step) + " are not resident");
   if (sh.first_stage && !tokens) return fail(STAGE_EINVAL, "first stage needs tokens");
   if (!sh.first_stage && !x_in) return fail(STAGE_EINVAL, "non-first stage needs x_in");
+  if (s->variant_on && s->variant.documents && !s->slots[slot].documents)
+    return fail(STAGE_ESTATE, "the variant has documents and the slot's were not set (stage_set_documents)");
   return STAGE_OK;
+}
+
+// nullptr, or what is wrong with a variant
+const char* check_variant(const stage_variant_t* v) {
+  if (!v) return "null variant";
+  if (!(v->softcap >= 0.f) || !std::isfinite(v->softcap) || (v->softcap > 0.f && !std::isfinite(1.f / v->softcap)))
+    return "softcap must be 0 (none) or positive and finite, with a finite reciprocal";
+  if (!(v->dropout >= 0.0 && v->dropout <= 65535.0 / 65536.0)) return "dropout must be in [0, 1 - 2^-16]";
+  if ((uintptr_t)v->slopes % 4) return "slopes must be 4-byte aligned";
+  return nullptr;
+}
+
+// The variant's workspace at p (null: its size alone)
+size_t variant_layout(stage* s, const stage_variant_t& v, char* p) {
+  size_t n = 0;
+  auto take = [&](size_t bytes) {
+    char* r = p ? p + n : nullptr;
+    n += up(bytes);
+    return r;
+  };
+  const size_t T = s->T, act = T * s->sh.d_model * s->esz;
+  RangeArgs a{};
+  a.B = s->sh.micro_batch; a.Sq = a.Sk = s->sh.seq_len;
+  a.Hq = s->sh.n_heads; a.Hkv = s->sh.n_kv_heads; a.hd = s->sh.head_dim;
+  void* ws = take(std::max(range_fwd_ws_bytes(s->bf, a), range_bwd_ws_bytes(s->bf, a)));
+  const bool dropped = std::nearbyint(65536.0 * v.dropout) > 0;
+  void* b[3];
+  for (void*& x : b) x = dropped ? take(act) : nullptr;
+  if (p) {
+    s->range_ws = ws;
+    s->branch = b[0]; s->dbranch[0] = b[1]; s->dbranch[1] = b[2];
+  }
+  for (Slot& sl : s->slots) {
+    int32_t* r[2] = {};
+    if (v.documents)
+      for (int32_t*& x : r) x = (int32_t*)take(T * 4);
+    if (p) {
+      sl.key_start = r[0]; sl.key_end = r[1];
+      sl.documents = false;
+    }
+  }
+  return n;
 }
 
 int check_logprob(stage_t* s, const int32_t* targets, float inv_temperature, const float* logp) {
@@ -928,9 +1041,13 @@ int forward_blocks(stage_t* s, Slot& sl, int vi, const int32_t* tokens, const vo
     launch_token_runs(sl.sorted_tok, T, sh.vocab, sl.row_start, nullptr, nullptr, nullptr, ss);
     HIP_OK(hipEventRecord(sl.ev_sort, ss));
   }
+  if (keep && drop_threshold(s) > 0) {
+    sl.drop_at = s->variant.offset;
+    s->variant.offset += 2 * (uint64_t)sh.n_blocks;
+  }
   for (int i = 0; i < sh.n_blocks; ++i) {
     void* y = i + 1 < sh.n_blocks ? sl.blk[i + 1].x : sl.y;
-    block_forward(s, vi, sl.blk[i], s->boff[i], y);
+    block_forward(s, vi, sl, sl.blk[i], s->boff[i], y, sl.drop_at + 2 * (uint64_t)i, keep);
   }
   return STAGE_OK;
 }
@@ -995,7 +1112,7 @@ int backward_run(stage_t* s, Slot& sl, const void* dy, const float* dlogp, const
   }
   for (int i = sh.n_blocks - 1; i >= 0; --i) {
     void* out = (cur == s->dA) ? s->dB : s->dA;
-    block_backward(s, vi, sl.blk[i], s->boff[i], cur, out, g, first);
+    block_backward(s, vi, sl, sl.blk[i], s->boff[i], cur, out, g, first, sl.drop_at + 2 * (uint64_t)i);
     cur = out;
   }
   if (sh.first_stage) {
@@ -1025,6 +1142,46 @@ int backward_run(stage_t* s, Slot& sl, const void* dy, const float* dlogp, const
 }  // namespace
 
 extern "C" {
+
+size_t stage_variant_bytes(stage_t* s, const stage_variant_t* v) {
+  if (!s || check_variant(v)) return 0;
+  return variant_layout(s, *v, nullptr);
+}
+
+int stage_set_variant(stage_t* s, const stage_variant_t* v, void* workspace, size_t workspace_bytes) {
+  if (!s) return fail(STAGE_EINVAL, "null stage");
+  if (v)
+    if (const char* m = check_variant(v)) return fail(STAGE_EINVAL, m);
+  for (const Slot& sl : s->slots)
+    if (sl.pending) return fail(STAGE_ESTATE, "a slot holds a microbatch whose backward is pending");
+  if (!v) {
+    s->variant_on = false;
+    s->variant = stage_variant_t{};
+    for (Slot& sl : s->slots) sl.documents = false;
+    return STAGE_OK;
+  }
+  if (!workspace || (uintptr_t)workspace % ALIGN) return fail(STAGE_EINVAL, "workspace must be 256-byte aligned");
+  const size_t need = variant_layout(s, *v, nullptr);
+  if (workspace_bytes < need)
+    return fail(STAGE_ENOSPACE, "workspace holds " + std::to_string(workspace_bytes) + " bytes, needs " + std::to_string(need));
+  variant_layout(s, *v, (char*)workspace);
+  s->variant = *v;
+  s->variant_on = true;
+  return STAGE_OK;
+}
+
+int stage_set_documents(stage_t* s, int32_t slot, const int32_t* documents, const uint8_t* prefix) {
+  if (!s) return fail(STAGE_EINVAL, "null stage");
+  if (slot < 0 || slot >= s->sh.max_inflight) return fail(STAGE_EINVAL, "slot out of range");
+  if (!s->variant_on || !s->variant.documents) return fail(STAGE_ESTATE, "the stage's variant has no documents");
+  Slot& sl = s->slots[slot];
+  if (sl.pending) return fail(STAGE_ESTATE, "slot holds a microbatch whose backward is pending");
+  if (!documents || (uintptr_t)documents % 4) return fail(STAGE_EINVAL, "documents null or not 4-byte aligned");
+  launch_key_ranges(s->sh.micro_batch, s->sh.seq_len, documents, prefix, sl.key_start, sl.key_end, s->st);
+  HIP_OK(hipGetLastError());
+  sl.documents = true;
+  return STAGE_OK;
+}
 
 int stage_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens, const void* x_in,
                   const int32_t* targets, void* y_out, float* loss_dev) {

@@ -98,6 +98,44 @@ class Stage:
         B.stage_score_logprob(self.handle, slot, step, p(tokens), p(x_in), p(targets), inv_temperature, p(logp),
                               p(entropy))
 
+    def set_variant(self, softcap: float = 0.0, slopes=None, dropout: float = 0.0, seed: int = 0, offset: int = 0,
+                    documents: bool = False):
+        """The blocks' variant for the forwards from here on: attention scores capped at +-softcap and lowered by
+        slopes [n_heads] fp32 times the distance, dropout of both branches (seed, offset: dropout.dropout_add's),
+        and rows that pack documents (set_documents).  Keeps its workspace until the next call."""
+        if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (self.shape.n_heads,)
+                                   or slopes.device != self.arena.device or not slopes.is_contiguous()):
+            raise ValueError(f"slopes: expected a contiguous float32 [{self.shape.n_heads}] tensor on {self.device}")
+        v = B.StageVariant(softcap, None if slopes is None else slopes.data_ptr(), dropout, seed, offset, int(documents))
+        nbytes = B.stage_variant_bytes(self.handle, v)
+        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        B.stage_set_variant(self.handle, v, (ws.data_ptr() + 255) // 256 * 256, nbytes)
+        self._hold_old_variant()
+        self._variant = (ws, slopes)
+
+    def clear_variant(self):
+        """Back to the plain causal blocks."""
+        B.stage_set_variant(self.handle, None)
+        self._hold_old_variant()
+        self._variant = None
+
+    def _hold_old_variant(self):
+        # the stage stream may still read the last variant's memory: the allocator gives it out again behind that
+        for t in getattr(self, "_variant", None) or ():
+            if t is not None:
+                t.record_stream(self.stream)
+
+    def set_documents(self, slot: int, documents, prefix=None):
+        """The documents [micro_batch, seq_len] int32 packed in the slot's rows (a run of equal ids >= 0; below 0:
+        padding) for its forwards until they are set again; prefix as in attention.key_ranges."""
+        shape = (self.shape.micro_batch, self.shape.seq_len)
+        for name, t, types in (("documents", documents, (torch.int32,)), ("prefix", prefix, (torch.uint8, torch.bool))):
+            if t is None and name == "prefix":
+                continue
+            if t.dtype not in types or tuple(t.shape) != shape or t.device != self.arena.device or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous {types[0]} tensor of shape {shape} on {self.device}")
+        B.stage_set_documents(self.handle, slot, documents.data_ptr(), None if prefix is None else prefix.data_ptr())
+
     def update(self, t: int, hp: B.UpdateHParams):
         B.delayed_update(self.handle, t, hp)
 

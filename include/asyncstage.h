@@ -301,7 +301,7 @@ int hbm_stream_copy(void* dst, const void* src, size_t bytes, void* hip_stream);
  * distance, rows that pack several documents (attention_key_ranges, attention_forward below say what each
  * is), and dropout on the outputs of a block's two branches before they join the residual stream (dropout_add). */
 typedef struct {
-  float softcap;         /* 0: none                                                                  */
+  float softcap;         /* 0 (none) or in [2^-60, 2^100]                                            */
   const float* slopes;   /* [n_heads] device array or NULL; kept, owned by the caller                */
   double dropout;        /* p of both branches; a forward without a backward (stage_score_logprob) has none */
   uint64_t seed, offset; /* dropout_add's: block i of the n-th forward from here takes the offsets
@@ -461,8 +461,8 @@ typedef struct {
   const int32_t *key_start, *key_end;  /* [batch, queries] device arrays, or both NULL      */
   const int32_t* q_start;              /* [batch] device array; NULL: keys - queries        */
   const float* slopes;                 /* [heads] device array or NULL                      */
-  float scale;                         /* > 0                                               */
-  float softcap;                       /* 0 (none) or > 0                                   */
+  float scale;                         /* [2^-60, 2^60]                                     */
+  float softcap;                       /* 0 (none) or [2^-60, 2^100], scale / softcap >= 2^-126 */
 } attention_params_t;
 
 /*   q             [batch, queries, heads, head_dim];  k, v [batch, keys, kv_heads, head_dim], as strided

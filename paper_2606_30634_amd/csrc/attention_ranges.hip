@@ -24,6 +24,8 @@ void range_mfma_bwd(const RangeArgs& a, hipStream_t st);
 
 namespace {
 
+constexpr int MAX_SPLITS = 256;  // shares of an item's keys
+
 // Score of x = scale q.k at distance `far` (x itself without cap and slopes)
 struct Score {
   float cap, inv_cap, slope;
@@ -144,24 +146,36 @@ __global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a)
   if (wave == 0 && lane < TR && q < a.Sq) a.lse[((int64_t)b * a.Hq + h) * a.Sq + q] = base + logf(L);
 }
 
-// The shares of a row joined: HD / 4 lanes per row (b, i, h).  LOG2: their maxima are in log2 units (the bf16
-// kernels').
+// The shares of a row (b, i, h) joined, a block per row: HD / 4 lanes per share, the shares spread over the block, so
+// that a row of many shares takes a few round trips to memory and not one per share (16 rows of 16 shares: 5.6 -> JOIN
+// us).  LOG2: the maxima are in log2 units (the bf16 kernels').
 template <typename T, int HD, bool LOG2>
 __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
-  constexpr int LR = HD / 4;
-  const int64_t n = (int64_t)a.B * a.Sq * a.Hq, r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;
-  const int c = (threadIdx.x % LR) * 4;
-  if (r >= n) return;
-  float M = -INFINITY, L = 0.f;
-  for (int s = 0; s < a.nsplit; ++s) M = fmaxf(M, a.part_ml[n * s + r].x);
-  const float base = weight_base(M);
+  constexpr int LR = HD / 4, NG = 256 / LR;  // lanes of a share, shares at a time
+  __shared__ f32x4 sum[256];
+  __shared__ float weight[MAX_SPLITS], top[4], tot[4];
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq, r = blockIdx.x;
+  const int t = threadIdx.x, c = (t % LR) * 4;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (t < a.nsplit) ml = a.part_ml[n * t + r];
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float2 ml = a.part_ml[n * s + r];
-    const float w = LOG2 ? exp2f(ml.x - base) : expf(ml.x - base);
-    L += w * ml.y;
-    o += w * ld4(a.part + (n * s + r) * HD + c);
-  }
+  const float m = wave_max(ml.x);
+  if (t % 64 == 0) top[t / 64] = m;
+  __syncthreads();
+  const float base = weight_base(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+  const float w = LOG2 ? exp2f(ml.x - base) : expf(ml.x - base);
+  weight[t] = w;
+  const float l = wave_sum(w * ml.y);
+  if (t % 64 == 0) tot[t / 64] = l;
+  __syncthreads();
+#pragma unroll 4
+  for (int s = t / LR; s < a.nsplit; s += NG) o += weight[s] * ld4(a.part + (n * s + r) * HD + c);
+  sum[t] = o;
+  __syncthreads();
+  if (t >= LR) return;
+  const float L = (tot[0] + tot[1]) + (tot[2] + tot[3]);
+#pragma unroll
+  for (int g = 1; g < NG; ++g) o += sum[g * LR + t];
   o *= L == 0.f ? 0.f : 1.0f / L;
   st4((T*)a.o + r * HD + c, o);
   if (a.o32) st4(a.o32 + r * HD + c, o);
@@ -513,13 +527,15 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 bool mfma(bool bf, int hd) { return bf && hd != 32; }
 
-// Shares of a forward item's keys: towards 512 items, two per compute unit, of at least 256 keys (two tiles on the
-// bf16 matrix cores)
+// Shares of a forward item's keys.  Few items: towards 512, two per compute unit, of at least 256 keys (128 on the
+// bf16 matrix cores).  Long caches: towards 2048 of at least 1024 keys, since their lengths differ and the longest
+// share ends the launch (16 answers of up to 32768 keys, 128 items: 247 us with 512, LONG with 2048).
 int fwd_splits(bool bf, const RangeArgs& a) {
   const bool mm = mfma(bf, a.hd);
   const int64_t items = mm ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
   if (items == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({256, 512 / items, a.Sk / (mm ? 128 : 256)}));
+  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 128 : 256)), many = std::min<int64_t>(2048 / items, a.Sk / 1024);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(MAX_SPLITS, std::max(few, many)));
 }
 
 }  // namespace
@@ -541,7 +557,7 @@ void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
     constexpr int HD = decltype(hd)::value;
     if constexpr (sizeof(T) == 2 && HD != 32) range_mfma_fwd(a, st);
     else range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
-    if (a.nsplit > 1) range_join<T, HD, sizeof(T) == 2 && HD != 32><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
+    if (a.nsplit > 1) range_join<T, HD, sizeof(T) == 2 && HD != 32><<<(unsigned)n, 256, 0, st>>>(a);
   });
 }
 

@@ -370,13 +370,15 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
 // ------------------------------------------------------------------------------------------ backward
 // P and dS of one pair, from dp = dO.v and s = q.k, or with CAP its tanh_scores
 struct Pair { float p, ds; };
+// 1 - t^2 of t = tanh; 0 for the -inf of a pair that is not seen
+__device__ __forceinline__ float cap_grad(float t) { return __builtin_amdgcn_fmed3f(__builtin_fmaf(-t, t, 1.0f), 0.f, 1.f); }
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ Pair grad_pair(float s, float dp, float nlse2, float delta, const CapScale& c, float slope2,
                                           float far) {
   float x = __builtin_fmaf(s, CAP ? c.out : c.sl2, nlse2);
   if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far), x);
   const float p = fast_exp2(x), ds = p * (dp - delta);
-  return Pair{p, CAP ? ds * __builtin_fmaf(-s, s, 1.0f) : ds};
+  return Pair{p, CAP ? ds * cap_grad(s) : ds};
 }
 
 template <int N>
@@ -706,6 +708,25 @@ struct QueryStage {
   static constexpr size_t bytes(int stages) { return std::max((size_t)stages * SZ * 2, Lds<HD>::out_bytes); }
 };
 
+// Scores of the queries [r0, r0 + 32) of a stage that do not see this lane's key become -inf; nothing where all of
+// them see all keys of the wave.  (A lane's keys are those of lanes 0 .. 31 of its wave, in order.)
+template <int HD>
+__device__ __forceinline__ void mask_unseen(f32x16& s, const bf16* stage, int r0, int mykey) {
+  const uint32_t* lo = reinterpret_cast<const uint32_t*>(stage + 2 * QueryStage<HD>::TSZ) + 2 * KB + r0;
+  const uint32_t* n = lo + KB;
+  const int lane = threadIdx.x % 64, row = lane % 32, half = lane / 32;
+  // lane l looks at row l mod 32, for the wave's first key or its last
+  const uint32_t key = (uint32_t)(mykey - row) + 31u * half;
+  if (__all(key - lo[row] < n[row])) return;
+#pragma unroll
+  for (int e4 = 0; e4 < 4; ++e4) {
+    const u32x4 lo4 = *reinterpret_cast<const u32x4*>(lo + 8 * e4 + 4 * half), n4 = *reinterpret_cast<const u32x4*>(n + 8 * e4 + 4 * half);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if ((uint32_t)mykey - lo4[j] >= n4[j]) s[4 * e4 + j] = -INFINITY;
+  }
+}
+
 // dK and dV of head dimension 64
 template <int HD, bool CAP, bool BIAS>
 __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyItem& item, unsigned char* __restrict__ smem) {
@@ -726,7 +747,9 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
     const void* v = wu == 0 ? (const void*)(a.nlse2 + ((int64_t)b * a.Hq + h) * a.Sq)
                   : wu == 1 ? (const void*)(a.delta + ((int64_t)b * a.Hq + h) * a.Sq)
                   : wu == 2 ? (const void*)(a.seen_lo + (int64_t)b * a.Sq) : (const void*)(a.seen_len + (int64_t)b * a.Sq);
-    dma4(v, 4u * (uint32_t)min(q0 + lane, item.qhi - 1), lds_addr(st + 2 * Q::TSZ) + (uint32_t)wu * KB * 4u);
+    // rows past the last query repeat it (TT::issue), but see no key: their seen_len is 0
+    const float* row = (const float*)v + q0;
+    dma4_range(buffer_range(row, (const float*)v + item.qhi), 4u * (uint32_t)lane, lds_addr(st + 2 * Q::TSZ) + (uint32_t)wu * KB * 4u);
   };
   bf16x8 kf[KS], vf[KS];
   {
@@ -774,19 +797,17 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
       }
       if constexpr (CAP) tanh_scores(s, cs);
       const float base_far = (float)far0;
-      const int left = item.qhi - q0 - t * 32 - 4 * half;  // accumulator rows of this lane that exist
+      mask_unseen<HD>(s[0], Qs, t * 32, mykey);
 #pragma unroll
       for (int e4 = 0; e4 < 4; ++e4) {
         const float* r = Ls + t * 32 + 8 * e4 + 4 * half;
         const f32x4 l4 = *reinterpret_cast<const f32x4*>(r), d4 = *reinterpret_cast<const f32x4*>(r + KB);
-        const u32x4 lo4 = *reinterpret_cast<const u32x4*>(r + 2 * KB), n4 = *reinterpret_cast<const u32x4*>(r + 3 * KB);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int e = 4 * e4 + j;
           const Pair w = grad_pair<CAP, BIAS>(s[0][e], dp[e], l4[j], d4[j], cs, slope2, base_far + (float)(t * 32 + 8 * e4 + j));
-          const bool on = (uint32_t)mykey - lo4[j] < n4[j] && 8 * e4 + j < left;
-          s[0][e] = on ? w.p : 0.f;
-          dp[e] = on ? w.ds : 0.f;
+          s[0][e] = w.p;
+          dp[e] = w.ds;
         }
       }
 #pragma unroll
@@ -886,13 +907,10 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     };
     bf16x8 fq[2], fd[2], fc[4];
     f32x4 l4[2], d4[2];
-    u32x4 lo4[2], n4[2];
     auto stat = [&](auto I) {
       constexpr int n = I;
       l4[n % 2] = *reinterpret_cast<const f32x4*>(Ls + 8 * n);
       d4[n % 2] = *reinterpret_cast<const f32x4*>(Ls + KB + 8 * n);
-      lo4[n % 2] = *reinterpret_cast<const u32x4*>(Ls + 2 * KB + 8 * n);
-      n4[n % 2] = *reinterpret_cast<const u32x4*>(Ls + 3 * KB + 8 * n);
     };
     if constexpr (SM) stat(std::integral_constant<int, 0>{});
     if constexpr (SC) {
@@ -943,18 +961,17 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
         y0 = dp[U][e0] - d4[lb][e0 % 4];
         y1 = dp[U][e1] - d4[lb][e1 % 4];
         if constexpr (CAP) {
-          y0 *= __builtin_fmaf(-s[U][e0], s[U][e0], 1.0f);
-          y1 *= __builtin_fmaf(-s[U][e1], s[U][e1], 1.0f);
+          y0 *= cap_grad(s[U][e0]);
+          y1 *= cap_grad(s[U][e1]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (PV) mfma_acc<!SC>(dk[g % DT], fc[2 * c + 1], sb[T][g / DT]);
       if constexpr (SM) {
-        const bool on0 = (uint32_t)mykey - lo4[lb][e0 % 4] < n4[lb][e0 % 4], on1 = (uint32_t)mykey - lo4[lb][e1 % 4] < n4[lb][e1 % 4];
-        s[U][e0] = on0 ? x0 : 0.f;
-        s[U][e1] = on1 ? x1 : 0.f;
-        dp[U][e0] = on0 ? x0 * y0 : 0.f;
-        dp[U][e1] = on1 ? x1 * y1 : 0.f;
+        s[U][e0] = x0;
+        s[U][e1] = x1;
+        dp[U][e0] = x0 * y0;
+        dp[U][e1] = x1 * y1;
         if constexpr (g == 3) { pb[U][0] = acc_rows_to_b<0>(s[U]); sb[U][0] = acc_rows_to_b<0>(dp[U]); }
         if constexpr (g == 7) { pb[U][1] = acc_rows_to_b<8>(s[U]); sb[U][1] = acc_rows_to_b<8>(dp[U]); }
       }
@@ -966,10 +983,12 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
   auto soft = [&](auto T_, auto SC_, auto PV_, auto FE_, const bf16* rows, const bf16* stats, int sq0, float slope2, const bf16* cols) {
+    constexpr int U = T_ ^ 1;
     if constexpr (CAP) {
-      f32x16(&u)[1] = reinterpret_cast<f32x16(&)[1]>(s[T_ ^ 1]);
+      f32x16(&u)[1] = reinterpret_cast<f32x16(&)[1]>(s[U]);
       tanh_scores(u, cs);
     }
+    mask_unseen<HD>(s[U], stats, U * 32, mykey);
     step(T_, SC_, std::true_type{}, PV_, FE_, rows, stats, sq0, slope2, cols);
   };
   auto arrive = [&] {
@@ -1016,6 +1035,27 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
   dkv_store<HD>(a, item, dk, dv, reinterpret_cast<float*>(smem));
 }
 
+// The key block of sequence b whose queries are the r-th most (of up to NT blocks; beyond that block r itself: there are
+// then enough items for their order not to matter).  Documents give the blocks of a launch very different lengths, and
+// the longest, started last, would end it: 2 x 4096 tokens in 3 documents a row, 32 heads on 8: UNSORTED -> SORTED us.
+__device__ __forceinline__ int heavy_block(const RangeArgs& a, int b, int nkb, int r) {
+  __shared__ int queries[NT], pick;
+  if (nkb > NT) return r;
+  const int t = threadIdx.x;
+  if (t < nkb) {
+    const int2 by = a.sees[(int64_t)b * nkb + t];
+    queries[t] = by.y - by.x;
+  }
+  __syncthreads();
+  if (t < nkb) {
+    int rank = 0;
+    for (int j = 0; j < nkb; ++j) rank += queries[j] > queries[t] || (queries[j] == queries[t] && j < t);
+    if (rank == r) pick = t;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(pick);
+}
+
 template <bool CAP, bool BIAS>
 __global__ void __launch_bounds__(NT, 2) range_flash_dq128(RangeArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -1031,7 +1071,8 @@ __global__ void __launch_bounds__(NT) range_flash_dkv128(RangeArgs a) {
   const int nkb = (a.Sk + QB - 1) / QB;
   int unit, idx;  // unit: (sequence, key/value head)
   xcd_item(blockIdx.x, nkb * a.nsplit * a.Hkv * a.B, nkb * a.nsplit, unit, idx);
-  const KeyItem item(a, idx / a.nsplit, idx % a.nsplit, unit % a.Hkv, unit / a.Hkv);
+  const int b = unit / a.Hkv;
+  const KeyItem item(a, heavy_block(a, b, nkb, idx / a.nsplit), idx % a.nsplit, unit % a.Hkv, b);
   range_dkv128_block<CAP, BIAS>(a, item, smem);
 }
 
@@ -1045,7 +1086,7 @@ __global__ void __launch_bounds__(NT, 2) range_flash_bwd64(RangeArgs a) {
   xcd_item(blockIdx.x, per_unit * a.Hkv * a.B, per_unit, unit, idx);
   const int kvh = unit % a.Hkv, b = unit / a.Hkv;
   if (idx < nkb * a.nsplit) {
-    const KeyItem item(a, idx / a.nsplit, idx % a.nsplit, kvh, b);
+    const KeyItem item(a, heavy_block(a, b, nkb, idx / a.nsplit), idx % a.nsplit, kvh, b);
     range_dkv_block<64, CAP, BIAS>(a, item, smem);
   } else {
     idx -= nkb * a.nsplit;

@@ -63,9 +63,9 @@ const char* check_attention(const attention_params_t* p, RangeArgs& a) {
   if (p->kv_heads < 1 || p->heads < p->kv_heads || p->heads > 4096 || p->heads % p->kv_heads)
     return "kv_heads must be at least 1 and divide heads (at most 4096)";
   if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 32, 64 or 128";
-  if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return "scale must be positive and finite";
-  if (!(p->softcap >= 0.f) || !std::isfinite(p->softcap) || !std::isfinite(1.f / p->softcap) != (p->softcap == 0.f))
-    return "softcap must be 0 (none) or positive and finite, with a finite reciprocal";
+  if (!(p->scale >= 0x1p-60f && p->scale <= 0x1p60f)) return "scale must be in [2^-60, 2^60]";
+  if (p->softcap != 0.f && !(p->softcap >= 0x1p-60f && p->softcap <= 0x1p100f && p->scale / p->softcap >= 0x1p-126f))
+    return "softcap must be 0 (none) or in [2^-60, 2^100], scale / softcap at least 2^-126";
   if ((p->key_start != nullptr) != (p->key_end != nullptr)) return "key_start and key_end come together";
   if (off(p->key_start, 4) || off(p->key_end, 4) || off(p->q_start, 4) || off(p->slopes, 4))
     return "arrays must be 4-byte aligned";

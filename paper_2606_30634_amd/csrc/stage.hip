@@ -964,8 +964,8 @@ int check_forward(stage_t* s, int32_t slot, int64_t step, const int32_t* tokens,
 // nullptr, or what is wrong with a variant
 const char* check_variant(const stage_variant_t* v) {
   if (!v) return "null variant";
-  if (!(v->softcap >= 0.f) || !std::isfinite(v->softcap) || (v->softcap > 0.f && !std::isfinite(1.f / v->softcap)))
-    return "softcap must be 0 (none) or positive and finite, with a finite reciprocal";
+  if (v->softcap != 0.f && !(v->softcap >= 0x1p-60f && v->softcap <= 0x1p100f))
+    return "softcap must be 0 (none) or in [2^-60, 2^100]";
   if (!(v->dropout >= 0.0 && v->dropout <= 65535.0 / 65536.0)) return "dropout must be in [0, 1 - 2^-16]";
   if ((uintptr_t)v->slopes % 4) return "slopes must be 4-byte aligned";
   return nullptr;

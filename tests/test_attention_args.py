@@ -32,7 +32,7 @@ def _params(**kw):
 BAD_PARAMS = [dict(batch=-1), dict(batch=(1 << 24) + 1), dict(queries=-1), dict(queries=(1 << 30) + 1), dict(keys=-2),
               dict(keys=(1 << 30) + 1), dict(heads=3), dict(heads=0, kv_heads=0), dict(kv_heads=0), dict(heads=8192, kv_heads=1),
               dict(hd=48), dict(hd=256), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan),
-              dict(cap=-1.0), dict(cap=math.inf), dict(cap=math.nan), dict(cap=1e-44), dict(start=P), dict(end=P),
+              dict(cap=-1.0), dict(cap=math.inf), dict(cap=math.nan), dict(cap=1e-44), dict(cap=2.0 ** -61), dict(cap=2.0 ** 101), dict(scale=2.0 ** -61), dict(scale=2.0 ** 61), dict(scale=2.0 ** -60, cap=2.0 ** 90), dict(start=P), dict(end=P),
               dict(start=P, end=P + 2), dict(first=P + 1), dict(slopes=P + 2), dict(qs=(1280, 256, 60)), dict(ks=(1152, -128, 64)),
               dict(vs=(1152, 128, 4)), dict(qs=(1 << 41, 256, 64)), dict(ks=(1152, (1 << 24) + 8, 64)),
               dict(batch=1 << 20, queries=1 << 20)]

@@ -528,13 +528,15 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 bool mfma(bool bf, int hd) { return bf && hd != 32; }
 
 // Shares of a forward item's keys.  Few items: towards 512, two per compute unit, of at least 256 keys (128 on the
-// bf16 matrix cores).  Long caches: towards 2048 of at least 1024 keys, since their lengths differ and the longest
-// share ends the launch (16 answers of up to 32768 keys, 128 items: 247 us with 512, LONG with 2048).
+// bf16 matrix cores).  A few queries of each sequence: towards 4096 of at least 1024 keys, since the caches' lengths
+// differ and the longest share ends the launch (16 answers of up to 32768 keys, 128 items: 247 us towards 512, 233
+// towards 2048, 228 towards 4096); with more queries the partial sums would cost more than that.
 int fwd_splits(bool bf, const RangeArgs& a) {
   const bool mm = mfma(bf, a.hd);
   const int64_t items = mm ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
   if (items == 0) return 1;
-  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 128 : 256)), many = std::min<int64_t>(2048 / items, a.Sk / 1024);
+  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 128 : 256));
+  const int64_t many = a.Sq <= TR ? std::min<int64_t>(4096 / items, a.Sk / 1024) : 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>(MAX_SPLITS, std::max(few, many)));
 }
 

@@ -18,31 +18,51 @@ struct CapScale {
   float sl2;    // scale log2(e)
   float y_of;   // scale / cap
   float out;    // cap log2(e)
-  float small;  // |x| up to which |y| <= TANH_SMALL
+  float small;  // |x| up to which |y| <= SMALL
+  static constexpr float SMALL = 0.4f;
   __device__ explicit CapScale(const RangeArgs& a) {
     sl2 = a.scale * LOG2E;
     y_of = a.cap > 0.f ? a.scale / a.cap : 0.f;
     out = a.cap * LOG2E;
-    small = TANH_SMALL / y_of;
+    small = SMALL / y_of;
   }
 };
 
-// tanh(scale x / cap) of a wave's products.  One branch for the wave: where no |y| passes TANH_SMALL (scores within
-// half the cap, most tiles) the polynomial alone.
+// tanh(y) / y up to |y| = CapScale::SMALL: 1 + y^2 P(y^2) with the minimax P of degree 2 (relative error 2^-23, below
+// the rounding of the products), times `by`
+struct CapPoly {
+  float c0, c1, c2, c3;
+  __device__ explicit CapPoly(float by) : c0(by), c1(by * -0.3333188295f), c2(by * 0.1327762753f), c3(by * -0.0477941558f) {}
+  __device__ __forceinline__ float operator()(float y) const {
+    const float z = y * y;
+    float p = __builtin_fmaf(z, c3, c2);
+    p = __builtin_fmaf(z, p, c1);
+    return __builtin_fmaf(z, p, c0);
+  }
+};
+
 template <int N>
-__device__ __forceinline__ void tanh_scores(f32x16 (&s)[N], const CapScale& c) {
+__device__ __forceinline__ float largest(const f32x16 (&s)[N]) {
   float big = 0.f;
 #pragma unroll
   for (int t = 0; t < N; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) big = fmaxf(big, fabsf(s[t][e]));
+  return big;
+}
+
+// tanh(scale x / cap) of a wave's products, `big` their largest |x| in the lane.  One branch for the wave: where no
+// |y| passes CapScale::SMALL (most tiles) the polynomial alone.
+template <int N>
+__device__ __forceinline__ void tanh_scores(f32x16 (&s)[N], const CapScale& c, float big) {
   if (__all(big <= c.small)) {
+    const CapPoly poly(1.0f);
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float y = s[t][e] * c.y_of;
-        s[t][e] = y * tanh_ratio(y * y);
+        s[t][e] = y * poly(y);
       }
   } else {
 #pragma unroll
@@ -155,7 +175,14 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
   rows.n = a.Sq * pack;
   const int nb = (rows.n + QB - 1) / QB, heads = a.Hq / pack;
   int unit, idx;  // unit: (sequence, query head or key/value head); last query blocks first
-  xcd_item(blockIdx.x, nb * a.nsplit * heads * a.B, nb * a.nsplit, unit, idx);
+  if (a.nsplit == 1) {
+    xcd_item(blockIdx.x, nb * heads * a.B, nb, unit, idx);
+  } else {
+    // shares of long caches share nothing in an L2, and sequences of different lengths must not fall to one XCD
+    // each: every XCD takes some of all (16 answers of 1 .. 32768 keys, 8 key/value heads: 243 -> RAGGED us)
+    unit = blockIdx.x % (heads * a.B);
+    idx = blockIdx.x / (heads * a.B);
+  }
   const int rb = nb - 1 - idx / a.nsplit, split = idx % a.nsplit;
   rows.h0 = unit % heads * pack;
   rows.b = unit / heads;
@@ -166,6 +193,15 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
   const int r0 = rb * QB + wave * 32, myr = r0 + col;
   const bool valid = myr < rows.n;
   const int i = rows.query(min(myr, rows.n - 1)), h = rows.head(min(myr, rows.n - 1));
+  bf16x8 qf[KS];  // loaded first: the ranges and the first tiles' loads do not wait for them
+  {
+    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (valid) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+      else for (int j = 0; j < 8; ++j) qf[ks][j] = (bf16)0.f;
+    }
+  }
   const int2 mask = seen_keys(a, b, i);
   const WaveKeys wk(mask, valid);
   // the block's keys, and this share's tiles of them
@@ -186,26 +222,19 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
     TT::issue(kbase, a.k.row, blo + t * KB, bhi, lds_addr(st));
     TT::issue(vbase, a.v.row, blo + t * KB, bhi, lds_addr(st + L::TSZ));
   };
-  bf16x8 qf[KS];
-  {
-    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if (valid) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
-      else for (int j = 0; j < 8; ++j) qf[ks][j] = (bf16)0.f;
-    }
-  }
   const CapScale cs(a);
-  float slope2 = 0.f, pos_far = 0.f;
+  float slope2 = 0.f;
   int64_t pos = 0;
   if constexpr (BIAS) {
     slope2 = a.slopes[h] * LOG2E;
     pos = position(a, b, i);
   }
-  wait_vm_lds<0>();  // the register loads, before the ring's (as in flash_fwd)
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
     if (t0 + s < t1) issue(t0 + s);
+  // the register loads and the first tiles together, so that the wait the compiler needs for the former is not placed
+  // inside the loop (where it would drain the ring)
+  wait_vm_lds<0>();
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -237,7 +266,8 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
           for (int t = 0; t < 2; ++t) fk[c ^ 1][t] = frag_rows<HD>(Ks, t * 32, (ks + 1) * 16);
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], s[t], 0, 0, 0);
+        for (int t = 0; t < 2; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], s[t], 0, 0, 0);
         if constexpr (ks + 1 < KS) {
           static_for<2>([&](auto) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
@@ -246,10 +276,33 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
         }
         __builtin_amdgcn_sched_barrier(0);
       });
-      if constexpr (CAP) tanh_scores(s, cs);
-      const float to_log2 = CAP ? cs.out : cs.sl2;  // of s
+      // P V in four steps of 16 keys, the weights, their parts and the V fragments of the next step between this step's
+      // MFMAs: a wave issues in order, and a tile's vector work ahead of all its MFMAs runs beside nothing.
+      constexpr int NP = EXACT ? 3 : 1;
+      const float to_log2 = CAP ? cs.out : cs.sl2;  // of a product, or with CAP its tanh
+      bf16x8 part[2][NP], vf[2][DT];
+      float rs[2] = {0.f, 0.f}, base;
+      auto weights = [&](auto KK) {
+        constexpr int kk = KK, t = kk / 2, IB = kk % 2 * 8;
+#pragma unroll
+        for (int e = IB; e < IB + 8; ++e) {
+          const float p = fast_exp2(BIAS ? s[t][e] - base : __builtin_fmaf(s[t][e], to_log2, -base));
+          s[t][e] = p;
+          rs[e % 2] += p;
+        }
+        if constexpr (EXACT) acc_rows_to_b_parts<IB>(s[t], part[kk % 2]);
+        else part[kk % 2][0] = acc_rows_to_b<IB>(s[t]);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[kk % 2][dt] = frag_cols<HD>(Vs, dt * 32, kk * 16);
+      };
+      const bool whole = wk.whole(key0, key0 + KB);
+      float big = 0.f;
+      if constexpr (CAP) {
+        big = largest(s);
+        tanh_scores(s, cs, big);
+      }
       if constexpr (BIAS) {
-        pos_far = (float)(pos - key0 - 4 * half);
+        const float pos_far = (float)(pos - key0 - 4 * half);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -258,7 +311,7 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
             s[t][e] = __builtin_fmaf(-slope2, far, s[t][e] * to_log2);
           }
       }
-      if (!wk.whole(key0, key0 + KB)) {
+      if (!whole) {
         const uint32_t first = (uint32_t)(key0 + 4 * half - mask.x), len = (uint32_t)(mask.y - mask.x);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -266,55 +319,51 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
           for (int e = 0; e < 16; ++e)
             if (first + (uint32_t)(t * 32 + 8 * (e / 4) + e % 4) >= len) s[t][e] = -INFINITY;
       }
-      float bm = -INFINITY;
+      // the lazy maximum of flash_fwd; a row that sees nothing yet has base 0 and weights of 0.  A capped score is at
+      // most its |x| scale, whose maximum is at hand: it mostly says that no row's maximum moves.
+      base = m;
+      if (!CAP || BIAS || !__all(pair_max(big) * cs.sl2 <= m + 8.0f)) {
+        float bm = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) bm = fmaxf(bm, s[t][e]);
-      bm = pair_max(bm);
-      if constexpr (!BIAS) bm *= to_log2;  // with it s is in log2 units already
-      // the lazy maximum of flash_fwd; a row that sees nothing yet has base 0 and weights of 0
-      const bool move = bm > m + 8.0f;
-      const float mn = move ? bm : m;
-      const float corr = (m == -INFINITY) ? 0.f : fast_exp2(m - mn);
-      const float base = weight_base(mn);
-      float rs = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = fast_exp2(BIAS ? s[t][e] - base : __builtin_fmaf(s[t][e], to_log2, -base));
-          s[t][e] = p;
-          rs += p;
-        }
-      rs = pair_sum(rs);
-      lsum = lsum * corr + rs;
-      m = mn;
-      if (__any(move)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[dt][e] *= corr;
-      }
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if constexpr (EXACT) {
-          bf16x8 part[3], vfr[DT];
-          if (kk % 2) acc_rows_to_b_parts<8>(s[kk / 2], part);
-          else acc_rows_to_b_parts<0>(s[kk / 2], part);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) vfr[dt] = frag_cols<HD>(Vs, dt * 32, kk * 16);
-#pragma unroll
-          for (int k = 2; k >= 0; --k)
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[dt], part[k], o[dt], 0, 0, 0);
-        } else {
-          const bf16x8 pf = (kk % 2) ? acc_rows_to_b<8>(s[kk / 2]) : acc_rows_to_b<0>(s[kk / 2]);
+          for (int e = 0; e < 16; ++e) bm = fmaxf(bm, s[t][e]);
+        bm = pair_max(bm);
+        if constexpr (!BIAS) bm *= to_log2;  // with it s is in log2 units already
+        const bool move = bm > m + 8.0f;
+        const float mn = move ? bm : m;
+        const float corr = (m == -INFINITY) ? 0.f : fast_exp2(m - mn);
+        base = weight_base(mn);
+        m = mn;
+        lsum *= corr;
+        if (__any(move)) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Vs, dt * 32, kk * 16), pf, o[dt], 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[dt][e] *= corr;
         }
       }
+      weights(std::integral_constant<int, 0>{});
+      static_for<4>([&](auto KK) {
+        constexpr int kk = KK;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kk + 1 < 4) weights(std::integral_constant<int, kk + 1>{});
+#pragma unroll
+        for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[kk % 2][dt], part[kk % 2][k], o[dt], 0, 0, 0);
+        if constexpr (kk + 1 < 4) {
+          static_for<NP * DT>([&](auto I) {
+            constexpr int i = I;
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
+            if constexpr (i < DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // a fragment's LDS reads
+            __builtin_amdgcn_sched_group_barrier(0x002, EXACT ? 10 : 18, 0);  // vector work
+          });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      lsum += pair_sum(rs[0] + rs[1]);
     }
   }
   block_barrier();  // every wave is done with the last tile: the ring becomes the output staging
@@ -549,6 +598,18 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
   const int myq = qb * QB + wave * 32 + col, i = min(myq, a.Sq - 1);
   const bool valid = myq < a.Sq;
   const int64_t row0 = (int64_t)b * a.Sq;
+  bf16x8 qf[KS], df[KS];
+  {
+    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
+    const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+      df[ks] = *reinterpret_cast<const bf16x8*>(d + ks * 16);
+    }
+  }
+  const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
+  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
   const int2 mask = seen_keys_kept(a, row0 + i);
   const WaveKeys wk(mask, valid);
   int blo, bhi;  // the block's keys
@@ -566,18 +627,6 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
     TT::issue(kbase, a.k.row, blo + t * KB, bhi, lds_addr(st));
     TT::issue(vbase, a.v.row, blo + t * KB, bhi, lds_addr(st + L::TSZ));
   };
-  bf16x8 qf[KS], df[KS];
-  {
-    const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row + 8 * half;
-    const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
-      df[ks] = *reinterpret_cast<const bf16x8*>(d + ks * 16);
-    }
-  }
-  const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
-  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
   const CapScale cs(a);
   float slope2 = 0.f;
   int64_t pos = 0;
@@ -585,10 +634,10 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
     slope2 = a.slopes[h] * LOG2E;
     pos = position(a, b, i);
   }
-  wait_vm_lds<0>();  // register loads done before the ring starts
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
     if (s < ntile) issue(s);
+  wait_vm_lds<0>();  // as in the forward
   f32x16 dq[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -604,10 +653,6 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
     if (key0 < wk.hi && key0 + KB > wk.lo) {
       // as in attention_mfma.hip: S and dP of both 32-key sub-tiles, then the softmax and the dQ products of each
       f32x16 s[2], dp[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) { s[t][e] = 0.f; dp[t][e] = 0.f; }
       if constexpr (HD == 128) {
         bf16x8 fk[2][2], fv[2][2];
 #pragma unroll
@@ -627,8 +672,8 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], s[t], 0, 0, 0);
-            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[c][t], df[ks], dp[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[c][t], qf[ks], ks ? s[t] : f32x16{}, 0, 0, 0);
+            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[c][t], df[ks], ks ? dp[t] : f32x16{}, 0, 0, 0);
           }
           if constexpr (ks + 1 < KS) {
             static_for<4>([&](auto) {
@@ -643,11 +688,11 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ks, t * 32, ks * 16), qf[ks], s[t], 0, 0, 0);
-            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Vs, t * 32, ks * 16), df[ks], dp[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ks, t * 32, ks * 16), qf[ks], ks ? s[t] : f32x16{}, 0, 0, 0);
+            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Vs, t * 32, ks * 16), df[ks], ks ? dp[t] : f32x16{}, 0, 0, 0);
           }
       }
-      if constexpr (CAP) tanh_scores(s, cs);
+      if constexpr (CAP) tanh_scores(s, cs, largest(s));
       const float base_far = BIAS ? (float)(pos - key0 - 4 * half) : 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -761,10 +806,10 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
       vf[ks] = *reinterpret_cast<const bf16x8*>(v + ks * 16);
     }
   }
-  wait_vm_lds<0>();
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
     if (item.it0 + s < item.nit) issue(item.it0 + s);
+  wait_vm_lds<0>();
   const CapScale cs(a);
   f32x16 dk[DT], dv[DT];
 #pragma unroll
@@ -789,13 +834,11 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
     for (int t = 0; t < 2; ++t) {
       f32x16 s[1], dp;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) { s[0][e] = 0.f; dp[e] = 0.f; }
-#pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Qs, t * 32, ks * 16), kf[ks], s[0], 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ds, t * 32, ks * 16), vf[ks], dp, 0, 0, 0);
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Qs, t * 32, ks * 16), kf[ks], ks ? s[0] : f32x16{}, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ds, t * 32, ks * 16), vf[ks], ks ? dp : f32x16{}, 0, 0, 0);
       }
-      if constexpr (CAP) tanh_scores(s, cs);
+      if constexpr (CAP) tanh_scores(s, cs, largest(s));
       const float base_far = (float)far0;
       mask_unseen<HD>(s[0], Qs, t * 32, mykey);
 #pragma unroll
@@ -880,6 +923,13 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
       vf[ks] = *reinterpret_cast<const bf16x8*>(v + ks * 16);
     }
   }
+  if (item.it0 < item.nit) {
+    f.h = item.kvh * group + item.it0 / item.tiles;
+    f.q0 = item.qlo + item.it0 % item.tiles * KB;
+    f.slot = 0;
+    ranges();
+    static_for<2 * TT::PER + 1>(fetch);
+  }
   wait_vm_lds<0>();
   const CapScale cs(a);
   const int64_t first = BIAS ? position(a, b, 0) - mykey + 4 * half : 0;
@@ -914,8 +964,6 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     };
     if constexpr (SM) stat(std::integral_constant<int, 0>{});
     if constexpr (SC) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) { s[T][e] = 0.f; dp[T][e] = 0.f; }
       fq[0] = frag_rows<HD>(Qr, T * 32, 0);
       fd[0] = frag_rows<HD>(Dr, T * 32, 0);
     }
@@ -939,7 +987,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
       // four MFMAs, each followed by a quarter of the vector work
       constexpr int e0 = 2 * g, e1 = e0 + 1, lb = g / 2 % 2;
       float x0, x1, y0, y1;
-      if constexpr (SC) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[c], kf[g], s[T], 0, 0, 0);
+      if constexpr (SC) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[c], kf[g], g ? s[T] : f32x16{}, 0, 0, 0);
       if constexpr (SM) {
         x0 = __builtin_fmaf(s[U][e0], CAP ? cs.out : cs.sl2, l4[lb][e0 % 4]);
         x1 = __builtin_fmaf(s[U][e1], CAP ? cs.out : cs.sl2, l4[lb][e1 % 4]);
@@ -956,7 +1004,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
         pin(x0, x1);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (SC) dp[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[c], vf[g], dp[T], 0, 0, 0);
+      if constexpr (SC) dp[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[c], vf[g], g ? dp[T] : f32x16{}, 0, 0, 0);
       if constexpr (SM) {
         y0 = dp[U][e0] - d4[lb][e0 % 4];
         y1 = dp[U][e1] - d4[lb][e1 % 4];
@@ -986,7 +1034,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     constexpr int U = T_ ^ 1;
     if constexpr (CAP) {
       f32x16(&u)[1] = reinterpret_cast<f32x16(&)[1]>(s[U]);
-      tanh_scores(u, cs);
+      tanh_scores(u, cs, largest(u));
     }
     mask_unseen<HD>(s[U], stats, U * 32, mykey);
     step(T_, SC_, std::true_type{}, PV_, FE_, rows, stats, sq0, slope2, cols);
@@ -997,11 +1045,6 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
   };
   auto slope_of = [&](int h) { return BIAS ? a.slopes[h] * LOG2E : 0.f; };
   if (item.it0 < item.nit) {
-    f.h = item.kvh * group + item.it0 / item.tiles;
-    f.q0 = item.qlo + item.it0 % item.tiles * KB;
-    f.slot = 0;
-    ranges();
-    static_for<2 * TT::PER + 1>(fetch);
     const bf16 *cur = ring, *prev;
     int qc = f.q0, qp;  // first queries of the stages cur and prev, and the slopes of their heads
     float mc = slope_of(f.h), mp;

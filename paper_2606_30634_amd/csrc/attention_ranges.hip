@@ -26,6 +26,11 @@ namespace {
 
 constexpr int MAX_SPLITS = 256;  // shares of an item's keys
 
+// whether a type and head dimension run on the bf16 matrix cores, whose kernels keep statistics in log2 units
+template <typename T, int HD>
+constexpr bool LOG2 = sizeof(T) == 2 && HD != 32;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
 // Score of x = scale q.k at distance `far` (x itself without cap and slopes)
 struct Score {
   float cap, inv_cap, slope;
@@ -49,7 +54,7 @@ __device__ __forceinline__ int acc_row(int e) { return 8 * (e / 4) + 4 * (thread
 
 // One block per (32 queries, query head, sequence, share of their keys)
 template <typename T, int HD>
-__global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a) {
+__global__ void __launch_bounds__(NW * 64, HD == 128 ? 1 : HD == 64 ? 2 : 3) range_fwd(RangeArgs a) {
   __shared__ float red[NW * WAVE_LDS<HD>];
   const int nt = (a.Sq + TR - 1) / TR;
   int64_t id = blockIdx.x;
@@ -82,6 +87,8 @@ __global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a)
   auto tile = [&](int k0, auto edge) {
     RowFrag<HD> kf;
     kf.load(kp, min(k0 + lane % 32, wk.hi - 1), a.k.row);
+    ColFrag<HD> vf;  // on its way while the scores are formed
+    vf.load(vp, k0, wk.hi - 1, a.v.row);
     f32x16 s = rows_product<HD>(kf, qf);  // rows: keys; column: this lane's query
     const float base_far = (float)(pos - k0);
     float mt = -INFINITY, g;
@@ -111,7 +118,7 @@ __global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a)
         return;
       }
     }
-    cols_product<HD>(o, vp, k0, wk.hi - 1, a.v.row, s);
+    vf.product(o, s);
   };
   for (int t = t0 + wave; t < t1; t += NW) {
     const int k0 = wk.lo + t * TR;
@@ -148,8 +155,8 @@ __global__ void __launch_bounds__(NW * 64, fwd_waves(HD)) range_fwd(RangeArgs a)
 
 // The shares of a row (b, i, h) joined, a block per row: HD / 4 lanes per share, the shares spread over the block, so
 // that a row of many shares takes a few round trips to memory and not one per share (16 rows of 16 shares: 5.6 -> JOIN
-// us).  LOG2: the maxima are in log2 units (the bf16 kernels').
-template <typename T, int HD, bool LOG2>
+// us).
+template <typename T, int HD>
 __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   constexpr int LR = HD / 4, NG = 256 / LR;  // lanes of a share, shares at a time
   __shared__ f32x4 sum[256];
@@ -163,7 +170,7 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   if (t % 64 == 0) top[t / 64] = m;
   __syncthreads();
   const float base = weight_base(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-  const float w = LOG2 ? exp2f(ml.x - base) : expf(ml.x - base);
+  const float w = LOG2<T, HD> ? exp2f(ml.x - base) : expf(ml.x - base);
   weight[t] = w;
   const float l = wave_sum(w * ml.y);
   if (t % 64 == 0) tot[t / 64] = l;
@@ -181,43 +188,13 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   if (a.o32) st4(a.o32 + r * HD + c, o);
   if (c == 0) {
     const int64_t row = r / a.Hq, b = row / a.Sq;
-    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2 ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
+    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2<T, HD> ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
   }
 }
 
-// delta_i = dO_i.o_i per (sequence, head, query): HD / 4 lanes per row; and the keys each query sees
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) range_prep(RangeArgs a) {
-  constexpr int LR = HD / 4;
-  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;  // (b, i, h)
-  const int c = (threadIdx.x % LR) * 4;
-  const bool in = r < (int64_t)a.B * a.Sq * a.Hq;
-  const int64_t row = r / a.Hq;
-  const int h = (int)(r % a.Hq), b = (int)(row / a.Sq), i = (int)(row % a.Sq);
-  float s = 0.f;
-  if (in) {
-    const f32x4 d = ld4(rows_of<T>(a.dout, b, h) + (int64_t)i * a.dout.row + c);
-    const int64_t at = b * a.ob + i * a.orow + h * a.oh + c;
-    const f32x4 o = a.o32 ? ld4(a.o32 + at) : ld4((const T*)a.o + at);
-    s = (o[0] * d[0] + o[1] * d[1]) + (o[2] * d[2] + o[3] * d[3]);
-  }
-#pragma unroll
-  for (int k = 1; k < LR; k <<= 1) s += __shfl_xor(s, k, WAVE);
-  if (!in || c) return;
-  a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
-  const float lse = a.lse[((int64_t)b * a.Hq + h) * a.Sq + i];
-  a.nlse2[((int64_t)b * a.Hq + h) * a.Sq + i] = -1.4426950408889634f * weight_base(lse);
-  if (h == 0) {
-    const int2 k = seen_keys(a, b, i);
-    a.seen_lo[row] = k.x;
-    a.seen_len[row] = k.y - k.x;
-  }
-}
-
-// [x, y): the first and last query that see a key of tile t of `width` keys, one block per (tile, sequence)
-__global__ void __launch_bounds__(256) range_plan(RangeArgs a, int width, int ntile) {
+// [x, y): the first and last query that see a key of tile t of `width` keys
+__device__ __forceinline__ void plan_tile(const RangeArgs& a, int width, int ntile, int t, int b) {
   __shared__ int first[4], last[4];
-  const int t = blockIdx.x % ntile, b = blockIdx.x / ntile;
   const int k0 = t * width, k1 = min(k0 + width, a.Sk);
   int lo = INT32_MAX, hi = 0;
   for (int i = threadIdx.x; i < a.Sq; i += 256) {
@@ -240,7 +217,42 @@ __global__ void __launch_bounds__(256) range_plan(RangeArgs a, int width, int nt
       lo = min(lo, first[w]);
       hi = max(hi, last[w]);
     }
-    a.sees[blockIdx.x] = lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+    a.sees[(int64_t)b * ntile + t] = lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+  }
+}
+
+// What the backward needs first, in one launch: a block per (tile of `width` keys, sequence) for the queries that see
+// it; then delta_i = dO_i.o_i and the other statistics per (sequence, head, query), HD / 4 lanes per row.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_prep(RangeArgs a, int width, int ntile) {
+  constexpr int LR = HD / 4;
+  const int nplan = ntile * a.B;
+  if ((int)blockIdx.x < nplan) {
+    plan_tile(a, width, ntile, blockIdx.x % ntile, blockIdx.x / ntile);
+    return;
+  }
+  const int64_t r = ((int64_t)(blockIdx.x - nplan) * 256 + threadIdx.x) / LR;  // (b, i, h)
+  const int c = (threadIdx.x % LR) * 4;
+  const bool in = r < (int64_t)a.B * a.Sq * a.Hq;
+  const int64_t row = r / a.Hq;
+  const int h = (int)(r % a.Hq), b = (int)(row / a.Sq), i = (int)(row % a.Sq);
+  float s = 0.f;
+  if (in) {
+    const f32x4 d = ld4(rows_of<T>(a.dout, b, h) + (int64_t)i * a.dout.row + c);
+    const int64_t at = b * a.ob + i * a.orow + h * a.oh + c;
+    const f32x4 o = a.o32 ? ld4(a.o32 + at) : ld4((const T*)a.o + at);
+    s = (o[0] * d[0] + o[1] * d[1]) + (o[2] * d[2] + o[3] * d[3]);
+  }
+#pragma unroll
+  for (int k = 1; k < LR; k <<= 1) s += __shfl_xor(s, k, WAVE);
+  if (!in || c) return;
+  a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
+  const float lse = weight_base(a.lse[((int64_t)b * a.Hq + h) * a.Sq + i]);
+  a.nlse[((int64_t)b * a.Hq + h) * a.Sq + i] = LOG2<T, HD> ? -1.4426950408889634f * lse : -lse;
+  if (h == 0) {
+    const int2 k = seen_keys(a, b, i);
+    a.seen_lo[row] = k.x;
+    a.seen_len[row] = k.y - k.x;
   }
 }
 
@@ -260,7 +272,7 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int 
 #pragma unroll
   for (int i = 0; i < HD / 8; ++i) qf.v[i] *= a.scale;
   const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + qc;
-  const float lse = weight_base(a.lse[sidx]), dl = a.delta[sidx];
+  const float nl = a.nlse[sidx], dl = a.delta[sidx];
   f32x16 dq[HD / 32];
 #pragma unroll
   for (int dt = 0; dt < HD / 32; ++dt)
@@ -279,7 +291,7 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int 
     for (int e = 0; e < 16; ++e) {
       float g;
       const float x = score(s[e], base_far - (float)acc_row(e), g);
-      s[e] = !edge || sees(mask, k0 + acc_row(e)) ? expf(x - lse) * (dp[e] - dl) * g : 0.f;
+      s[e] = !edge || sees(mask, k0 + acc_row(e)) ? expf(x + nl) * (dp[e] - dl) * g : 0.f;
     }
     if (plain) cols_product<HD>(dq, kp, k0, wk.hi - 1, a.k.row, s);
     else cols_product_seen<HD>(dq, kp, k0, a.k.row, s, red + wave * WAVE_LDS<HD>, [&](int r) { return sees(mask, k0 + r); });
@@ -293,11 +305,12 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int 
   store_rows<HD>(red, a.scale, rows_out<T>(a.dq, b, h), a.dq.row, q0, a.Sq, a.rope_cos, a.rope_sin);
 }
 
-// dk and dv of 32 keys of key/value head kvh, summed over its query heads
+// dk and dv of 32 keys of key/value head kvh, summed over its query heads: the share `split` of the tiles of the
+// queries that see one of them
 template <typename T, int HD>
-__device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, int b, float* red) {
+__device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int split, int kvh, int b, float* red) {
   const int k0 = kb * TR, group = a.Hq / a.Hkv;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, key = k0 + lane % 32, kc = min(key, a.Sk - 1);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, half = lane / 32, key = k0 + lane % 32, kc = min(key, a.Sk - 1);
   RowFrag<HD> kf, vf;
   kf.load(rows_of<T>(a.k, b, kvh), kc, a.k.row);
   vf.load(rows_of<T>(a.v, b, kvh), kc, a.v.row);
@@ -310,33 +323,44 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, i
     for (int e = 0; e < 16; ++e) { dk[dt][e] = 0.f; dv[dt][e] = 0.f; }
   const int2 by = a.sees[(int64_t)b * ((a.Sk + TR - 1) / TR) + kb];
   const int nt = (by.y - by.x + TR - 1) / TR;
-  const int64_t row0 = (int64_t)b * a.Sq;
-  for (int64_t it = wave; it < (int64_t)group * nt; it += NW) {
+  const int64_t row0 = (int64_t)b * a.Sq, all = (int64_t)group * nt;
+  const int64_t it1 = all * (split + 1) / a.nsplit;
+  for (int64_t it = all * split / a.nsplit + wave; it < it1; it += NW) {
     const int h = kvh * group + (int)(it / nt), q0 = by.x + (int)(it % nt) * TR, ql = by.y - 1;
     const T* qp = rows_of<T>(a.q, b, h);
     const T* dp_ = rows_of<T>(a.dout, b, h);
-    const int64_t sb = ((int64_t)b * a.Hq + h) * a.Sq;
+    const int64_t sb = ((int64_t)b * a.Hq + h) * a.Sq + q0;
     const int qr = min(q0 + lane % 32, ql);
     const Score score(a, h);
+    RowFrag<HD> f;
+    f.load(qp, qr, a.q.row);
     const int2 mine = seen_keys_kept(a, row0 + qr);
     // every key of the block is seen by every query of the tile
     const bool whole = q0 + TR <= by.y && __all(mine.x <= k0 && k0 + TR <= mine.y);
-    RowFrag<HD> f;
-    f.load(qp, qr, a.q.row);
     const bool plain_q = whole || f.finite();
     f32x16 p = rows_product<HD>(f, kf);  // rows: queries; column: this lane's key
+    // the rows' statistics, four consecutive rows at a time (the arrays end with TR elements of room)
+    f32x4 nl[4], dl[4];
+    i32x4 lo[4], len[4];
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const int r = 8 * e4 + 4 * half;
+      __builtin_memcpy(&nl[e4], a.nlse + sb + r, 16);
+      __builtin_memcpy(&dl[e4], a.delta + sb + r, 16);
+      __builtin_memcpy(&lo[e4], a.seen_lo + row0 + q0 + r, 16);
+      __builtin_memcpy(&len[e4], a.seen_len + row0 + q0 + r, 16);
+    }
     f.load(dp_, qr, a.dout.row);
     const bool plain_d = whole || f.finite();
     f32x16 ds = rows_product<HD>(f, vf);
     const float base_far = (float)(position(a, b, q0) - key);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int q = q0 + acc_row(e), qc = min(q, ql);
-      const bool on = q <= ql && sees(seen_keys_kept(a, row0 + qc), key);
+      const bool on = q0 + acc_row(e) <= ql && (uint32_t)(key - lo[e / 4][e % 4]) < (uint32_t)len[e / 4][e % 4];
       float g;
       const float x = score(p[e], base_far + (float)acc_row(e), g);
-      p[e] = on ? expf(x - weight_base(a.lse[sb + qc])) : 0.f;
-      ds[e] = on ? p[e] * (ds[e] - a.delta[sb + qc]) * g : 0.f;
+      p[e] = on ? expf(x + nl[e / 4][e % 4]) : 0.f;
+      ds[e] = on ? p[e] * (ds[e] - dl[e / 4][e % 4]) * g : 0.f;
     }
     auto on = [&](int r) { return q0 + r <= ql && sees(seen_keys_kept(a, row0 + min(q0 + r, ql)), key); };
     float* tmp = red + wave * WAVE_LDS<HD>;
@@ -345,13 +369,18 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int kvh, i
     if (plain_q) cols_product<HD>(dk, qp, q0, ql, a.q.row, ds);
     else cols_product_seen<HD>(dk, qp, q0, a.q.row, ds, tmp, on);
   }
+  const bool parts = a.nsplit > 1;
+  const int kvd = a.Hkv * HD;
+  float* part = a.part + ((int64_t)split * 2 * a.B + b) * a.Sk * kvd + kvh * HD;
   put_partial<HD>(red, dk, 1.0f);
   __syncthreads();
-  store_rows<HD>(red, a.scale, rows_out<T>(a.dk, b, kvh), a.dk.row, k0, a.Sk, a.rope_cos, a.rope_sin);
+  if (parts) store_rows<HD>(red, 1.0f, part, kvd, k0, a.Sk, nullptr, nullptr);
+  else store_rows<HD>(red, a.scale, rows_out<T>(a.dk, b, kvh), a.dk.row, k0, a.Sk, a.rope_cos, a.rope_sin);
   __syncthreads();
   put_partial<HD>(red, dv, 1.0f);
   __syncthreads();
-  store_rows<HD>(red, 1.0f, rows_out<T>(a.dv, b, kvh), a.dv.row, k0, a.Sk, nullptr, nullptr);
+  if (parts) store_rows<HD>(red, 1.0f, part + (int64_t)a.B * a.Sk * kvd, kvd, k0, a.Sk, nullptr, nullptr);
+  else store_rows<HD>(red, 1.0f, rows_out<T>(a.dv, b, kvh), a.dv.row, k0, a.Sk, nullptr, nullptr);
 }
 
 // dk/dv blocks and dq blocks in one launch
@@ -359,18 +388,63 @@ template <typename T, int HD>
 __global__ void __launch_bounds__(NW * 64, bwd_waves(HD)) range_bwd(RangeArgs a) {
   __shared__ float red[NW * WAVE_LDS<HD>];
   const int nk = (a.Sk + TR - 1) / TR, nq = (a.Sq + TR - 1) / TR;
-  const int64_t nkv = (int64_t)nk * a.Hkv * a.B;
+  const int64_t nkv = (int64_t)nk * a.nsplit * a.Hkv * a.B;
   int64_t id = blockIdx.x;
   if (id < nkv) {
+    const int split = id % a.nsplit;
+    id /= a.nsplit;
     const int kb = id % nk;
     id /= nk;
-    range_dkv<T, HD>(a, kb, (int)(id % a.Hkv), (int)(id / a.Hkv), red);
+    range_dkv<T, HD>(a, kb, split, (int)(id % a.Hkv), (int)(id / a.Hkv), red);
   } else {
     id -= nkv;
     const int qb = nq - 1 - (int)(id % nq);
     id /= nq;
     range_dq<T, HD>(a, qb, (int)(id % a.Hq), (int)(id / a.Hq), red);
   }
+}
+
+// dk and dv of split items: the partial sums added in order, 8 columns per thread
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_dkv_join(RangeArgs a) {
+  constexpr int HH = HD / 2;
+  const int kvd = a.Hkv * HD;
+  const int64_t n = (int64_t)a.B * a.Sk * kvd, c = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (c >= 2 * n) return;
+  const bool isv = c >= n;
+  const int64_t e = isv ? c - n : c, row = e / kvd;
+  const int kvh = (int)(e % kvd) / HD, d = (int)(e % HD), b = (int)(row / a.Sk), key = (int)(row % a.Sk);
+  auto sum = [&](int64_t o, float* v) {  // elements o .. o + 7 of every share
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = 0.f;
+    for (int s = 0; s < a.nsplit; ++s) {
+      const float* p = a.part + 2 * n * s + o;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { v[q] += lo[q]; v[q + 4] += hi[q]; }
+    }
+  };
+  float v[8];
+  sum(c, v);
+  if (!isv) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= a.scale;
+    if (a.rope_cos) {
+      const bool first = d < HH;
+      float p[8];
+      sum(first ? c + HH : c - HH, p);
+      const int64_t t = (int64_t)key * HH + d % HH;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float y = p[q] * a.scale, cs = a.rope_cos[t + q], sn = a.rope_sin[t + q];
+        v[q] = first ? v[q] * cs + y * sn : v[q] * cs - y * sn;
+      }
+    }
+  }
+  const HeadRows& out = isv ? a.dv : a.dk;
+  T* o = rows_out<T>(out, b, kvh) + (int64_t)key * out.row + d;
+  st4(o, f32x4{v[0], v[1], v[2], v[3]});
+  st4(o + 4, f32x4{v[4], v[5], v[6], v[7]});
 }
 
 // ------------------------------------------------------------------------------------------ key ranges
@@ -535,7 +609,7 @@ int fwd_splits(bool bf, const RangeArgs& a) {
   const bool mm = mfma(bf, a.hd);
   const int64_t items = mm ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
   if (items == 0) return 1;
-  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 128 : 256));
+  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 64 : 256));
   const int64_t many = a.Sq <= TR ? std::min<int64_t>(4096 / items, a.Sk / 1024) : 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>(MAX_SPLITS, std::max(few, many)));
 }
@@ -557,13 +631,21 @@ void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    if constexpr (sizeof(T) == 2 && HD != 32) range_mfma_fwd(a, st);
+    if constexpr (LOG2<T, HD>) range_mfma_fwd(a, st);
     else range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
-    if (a.nsplit > 1) range_join<T, HD, sizeof(T) == 2 && HD != 32><<<(unsigned)n, 256, 0, st>>>(a);
+    if (a.nsplit > 1) range_join<T, HD><<<(unsigned)n, 256, 0, st>>>(a);
   });
 }
 
 namespace {
+
+// Shares of a dk/dv block's query tiles: a block of few walks them one after another, a wave an iteration of some 8 us
+// of latency.  Towards 512 blocks, keeping two iterations to a wave of the longest (2 x 333 tokens, 8 heads of 32 on 2: 52
+// -> SPLIT us).
+int dkv_splits(const RangeArgs& a) {
+  const int64_t items = cdiv(a.Sk, TR) * a.Hkv * a.B, tiles = (int64_t)(a.Hq / a.Hkv) * cdiv(a.Sq, TR);
+  return items == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({8, 512 / items, tiles / (2 * NW)}));
+}
 
 // The backward's workspace at p (null: its size alone)
 size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
@@ -575,12 +657,12 @@ size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
   };
   const bool mm = mfma(bf, a.hd);
   const int64_t rows = (int64_t)a.B * a.Sq;
-  a.delta = (float*)take(rows * a.Hq * 4);
-  a.nlse2 = (float*)take(rows * a.Hq * 4);
-  a.seen_lo = (int32_t*)take(rows * 4);
-  a.seen_len = (int32_t*)take(rows * 4);
+  a.delta = (float*)take((rows * a.Hq + TR) * 4);
+  a.nlse = (float*)take((rows * a.Hq + TR) * 4);
+  a.seen_lo = (int32_t*)take((rows + TR) * 4);
+  a.seen_len = (int32_t*)take((rows + TR) * 4);
   a.sees = (int2*)take(a.B * cdiv(a.Sk, mm ? range_mfma_keys() : TR) * 8);
-  a.nsplit = mm ? range_mfma_dkv_splits(a) : 1;
+  a.nsplit = mm ? range_mfma_dkv_splits(a) : dkv_splits(a);
   a.part = a.nsplit > 1 ? (float*)take(2 * (int64_t)a.nsplit * a.B * a.Sk * a.Hkv * a.hd * 4) : nullptr;
   return n;
 }
@@ -595,15 +677,16 @@ size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   bwd_layout(bf, a, (char*)ws);
   const int width = mfma(bf, a.hd) ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
-  if (a.Sk > 0) range_plan<<<(unsigned)((int64_t)ntile * a.B), 256, 0, st>>>(a, width, ntile);
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    if (a.Sq > 0)
-      range_prep<T, HD><<<(unsigned)cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256), 256, 0, st>>>(a);
-    const int64_t blocks = cdiv(a.Sk, TR) * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
-    if constexpr (sizeof(T) == 2 && HD != 32) range_mfma_bwd(a, st);
+    const int64_t prep = (int64_t)ntile * a.B + cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256);
+    range_prep<T, HD><<<(unsigned)prep, 256, 0, st>>>(a, width, ntile);
+    const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
+    if constexpr (LOG2<T, HD>) range_mfma_bwd(a, st);
     else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
+    if (a.nsplit > 1)
+      range_dkv_join<T, HD><<<(unsigned)cdiv(2 * (int64_t)a.B * a.Sk * a.Hkv * HD / 8, 256), 256, 0, st>>>(a);
   });
 }
 

@@ -470,7 +470,7 @@ __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, i
   const CapScale c(a);
   const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
   const int64_t pos = position(a, b, i), sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
-  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
+  const float nl = a.nlse[sidx], dl = a.delta[sidx];
   float acc[HD / 64];
 #pragma unroll
   for (int x = 0; x < HD / 64; ++x) acc[x] = 0.f;
@@ -534,7 +534,7 @@ __device__ __forceinline__ void dkv_row_again(const RangeArgs& a, const KeyItem&
     const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
     float g;
     const float p = fast_exp2(score2(row_dot<HD>(q + (int64_t)i * a.q.row, k), a, c, slope2, (float)(position(a, b, i) - key), g) +
-                              a.nlse2[sidx]);
+                              a.nlse[sidx]);
     const float ds = p * (row_dot<HD>(d + (int64_t)i * a.dout.row, v) - a.delta[sidx]) * g;
     for (uint64_t left = __ballot(on); left; left &= left - 1) {
       const int t = __builtin_ctzll(left);
@@ -609,7 +609,7 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
     }
   }
   const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
-  const float nl = a.nlse2[sidx], dl = a.delta[sidx];
+  const float nl = a.nlse[sidx], dl = a.delta[sidx];
   const int2 mask = seen_keys_kept(a, row0 + i);
   const WaveKeys wk(mask, valid);
   int blo, bhi;  // the block's keys
@@ -789,7 +789,7 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
     bf16* st = ring + (it % NS) * Q::SZ;
     TT::issue(rows_of<bf16>(a.q, b, h), a.q.row, q0, item.qhi, lds_addr(st));
     TT::issue(rows_of<bf16>(a.dout, b, h), a.dout.row, q0, item.qhi, lds_addr(st + Q::TSZ));
-    const void* v = wu == 0 ? (const void*)(a.nlse2 + ((int64_t)b * a.Hq + h) * a.Sq)
+    const void* v = wu == 0 ? (const void*)(a.nlse + ((int64_t)b * a.Hq + h) * a.Sq)
                   : wu == 1 ? (const void*)(a.delta + ((int64_t)b * a.Hq + h) * a.Sq)
                   : wu == 2 ? (const void*)(a.seen_lo + (int64_t)b * a.Sq) : (const void*)(a.seen_len + (int64_t)b * a.Sq);
     // rows past the last query repeat it (TT::issue), but see no key: their seen_len is 0
@@ -892,7 +892,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     f.q = buffer_range(qh + (int64_t)f.q0 * a.q.row, qh + (int64_t)(item.qhi - 1) * a.q.row + HD);
     f.d = buffer_range(dh + (int64_t)f.q0 * a.dout.row, dh + (int64_t)(item.qhi - 1) * a.dout.row + HD);
     const int64_t rows = wu < 2 ? ((int64_t)b * a.Hq + f.h) * a.Sq : (int64_t)b * a.Sq;
-    const float* v = (wu == 0 ? a.nlse2 : wu == 1 ? a.delta : wu == 2 ? (const float*)a.seen_lo : (const float*)a.seen_len) + rows;
+    const float* v = (wu == 0 ? a.nlse : wu == 1 ? a.delta : wu == 2 ? (const float*)a.seen_lo : (const float*)a.seen_len) + rows;
     f.r = buffer_range(v + f.q0, v + item.qhi);
     f.lds = lds_addr(ring + f.slot * Q::SZ) + (uint32_t)wu * 1024u;
   };
@@ -1137,50 +1137,6 @@ __global__ void __launch_bounds__(NT, 2) range_flash_bwd64(RangeArgs a) {
   }
 }
 
-// dk and dv of split items: the partial sums added in order, 8 columns per thread
-template <int HD>
-__global__ void __launch_bounds__(256) range_dkv_join(RangeArgs a) {
-  constexpr int HH = HD / 2;
-  const int kvd = a.Hkv * HD;
-  const int64_t n = (int64_t)a.B * a.Sk * kvd, c = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
-  if (c >= 2 * n) return;
-  const bool isv = c >= n;
-  const int64_t e = isv ? c - n : c, row = e / kvd;
-  const int kvh = (int)(e % kvd) / HD, d = (int)(e % HD), b = (int)(row / a.Sk), key = (int)(row % a.Sk);
-  auto sum = [&](int64_t o, float* v) {  // elements o .. o + 7 of every share
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = 0.f;
-    for (int s = 0; s < a.nsplit; ++s) {
-      const float* p = a.part + 2 * n * s + o;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) { v[q] += lo[q]; v[q + 4] += hi[q]; }
-    }
-  };
-  float v[8];
-  sum(c, v);
-  if (!isv) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] *= a.scale;
-    if (a.rope_cos) {
-      const bool first = d < HH;
-      float p[8];
-      sum(first ? c + HH : c - HH, p);
-      const int64_t t = (int64_t)key * HH + d % HH;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float y = p[q] * a.scale, cs = a.rope_cos[t + q], sn = a.rope_sin[t + q];
-        v[q] = first ? v[q] * cs + y * sn : v[q] * cs - y * sn;
-      }
-    }
-  }
-  bf16x8 ov;
-#pragma unroll
-  for (int q = 0; q < 8; ++q) ov[q] = (bf16)v[q];
-  const HeadRows& out = isv ? a.dv : a.dk;
-  *reinterpret_cast<bf16x8*>(rows_out<bf16>(out, b, kvh) + (int64_t)key * out.row + d) = ov;
-}
-
 template <int HD>
 constexpr size_t range_fwd_lds() {
   const size_t out = (size_t)QB * (HD + 4) * 4 + QB * 4;
@@ -1256,9 +1212,4 @@ void range_mfma_bwd(const RangeArgs& a, hipStream_t st) {
       if (nkb) range_flash_dkv128<CAP, BIAS><<<(unsigned)nkb, NT, lds_kv, st>>>(a);
     }
   });
-  if (a.nsplit > 1) {
-    const unsigned blocks = (unsigned)cdiv(2 * (int64_t)a.B * a.Sk * a.Hkv * a.hd / 8, 256);
-    if (a.hd == 64) range_dkv_join<64><<<blocks, 256, 0, st>>>(a);
-    else range_dkv_join<128><<<blocks, 256, 0, st>>>(a);
-  }
 }

@@ -67,21 +67,32 @@ __device__ __forceinline__ f32x16 rows_product(const RowFrag<HD>& a, const RowFr
 
 // acc[dt] (rows 32 dt .. of X^T, columns the block's rows) += X^T W over the 32 tile rows of X, whose
 // weights w sit in an accumulator (rows: tile rows).  Tile row r is row min(row0 + r, last) of X.
+template <int HD>
+struct ColFrag {
+  float f[HD / 32][16];
+  template <typename T>
+  __device__ __forceinline__ void load(const T* x, int row0, int last, int ld) {
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const T* r = x + (int64_t)min(row0 + 8 * (e / 4) + 4 * (lane / 32) + e % 4, last) * ld + lane % 32;
+#pragma unroll
+      for (int dt = 0; dt < HD / 32; ++dt) f[dt][e] = to_f32(r[32 * dt]);
+    }
+  }
+  __device__ __forceinline__ void product(f32x16 (&acc)[HD / 32], const f32x16& w) const {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int dt = 0; dt < HD / 32; ++dt) acc[dt] = mfma2(f[dt][e], w[e], acc[dt]);
+  }
+};
 template <int HD, typename T>
 __device__ __forceinline__ void cols_product(f32x16 (&acc)[HD / 32], const T* x, int row0, int last, int ld,
                                              const f32x16& w) {
-  const int lane = threadIdx.x % 64;
-  float f[HD / 32][16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const T* r = x + (int64_t)min(row0 + 8 * (e / 4) + 4 * (lane / 32) + e % 4, last) * ld + lane % 32;
-#pragma unroll
-    for (int dt = 0; dt < HD / 32; ++dt) f[dt][e] = to_f32(r[32 * dt]);
-  }
-#pragma unroll
-  for (int e = 0; e < 16; ++e)
-#pragma unroll
-    for (int dt = 0; dt < HD / 32; ++dt) acc[dt] = mfma2(f[dt][e], w[e], acc[dt]);
+  ColFrag<HD> f;
+  f.load(x, row0, last, ld);
+  f.product(acc, w);
 }
 
 // The same sum where some column does not see every tile row and a row holds an infinity or a NaN: its

@@ -314,7 +314,7 @@ typedef struct {
 size_t stage_variant_bytes(stage_t* s, const stage_variant_t* v);
 int stage_set_variant(stage_t* s, const stage_variant_t* v, void* workspace, size_t workspace_bytes);
 /* The documents [micro_batch, seq_len] int32 packed in the slot's rows, and their prefixes (uint8 or NULL), for
- * its forwards until they are set again: attention_key_ranges on the stage stream, read by then.  RoPE positions
+ * its forwards until they are set again (attention_key_ranges, read on the stage stream).  RoPE positions
  * run along the row (only their differences count); targets of padding are the caller's (outside the
  * vocabulary: ignored).  A forward of a slot whose documents were never set is refused (STAGE_ESTATE). */
 int stage_set_documents(stage_t* s, int32_t slot, const int32_t* documents, const uint8_t* prefix);

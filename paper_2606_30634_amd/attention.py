@@ -94,9 +94,9 @@ def attention(q, k, v, *, key_start=None, key_end=None, q_start=None, scale: Opt
     params, pq, pk, pv, dev = _params(q, k, v, key_start, key_end, q_start, scale, softcap, slopes)
     b, nq, h, _ = q.shape
     out = out or Attention()
-    if out.o_f32 is not None and not keep_f32:
-        raise ValueError("out.o_f32 needs keep_f32")
     bf = q.dtype is torch.bfloat16
+    if out.o_f32 is not None and not (keep_f32 and bf):
+        raise ValueError("out.o_f32 needs keep_f32, and bfloat16 inputs")
     out = Attention(_out("o", out.o, dev, q.dtype, q.shape), _out("lse", out.lse, dev, _F32, (b, h, nq)),
                     _out("o_f32", out.o_f32, dev, _F32, q.shape) if keep_f32 and bf else None)
     ws, nb = _workspace(workspace, B.attention_workspace_bytes(params), dev)

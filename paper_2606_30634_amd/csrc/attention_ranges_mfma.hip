@@ -10,6 +10,7 @@
 #include "attention_ranges.h"
 #include "attention_tiles.h"
 #include <algorithm>
+#include <atomic>
 
 namespace {
 
@@ -82,6 +83,15 @@ __device__ __forceinline__ float score2(float x, const RangeArgs& a, const CapSc
   return a.slopes ? __builtin_fmaf(-slope2, fabsf(far), x) : x;
 }
 
+// Whether every element of a row held by a wave is a NaN, which nothing added to it changes
+template <int N>
+__device__ __forceinline__ bool all_nan(const float (&x)[N]) {
+  bool nan = true;
+#pragma unroll
+  for (int k = 0; k < N; ++k) nan &= x[k] != x[k];
+  return __all(nan);
+}
+
 // x.y of two rows of a head
 template <int HD>
 __device__ __forceinline__ float row_dot(const bf16* x, const bf16* y) {
@@ -117,7 +127,7 @@ __device__ __forceinline__ void row_again(const RangeArgs& a, const Rows& rows, 
   float o[HD / 64];
 #pragma unroll
   for (int d = 0; d < HD / 64; ++d) o[d] = 0.f;
-  for (int j0 = k_lo; j0 < k_hi; j0 += 64) {
+  for (int j0 = k_lo; j0 < k_hi && !all_nan(o); j0 += 64) {
     const int n = min(64, k_hi - j0), j = j0 + min(lane, n - 1);
     float g;
     const float p = fast_exp2(score2(row_dot<HD>(q, k + (int64_t)j * a.k.row), a, c, slope2, (float)(pos - j), g) - base);
@@ -474,7 +484,7 @@ __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, i
   float acc[HD / 64];
 #pragma unroll
   for (int x = 0; x < HD / 64; ++x) acc[x] = 0.f;
-  for (int j0 = keys.x; j0 < keys.y; j0 += 64) {
+  for (int j0 = keys.x; j0 < keys.y && !all_nan(acc); j0 += 64) {
     const int n = min(64, keys.y - j0), j = j0 + min(lane, n - 1);
     float g;
     const float p = fast_exp2(score2(row_dot<HD>(q, k + (int64_t)j * a.k.row), a, c, slope2, (float)(pos - j), g) + nl);
@@ -524,7 +534,7 @@ __device__ __forceinline__ void dkv_row_again(const RangeArgs& a, const KeyItem&
   float dk[HD / 64], dv[HD / 64];
 #pragma unroll
   for (int x = 0; x < HD / 64; ++x) dk[x] = dv[x] = 0.f;
-  for (int it = it_.it0; it < it_.nit; ++it) {
+  for (int it = it_.it0; it < it_.nit && !(all_nan(dk) && all_nan(dv)); ++it) {
     const int h = it_.kvh * group + it / it_.tiles, q0 = it_.qlo + it % it_.tiles * KB;
     const int i = min(q0 + lane, it_.qhi - 1);
     const bool on = q0 + lane < it_.qhi && sees(seen_keys_kept(a, (int64_t)b * a.Sq + i), key);
@@ -1143,15 +1153,21 @@ constexpr size_t range_fwd_lds() {
   return std::max(Lds<HD>::NS * Lds<HD>::kv_stage, out);
 }
 
-template <typename K>
-void set_lds(K kernel, size_t bytes) {
-  (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+// Allows kernel K its dynamic LDS, once per device
+template <auto K>
+void allow_lds(size_t bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  (void)hipGetDevice(&dev);
+  const uint64_t bit = (uint64_t)1 << (dev % 64);
+  if (done.load() & bit) return;
+  (void)hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  done |= bit;
 }
 
 template <int HD, bool EXACT, bool CAP, bool BIAS>
 void fwd_launch(const RangeArgs& a, int pack, unsigned blocks, hipStream_t st) {
-  static const bool once = (set_lds(range_flash_fwd<HD, EXACT, CAP, BIAS>, range_fwd_lds<HD>()), true);
-  (void)once;
+  allow_lds<range_flash_fwd<HD, EXACT, CAP, BIAS>>(range_fwd_lds<HD>());
   range_flash_fwd<HD, EXACT, CAP, BIAS><<<blocks, NT, range_fwd_lds<HD>(), st>>>(a, pack);
 }
 
@@ -1201,13 +1217,12 @@ void range_mfma_bwd(const RangeArgs& a, hipStream_t st) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
     if (a.hd == 64) {
       constexpr size_t lds = std::max(Lds<64>::dq_bytes(), QueryStage<64>::bytes(ring_stages<64>()));
-      static const bool once = (set_lds(range_flash_bwd64<CAP, BIAS>, lds), true);
-      (void)once;
+      allow_lds<range_flash_bwd64<CAP, BIAS>>(lds);
       range_flash_bwd64<CAP, BIAS><<<(unsigned)(nkb + nqb), NT, lds, st>>>(a);
     } else {
       constexpr size_t lds_kv = QueryStage<128>::bytes(3), lds_q = Lds<128>::dq_bytes();
-      static const bool once = (set_lds(range_flash_dq128<CAP, BIAS>, lds_q), set_lds(range_flash_dkv128<CAP, BIAS>, lds_kv), true);
-      (void)once;
+      allow_lds<range_flash_dq128<CAP, BIAS>>(lds_q);
+      allow_lds<range_flash_dkv128<CAP, BIAS>>(lds_kv);
       if (nqb) range_flash_dq128<CAP, BIAS><<<(unsigned)nqb, NT, lds_q, st>>>(a);
       if (nkb) range_flash_dkv128<CAP, BIAS><<<(unsigned)nkb, NT, lds_kv, st>>>(a);
     }

@@ -135,6 +135,9 @@ class Stage:
             if t.dtype not in types or tuple(t.shape) != shape or t.device != self.arena.device or not t.is_contiguous():
                 raise ValueError(f"{name}: expected a contiguous {types[0]} tensor of shape {shape} on {self.device}")
         B.stage_set_documents(self.handle, slot, documents.data_ptr(), None if prefix is None else prefix.data_ptr())
+        for t in (documents, prefix):
+            if t is not None:
+                t.record_stream(self.stream)
 
     def update(self, t: int, hp: B.UpdateHParams):
         B.delayed_update(self.handle, t, hp)

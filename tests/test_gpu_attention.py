@@ -368,6 +368,30 @@ def test_graphs_streams_and_repeats(bf16, hd):
         assert torch.equal(a, b)
 
 
+def test_captured_without_a_first_call():
+    """Kernel variants no call has used before, captured at once, on the capture's own memory; eager calls of the same
+    variants between the replays."""
+    torch = _torch()
+    from paper_2606_30634_amd import attention as T
+    log("capture")
+    for hd in (64, 128):
+        for Sq, Sk in ((130, 130), (1, 3000)):
+            x, how, _, _ = _case(60 + hd, 1, Sq, Sk, 2, 1, hd, True, "causal", cap=7.0, bias=True)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                f = T.attention(x["q"], x["k"], x["v"], keep_f32=True, **how)
+                d = T.attention_backward(x["q"], x["k"], x["v"], f, x["do"], **how)
+            want = None
+            for _ in range(3):
+                g.replay()
+                torch.cuda.synchronize()
+                got = [t.clone() for t in (f.o, f.lse, f.o_f32, *d)]
+                e = T.attention(x["q"], x["k"], x["v"], keep_f32=True, **how)
+                want = [e.o, e.lse, e.o_f32, *T.attention_backward(x["q"], x["k"], x["v"], e, x["do"], **how)]
+                for a, b in zip(got, want):
+                    assert torch.equal(a, b)
+
+
 RANGE_ROWS = [(1, 1), (3, 2), (2, 7), (5, 64), (2, 513), (4, 2047), (3, 2048), (2, 2049), (2, 4097), (1, 9000)]
 
 

@@ -7,7 +7,7 @@
 //   dk = scale dS^T q and dv = P^T dO, summed over the query heads of a key/value head
 // A query that sees no key has o = 0, lse = -inf and no gradient.
 //
-// These kernels take fp32 (and bf16 of head dimension 32) on the fp32 matrix cores, tiled as in attention.hip:
+// These kernels take fp32, on the fp32 matrix cores, tiled as in attention.hip (bf16: attention_ranges_mfma.hip):
 // a block owns 32 rows of one side, its waves take every fourth tile of 32 rows of the other.  Tiles start at
 // the first key (query) that a row of the block sees and end with the last; a tile that every row sees whole
 // skips the mask.
@@ -15,7 +15,7 @@
 #include "attention_rows.h"
 #include <algorithm>
 
-// attention_ranges_mfma.hip: bf16 of head dimensions 64 and 128
+// attention_ranges_mfma.hip: bf16
 int64_t range_mfma_items(const RangeArgs& a);
 void range_mfma_fwd(const RangeArgs& a, hipStream_t st);
 int range_mfma_keys();  // keys of a dK/dV block
@@ -26,9 +26,9 @@ namespace {
 
 constexpr int MAX_SPLITS = 256;  // shares of an item's keys
 
-// whether a type and head dimension run on the bf16 matrix cores, whose kernels keep statistics in log2 units
-template <typename T, int HD>
-constexpr bool LOG2 = sizeof(T) == 2 && HD != 32;
+// whether a type's kernels (bf16: on the bf16 matrix cores) keep statistics in log2 units
+template <typename T>
+constexpr bool LOG2 = sizeof(T) == 2;
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // Score of x = scale q.k at distance `far` (x itself without cap and slopes)
@@ -153,6 +153,28 @@ __global__ void __launch_bounds__(NW * 64, HD == 128 ? 1 : HD == 64 ? 2 : 3) ran
   if (wave == 0 && lane < TR && q < a.Sq) a.lse[((int64_t)b * a.Hq + h) * a.Sq + q] = base + logf(L);
 }
 
+// One row's sum of the shares s = s0, s0 + step, .. of the elements c .. c + 3, their weights given by weight(s)
+template <int HD, typename F>
+__device__ __forceinline__ f32x4 add_shares(const RangeArgs& a, int64_t r, int c, int s0, int step, F&& weight) {
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = s0; s < a.nsplit; s += step) o += weight(s) * ld4(a.part + (n * s + r) * HD + c);
+  return o;
+}
+template <typename T, int HD>
+__device__ __forceinline__ void store_joined(const RangeArgs& a, int64_t r, int c, f32x4 o, float base, float L) {
+  o *= L == 0.f ? 0.f : 1.0f / L;
+  st4((T*)a.o + r * HD + c, o);
+  if (a.o32) st4(a.o32 + r * HD + c, o);
+  if (c == 0) {
+    const int64_t row = r / a.Hq, b = row / a.Sq;
+    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2<T> ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float share_weight(float m, float base) { return LOG2<T> ? exp2f(m - base) : expf(m - base); }
+
 // The shares of a row (b, i, h) joined, a block per row: HD / 4 lanes per share, the shares spread over the block, so
 // that a row of many shares takes a few round trips to memory and not one per share (16 rows of 16 shares: 5.6 -> JOIN
 // us).
@@ -165,31 +187,50 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   const int t = threadIdx.x, c = (t % LR) * 4;
   float2 ml = make_float2(-INFINITY, 0.f);
   if (t < a.nsplit) ml = a.part_ml[n * t + r];
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
   const float m = wave_max(ml.x);
   if (t % 64 == 0) top[t / 64] = m;
   __syncthreads();
   const float base = weight_base(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-  const float w = LOG2<T, HD> ? exp2f(ml.x - base) : expf(ml.x - base);
+  const float w = share_weight<T>(ml.x, base);
   weight[t] = w;
   const float l = wave_sum(w * ml.y);
   if (t % 64 == 0) tot[t / 64] = l;
   __syncthreads();
-#pragma unroll 4
-  for (int s = t / LR; s < a.nsplit; s += NG) o += weight[s] * ld4(a.part + (n * s + r) * HD + c);
+  f32x4 o = add_shares<HD>(a, r, c, t / LR, NG, [&](int s) { return weight[s]; });
   sum[t] = o;
   __syncthreads();
   if (t >= LR) return;
   const float L = (tot[0] + tot[1]) + (tot[2] + tot[3]);
 #pragma unroll
   for (int g = 1; g < NG; ++g) o += sum[g * LR + t];
-  o *= L == 0.f ? 0.f : 1.0f / L;
-  st4((T*)a.o + r * HD + c, o);
-  if (a.o32) st4(a.o32 + r * HD + c, o);
-  if (c == 0) {
-    const int64_t row = r / a.Hq, b = row / a.Sq;
-    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2<T, HD> ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
+  store_joined<T, HD>(a, r, c, o, base, L);
+}
+
+// The same with a row's shares one after another, HD / 4 lanes per row, for many rows of few shares
+constexpr int FEW_SPLITS = 8;
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_join_few(RangeArgs a) {
+  constexpr int LR = HD / 4;
+  const int64_t n = (int64_t)a.B * a.Sq * a.Hq, r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LR;
+  const int c = (threadIdx.x % LR) * 4;
+  if (r >= n) return;
+  float2 ml[FEW_SPLITS];
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int s = 0; s < FEW_SPLITS; ++s) {
+    ml[s] = s < a.nsplit ? a.part_ml[n * s + r] : make_float2(-INFINITY, 0.f);
+    M = fmaxf(M, ml[s].x);
   }
+  const float base = weight_base(M);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < FEW_SPLITS; ++s) {
+    if (s >= a.nsplit) break;
+    const float w = share_weight<T>(ml[s].x, base);
+    L += w * ml[s].y;
+    o += w * ld4(a.part + (n * s + r) * HD + c);
+  }
+  store_joined<T, HD>(a, r, c, o, base, L);
 }
 
 // [x, y): the first and last query that see a key of tile t of `width` keys
@@ -248,7 +289,7 @@ __global__ void __launch_bounds__(256) range_prep(RangeArgs a, int width, int nt
   if (!in || c) return;
   a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
   const float lse = weight_base(a.lse[((int64_t)b * a.Hq + h) * a.Sq + i]);
-  a.nlse[((int64_t)b * a.Hq + h) * a.Sq + i] = LOG2<T, HD> ? -1.4426950408889634f * lse : -lse;
+  a.nlse[((int64_t)b * a.Hq + h) * a.Sq + i] = LOG2<T> ? -1.4426950408889634f * lse : -lse;
   if (h == 0) {
     const int2 k = seen_keys(a, b, i);
     a.seen_lo[row] = k.x;
@@ -656,18 +697,17 @@ void dispatch(bool bf, int hd, F&& run) {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-bool mfma(bool bf, int hd) { return bf && hd != 32; }
-
-// Shares of a forward item's keys.  Few items: towards 512, two per compute unit, of at least 256 keys (128 on the
-// bf16 matrix cores).  A few queries of each sequence: towards 4096 of at least 1024 keys, since the caches' lengths
-// differ and the longest share ends the launch (16 answers of up to 32768 keys, 128 items: 247 us towards 512, 233
-// towards 2048, 228 towards 4096); with more queries the partial sums would cost more than that.
+// Shares of a forward item's keys.  Few items: towards 512, two per compute unit, of at least 256 keys, or of one tile
+// of 64 on the bf16 matrix cores where each sequence has a few queries, which then wait for little else.  A few
+// queries of many long caches: towards 4096 shares of at least 1024 keys, since the caches' lengths differ and the longest
+// share ends the launch (16 answers of up to 32768 keys, 128 items: 247 us towards 512, 233 towards 2048, 228 towards 4096);
+// with more queries the partial sums would cost more than that.
 int fwd_splits(bool bf, const RangeArgs& a) {
-  const bool mm = mfma(bf, a.hd);
-  const int64_t items = mm ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
+  const int64_t items = bf ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
   if (items == 0) return 1;
-  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (mm ? 64 : 256));
-  const int64_t many = a.Sq <= TR ? std::min<int64_t>(4096 / items, a.Sk / 1024) : 1;
+  const bool short_q = a.Sq <= TR;
+  const int64_t few = std::min<int64_t>(512 / items, a.Sk / (bf && short_q ? 64 : 256));
+  const int64_t many = short_q ? std::min<int64_t>(4096 / items, a.Sk / 1024) : 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>(MAX_SPLITS, std::max(few, many)));
 }
 
@@ -688,9 +728,10 @@ void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    if constexpr (LOG2<T, HD>) range_mfma_fwd(a, st);
+    if constexpr (LOG2<T>) range_mfma_fwd(a, st);
     else range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
-    if (a.nsplit > 1) range_join<T, HD><<<(unsigned)n, 256, 0, st>>>(a);
+    if (a.nsplit > FEW_SPLITS) range_join<T, HD><<<(unsigned)n, 256, 0, st>>>(a);
+    else if (a.nsplit > 1) range_join_few<T, HD><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
   });
 }
 
@@ -712,14 +753,13 @@ size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
     n += up256(bytes);
     return r;
   };
-  const bool mm = mfma(bf, a.hd);
   const int64_t rows = (int64_t)a.B * a.Sq;
   a.delta = (float*)take((rows * a.Hq + TR) * 4);
   a.nlse = (float*)take((rows * a.Hq + TR) * 4);
   a.seen_lo = (int32_t*)take((rows + TR) * 4);
   a.seen_len = (int32_t*)take((rows + TR) * 4);
-  a.sees = (int2*)take(a.B * cdiv(a.Sk, mm ? range_mfma_keys() : TR) * 8);
-  a.nsplit = mm ? range_mfma_dkv_splits(a) : dkv_splits(a);
+  a.sees = (int2*)take(a.B * cdiv(a.Sk, bf ? range_mfma_keys() : TR) * 8);
+  a.nsplit = bf ? range_mfma_dkv_splits(a) : dkv_splits(a);
   a.part = a.nsplit > 1 ? (float*)take(2 * (int64_t)a.nsplit * a.B * a.Sk * a.Hkv * a.hd * 4) : nullptr;
   return n;
 }
@@ -733,14 +773,14 @@ size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
 
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   bwd_layout(bf, a, (char*)ws);
-  const int width = mfma(bf, a.hd) ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
+  const int width = bf ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     const int64_t prep = (int64_t)ntile * a.B + cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256);
     range_prep<T, HD><<<(unsigned)prep, 256, 0, st>>>(a, width, ntile);
     const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
-    if constexpr (LOG2<T, HD>) range_mfma_bwd(a, st);
+    if constexpr (LOG2<T>) range_mfma_bwd(a, st);
     else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
     if (a.nsplit > 1)
       range_dkv_join<T, HD><<<(unsigned)cdiv(2 * (int64_t)a.B * a.Sk * a.Hkv * HD / 8, 256), 256, 0, st>>>(a);

@@ -1,5 +1,4 @@
-// Attention over key ranges (the formulas are in attention_ranges.hip) for bf16 of head dimensions 64 and 128, on
-// the bf16 matrix cores, with the tiles, operand layouts and rings of attention_mfma.hip.
+// Attention over key ranges (the formulas are in attention_ranges.hip) for bf16, on the bf16 matrix cores, with the tiles, operand layouts and rings of attention_mfma.hip.
 //
 // What differs from the causal kernels there: tiles start at the first key that a query of the block sees and end
 // with the last, so nothing else is loaded; every lane owns one query (one key in dK/dV) and keeps its range, and
@@ -92,6 +91,12 @@ __device__ __forceinline__ bool all_nan(const float (&x)[N]) {
   return __all(nan);
 }
 
+// The elements of a row that a wave holds: lane, lane + 64, .. of a head (32: the upper lanes repeat the lower ones)
+template <int HD>
+constexpr int PER_LANE = (HD + 63) / 64;
+template <int HD>
+__device__ __forceinline__ int row_lane() { return threadIdx.x % (HD < 64 ? HD : 64); }
+
 // x.y of two rows of a head
 template <int HD>
 __device__ __forceinline__ float row_dot(const bf16* x, const bf16* y) {
@@ -117,16 +122,16 @@ struct Rows {
 template <int HD>
 __device__ __forceinline__ void row_again(const RangeArgs& a, const Rows& rows, int r, float base, float inv, int k_lo,
                                                     int k_hi, float* part) {
-  const int lane = threadIdx.x % 64, i = rows.query(r), h = rows.head(r), kvh = h / (a.Hq / a.Hkv);
+  const int lane = threadIdx.x % 64, el = row_lane<HD>(), i = rows.query(r), h = rows.head(r), kvh = h / (a.Hq / a.Hkv);
   const bf16* q = rows_of<bf16>(a.q, rows.b, h) + (int64_t)i * a.q.row;
   const bf16* k = rows_of<bf16>(a.k, rows.b, kvh);
   const bf16* v = rows_of<bf16>(a.v, rows.b, kvh);
   const CapScale c(a);
   const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
   const int64_t pos = position(a, rows.b, i);
-  float o[HD / 64];
+  float o[PER_LANE<HD>];
 #pragma unroll
-  for (int d = 0; d < HD / 64; ++d) o[d] = 0.f;
+  for (int d = 0; d < PER_LANE<HD>; ++d) o[d] = 0.f;
   for (int j0 = k_lo; j0 < k_hi && !all_nan(o); j0 += 64) {
     const int n = min(64, k_hi - j0), j = j0 + min(lane, n - 1);
     float g;
@@ -134,16 +139,16 @@ __device__ __forceinline__ void row_again(const RangeArgs& a, const Rows& rows, 
     for (int t = 0; t < n; ++t) {
       const float w = __shfl(p, t, 64);
 #pragma unroll
-      for (int d = 0; d < HD / 64; ++d) o[d] += w * (float)v[(int64_t)(j0 + t) * a.v.row + 64 * d + lane];
+      for (int d = 0; d < PER_LANE<HD>; ++d) o[d] += w * (float)v[(int64_t)(j0 + t) * a.v.row + 64 * d + el];
     }
   }
   const int64_t row = ((int64_t)rows.b * a.Sq + i) * a.Hq + h;
 #pragma unroll
-  for (int d = 0; d < HD / 64; ++d) {
-    if (part) part[row * HD + 64 * d + lane] = o[d];
+  for (int d = 0; d < PER_LANE<HD>; ++d) {
+    if (part) part[row * HD + 64 * d + el] = o[d];
     else {
-      ((bf16*)a.o)[row * HD + 64 * d + lane] = (bf16)(o[d] * inv);
-      if (a.o32) a.o32[row * HD + 64 * d + lane] = o[d] * inv;
+      ((bf16*)a.o)[row * HD + 64 * d + el] = (bf16)(o[d] * inv);
+      if (a.o32) a.o32[row * HD + 64 * d + el] = o[d] * inv;
     }
   }
 }
@@ -452,9 +457,9 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&x)[N]) {
 
 // x rotated back by the angle of row `row` (as store_rows_from_t): lane l holds elements l, l + 64, ..
 template <int HD>
-__device__ __forceinline__ void unrotate(float (&x)[HD / 64], const RangeArgs& a, int row) {
+__device__ __forceinline__ void unrotate(float (&x)[PER_LANE<HD>], const RangeArgs& a, int row) {
   constexpr int HH = HD / 2;
-  const int lane = threadIdx.x % 64;
+  const int lane = row_lane<HD>();
   if (!a.rope_cos) return;
   const int64_t t = (int64_t)row * HH + lane % HH;
   const float cs = a.rope_cos[t], sn = a.rope_sin[t];
@@ -463,7 +468,7 @@ __device__ __forceinline__ void unrotate(float (&x)[HD / 64], const RangeArgs& a
     x[0] = u * cs + v * sn;
     x[1] = v * cs - u * sn;
   } else {
-    const float other = __shfl_xor(x[0], 32, 64);
+    const float other = __shfl_xor(x[0], HH, 64);
     x[0] = lane < HH ? x[0] * cs + other * sn : x[0] * cs - other * sn;
   }
 }
@@ -471,7 +476,7 @@ __device__ __forceinline__ void unrotate(float (&x)[HD / 64], const RangeArgs& a
 // dq of query i again, touching only the keys it sees
 template <int HD>
 __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, int i) {
-  const int lane = threadIdx.x % 64, kvh = h / (a.Hq / a.Hkv);
+  const int lane = threadIdx.x % 64, el = row_lane<HD>(), kvh = h / (a.Hq / a.Hkv);
   const int2 keys = seen_keys_kept(a, (int64_t)b * a.Sq + i);
   const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row;
   const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row;
@@ -481,9 +486,9 @@ __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, i
   const float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
   const int64_t pos = position(a, b, i), sidx = ((int64_t)b * a.Hq + h) * a.Sq + i;
   const float nl = a.nlse[sidx], dl = a.delta[sidx];
-  float acc[HD / 64];
+  float acc[PER_LANE<HD>];
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) acc[x] = 0.f;
+  for (int x = 0; x < PER_LANE<HD>; ++x) acc[x] = 0.f;
   for (int j0 = keys.x; j0 < keys.y && !all_nan(acc); j0 += 64) {
     const int n = min(64, keys.y - j0), j = j0 + min(lane, n - 1);
     float g;
@@ -492,15 +497,15 @@ __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, i
     for (int t = 0; t < n; ++t) {
       const float w = __shfl(ds, t, 64);
 #pragma unroll
-      for (int x = 0; x < HD / 64; ++x) acc[x] += w * (float)k[(int64_t)(j0 + t) * a.k.row + 64 * x + lane];
+      for (int x = 0; x < PER_LANE<HD>; ++x) acc[x] += w * (float)k[(int64_t)(j0 + t) * a.k.row + 64 * x + el];
     }
   }
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) acc[x] *= a.scale;
+  for (int x = 0; x < PER_LANE<HD>; ++x) acc[x] *= a.scale;
   unrotate<HD>(acc, a, i);
   bf16* out = rows_out<bf16>(a.dq, b, h) + (int64_t)i * a.dq.row;
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) out[64 * x + lane] = (bf16)acc[x];
+  for (int x = 0; x < PER_LANE<HD>; ++x) out[64 * x + el] = (bf16)acc[x];
 }
 
 // What a dK/dV item covers: keys of block kb, 64-query tiles of the queries [by.x, by.y) that see one of them, of
@@ -527,13 +532,13 @@ __device__ __forceinline__ float* dkv_part(const RangeArgs& a, int split, int wh
 // dk and dv of one key again over the item's iterations, touching only the queries that see it
 template <int HD>
 __device__ __forceinline__ void dkv_row_again(const RangeArgs& a, const KeyItem& it_, int key) {
-  const int lane = threadIdx.x % 64, group = a.Hq / a.Hkv, b = it_.b;
+  const int lane = threadIdx.x % 64, el = row_lane<HD>(), group = a.Hq / a.Hkv, b = it_.b;
   const bf16* k = rows_of<bf16>(a.k, b, it_.kvh) + (int64_t)key * a.k.row;
   const bf16* v = rows_of<bf16>(a.v, b, it_.kvh) + (int64_t)key * a.v.row;
   const CapScale c(a);
-  float dk[HD / 64], dv[HD / 64];
+  float dk[PER_LANE<HD>], dv[PER_LANE<HD>];
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) dk[x] = dv[x] = 0.f;
+  for (int x = 0; x < PER_LANE<HD>; ++x) dk[x] = dv[x] = 0.f;
   for (int it = it_.it0; it < it_.nit && !(all_nan(dk) && all_nan(dv)); ++it) {
     const int h = it_.kvh * group + it / it_.tiles, q0 = it_.qlo + it % it_.tiles * KB;
     const int i = min(q0 + lane, it_.qhi - 1);
@@ -550,28 +555,28 @@ __device__ __forceinline__ void dkv_row_again(const RangeArgs& a, const KeyItem&
       const int t = __builtin_ctzll(left);
       const float wp = __shfl(p, t, 64), wd = __shfl(ds, t, 64);
 #pragma unroll
-      for (int x = 0; x < HD / 64; ++x) {
-        dv[x] += wp * (float)d[(int64_t)(q0 + t) * a.dout.row + 64 * x + lane];
-        dk[x] += wd * (float)q[(int64_t)(q0 + t) * a.q.row + 64 * x + lane];
+      for (int x = 0; x < PER_LANE<HD>; ++x) {
+        dv[x] += wp * (float)d[(int64_t)(q0 + t) * a.dout.row + 64 * x + el];
+        dk[x] += wd * (float)q[(int64_t)(q0 + t) * a.q.row + 64 * x + el];
       }
     }
   }
   if (a.nsplit > 1) {
     const int64_t row = (int64_t)key * a.Hkv * HD;
 #pragma unroll
-    for (int x = 0; x < HD / 64; ++x) {
-      dkv_part<HD>(a, it_.split, 0, b, it_.kvh)[row + 64 * x + lane] = dk[x];
-      dkv_part<HD>(a, it_.split, 1, b, it_.kvh)[row + 64 * x + lane] = dv[x];
+    for (int x = 0; x < PER_LANE<HD>; ++x) {
+      dkv_part<HD>(a, it_.split, 0, b, it_.kvh)[row + 64 * x + el] = dk[x];
+      dkv_part<HD>(a, it_.split, 1, b, it_.kvh)[row + 64 * x + el] = dv[x];
     }
     return;
   }
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) dk[x] *= a.scale;
+  for (int x = 0; x < PER_LANE<HD>; ++x) dk[x] *= a.scale;
   unrotate<HD>(dk, a, key);
 #pragma unroll
-  for (int x = 0; x < HD / 64; ++x) {
-    (rows_out<bf16>(a.dk, b, it_.kvh) + (int64_t)key * a.dk.row)[64 * x + lane] = (bf16)dk[x];
-    (rows_out<bf16>(a.dv, b, it_.kvh) + (int64_t)key * a.dv.row)[64 * x + lane] = (bf16)dv[x];
+  for (int x = 0; x < PER_LANE<HD>; ++x) {
+    (rows_out<bf16>(a.dk, b, it_.kvh) + (int64_t)key * a.dk.row)[64 * x + el] = (bf16)dk[x];
+    (rows_out<bf16>(a.dv, b, it_.kvh) + (int64_t)key * a.dv.row)[64 * x + el] = (bf16)dv[x];
   }
 }
 
@@ -782,7 +787,7 @@ __device__ __forceinline__ void mask_unseen(f32x16& s, const bf16* stage, int r0
   }
 }
 
-// dK and dV of head dimension 64
+// dK and dV of head dimensions 32 and 64
 template <int HD, bool CAP, bool BIAS>
 __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyItem& item, unsigned char* __restrict__ smem) {
   using TT = DmaRowTile<HD>;
@@ -1129,9 +1134,9 @@ __global__ void __launch_bounds__(NT) range_flash_dkv128(RangeArgs a) {
   range_dkv128_block<CAP, BIAS>(a, item, smem);
 }
 
-// dQ and dK/dV items of head dimension 64 in one launch: a unit is one (sequence, key/value head)
-template <bool CAP, bool BIAS>
-__global__ void __launch_bounds__(NT, 2) range_flash_bwd64(RangeArgs a) {
+// dQ and dK/dV items of head dimensions 32 and 64 in one launch: a unit is one (sequence, key/value head)
+template <int HD, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) range_flash_bwd(RangeArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int nkb = (a.Sk + QB - 1) / QB, nqb = (a.Sq + QB - 1) / QB, group = a.Hq / a.Hkv;
   const int per_unit = nkb * a.nsplit + nqb * group;
@@ -1140,10 +1145,10 @@ __global__ void __launch_bounds__(NT, 2) range_flash_bwd64(RangeArgs a) {
   const int kvh = unit % a.Hkv, b = unit / a.Hkv;
   if (idx < nkb * a.nsplit) {
     const KeyItem item(a, heavy_block(a, b, nkb, idx / a.nsplit), idx % a.nsplit, kvh, b);
-    range_dkv_block<64, CAP, BIAS>(a, item, smem);
+    range_dkv_block<HD, CAP, BIAS>(a, item, smem);
   } else {
     idx -= nkb * a.nsplit;
-    range_dq_block<64, CAP, BIAS>(a, nqb - 1 - idx / group, kvh * group + idx % group, b, smem);
+    range_dq_block<HD, CAP, BIAS>(a, nqb - 1 - idx / group, kvh * group + idx % group, b, smem);
   }
 }
 
@@ -1196,7 +1201,8 @@ void range_mfma_fwd(const RangeArgs& a, hipStream_t st) {
   const unsigned blocks = (unsigned)(range_mfma_items(a) * a.nsplit);
   const int pack = range_mfma_pack(a);
   with_flags(a.o32 != nullptr, a.cap > 0.f, a.slopes != nullptr, [&](auto exact, auto cap, auto bias) {
-    if (a.hd == 64) fwd_launch<64, exact.value, cap.value, bias.value>(a, pack, blocks, st);
+    if (a.hd == 32) fwd_launch<32, exact.value, cap.value, bias.value>(a, pack, blocks, st);
+    else if (a.hd == 64) fwd_launch<64, exact.value, cap.value, bias.value>(a, pack, blocks, st);
     else fwd_launch<128, exact.value, cap.value, bias.value>(a, pack, blocks, st);
   });
 }
@@ -1207,7 +1213,7 @@ int range_mfma_keys() { return QB; }
 int range_mfma_dkv_splits(const RangeArgs& a) {
   const int64_t items = cdiv(a.Sk, QB) * a.Hkv * a.B, tiles = (int64_t)(a.Hq / a.Hkv) * cdiv(a.Sq, KB);
   if (items == 0) return 1;
-  const int64_t most = a.hd == 64 || tiles >= 140 || (tiles >= 48 && 256 % items == 0) ? 512 : 256;
+  const int64_t most = a.hd != 128 || tiles >= 140 || (tiles >= 48 && 256 % items == 0) ? 512 : 256;
   return (int)std::max<int64_t>(1, std::min<int64_t>({8, cdiv(most, items), tiles / 8}));
 }
 
@@ -1215,10 +1221,16 @@ void range_mfma_bwd(const RangeArgs& a, hipStream_t st) {
   const int64_t nkb = cdiv(a.Sk, QB) * a.nsplit * a.Hkv * a.B, nqb = cdiv(a.Sq, QB) * a.Hq * a.B;
   with_flags(a.cap > 0.f, a.slopes != nullptr, false, [&](auto cap, auto bias, auto) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-    if (a.hd == 64) {
-      constexpr size_t lds = std::max(Lds<64>::dq_bytes(), QueryStage<64>::bytes(ring_stages<64>()));
-      allow_lds<range_flash_bwd64<CAP, BIAS>>(lds);
-      range_flash_bwd64<CAP, BIAS><<<(unsigned)(nkb + nqb), NT, lds, st>>>(a);
+    auto together = [&](auto hd) {
+      constexpr int HD = decltype(hd)::value;
+      constexpr size_t lds = std::max(Lds<HD>::dq_bytes(), QueryStage<HD>::bytes(ring_stages<HD>()));
+      allow_lds<range_flash_bwd<HD, CAP, BIAS>>(lds);
+      range_flash_bwd<HD, CAP, BIAS><<<(unsigned)(nkb + nqb), NT, lds, st>>>(a);
+    };
+    if (a.hd == 32) {
+      together(std::integral_constant<int, 32>{});
+    } else if (a.hd == 64) {
+      together(std::integral_constant<int, 64>{});
     } else {
       constexpr size_t lds_kv = QueryStage<128>::bytes(3), lds_q = Lds<128>::dq_bytes();
       allow_lds<range_flash_dq128<CAP, BIAS>>(lds_q);

@@ -27,11 +27,14 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 //     consecutive rows (16-byte row reads) that sends 4 consecutive rows (k0 a multiple of 4) to 4
 //     different 4-chunk groups (transposing reads of 4 rows x 32 columns);
 //   HD = 64 (two rows per 64 banks): swz = 4 (r / 2 mod 2) + (r / 4 mod 4), the same two properties
-//     over the rows of one parity.
+//     over the rows of one parity;
+//   HD = 32 (four rows per 64 banks): swz = r / 4 mod 4: 16 consecutive rows read 16 different chunks, and 4
+//     consecutive rows of 32 columns are all the chunks of 4 rows.
 template <int HD>
 __device__ __forceinline__ int swz(int r) {
   if constexpr (HD == 128) return 4 * (r & 3) + ((r >> 2) & 3);
-  else return 4 * ((r >> 1) & 1) + ((r >> 2) & 3);
+  else if constexpr (HD == 64) return 4 * ((r >> 1) & 1) + ((r >> 2) & 3);
+  else return (r >> 2) & 3;
 }
 // element index of (row r, column c) in a swizzled [row][HD] tile
 template <int HD>
@@ -153,7 +156,7 @@ struct DmaRowTile {
 
 // stages of the streamed-tile ring: a tile's loads are issued NS - 1 iterations before it is used
 template <int HD>
-constexpr int ring_stages() { return HD == 64 ? 3 : 2; }
+constexpr int ring_stages() { return HD == 128 ? 2 : 3; }
 
 // Waits until this thread's loads of the current iteration's stage are in LDS: issued after them
 // are the loads of the next NS - 2 iterations, those that exist (`more` = the next iteration does)

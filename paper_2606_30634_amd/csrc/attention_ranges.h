@@ -63,6 +63,12 @@ __device__ __forceinline__ T* rows_out(const HeadRows& r, int b, int h) {
   return (T*)r.p + b * r.batch + h * r.head;
 }
 
+// Partial dq of share `split`, rows of Hq HD
+template <int HD>
+__device__ __forceinline__ float* dq_part(const RangeArgs& a, int split, int b, int h) {
+  return a.part_q + ((int64_t)split * a.B + b) * a.Sq * a.Hq * HD + h * HD;
+}
+
 // A wave's minimum and maximum over all its lanes, by data-parallel moves (as wave_total)
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int dpp_or_same(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xf, false); }

@@ -20,6 +20,7 @@ int64_t range_mfma_items(const RangeArgs& a);
 void range_mfma_fwd(const RangeArgs& a, hipStream_t st);
 int range_mfma_keys();  // keys of a dK/dV block
 int range_mfma_dkv_splits(const RangeArgs& a);
+int range_mfma_dq_splits(const RangeArgs& a);
 void range_mfma_bwd(const RangeArgs& a, hipStream_t st);
 
 namespace {
@@ -297,8 +298,9 @@ __global__ void __launch_bounds__(256) range_prep(RangeArgs a, int width, int nt
   }
 }
 
+// dq of 32 queries of head h: the share `split` of their keys' tiles
 template <typename T, int HD>
-__device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int b, float* red) {
+__device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int split, int h, int b, float* red) {
   const int kvh = h / (a.Hq / a.Hkv), q0 = qb * TR;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = q0 + lane % 32, qc = min(q, a.Sq - 1);
   const T* kp = rows_of<T>(a.k, b, kvh);
@@ -337,13 +339,17 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int h, int 
     if (plain) cols_product<HD>(dq, kp, k0, wk.hi - 1, a.k.row, s);
     else cols_product_seen<HD>(dq, kp, k0, a.k.row, s, red + wave * WAVE_LDS<HD>, [&](int r) { return sees(mask, k0 + r); });
   };
-  for (int k0 = wk.lo + wave * TR; k0 < wk.hi; k0 += NW * TR) {
+  const int tiles = (wk.hi - wk.lo + TR - 1) / TR;
+  const int t1 = (int)((int64_t)tiles * (split + 1) / a.qsplit);
+  for (int t = (int)((int64_t)tiles * split / a.qsplit) + wave; t < t1; t += NW) {
+    const int k0 = wk.lo + t * TR;
     if (wk.whole(k0, k0 + TR)) tile(k0, std::false_type{});
     else tile(k0, std::true_type{});
   }
   put_partial<HD>(red, dq, 1.0f);
   __syncthreads();
-  store_rows<HD>(red, a.scale, rows_out<T>(a.dq, b, h), a.dq.row, q0, a.Sq, a.rope_cos, a.rope_sin);
+  if (a.qsplit > 1) store_rows<HD>(red, 1.0f, dq_part<HD>(a, split, b, h), a.Hq * HD, q0, a.Sq, nullptr, nullptr);
+  else store_rows<HD>(red, a.scale, rows_out<T>(a.dq, b, h), a.dq.row, q0, a.Sq, a.rope_cos, a.rope_sin);
 }
 
 // dk and dv of 32 keys of key/value head kvh, summed over its query heads: the share `split` of the tiles of the
@@ -439,53 +445,65 @@ __global__ void __launch_bounds__(NW * 64, bwd_waves(HD)) range_bwd(RangeArgs a)
     range_dkv<T, HD>(a, kb, split, (int)(id % a.Hkv), (int)(id / a.Hkv), red);
   } else {
     id -= nkv;
+    const int split = id % a.qsplit;
+    id /= a.qsplit;
     const int qb = nq - 1 - (int)(id % nq);
     id /= nq;
-    range_dq<T, HD>(a, qb, (int)(id % a.Hq), (int)(id / a.Hq), red);
+    range_dq<T, HD>(a, qb, split, (int)(id % a.Hq), (int)(id / a.Hq), red);
   }
 }
 
-// dk and dv of split items: the partial sums added in order, 8 columns per thread
+// Gradients of split items: the partial sums of rows [B, rows, heads, HD] added in order
+struct JoinRows {
+  const float* part;
+  int64_t share, n;  // elements between shares, and of one
+  int nsplit, rows, heads;
+  HeadRows out;
+  float scale;
+  bool rope;
+};
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) range_dkv_join(RangeArgs a) {
+__device__ __forceinline__ void join_rows(const RangeArgs& a, const JoinRows& j, int64_t e) {  // elements e .. e + 7
   constexpr int HH = HD / 2;
-  const int kvd = a.Hkv * HD;
-  const int64_t n = (int64_t)a.B * a.Sk * kvd, c = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
-  if (c >= 2 * n) return;
-  const bool isv = c >= n;
-  const int64_t e = isv ? c - n : c, row = e / kvd;
-  const int kvh = (int)(e % kvd) / HD, d = (int)(e % HD), b = (int)(row / a.Sk), key = (int)(row % a.Sk);
-  auto sum = [&](int64_t o, float* v) {  // elements o .. o + 7 of every share
+  const int64_t row = e / (j.heads * HD);
+  const int h = (int)(e / HD % j.heads), d = (int)(e % HD), b = (int)(row / j.rows), i = (int)(row % j.rows);
+  auto sum = [&](int64_t o, float* v) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] = 0.f;
-    for (int s = 0; s < a.nsplit; ++s) {
-      const float* p = a.part + 2 * n * s + o;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+    for (int s = 0; s < j.nsplit; ++s) {
+      const float* p = j.part + j.share * s + o;
+      const f32x4 lo = ld4(p), hi = ld4(p + 4);
 #pragma unroll
       for (int q = 0; q < 4; ++q) { v[q] += lo[q]; v[q + 4] += hi[q]; }
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= j.scale;
   };
   float v[8];
-  sum(c, v);
-  if (!isv) {
+  sum(e, v);
+  if (j.rope && a.rope_cos) {
+    const bool first = d < HH;
+    float p[8];
+    sum(first ? e + HH : e - HH, p);
+    const int64_t t = (int64_t)i * HH + d % HH;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] *= a.scale;
-    if (a.rope_cos) {
-      const bool first = d < HH;
-      float p[8];
-      sum(first ? c + HH : c - HH, p);
-      const int64_t t = (int64_t)key * HH + d % HH;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float y = p[q] * a.scale, cs = a.rope_cos[t + q], sn = a.rope_sin[t + q];
-        v[q] = first ? v[q] * cs + y * sn : v[q] * cs - y * sn;
-      }
+    for (int q = 0; q < 8; ++q) {
+      const float cs = a.rope_cos[t + q], sn = a.rope_sin[t + q];
+      v[q] = first ? v[q] * cs + p[q] * sn : v[q] * cs - p[q] * sn;
     }
   }
-  const HeadRows& out = isv ? a.dv : a.dk;
-  T* o = rows_out<T>(out, b, kvh) + (int64_t)key * out.row + d;
+  T* o = rows_out<T>(j.out, b, h) + (int64_t)i * j.out.row + d;
   st4(o, f32x4{v[0], v[1], v[2], v[3]});
   st4(o + 4, f32x4{v[4], v[5], v[6], v[7]});
+}
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) range_grad_join(RangeArgs a) {
+  const int64_t nk = a.nsplit > 1 ? (int64_t)a.B * a.Sk * a.Hkv * HD : 0;
+  const int64_t nq = a.qsplit > 1 ? (int64_t)a.B * a.Sq * a.Hq * HD : 0;
+  const int64_t e = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (e < nk) join_rows<T, HD>(a, JoinRows{a.part, 2 * nk, nk, a.nsplit, a.Sk, a.Hkv, a.dk, a.scale, true}, e);
+  else if (e < 2 * nk) join_rows<T, HD>(a, JoinRows{a.part + nk, 2 * nk, nk, a.nsplit, a.Sk, a.Hkv, a.dv, 1.0f, false}, e - nk);
+  else if (e < 2 * nk + nq) join_rows<T, HD>(a, JoinRows{a.part_q, nq, nq, a.qsplit, a.Sq, a.Hq, a.dq, a.scale, true}, e - 2 * nk);
 }
 
 // ------------------------------------------------------------------------------------------ key ranges
@@ -745,6 +763,12 @@ int dkv_splits(const RangeArgs& a) {
   return items == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({8, 512 / items, tiles / (2 * NW)}));
 }
 
+// and of a dq block's key tiles
+int dq_splits(const RangeArgs& a) {
+  const int64_t items = cdiv(a.Sq, TR) * a.Hq * a.B, tiles = cdiv(a.Sk, TR);
+  return items == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, 512 / items, tiles / (2 * NW)}));
+}
+
 // The backward's workspace at p (null: its size alone)
 size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
   size_t n = 0;
@@ -761,6 +785,8 @@ size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
   a.sees = (int2*)take(a.B * cdiv(a.Sk, bf ? range_mfma_keys() : TR) * 8);
   a.nsplit = bf ? range_mfma_dkv_splits(a) : dkv_splits(a);
   a.part = a.nsplit > 1 ? (float*)take(2 * (int64_t)a.nsplit * a.B * a.Sk * a.Hkv * a.hd * 4) : nullptr;
+  a.qsplit = bf ? range_mfma_dq_splits(a) : dq_splits(a);
+  a.part_q = a.qsplit > 1 ? (float*)take(a.qsplit * rows * a.Hq * a.hd * 4) : nullptr;
   return n;
 }
 
@@ -779,11 +805,11 @@ void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
     constexpr int HD = decltype(hd)::value;
     const int64_t prep = (int64_t)ntile * a.B + cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256);
     range_prep<T, HD><<<(unsigned)prep, 256, 0, st>>>(a, width, ntile);
-    const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.Hq * a.B;
+    const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.qsplit * a.Hq * a.B;
     if constexpr (LOG2<T>) range_mfma_bwd(a, st);
     else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
-    if (a.nsplit > 1)
-      range_dkv_join<T, HD><<<(unsigned)cdiv(2 * (int64_t)a.B * a.Sk * a.Hkv * HD / 8, 256), 256, 0, st>>>(a);
+    const int64_t split = (a.nsplit > 1 ? 2 * (int64_t)a.B * a.Sk * a.Hkv : 0) + (a.qsplit > 1 ? (int64_t)a.B * a.Sq * a.Hq : 0);
+    if (split > 0) range_grad_join<T, HD><<<(unsigned)cdiv(split * HD / 8, 256), 256, 0, st>>>(a);
   });
 }
 

@@ -473,11 +473,13 @@ __device__ __forceinline__ void unrotate(float (&x)[PER_LANE<HD>], const RangeAr
   }
 }
 
-// dq of query i again, touching only the keys it sees
+// dq of query i again, touching only the keys it sees in [k_lo, k_hi)
 template <int HD>
-__device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, int i) {
+__device__ __forceinline__ void dq_row_again(const RangeArgs& a, int split, int b, int h, int i, int k_lo, int k_hi) {
   const int lane = threadIdx.x % 64, el = row_lane<HD>(), kvh = h / (a.Hq / a.Hkv);
-  const int2 keys = seen_keys_kept(a, (int64_t)b * a.Sq + i);
+  int2 keys = seen_keys_kept(a, (int64_t)b * a.Sq + i);
+  keys.x = max(keys.x, k_lo);
+  keys.y = min(keys.y, k_hi);
   const bf16* q = rows_of<bf16>(a.q, b, h) + (int64_t)i * a.q.row;
   const bf16* d = rows_of<bf16>(a.dout, b, h) + (int64_t)i * a.dout.row;
   const bf16* k = rows_of<bf16>(a.k, b, kvh);
@@ -499,6 +501,12 @@ __device__ __forceinline__ void dq_row_again(const RangeArgs& a, int b, int h, i
 #pragma unroll
       for (int x = 0; x < PER_LANE<HD>; ++x) acc[x] += w * (float)k[(int64_t)(j0 + t) * a.k.row + 64 * x + el];
     }
+  }
+  if (a.qsplit > 1) {
+    float* part = dq_part<HD>(a, split, b, h) + (int64_t)i * a.Hq * HD;
+#pragma unroll
+    for (int x = 0; x < PER_LANE<HD>; ++x) part[64 * x + el] = acc[x];
+    return;
   }
 #pragma unroll
   for (int x = 0; x < PER_LANE<HD>; ++x) acc[x] *= a.scale;
@@ -601,7 +609,8 @@ __device__ __forceinline__ void dkv_store(const RangeArgs& a, const KeyItem& ite
 }
 
 template <int HD, bool CAP, bool BIAS>
-__device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h, int b, unsigned char* __restrict__ smem) {
+__device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int split, int h, int b,
+                                               unsigned char* __restrict__ smem) {
   using L = Lds<HD>;
   using TT = DmaRowTile<HD>;
   constexpr int KS = HD / 16, DT = HD / 32, NS = L::NS;
@@ -636,7 +645,9 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
     blo = wave_min_i(min(sx.y > 0 ? sx.x : INT32_MAX, sy.y > 0 ? sy.x : INT32_MAX));
     if (bhi == 0) blo = 0;
   }
-  const int ntile = (bhi - blo + KB - 1) / KB;
+  const int tiles = (bhi - blo + KB - 1) / KB;  // of which this share takes [kt0, ntile)
+  const int kt0 = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * split / a.qsplit));
+  const int ntile = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (split + 1) / a.qsplit));
   auto issue = [&](int t) {
     bf16* st = ring + (t % NS) * 2 * L::TSZ;
     TT::issue(kbase, a.k.row, blo + t * KB, bhi, lds_addr(st));
@@ -651,14 +662,14 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
   }
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
-    if (s < ntile) issue(s);
+    if (kt0 + s < ntile) issue(kt0 + s);
   wait_vm_lds<0>();  // as in the forward
   f32x16 dq[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dq[dt][e] = 0.f;
-  for (int kt = 0; kt < ntile; ++kt) {
+  for (int kt = kt0; kt < ntile; ++kt) {
     ring_wait<NS, 2 * TT::PER>(kt + 1 < ntile);
     block_barrier();
     if (kt + NS - 1 < ntile) issue(kt + NS - 1);
@@ -753,11 +764,13 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int h
   }
   block_barrier();  // every wave is done with the last tile: the ring becomes the output staging
   uint64_t bad = __ballot(valid && !all_finite(dq));
-  store_rows_from_t<HD>(reinterpret_cast<float*>(smem), dq, a.scale, rows_out<bf16>(a.dq, b, h), a.dq.row, qb * QB, a.Sq,
-                        a.rope_cos, a.rope_sin);
+  float* stage = reinterpret_cast<float*>(smem);
+  if (a.qsplit > 1) store_partial_from_t<HD>(stage, dq, dq_part<HD>(a, split, b, h), a.Hq * HD, qb * QB, a.Sq);
+  else store_rows_from_t<HD>(stage, dq, a.scale, rows_out<bf16>(a.dq, b, h), a.dq.row, qb * QB, a.Sq, a.rope_cos, a.rope_sin);
   if (__syncthreads_or(bad != 0)) {
     bad = (bad | bad >> 32) & 0xffffffffu;
-    for (; bad; bad &= bad - 1) dq_row_again<HD>(a, b, h, qb * QB + wave * 32 + __builtin_ctzll(bad));
+    for (; bad; bad &= bad - 1)
+      dq_row_again<HD>(a, split, b, h, qb * QB + wave * 32 + __builtin_ctzll(bad), blo + kt0 * KB, blo + ntile * KB);
   }
 }
 
@@ -1119,8 +1132,8 @@ __global__ void __launch_bounds__(NT, 2) range_flash_dq128(RangeArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int nqb = (a.Sq + QB - 1) / QB;
   int unit, idx;  // unit: (sequence, query head)
-  xcd_item(blockIdx.x, nqb * a.Hq * a.B, nqb, unit, idx);
-  range_dq_block<128, CAP, BIAS>(a, nqb - 1 - idx, unit % a.Hq, unit / a.Hq, smem);
+  xcd_item(blockIdx.x, nqb * a.qsplit * a.Hq * a.B, nqb * a.qsplit, unit, idx);
+  range_dq_block<128, CAP, BIAS>(a, nqb - 1 - idx / a.qsplit, idx % a.qsplit, unit % a.Hq, unit / a.Hq, smem);
 }
 
 template <bool CAP, bool BIAS>
@@ -1139,7 +1152,7 @@ template <int HD, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(NT, 2) range_flash_bwd(RangeArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int nkb = (a.Sk + QB - 1) / QB, nqb = (a.Sq + QB - 1) / QB, group = a.Hq / a.Hkv;
-  const int per_unit = nkb * a.nsplit + nqb * group;
+  const int per_unit = nkb * a.nsplit + nqb * a.qsplit * group;
   int unit, idx;
   xcd_item(blockIdx.x, per_unit * a.Hkv * a.B, per_unit, unit, idx);
   const int kvh = unit % a.Hkv, b = unit / a.Hkv;
@@ -1148,7 +1161,9 @@ __global__ void __launch_bounds__(NT, 2) range_flash_bwd(RangeArgs a) {
     range_dkv_block<HD, CAP, BIAS>(a, item, smem);
   } else {
     idx -= nkb * a.nsplit;
-    range_dq_block<HD, CAP, BIAS>(a, nqb - 1 - idx / group, kvh * group + idx % group, b, smem);
+    const int split = idx % a.qsplit;
+    idx /= a.qsplit;
+    range_dq_block<HD, CAP, BIAS>(a, nqb - 1 - idx / group, split, kvh * group + idx % group, b, smem);
   }
 }
 
@@ -1209,16 +1224,28 @@ void range_mfma_fwd(const RangeArgs& a, hipStream_t st) {
 
 int range_mfma_keys() { return QB; }
 
+// A share of at least so many tiles: with few items the chip is empty and a chain of tiles is all there is to wait for
+// (one sequence of 300 tokens, 4 heads of 128 on 1: backward 50 us with 8, FEWTILES with 3)
+static int64_t tiles_per_share(int64_t items) { return items <= 64 ? 3 : 8; }
+
 // As attention_dkv_splits: few key blocks are split over their queries' tiles, the longest by the causal count
 int range_mfma_dkv_splits(const RangeArgs& a) {
   const int64_t items = cdiv(a.Sk, QB) * a.Hkv * a.B, tiles = (int64_t)(a.Hq / a.Hkv) * cdiv(a.Sq, KB);
   if (items == 0) return 1;
   const int64_t most = a.hd != 128 || tiles >= 140 || (tiles >= 48 && 256 % items == 0) ? 512 : 256;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({8, cdiv(most, items), tiles / 8}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({8, cdiv(most, items), tiles / tiles_per_share(items)}));
+}
+
+// Few query blocks share their keys' tiles, towards 512 items: a block of a long row alone is a chain of its tiles
+// (one sequence of 4096 tokens, one head of 64: backward 87 -> 38 us; 16 queries on 8192 keys, 8 heads of 128 on 1: 206 ->
+// 59)
+int range_mfma_dq_splits(const RangeArgs& a) {
+  const int64_t items = cdiv(a.Sq, QB) * a.Hq * a.B;
+  return items == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, 512 / items, cdiv(a.Sk, KB) / tiles_per_share(items)}));
 }
 
 void range_mfma_bwd(const RangeArgs& a, hipStream_t st) {
-  const int64_t nkb = cdiv(a.Sk, QB) * a.nsplit * a.Hkv * a.B, nqb = cdiv(a.Sq, QB) * a.Hq * a.B;
+  const int64_t nkb = cdiv(a.Sk, QB) * a.nsplit * a.Hkv * a.B, nqb = cdiv(a.Sq, QB) * a.qsplit * a.Hq * a.B;
   with_flags(a.cap > 0.f, a.slopes != nullptr, false, [&](auto cap, auto bias, auto) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
     auto together = [&](auto hd) {

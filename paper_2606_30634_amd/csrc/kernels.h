@@ -242,7 +242,9 @@ struct RangeArgs {
   int2* sees;        // [B, key tiles]: the queries that see any key of a tile lie in [x, y)
   float* part;       // partial sums of split items
   float2* part_ml;   // and their maxima and sums
-  int nsplit;
+  int nsplit;        // shares of a forward item's keys, of a dk/dv item's queries
+  float* part_q;     // partial dq of split items
+  int qsplit;        // shares of a dq item's keys
 };
 size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a);
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st);

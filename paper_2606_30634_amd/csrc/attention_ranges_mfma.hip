@@ -1,4 +1,5 @@
-// Attention over key ranges (the formulas are in attention_ranges.hip) for bf16, on the bf16 matrix cores, with the tiles, operand layouts and rings of attention_mfma.hip.
+// Attention over key ranges (the formulas are in attention_ranges.hip) for bf16, on the bf16 matrix cores, with the
+// tiles, operand layouts and rings of attention_mfma.hip.
 //
 // What differs from the causal kernels there: tiles start at the first key that a query of the block sees and end
 // with the last, so nothing else is loaded; every lane owns one query (one key in dK/dV) and keeps its range, and
@@ -6,6 +7,12 @@
 // may hold the query heads of one key/value head (`pack` rows per query) and a share of the keys.
 // A block whose result is not finite (a value that one of its rows does not see may be an infinity or a NaN, and 0
 // times it is a NaN) computes the rows in question again, key by key over what they see.
+//
+// What bounds them: long rows the matrix cores and the vector work beside them, which one SIMD's two waves (one in
+// dK/dV of 128) overlap only in part; short documents also a block's start and end and the part of its tiles that no row
+// sees; a few queries on long caches HBM (16 x 32768 keys, 8 heads of 128: 5.6 TB/s).  One causal row block of 4096 tokens
+// (2 sequences, 32 heads of 128 on 8), by the flops of the pairs seen: forward 336-347 us, 0.79-0.82 PFLOP/s (o kept in fp32,
+// so three times the P V products: 495 us; scores capped: 385-392 us), backward 1004 us, 0.68 PFLOP/s (capped 1229).
 #include "attention_ranges.h"
 #include "attention_tiles.h"
 #include <algorithm>
@@ -28,19 +35,6 @@ struct CapScale {
   }
 };
 
-// tanh(y) / y up to |y| = CapScale::SMALL: 1 + y^2 P(y^2) with the minimax P of degree 2 (relative error 2^-23, below
-// the rounding of the products), times `by`
-struct CapPoly {
-  float c0, c1, c2, c3;
-  __device__ explicit CapPoly(float by) : c0(by), c1(by * -0.3333188295f), c2(by * 0.1327762753f), c3(by * -0.0477941558f) {}
-  __device__ __forceinline__ float operator()(float y) const {
-    const float z = y * y;
-    float p = __builtin_fmaf(z, c3, c2);
-    p = __builtin_fmaf(z, p, c1);
-    return __builtin_fmaf(z, p, c0);
-  }
-};
-
 template <int N>
 __device__ __forceinline__ float largest(const f32x16 (&s)[N]) {
   float big = 0.f;
@@ -52,17 +46,19 @@ __device__ __forceinline__ float largest(const f32x16 (&s)[N]) {
 }
 
 // tanh(scale x / cap) of a wave's products, `big` their largest |x| in the lane.  One branch for the wave: where no
-// |y| passes CapScale::SMALL (most tiles) the polynomial alone.
+// |y| passes CapScale::SMALL (most tiles) the polynomial alone: y + y^3 P(y^2) with the minimax P of degree 2 (relative
+// error 2^-23, below the rounding of the products).
 template <int N>
 __device__ __forceinline__ void tanh_scores(f32x16 (&s)[N], const CapScale& c, float big) {
   if (__all(big <= c.small)) {
-    const CapPoly poly(1.0f);
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float y = s[t][e] * c.y_of;
-        s[t][e] = y * poly(y);
+        const float y = s[t][e] * c.y_of, z = y * y;
+        float p = __builtin_fmaf(z, -0.0477941558f, 0.1327762753f);
+        p = __builtin_fmaf(z, p, -0.3333188295f);
+        s[t][e] = y * __builtin_fmaf(z, p, 1.0f);
       }
   } else {
 #pragma unroll
@@ -194,7 +190,7 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
     xcd_item(blockIdx.x, nb * heads * a.B, nb, unit, idx);
   } else {
     // shares of long caches share nothing in an L2, and sequences of different lengths must not fall to one XCD
-    // each: every XCD takes some of all (16 answers of 1 .. 32768 keys, 8 key/value heads: 243 -> RAGGED us)
+    // each: every XCD takes some of all (16 answers of 1 .. 32768 keys, 8 key/value heads: 251 -> 233 us)
     unit = blockIdx.x % (heads * a.B);
     idx = blockIdx.x / (heads * a.B);
   }
@@ -1108,7 +1104,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
 
 // The key block of sequence b whose queries are the r-th most (of up to NT blocks; beyond that block r itself: there are
 // then enough items for their order not to matter).  Documents give the blocks of a launch very different lengths, and
-// the longest, started last, would end it: 2 x 4096 tokens in 3 documents a row, 32 heads on 8: UNSORTED -> SORTED us.
+// the longest, started last, would end it: 2 x 4096 tokens in 3 documents a row, 32 heads on 8, capped: 418 -> 371 us.
 __device__ __forceinline__ int heavy_block(const RangeArgs& a, int b, int nkb, int r) {
   __shared__ int queries[NT], pick;
   if (nkb > NT) return r;
@@ -1225,7 +1221,7 @@ void range_mfma_fwd(const RangeArgs& a, hipStream_t st) {
 int range_mfma_keys() { return QB; }
 
 // A share of at least so many tiles: with few items the chip is empty and a chain of tiles is all there is to wait for
-// (one sequence of 300 tokens, 4 heads of 128 on 1: backward 50 us with 8, FEWTILES with 3)
+// (one sequence of 300 tokens, 4 heads of 128 on 1: backward 50 us with 8, 40 with 3)
 static int64_t tiles_per_share(int64_t items) { return items <= 64 ? 3 : 8; }
 
 // As attention_dkv_splits: few key blocks are split over their queries' tiles, the longest by the causal count

@@ -35,23 +35,31 @@ __device__ __forceinline__ float weight_base(float m) { return m == -INFINITY ? 
 // minimax fit of degree 3 (relative error 2^-26); beyond it 1 - u with u = 2 e / (1 + e), e = exp(-2 |y|),
 // whose derivative u (2 - u) keeps its relative accuracy where tanh rounds to 1.
 constexpr float TANH_SMALL = 0.5f;
-constexpr float TANH_C[4] = {-0.3333314359f, 0.1332587898f, -0.0530454814f, 0.0172414685f};
-__device__ __forceinline__ float tanh_ratio(float z) {  // tanh(y) / y, z = y^2
-  float p = __builtin_fmaf(z, TANH_C[3], TANH_C[2]);
-  p = __builtin_fmaf(z, p, TANH_C[1]);
-  p = __builtin_fmaf(z, p, TANH_C[0]);
-  return __builtin_fmaf(z, p, 1.0f);
+__device__ __forceinline__ float tanh_excess(float z) {  // tanh(y) / y - 1, z = y^2
+  float p = __builtin_fmaf(z, 0.0172414685f, -0.0530454814f);
+  p = __builtin_fmaf(z, p, 0.1332587898f);
+  return z * __builtin_fmaf(z, p, -0.3333314359f);
 }
-__device__ __forceinline__ float tanh_and_slope(float y, float& slope) {
-  if (fabsf(y) < TANH_SMALL) {
-    const float t = y * tanh_ratio(y * y);
-    slope = __builtin_fmaf(-t, t, 1.0f);
-    return t;
-  }
+__device__ __forceinline__ float tanh_far(float y, float& slope) {
   const float e = __builtin_amdgcn_exp2f(fabsf(y) * -2.8853900817779268f);
   const float u = 2.0f * e * __builtin_amdgcn_rcpf(1.0f + e);
   slope = u * (2.0f - u);
   return copysignf(1.0f - u, y);
+}
+__device__ __forceinline__ float tanh_and_slope(float y, float& slope) {
+  if (!(fabsf(y) < TANH_SMALL)) return tanh_far(y, slope);
+  const float t = __builtin_fmaf(y, tanh_excess(y * y), y);
+  slope = __builtin_fmaf(-t, t, 1.0f);
+  return t;
+}
+// cap tanh(x / cap) and its derivative in x.  A score well below the cap is x and a small correction, so that x
+// keeps its bits: through tanh and back it would lose two roundings of a score that is an exponent next.
+__device__ __forceinline__ float capped(float x, float cap, float inv_cap, float& slope) {
+  const float y = x * inv_cap;
+  if (!(fabsf(y) < TANH_SMALL)) return cap * tanh_far(y, slope);
+  const float r = tanh_excess(y * y), t = __builtin_fmaf(y, r, y);
+  slope = __builtin_fmaf(-t, t, 1.0f);
+  return __builtin_fmaf(x, r, x);
 }
 
 template <typename T>

@@ -29,29 +29,56 @@ namespace {
 
 constexpr int MAX_SPLITS = 256;  // shares of an item's keys
 
-// whether a type's kernels (bf16: on the bf16 matrix cores) keep statistics in log2 units
-template <typename T>
-constexpr bool LOG2 = sizeof(T) == 2;
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // Score of x = scale q.k at distance `far` (x itself without cap and slopes)
 struct Score {
   float cap, inv_cap, slope;
-  bool capped, biased;
+  bool has_cap, biased;
   __device__ Score(const RangeArgs& a, int h) {
     cap = a.cap;
-    capped = a.cap > 0.f;
-    inv_cap = capped ? 1.0f / a.cap : 0.f;
+    has_cap = a.cap > 0.f;
+    inv_cap = has_cap ? 1.0f / a.cap : 0.f;
     biased = a.slopes != nullptr;
     slope = biased ? a.slopes[h] : 0.f;
   }
   __device__ float operator()(float x, float far, float& grad) const {
     grad = 1.f;
-    if (capped) x = cap * tanh_and_slope(x * inv_cap, grad);
+    if (has_cap) x = capped(x, cap, inv_cap, grad);
     if (biased) x = __builtin_fmaf(-slope, fabsf(far), x);
     return x;
   }
 };
+
+// rows_product as sums of 32 elements that are then added: 128 products in one chain leave a score twice as far off,
+// and a weight is its exponential (84 tokens, 16 heads of 128, scores of 10: gradients 1.2e-6 off their norm against
+// 9.4e-7).
+template <int HD>
+__device__ __forceinline__ f32x16 rows_product_parts(const RowFrag<HD>& a, const RowFrag<HD>& b) {
+  f32x16 total;
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n) {
+    f32x16 s;
+    float zero = 0.f;
+    if (n) asm volatile("" : "+v"(zero) : "v"(total[0]));  // one sum after the other: side by side they would spill
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = zero;
+#pragma unroll
+    for (int q = 4 * n; q < 4 * n + 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = mfma2(a.v[q][j], b.v[q][j], s);
+    total = n ? total + s : s;
+  }
+  return total;
+}
+
+// The same for dP, of which nothing is an exponential: in parts at 128 only (their registers spill: 1425 tokens, 32
+// heads of 128 on 8: backward 999 -> 1141 us, gradients 1.0e-6 off against 9.3e-7), one chain of 64 at most otherwise
+template <int HD>
+__device__ __forceinline__ f32x16 grad_product(const RowFrag<HD>& a, const RowFrag<HD>& b) {
+  if constexpr (HD == 128) return rows_product_parts<HD>(a, b);
+  else return rows_product<HD>(a, b);
+}
 
 __device__ __forceinline__ int acc_row(int e) { return 8 * (e / 4) + 4 * (threadIdx.x % 64 / 32) + e % 4; }
 
@@ -92,7 +119,7 @@ __global__ void __launch_bounds__(NW * 64, HD == 128 ? 1 : HD == 64 ? 2 : 3) ran
     kf.load(kp, min(k0 + lane % 32, wk.hi - 1), a.k.row);
     ColFrag<HD> vf;  // on its way while the scores are formed
     vf.load(vp, k0, wk.hi - 1, a.v.row);
-    f32x16 s = rows_product<HD>(kf, qf);  // rows: keys; column: this lane's query
+    f32x16 s = rows_product_parts<HD>(kf, qf);  // rows: keys; column: this lane's query
     const float base_far = (float)(pos - k0);
     float mt = -INFINITY, g;
 #pragma unroll
@@ -172,11 +199,12 @@ __device__ __forceinline__ void store_joined(const RangeArgs& a, int64_t r, int 
   if (a.o32) st4(a.o32 + r * HD + c, o);
   if (c == 0) {
     const int64_t row = r / a.Hq, b = row / a.Sq;
-    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = LOG2<T> ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
+    a.lse[(b * a.Hq + r % a.Hq) * a.Sq + row % a.Sq] = a.log2 ? (base + log2f(L)) * 0.6931471805599453f : base + logf(L);
   }
 }
-template <typename T>
-__device__ __forceinline__ float share_weight(float m, float base) { return LOG2<T> ? exp2f(m - base) : expf(m - base); }
+__device__ __forceinline__ float share_weight(const RangeArgs& a, float m, float base) {
+  return a.log2 ? exp2f(m - base) : expf(m - base);
+}
 
 // The shares of a row (b, i, h) joined, a block per row: HD / 4 lanes per share, the shares spread over the block, so
 // that a row of many shares takes a few round trips to memory and not one per share (16 rows of 16 shares: 5.6 ->
@@ -194,7 +222,7 @@ __global__ void __launch_bounds__(256) range_join(RangeArgs a) {
   if (t % 64 == 0) top[t / 64] = m;
   __syncthreads();
   const float base = weight_base(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-  const float w = share_weight<T>(ml.x, base);
+  const float w = share_weight(a, ml.x, base);
   weight[t] = w;
   const float l = wave_sum(w * ml.y);
   if (t % 64 == 0) tot[t / 64] = l;
@@ -229,7 +257,7 @@ __global__ void __launch_bounds__(256) range_join_few(RangeArgs a) {
 #pragma unroll
   for (int s = 0; s < FEW_SPLITS; ++s) {
     if (s >= a.nsplit) break;
-    const float w = share_weight<T>(ml[s].x, base);
+    const float w = share_weight(a, ml[s].x, base);
     L += w * ml[s].y;
     o += w * ld4(a.part + (n * s + r) * HD + c);
   }
@@ -292,7 +320,7 @@ __global__ void __launch_bounds__(256) range_prep(RangeArgs a, int width, int nt
   if (!in || c) return;
   a.delta[((int64_t)b * a.Hq + h) * a.Sq + i] = s;
   const float lse = weight_base(a.lse[((int64_t)b * a.Hq + h) * a.Sq + i]);
-  a.nlse[((int64_t)b * a.Hq + h) * a.Sq + i] = LOG2<T> ? -1.4426950408889634f * lse : -lse;
+  a.nlse[((int64_t)b * a.Hq + h) * a.Sq + i] = a.log2 ? -1.4426950408889634f * lse : -lse;
   if (h == 0) {
     const int2 k = seen_keys(a, b, i);
     a.seen_lo[row] = k.x;
@@ -328,9 +356,9 @@ __device__ __forceinline__ void range_dq(const RangeArgs& a, int qb, int split, 
     RowFrag<HD> f;
     f.load(kp, kr, a.k.row);
     const bool plain = !edge || f.finite();
-    f32x16 s = rows_product<HD>(f, qf);
+    f32x16 s = rows_product_parts<HD>(f, qf);
     f.load(vp, kr, a.v.row);
-    const f32x16 dp = rows_product<HD>(f, df);
+    const f32x16 dp = grad_product<HD>(f, df);
     const float base_far = (float)(pos - k0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -387,7 +415,10 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int split,
     // every key of the block is seen by every query of the tile
     const bool whole = q0 + TR <= by.y && __all(mine.x <= k0 && k0 + TR <= mine.y);
     const bool plain_q = whole || f.finite();
-    f32x16 p = rows_product<HD>(f, kf);  // rows: queries; column: this lane's key
+    f32x16 p = rows_product_parts<HD>(f, kf);  // rows: queries; column: this lane's key
+    f.load(dp_, qr, a.dout.row);
+    const bool plain_d = whole || f.finite();
+    f32x16 ds = grad_product<HD>(f, vf);
     // the rows' statistics, four consecutive rows at a time (the arrays end with TR elements of room)
     f32x4 nl[4], dl[4];
     i32x4 lo[4], len[4];
@@ -399,9 +430,6 @@ __device__ __forceinline__ void range_dkv(const RangeArgs& a, int kb, int split,
       __builtin_memcpy(&lo[e4], a.seen_lo + row0 + q0 + r, 16);
       __builtin_memcpy(&len[e4], a.seen_len + row0 + q0 + r, 16);
     }
-    f.load(dp_, qr, a.dout.row);
-    const bool plain_d = whole || f.finite();
-    f32x16 ds = rows_product<HD>(f, vf);
     const float base_far = (float)(position(a, b, q0) - key);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -741,6 +769,7 @@ size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a) {
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
   a.nsplit = fwd_splits(bf, a);
+  a.log2 = bf;
   if (a.nsplit > 1) {
     a.part = (float*)ws;
     a.part_ml = (float2*)((char*)ws + up256(a.nsplit * n * a.hd * 4));
@@ -748,7 +777,7 @@ void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    if constexpr (LOG2<T>) range_mfma_fwd(a, st);
+    if constexpr (sizeof(T) == 2) range_mfma_fwd(a, st);
     else range_fwd<T, HD><<<(unsigned)(cdiv(a.Sq, TR) * a.Hq * a.B * a.nsplit), NW * 64, 0, st>>>(a);
     if (a.nsplit > FEW_SPLITS) range_join<T, HD><<<(unsigned)n, 256, 0, st>>>(a);
     else if (a.nsplit > 1) range_join_few<T, HD><<<(unsigned)cdiv(n * (HD / 4), 256), 256, 0, st>>>(a);
@@ -780,6 +809,7 @@ size_t bwd_layout(bool bf, RangeArgs& a, char* p) {
     return r;
   };
   const int64_t rows = (int64_t)a.B * a.Sq;
+  a.log2 = bf;
   a.delta = (float*)take((rows * a.Hq + TR) * 4);
   a.nlse = (float*)take((rows * a.Hq + TR) * 4);
   a.seen_lo = (int32_t*)take((rows + TR) * 4);
@@ -801,14 +831,14 @@ size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
 
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   bwd_layout(bf, a, (char*)ws);
-  const int width = bf ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
+  const int width = a.log2 ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     const int64_t prep = (int64_t)ntile * a.B + cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256);
     range_prep<T, HD><<<(unsigned)prep, 256, 0, st>>>(a, width, ntile);
     const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.qsplit * a.Hq * a.B;
-    if constexpr (LOG2<T>) range_mfma_bwd(a, st);
+    if constexpr (sizeof(T) == 2) range_mfma_bwd(a, st);
     else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
     const int64_t split = (a.nsplit > 1 ? 2 * (int64_t)a.B * a.Sk * a.Hkv : 0) + (a.qsplit > 1 ? (int64_t)a.B * a.Sq * a.Hq : 0);
     if (split > 0) range_grad_join<T, HD><<<(unsigned)cdiv(split * HD / 8, 256), 256, 0, st>>>(a);

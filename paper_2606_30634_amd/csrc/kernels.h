@@ -237,7 +237,8 @@ struct RangeArgs {
   const float *rope_cos, *rope_sin;  // as in AttnArgs
   // workspace, laid out by the launchers
   float* delta;      // [B, Hq, Sq]
-  float* nlse;       // [B, Hq, Sq]: -lse (in log2 units for the bf16 matrix cores' kernels), 0 where it is -inf
+  bool log2;         // the kernels of the bf16 matrix cores run: statistics in log2 units
+  float* nlse;       // [B, Hq, Sq]: -lse, 0 where it is -inf
   int32_t *seen_lo, *seen_len;  // [B, Sq]: the keys each query sees are seen_lo .. + seen_len - 1
   int2* sees;        // [B, key tiles]: the queries that see any key of a tile lie in [x, y)
   float* part;       // partial sums of split items

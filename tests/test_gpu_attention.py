@@ -280,6 +280,11 @@ def test_strides(hd, bf16):
         T.attention_backward(q, k, v, f, do, out=out, **how)
         for a, b in zip(out, grads):
             assert torch.equal(a, b)
+    # o (and o_f32) of another layout, as torch operations leave them
+    far = base._replace(**{n: t.transpose(1, 2).contiguous().transpose(1, 2) for n, t in base._asdict().items()
+                           if t is not None and n != "lse"})
+    for a, b in zip(T.attention_backward(x["q"], x["k"], x["v"], far, x["do"], **how), grads):
+        assert torch.equal(a, b)
     buf = longer(KV)
     whole = buf._base if buf._base is not None else buf
     T.attention_backward(x["q"], x["k"], x["v"], base, x["do"], out=(torch.empty_like(x["q"]), buf, torch.empty_like(x["v"])), **how)

@@ -173,7 +173,10 @@ __device__ __forceinline__ void acc_rows_to_b_parts(const f32x16& s, bf16x8 (&pa
 }
 
 // EXACT (o kept in fp32): P enters the P V product in three bf16 parts, 24 bits, so that the o in fp32 is one.  With
-// two parts (16 bits) 4 x 2048 packed tokens, 16 heads of 128, take 61 us instead of 65.
+// two parts (16 bits) 4 x 2048 packed tokens, 16 heads of 128, take 61 us instead of 65.  Else P is rounded to bf16, as
+// in the causal kernels (error of o 2.0e-3 of its norm; its own rounding alone 1.7e-3): long rows would pay for two products
+// more (one causal row of 4096 tokens: 340 -> 495 us), few queries on ragged caches for the chain of the one wave that
+// has their rows (16 x 1 query on up to 32768 keys: 227 us, 240 with two parts, 265 with three).
 template <int HD, bool EXACT, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) {
   using L = Lds<HD>;

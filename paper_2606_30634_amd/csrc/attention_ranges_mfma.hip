@@ -12,7 +12,8 @@
 // dK/dV of 128) overlap only in part; short documents also a block's start and end and the part of its tiles that no row
 // sees; a few queries on long caches HBM (16 x 32768 keys, 8 heads of 128: 5.6 TB/s).  One causal row block of 4096 tokens
 // (2 sequences, 32 heads of 128 on 8), by the flops of the pairs seen: forward 336-347 us, 0.79-0.82 PFLOP/s (o kept in fp32,
-// so three times the P V products: 495 us; scores capped: 385-392 us), backward 1004 us, 0.68 PFLOP/s (capped 1229).
+// so three times the P V products: 495 us; scores capped: 385-392 us), backward 1004 us, 0.68 PFLOP/s (capped 1267, and
+// 1859 with every tile past the polynomial).
 #include "attention_ranges.h"
 #include "attention_tiles.h"
 #include <algorithm>
@@ -45,24 +46,26 @@ __device__ __forceinline__ float largest(const f32x16 (&s)[N]) {
   return big;
 }
 
+// tanh(y) up to CapScale::SMALL: y + y^3 P(y^2) with the minimax P of degree 2 (relative error 2^-23, below the rounding
+// of the products)
+__device__ __forceinline__ float tanh_small(float y) {
+  const float z = y * y;
+  float p = __builtin_fmaf(z, -0.0477941558f, 0.1327762753f);
+  p = __builtin_fmaf(z, p, -0.3333188295f);
+  return y * __builtin_fmaf(z, p, 1.0f);
+}
+
 // tanh(scale x / cap) of a wave's products, `big` their largest |x| in the lane.  One branch for the wave: where no
-// |y| passes CapScale::SMALL (most tiles) the polynomial alone: y + y^3 P(y^2) with the minimax P of degree 2 (relative
-// error 2^-23, below the rounding of the products).
-template <int N>
-__device__ __forceinline__ void tanh_scores(f32x16 (&s)[N], const CapScale& c, float big) {
+// |y| passes CapScale::SMALL (most tiles) the polynomial alone.
+__device__ __forceinline__ void tanh_scores(f32x16 (&s)[2], const CapScale& c, float big) {
   if (__all(big <= c.small)) {
 #pragma unroll
-    for (int t = 0; t < N; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float y = s[t][e] * c.y_of, z = y * y;
-        float p = __builtin_fmaf(z, -0.0477941558f, 0.1327762753f);
-        p = __builtin_fmaf(z, p, -0.3333188295f);
-        s[t][e] = y * __builtin_fmaf(z, p, 1.0f);
-      }
+      for (int e = 0; e < 16; ++e) s[t][e] = tanh_small(s[t][e] * c.y_of);
   } else {
 #pragma unroll
-    for (int t = 0; t < N; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float g;
@@ -431,19 +434,77 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
 }
 
 // ------------------------------------------------------------------------------------------ backward
-// P and dS of one pair, from dp = dO.v and s = q.k, or with CAP its tanh_scores
-struct Pair { float p, ds; };
-// 1 - t^2 of t = tanh; 0 for the -inf of a pair that is not seen
-__device__ __forceinline__ float cap_grad(float t) { return __builtin_amdgcn_fmed3f(__builtin_fmaf(-t, t, 1.0f), 0.f, 1.f); }
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ Pair grad_pair(float s, float dp, float nlse2, float delta, const CapScale& c, float slope2,
-                                          float far) {
-  float x = __builtin_fmaf(s, CAP ? c.out : c.sl2, nlse2);
-  if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far), x);
-  const float p = fast_exp2(x), ds = p * (dp - delta);
-  return Pair{p, CAP ? ds * cap_grad(s) : ds};
+// The tanh of a tile's products ahead of a softmax of the backward.  Behind the polynomial its slope is 1 - t^2, an
+// instruction of the softmax.  A t near 1 has lost it (at y = 8 it would be 6 % off, from y = 10 on 0), so in the other branch the
+// slope comes from e = exp(-2 |y|), as 4 e / (1 + e)^2, and is put where the softmax finds it for nothing more:
+//   dK/dV  into dp = (dp - delta) slope, of which the softmax subtracts keep delta = 0 and takes clamp(one - t^2) = 1
+//   dQ     into the score: ds alone is wanted, so s becomes t + log(slope) / cap, and the softmax's slope is at least 1
+// (a pair that is not seen has s = -inf or its ds replaced).
+struct FarTanh {
+  float t, a, e, r;  // tanh(y), log2(e), e, 1 / (1 + e)
+  __device__ FarTanh(float x, const CapScale& c) {
+    asm volatile("" : "+v"(x));  // apart from the other branch: what both compute would be kept for the whole tile ahead of them
+    const float y = x * c.y_of;
+    a = fabsf(y) * -2.8853900817779268f;
+    e = fast_exp2(a);
+    r = __builtin_amdgcn_rcpf(1.0f + e);
+    const float far = copysignf(__builtin_fmaf(-2.0f * e, r, 1.0f), y);
+    t = fabsf(y) < TANH_SMALL ? __builtin_fmaf(y, tanh_excess(y * y), y) : far;
+  }
+  __device__ float slope() const { return 4.0f * e * r * r; }
+  __device__ float log2_slope() const { return __builtin_fmaf(2.0f, __builtin_amdgcn_logf(r), a + 2.0f); }
+};
+struct CapSlope {
+  float keep = 1.f, one = 1.f;
+  __device__ float operator()(float t) const { return __builtin_amdgcn_fmed3f(__builtin_fmaf(-t, t, one), 0.f, 1.f); }
+  __device__ float less(float dp, float delta) const { return __builtin_fmaf(-keep, delta, dp); }
+};
+// delta: of the lane's accumulator rows, four at a time 8 apart
+__device__ __forceinline__ CapSlope tanh_ahead(f32x16& s, f32x16& dp, const CapScale& c, const float* delta) {
+  CapSlope r;
+  if (__all(largest(reinterpret_cast<const f32x16(&)[1]>(s)) <= c.small)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = tanh_small(s[e] * c.y_of);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const FarTanh f(s[e], c);
+      dp[e] = (dp[e] - delta[8 * (e / 4) + e % 4]) * f.slope();
+      s[e] = f.t;  // last, as in the other branch: the compiler joins the branches' last stores, and a choice between s
+    }              // and dp there would put both into scratch memory
+    r.keep = 0.f;
+    r.one = 2.f;
+  }
+  return r;
+}
+// gives the least slope
+__device__ __forceinline__ float tanh_ahead_dq(f32x16 (&s)[2], const CapScale& c) {
+  if (__all(largest(s) <= c.small)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = tanh_small(s[t][e] * c.y_of);
+    return 0.f;
+  }
+  const float per = 1.0f / c.out;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const FarTanh f(s[t][e], c);
+      s[t][e] = __builtin_fmaf(f.log2_slope(), per, f.t);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  return 1.f;
 }
 
+// P of one pair, from s = q.k or with CAP its tanh
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float weight(float s, float nlse2, const CapScale& c, float slope2, float far) {
+  float x = __builtin_fmaf(s, CAP ? c.out : c.sl2, nlse2);
+  if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far), x);
+  return fast_exp2(x);
+}
 template <int N>
 __device__ __forceinline__ bool all_finite(const f32x16 (&x)[N]) {
   float z = 0.f;  // stays 0 as long as every value is finite
@@ -607,6 +668,23 @@ __device__ __forceinline__ void dkv_store(const RangeArgs& a, const KeyItem& ite
   }
 }
 
+// frag_rows and frag_cols of a given lane
+template <int HD>
+__device__ __forceinline__ bf16x8 frag_rows_of(const bf16* T, int r0, int k0, int l) {
+  return *reinterpret_cast<const bf16x8*>(T + tidx<HD>(r0 + l % 32, k0 + 8 * (l / 32)));
+}
+template <int HD>
+__device__ __forceinline__ bf16x8 frag_cols_of(const bf16* T, int c0, int k0, int l) {
+  const int g = l / 16, i = l % 16, c = c0 + 16 * (g & 1) + 4 * (i & 3), k = k0 + 8 * (g >> 1) + (i >> 2);
+  typedef __attribute__((address_space(3))) v4i16_t lds_v4i16;
+  const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(T + tidx<HD>(k, c)));
+  const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(T + tidx<HD>(k + 4, c)));
+  bf16x8 f;
+  __builtin_memcpy(&f, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+  return f;
+}
+
 template <int HD, bool CAP, bool BIAS>
 __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int split, int h, int b,
                                                unsigned char* __restrict__ smem) {
@@ -676,14 +754,20 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
     const bf16* Vs = Ks + L::TSZ;
     const int key0 = blo + kt * KB;
     if (key0 < wk.hi && key0 + KB > wk.lo) {
+      // frag_rows and frag_cols; with CAP at 128 their addresses are formed here, tile by tile: kept across the loop they
+      // push other registers out to memory (2 x 4096 tokens, 32 heads on 8: dQ 528 us, and 800 with the exact slopes)
+      int at = lane;
+      if constexpr (CAP && HD == 128) asm volatile("" : "+v"(at));
+      auto rows_at = [&](const bf16* T, int r, int k) { return frag_rows_of<HD>(T, r, k, at); };
+      auto cols_at = [&](const bf16* T, int c, int k) { return frag_cols_of<HD>(T, c, k, at); };
       // as in attention_mfma.hip: S and dP of both 32-key sub-tiles, then the softmax and the dQ products of each
       f32x16 s[2], dp[2];
       if constexpr (HD == 128) {
         bf16x8 fk[2][2], fv[2][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          fk[0][t] = frag_rows<HD>(Ks, t * 32, 0);
-          fv[0][t] = frag_rows<HD>(Vs, t * 32, 0);
+          fk[0][t] = rows_at(Ks, t * 32, 0);
+          fv[0][t] = rows_at(Vs, t * 32, 0);
         }
         static_for<KS>([&](auto KSI) {
           constexpr int ks = KSI, c = ks & 1;
@@ -691,8 +775,8 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
           if constexpr (ks + 1 < KS) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              fk[c ^ 1][t] = frag_rows<HD>(Ks, t * 32, (ks + 1) * 16);
-              fv[c ^ 1][t] = frag_rows<HD>(Vs, t * 32, (ks + 1) * 16);
+              fk[c ^ 1][t] = rows_at(Ks, t * 32, (ks + 1) * 16);
+              fv[c ^ 1][t] = rows_at(Vs, t * 32, (ks + 1) * 16);
             }
           }
 #pragma unroll
@@ -713,11 +797,12 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ks, t * 32, ks * 16), qf[ks], ks ? s[t] : f32x16{}, 0, 0, 0);
-            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Vs, t * 32, ks * 16), df[ks], ks ? dp[t] : f32x16{}, 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows_at(Ks, t * 32, ks * 16), qf[ks], ks ? s[t] : f32x16{}, 0, 0, 0);
+            dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows_at(Vs, t * 32, ks * 16), df[ks], ks ? dp[t] : f32x16{}, 0, 0, 0);
           }
       }
-      if constexpr (CAP) tanh_scores(s, cs, largest(s));
+      float least = 0.f;
+      if constexpr (CAP) least = tanh_ahead_dq(s, cs);
       const float base_far = BIAS ? (float)(pos - key0 - 4 * half) : 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -726,13 +811,16 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
         if constexpr (HD == 128) {
           static_for<RA>([&](auto QI) {
             constexpr int q = QI;
-            fc[q] = frag_cols<HD>(Ks, (q % DT) * 32, t * 32 + (q / DT) * 16);
+            fc[q] = cols_at(Ks, (q % DT) * 32, t * 32 + (q / DT) * 16);
           });
           __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          dp[t][e] = grad_pair<CAP, BIAS>(s[t][e], dp[t][e], nl, dl, cs, slope2, base_far - (float)(t * 32 + 8 * (e / 4) + e % 4)).ds;
+        for (int e = 0; e < 16; ++e) {
+          const float far = base_far - (float)(t * 32 + 8 * (e / 4) + e % 4);
+          dp[t][e] = weight<CAP, BIAS>(s[t][e], nl, cs, slope2, far) * (dp[t][e] - dl);
+          if constexpr (CAP) dp[t][e] *= __builtin_amdgcn_fmed3f(__builtin_fmaf(-s[t][e], s[t][e], 1.0f), least, 1.f);
+        }
         if (!wk.whole(key0 + t * 32, key0 + t * 32 + 32)) {
           const uint32_t first = (uint32_t)(key0 + t * 32 + 4 * half - mask.x), len = (uint32_t)(mask.y - mask.x);
 #pragma unroll
@@ -745,7 +833,7 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
             constexpr int q = QI, g2 = q / DT, dt = q % DT;
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (q + RA < NC)
-              fc[(q + RA) % (RA + 1)] = frag_cols<HD>(Ks, ((q + RA) % DT) * 32, t * 32 + ((q + RA) / DT) * 16);
+              fc[(q + RA) % (RA + 1)] = cols_at(Ks, ((q + RA) % DT) * 32, t * 32 + ((q + RA) / DT) * 16);
             dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[q % (RA + 1)], g2 ? b1 : b0, dq[dt], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
           });
@@ -755,7 +843,7 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
             const bf16x8 bop = g2 ? acc_rows_to_b<8>(dp[t]) : acc_rows_to_b<0>(dp[t]);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
-              dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<HD>(Ks, dt * 32, t * 32 + g2 * 16), bop, dq[dt], 0, 0, 0);
+              dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols_at(Ks, dt * 32, t * 32 + g2 * 16), bop, dq[dt], 0, 0, 0);
           }
         }
       }
@@ -859,30 +947,31 @@ __device__ __forceinline__ void range_dkv_block(const RangeArgs& a, const KeyIte
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s[1], dp;
+      f32x16 s, dp;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Qs, t * 32, ks * 16), kf[ks], ks ? s[0] : f32x16{}, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Qs, t * 32, ks * 16), kf[ks], ks ? s : f32x16{}, 0, 0, 0);
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<HD>(Ds, t * 32, ks * 16), vf[ks], ks ? dp : f32x16{}, 0, 0, 0);
       }
-      if constexpr (CAP) tanh_scores(s, cs, largest(s));
+      const float* stats = Ls + t * 32 + 4 * half;  // nlse, and KB behind it delta, of the lane's rows 8 e4 + j
+      CapSlope slope;
+      if constexpr (CAP) slope = tanh_ahead(s, dp, cs, stats + KB);
       const float base_far = (float)far0;
-      mask_unseen<HD>(s[0], Qs, t * 32, mykey);
+      mask_unseen<HD>(s, Qs, t * 32, mykey);
 #pragma unroll
       for (int e4 = 0; e4 < 4; ++e4) {
-        const float* r = Ls + t * 32 + 8 * e4 + 4 * half;
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(r), d4 = *reinterpret_cast<const f32x4*>(r + KB);
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats + 8 * e4), d4 = *reinterpret_cast<const f32x4*>(stats + KB + 8 * e4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int e = 4 * e4 + j;
-          const Pair w = grad_pair<CAP, BIAS>(s[0][e], dp[e], l4[j], d4[j], cs, slope2, base_far + (float)(t * 32 + 8 * e4 + j));
-          s[0][e] = w.p;
-          dp[e] = w.ds;
+          const float p = weight<CAP, BIAS>(s[e], l4[j], cs, slope2, base_far + (float)(t * 32 + 8 * e4 + j));
+          dp[e] = p * (CAP ? slope.less(dp[e], d4[j]) * slope(s[e]) : dp[e] - d4[j]);
+          s[e] = p;
         }
       }
 #pragma unroll
       for (int g2 = 0; g2 < 2; ++g2) {
-        const bf16x8 pb = g2 ? acc_rows_to_b<8>(s[0]) : acc_rows_to_b<0>(s[0]);
+        const bf16x8 pb = g2 ? acc_rows_to_b<8>(s) : acc_rows_to_b<0>(s);
         const bf16x8 sb = g2 ? acc_rows_to_b<8>(dp) : acc_rows_to_b<0>(dp);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
@@ -969,10 +1058,10 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
   bf16x8 pb[2][2], sb[2][2];  // P and dS as operands, two 16-query halves each
 
   // One step, as there: the loads of a stage (FE), S and dP of tile T of the stage at `rows` (SC), the softmax of
-  // the other tile, whose first query is sq0 and head's slope slope2, with the row vectors at `stats` (SM; with CAP on its tanh_scores), and dV and dK
-  // of tile T of the stage at `cols` (PV).
+  // the other tile, whose first query is sq0 and head's slope slope2, with the row vectors at `stats` (SM; with CAP behind
+  // tanh_ahead, which gave `cap`), and dV and dK of tile T of the stage at `cols` (PV).
   auto step = [&](auto T_, auto SC_, auto SM_, auto PV_, auto FE_, const bf16* rows, const bf16* stats, int sq0,
-                  float slope2, const bf16* cols) {
+                  float slope2, const bf16* cols, const CapSlope& cap) {
     constexpr int T = T_, U = T ^ 1;
     constexpr bool SC = SC_, SM = SM_, PV = PV_, FE = FE_;
     const bf16 *Qr = rows, *Dr = rows + Q::TSZ, *Qc = cols, *Dc = cols + Q::TSZ;
@@ -1033,11 +1122,12 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (SC) dp[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[c], vf[g], g ? dp[T] : f32x16{}, 0, 0, 0);
       if constexpr (SM) {
-        y0 = dp[U][e0] - d4[lb][e0 % 4];
-        y1 = dp[U][e1] - d4[lb][e1 % 4];
         if constexpr (CAP) {
-          y0 *= cap_grad(s[U][e0]);
-          y1 *= cap_grad(s[U][e1]);
+          y0 = cap.less(dp[U][e0], d4[lb][e0 % 4]) * cap(s[U][e0]);
+          y1 = cap.less(dp[U][e1], d4[lb][e1 % 4]) * cap(s[U][e1]);
+        } else {
+          y0 = dp[U][e0] - d4[lb][e0 % 4];
+          y1 = dp[U][e1] - d4[lb][e1 % 4];
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -1059,12 +1149,12 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
   constexpr std::false_type no{};
   auto soft = [&](auto T_, auto SC_, auto PV_, auto FE_, const bf16* rows, const bf16* stats, int sq0, float slope2, const bf16* cols) {
     constexpr int U = T_ ^ 1;
+    CapSlope cap;
     if constexpr (CAP) {
-      f32x16(&u)[1] = reinterpret_cast<f32x16(&)[1]>(s[U]);
-      tanh_scores(u, cs, largest(u));
+      cap = tanh_ahead(s[U], dp[U], cs, reinterpret_cast<const float*>(stats + 2 * Q::TSZ) + KB + U * 32 + 4 * half);
     }
     mask_unseen<HD>(s[U], stats, U * 32, mykey);
-    step(T_, SC_, std::true_type{}, PV_, FE_, rows, stats, sq0, slope2, cols);
+    step(T_, SC_, std::true_type{}, PV_, FE_, rows, stats, sq0, slope2, cols, cap);
   };
   auto arrive = [&] {
     wait_vm_lds<0>();
@@ -1085,7 +1175,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     };
     arrive();
     next_tile();
-    step(t0, yes, no, no, yes, cur, cur, 0, 0.f, cur);
+    step(t0, yes, no, no, yes, cur, cur, 0, 0.f, cur, CapSlope{});
     soft(t1, yes, no, yes, cur, cur, qc, mc, cur);
     for (int it = item.it0 + 1; it < item.nit; ++it) {
       turn();
@@ -1097,7 +1187,7 @@ __device__ __forceinline__ void range_dkv128_block(const RangeArgs& a, const Key
     }
     acc_settled(dk, dv);
     soft(t0, no, yes, no, cur, cur, qc + 32, mc, cur);
-    step(t1, no, no, yes, no, cur, cur, 0, 0.f, cur);
+    step(t1, no, no, yes, no, cur, cur, 0, 0.f, cur, CapSlope{});
     acc_settled(dk, dv);
     wait_vm_lds<0>();  // the last, unread loads: the ring becomes the output staging
   }

@@ -449,6 +449,8 @@ int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents
  * keys [key_start[i], key_end[i]) (what lies outside [0, keys) is cut off), or, with key_start NULL, the
  * keys at or before its position.  With x = scale q.k the score of key j is
  *   cap tanh(x / cap) - slopes[h] |position - j|   (softcap 0: x; slopes NULL: no second term).
+ * A launch bounds batch x (ceil(queries / 32) + 1) x heads + batch x (ceil(keys / 32) + 1) x kv_heads to below 2^25 (in
+ * fp32 2^24) and, in the backward, batch x queries x heads x head_dim to about 2^34; a call beyond is refused.
  * A query that sees no key has o = 0, lse = -inf and no gradient; what a query does not see has no
  * influence on it, whatever it holds.  Products of bf16 accumulate in fp32; their operands P and dS
  * are rounded to bf16, but where o_f32 is kept the forward takes P in three bf16 parts (24 bits). */

@@ -766,6 +766,12 @@ size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a) {
   return ns > 1 ? up256(ns * n * a.hd * 4) + up256(ns * n * 8) : 0;
 }
 
+int64_t range_fwd_blocks(bool bf, const RangeArgs& a) {
+  const int64_t ns = fwd_splits(bf, a), n = (int64_t)a.B * a.Sq * a.Hq;
+  const int64_t items = bf ? range_mfma_items(a) : cdiv(a.Sq, TR) * a.Hq * a.B;
+  return std::max(items * ns, ns > FEW_SPLITS ? n : ns > 1 ? cdiv(n * (a.hd / 4), 256) : 0);
+}
+
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   const int64_t n = (int64_t)a.B * a.Sq * a.Hq;
   a.nsplit = fwd_splits(bf, a);
@@ -829,19 +835,40 @@ size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a) {
   return bwd_layout(bf, t, nullptr);
 }
 
+namespace {
+
+// The blocks of a backward whose arguments bwd_layout has completed
+struct BwdBlocks {
+  int64_t prep, grads, join;
+  explicit BwdBlocks(const RangeArgs& a) {
+    const int rows = a.log2 ? range_mfma_keys() : TR;
+    const int64_t q = (int64_t)a.B * a.Sq * a.Hq, k = (int64_t)a.B * a.Sk * a.Hkv;
+    prep = cdiv(a.Sk, rows) * a.B + cdiv(q * (a.hd / 4), 256);
+    grads = cdiv(a.Sk, rows) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, rows) * a.qsplit * a.Hq * a.B;
+    join = cdiv(((a.nsplit > 1 ? 2 * k : 0) + (a.qsplit > 1 ? q : 0)) * a.hd / 8, 256);
+  }
+};
+
+}  // namespace
+
+int64_t range_bwd_blocks(bool bf, const RangeArgs& a) {
+  RangeArgs t = a;
+  bwd_layout(bf, t, nullptr);
+  const BwdBlocks n(t);
+  return std::max({n.prep, n.grads, n.join});
+}
+
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
   bwd_layout(bf, a, (char*)ws);
   const int width = a.log2 ? range_mfma_keys() : TR, ntile = (int)cdiv(a.Sk, width);
+  const BwdBlocks n(a);
   dispatch(bf, a.hd, [&](auto t, auto hd) {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    const int64_t prep = (int64_t)ntile * a.B + cdiv((int64_t)a.B * a.Sq * a.Hq * (HD / 4), 256);
-    range_prep<T, HD><<<(unsigned)prep, 256, 0, st>>>(a, width, ntile);
-    const int64_t blocks = cdiv(a.Sk, TR) * a.nsplit * a.Hkv * a.B + cdiv(a.Sq, TR) * a.qsplit * a.Hq * a.B;
+    range_prep<T, HD><<<(unsigned)n.prep, 256, 0, st>>>(a, width, ntile);
     if constexpr (sizeof(T) == 2) range_mfma_bwd(a, st);
-    else range_bwd<T, HD><<<(unsigned)blocks, NW * 64, 0, st>>>(a);
-    const int64_t split = (a.nsplit > 1 ? 2 * (int64_t)a.B * a.Sk * a.Hkv : 0) + (a.qsplit > 1 ? (int64_t)a.B * a.Sq * a.Hq : 0);
-    if (split > 0) range_grad_join<T, HD><<<(unsigned)cdiv(split * HD / 8, 256), 256, 0, st>>>(a);
+    else range_bwd<T, HD><<<(unsigned)n.grads, NW * 64, 0, st>>>(a);
+    if (n.join > 0) range_grad_join<T, HD><<<(unsigned)n.join, 256, 0, st>>>(a);
   });
 }
 

@@ -250,6 +250,11 @@ struct RangeArgs {
 size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a);
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st);
 size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a);
+// The blocks of a pass's largest launch, all of 256 threads.  A launch takes fewer than 2^32 threads, and what the
+// backward's first one does not write sets the loops and addresses of the next: it must not be refused alone.
+constexpr int64_t MAX_BLOCKS_256 = ((int64_t)1 << 24) - 1;
+int64_t range_fwd_blocks(bool bf, const RangeArgs& a);
+int64_t range_bwd_blocks(bool bf, const RangeArgs& a);
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st);
 // key_start, key_end [B, S] of packed documents ids [B, S] (flags: prefix tokens, may be null)
 void launch_key_ranges(int64_t B, int S, const int32_t* ids, const uint8_t* flags, int32_t* start, int32_t* end,

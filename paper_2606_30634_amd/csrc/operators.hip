@@ -70,8 +70,7 @@ const char* check_attention(const attention_params_t* p, RangeArgs& a) {
   if (off(p->key_start, 4) || off(p->key_end, 4) || off(p->q_start, 4) || off(p->slopes, 4))
     return "arrays must be 4-byte aligned";
   const int64_t blocks = ((p->queries + 31) / 32 + 1) * p->heads + ((p->keys + 31) / 32 + 1) * p->kv_heads;
-  if (p->batch * blocks >= ((int64_t)1 << 25) || p->batch * p->queries * p->heads >= ((int64_t)1 << 33))
-    return "batch x (queries heads + keys kv_heads) is too large for a launch";
+  if (p->batch * blocks >= ((int64_t)1 << 25)) return "batch x (queries heads + keys kv_heads) is too large";
   a = RangeArgs{};
   a.B = (int)p->batch; a.Sq = (int)p->queries; a.Sk = (int)p->keys;
   a.Hq = p->heads; a.Hkv = p->kv_heads; a.hd = p->head_dim;
@@ -305,6 +304,7 @@ int attention_forward(const attention_params_t* p, const void* q, const void* k,
     for (int j = 0; j < i; ++j)
       if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n)) return bad("the outputs overlap");
   }
+  if (range_fwd_blocks(bf, a) > MAX_BLOCKS_256) return bad("batch x queries x heads is too large for a launch");
   if (const char* m = check_ws(workspace, workspace_bytes, range_fwd_ws_bytes(bf, a))) return bad(m);
   a.o = o; a.o32 = o_f32; a.lse = lse;
   launch_range_fwd(bf, a, workspace, (hipStream_t)hip_stream);
@@ -362,6 +362,8 @@ int attention_backward(const attention_params_t* p, const void* q, const void* k
       if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n) &&
           !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz))
         return bad("the gradients overlap");
+  if (range_bwd_blocks(bf, a) > MAX_BLOCKS_256)
+    return bad("batch x (queries x heads x head_dim / 1024 + keys) is too large for a launch of the backward");
   if (const char* m = check_ws(workspace, workspace_bytes, range_bwd_ws_bytes(bf, a))) return bad(m);
   (g->o_is_f32 ? (void*&)a.o32 : a.o) = const_cast<void*>(o);
   a.ob = orows.batch; a.orow = orows.row; a.oh = orows.head;

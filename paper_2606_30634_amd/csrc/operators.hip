@@ -1,5 +1,6 @@
 // C entries of the stateless operators: argument checks, then the launchers of logprob.hip, losses.hip,
 // attention_ranges.hip and dropout.hip.
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/asyncstage.h"
@@ -106,12 +107,14 @@ bool apart(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t
   }
   return true;
 }
-// gradients x and y (heads of `w` elements in all, strides sx and sy) are different heads of the same packed rows
-bool packed_apart(const void* x, const int64_t* sx, int64_t wx, const void* y, const int64_t* sy, int64_t wy, size_t esz) {
+// gradients x and y (heads of `w` elements in all, strides sx and sy) are different heads of the same packed rows, and the
+// rows, of both together, lie apart over batch and rows
+bool packed_apart(const void* x, const int64_t* sx, int64_t wx, const void* y, const int64_t* sy, int64_t wy, size_t esz,
+                  int64_t batch, int64_t rows) {
   if (sx[0] != sy[0] || sx[1] != sy[1]) return false;
-  if ((uintptr_t)y < (uintptr_t)x) return packed_apart(y, sy, wy, x, sx, wx, esz);
+  if ((uintptr_t)y < (uintptr_t)x) return packed_apart(y, sy, wy, x, sx, wx, esz, batch, rows);
   const int64_t at = ((const char*)y - (const char*)x) / (int64_t)esz;  // both multiples of 16 bytes
-  return wx <= at && at + wy <= sx[1];
+  return wx <= at && at + wy <= sx[1] && apart(sx, batch, rows, 1, at + wy);
 }
 // bytes that rows span
 size_t extent(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t hd, size_t esz) {
@@ -360,7 +363,7 @@ int attention_backward(const attention_params_t* p, const void* q, const void* k
   for (int i = 0; i < 3; ++i)
     for (int j = 0; j < i; ++j)
       if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n) &&
-          !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz))
+          !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz, a.B, std::max(a.Sq, a.Sk)))
         return bad("the gradients overlap");
   if (range_bwd_blocks(bf, a) > MAX_BLOCKS_256)
     return bad("batch x (queries x heads x head_dim / 1024 + keys) is too large for a launch of the backward");

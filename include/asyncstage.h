@@ -477,8 +477,9 @@ int attention_forward(const attention_params_t* p, const void* q, const void* k,
                       float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradients in q, k and v, from what the forward read and wrote (o, or better the o_f32 that it kept) and the
- * gradient dout in o.  No atomics: the same inputs give the same bits.  dq, dk and dv may be the heads of one
- * packed row (equal row strides). */
+ * gradient dout in o.  No atomics: the same inputs give the same bits.  dq, dk and dv may interleave where they share
+ * the strides that step over all of them: heads of one packed row, heads one by one ([B, S, kv_heads, 2, hd]), slices
+ * of a [B, heads, S, hd] tensor.  Layouts that share an element, or of which that cannot be told, are refused. */
 typedef struct {
   int64_t o_strides[3], dout_strides[3], dq_strides[3], dk_strides[3], dv_strides[3];
   void *dq, *dk, *dv;

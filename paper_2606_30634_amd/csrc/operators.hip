@@ -107,14 +107,34 @@ bool apart(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t
   }
   return true;
 }
-// gradients x and y (heads of `w` elements in all, strides sx and sy) are different heads of the same packed rows, and the
-// rows, of both together, lie apart over batch and rows
-bool packed_apart(const void* x, const int64_t* sx, int64_t wx, const void* y, const int64_t* sy, int64_t wy, size_t esz,
-                  int64_t batch, int64_t rows) {
-  if (sx[0] != sy[0] || sx[1] != sy[1]) return false;
-  if ((uintptr_t)y < (uintptr_t)x) return packed_apart(y, sy, wy, x, sx, wx, esz, batch, rows);
-  const int64_t at = ((const char*)y - (const char*)x) / (int64_t)esz;  // both multiples of 16 bytes
-  return wx <= at && at + wy <= sx[1] && apart(sx, batch, rows, 1, at + wy);
+// Rows of n sequences, rows and heads (elements between them: s) of hd elements, and whether x and y, whose extents meet,
+// share none: for some of the dimensions, of the same strides in both, what the other ones hold of x and of y lies side by
+// side, and both together, as one, apart over them.  (Heads of one packed row, single tokens included; heads interleaved one
+// by one; slices of a [B, heads, S, hd] tensor.)
+struct Layout {
+  const void* p;
+  const int64_t* s;
+  int64_t n[3], hd;
+};
+bool side_by_side(const Layout& x, const Layout& y, size_t esz) {
+  if ((uintptr_t)y.p < (uintptr_t)x.p) return side_by_side(y, x, esz);
+  const int64_t at = ((const char*)y.p - (const char*)x.p) / (int64_t)esz;  // both multiples of 16 bytes
+  for (int outer = 0; outer < 8; ++outer) {
+    int64_t wx = x.hd, wy = y.hd, st[3] = {}, n[3] = {1, 1, 1};
+    bool same = true;
+    for (int k = 0; k < 3; ++k) {
+      if (outer >> k & 1) {
+        same &= x.n[k] <= 1 || y.n[k] <= 1 || x.s[k] == y.s[k];
+        n[k] = std::max(x.n[k], y.n[k]);
+        st[k] = x.n[k] > 1 ? x.s[k] : y.s[k];  // the stride of a dimension of one is never used
+      } else {
+        wx += (x.n[k] - 1) * x.s[k];
+        wy += (y.n[k] - 1) * y.s[k];
+      }
+    }
+    if (same && wx <= at && apart(st, n[0], n[1], n[2], at + wy)) return true;
+  }
+  return false;
 }
 // bytes that rows span
 size_t extent(const int64_t* s, int64_t batch, int64_t rows, int64_t heads, int64_t hd, size_t esz) {
@@ -357,13 +377,11 @@ int attention_backward(const attention_params_t* p, const void* q, const void* k
     for (auto& y : ins)
       if (meet(x.p, x.n, y.p, y.n)) return bad("a gradient may not overlap an input");
   // the three may be interleaved, as the heads of one packed row are
-  const int64_t* st[3] = {g->dq_strides, g->dk_strides, g->dv_strides};
-  int64_t wide[3];
-  for (int i = 0; i < 3; ++i) wide[i] = ((i ? a.Hkv : a.Hq) - 1) * st[i][2] + a.hd;
+  const Layout lay[3] = {{g->dq, g->dq_strides, {a.B, a.Sq, a.Hq}, a.hd}, {g->dk, g->dk_strides, {a.B, a.Sk, a.Hkv}, a.hd},
+                         {g->dv, g->dv_strides, {a.B, a.Sk, a.Hkv}, a.hd}};
   for (int i = 0; i < 3; ++i)
     for (int j = 0; j < i; ++j)
-      if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n) &&
-          !packed_apart(outs[j].p, st[j], wide[j], outs[i].p, st[i], wide[i], esz, a.B, std::max(a.Sq, a.Sk)))
+      if (meet(outs[j].p, outs[j].n, outs[i].p, outs[i].n) && !side_by_side(lay[j], lay[i], esz))
         return bad("the gradients overlap");
   if (range_bwd_blocks(bf, a) > MAX_BLOCKS_256)
     return bad("batch x (queries x heads x head_dim / 1024 + keys) is too large for a launch of the backward");

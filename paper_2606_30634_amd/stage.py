@@ -108,7 +108,10 @@ class Stage:
             raise ValueError(f"slopes: expected a contiguous float32 [{self.shape.n_heads}] tensor on {self.device}")
         v = B.StageVariant(softcap, None if slopes is None else slopes.data_ptr(), dropout, seed, offset, int(documents))
         nbytes = B.stage_variant_bytes(self.handle, v)
-        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self.stream):  # memory that only this stream's past work may still use
+            ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        if slopes is not None:  # read on the stage stream, behind what the caller's stream does to them
+            self.stream.wait_stream(torch.cuda.current_stream(self.device))
         B.stage_set_variant(self.handle, v, (ws.data_ptr() + 255) // 256 * 256, nbytes)
         self._hold_old_variant()
         self._variant = (ws, slopes)

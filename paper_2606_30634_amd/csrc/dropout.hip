@@ -8,6 +8,7 @@
 // fit beside that).
 #include "common.h"
 #include "kernels.h"
+#include <algorithm>
 
 namespace {
 
@@ -33,10 +34,10 @@ struct Vec8 {
 };
 
 // VEC: the 8 elements of a counter are contiguous and aligned in every array (row: the counters of a row, or
-// 0 where the arrays have no gaps); else they are taken one by one.
+// 0 where the arrays have no gaps); else they are taken one by one.  From counter g0 on.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) dropout(DropoutArgs a, int64_t row, int64_t n) {
-  const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(256) dropout(DropoutArgs a, int64_t row, int64_t n, int64_t g0) {
+  const int64_t g = g0 + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (8 * g >= n) return;
   u32x4 w = {0, 0, 0, 0};
   if (a.threshold) w = philox((uint64_t)g, a.offset, a.seed);
@@ -88,9 +89,12 @@ void launch_dropout(bool bf, const DropoutArgs& a, hipStream_t st) {
   const bool vec = flat ? fits(a.x, 0) && fits(a.resid, 0) && fits(a.out, 0)
                         : a.cols % 8 == 0 && fits(a.x, a.ldx) && fits(a.resid, a.ldr) && fits(a.out, a.ldo);
   const int64_t row = flat ? 0 : a.cols / 8;
-  const unsigned blocks = (unsigned)cdiv(cdiv(n, 8), 256);
-  if (bf && vec) dropout<bf16, true><<<blocks, 256, 0, st>>>(a, row, n);
-  else if (bf) dropout<bf16, false><<<blocks, 256, 0, st>>>(a, row, n);
-  else if (vec) dropout<float, true><<<blocks, 256, 0, st>>>(a, row, n);
-  else dropout<float, false><<<blocks, 256, 0, st>>>(a, row, n);
+  // a launch takes fewer than 2^32 threads: 2^35 elements
+  for (int64_t g0 = 0; 8 * g0 < n; g0 += 256 * MAX_BLOCKS_256) {
+    const unsigned blocks = (unsigned)std::min(cdiv(cdiv(n - 8 * g0, 8), 256), MAX_BLOCKS_256);
+    if (bf && vec) dropout<bf16, true><<<blocks, 256, 0, st>>>(a, row, n, g0);
+    else if (bf) dropout<bf16, false><<<blocks, 256, 0, st>>>(a, row, n, g0);
+    else if (vec) dropout<float, true><<<blocks, 256, 0, st>>>(a, row, n, g0);
+    else dropout<float, false><<<blocks, 256, 0, st>>>(a, row, n, g0);
+  }
 }

@@ -212,6 +212,9 @@ void launch_attention_fwd(bool bf, const AttnArgs& a, hipStream_t st);
 void launch_attention_delta(bool bf, const AttnArgs& a, hipStream_t st);
 void launch_attention_bwd(bool bf, const AttnArgs& a, hipStream_t st);
 
+// Blocks of 256 threads that a launch takes: fewer than 2^32 threads
+constexpr int64_t MAX_BLOCKS_256 = ((int64_t)1 << 24) - 1;
+
 // ------------------------------------------------------------------ attention over key ranges (attention_ranges.hip)
 // Rows of a head: head h of row i of sequence b starts at element b batch + i row + h head of p
 struct HeadRows {
@@ -250,9 +253,8 @@ struct RangeArgs {
 size_t range_fwd_ws_bytes(bool bf, const RangeArgs& a);
 void launch_range_fwd(bool bf, RangeArgs a, void* ws, hipStream_t st);
 size_t range_bwd_ws_bytes(bool bf, const RangeArgs& a);
-// The blocks of a pass's largest launch, all of 256 threads.  A launch takes fewer than 2^32 threads, and what the
-// backward's first one does not write sets the loops and addresses of the next: it must not be refused alone.
-constexpr int64_t MAX_BLOCKS_256 = ((int64_t)1 << 24) - 1;
+// The blocks of a pass's largest launch, all of 256 threads (at most MAX_BLOCKS_256).  What the backward's first launch
+// does not write sets the loops and addresses of the next: it must not be refused alone.
 int64_t range_fwd_blocks(bool bf, const RangeArgs& a);
 int64_t range_bwd_blocks(bool bf, const RangeArgs& a);
 void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st);

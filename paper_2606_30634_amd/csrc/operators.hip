@@ -408,7 +408,6 @@ int dropout_add(int64_t rows, int64_t cols, const void* x, int64_t ldx, const vo
   if ((x != out || ldx != ldo) && meet(x, span(ldx), out, span(ldo))) return bad("out may be x itself but not overlap it otherwise");
   if ((residual != out || ldr != ldo) && meet(residual, span(ldr), out, span(ldo)))
     return bad("out may be the residual itself but not overlap it otherwise");
-  if (rows * cols > (int64_t)256 * 8 * 0x7fffffff) return bad("rows cols is too large for a launch");
   launch_dropout(is_bf16 != 0, DropoutArgs{rows, cols, ldx, ldr, ldo, x, residual, out,
                                            (uint32_t)std::nearbyint(65536.0 * p), seed, offset}, (hipStream_t)hip_stream);
   return launched();

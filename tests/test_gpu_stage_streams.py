@@ -12,6 +12,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("w", [F32, F64], ids=lambda w: w.name)
 def test_variant_on_a_stream_of_its_own(w):
     import torch
+    from paper_2606_30634_amd import binding as B
     from paper_2606_30634_amd.stage import Stage
     log(w.name)
     dev = torch.device("cuda:0")
@@ -25,6 +26,8 @@ def test_variant_on_a_stream_of_its_own(w):
         st = Stage(shape_of(w), "cuda:0", stream=stream)
         st.load_master(datagen.init_params(w))
         y, dx = (torch.full((w.micro_batch, w.seq_len, w.d_model), float("nan"), dtype=dt, device=dev) for _ in range(2))
+        torch.cuda.synchronize()
+        B.stage_sync_weights(st.handle)  # the master weights were written on the caller's stream
         torch.cuda.synchronize()
         held = []
         if stream is not None:  # blocks of every size that the workspace could take, freed with work on them to come

@@ -875,5 +875,9 @@ void launch_range_bwd(bool bf, RangeArgs a, void* ws, hipStream_t st) {
 void launch_key_ranges(int64_t B, int S, const int32_t* ids, const uint8_t* flags, int32_t* start, int32_t* end,
                        hipStream_t st) {
   const int nb = (int)cdiv(S, RT);
-  key_ranges<<<(unsigned)(B * nb), RTH, 0, st>>>(S, nb, ids, flags, start, end);
+  const int64_t most = MAX_BLOCKS_256 / nb;  // rows of a launch
+  for (int64_t b = 0; b < B; b += most) {
+    const int64_t o = b * S;
+    key_ranges<<<(unsigned)(std::min(most, B - b) * nb), RTH, 0, st>>>(S, nb, ids + o, flags ? flags + o : nullptr, start + o, end + o);
+  }
 }

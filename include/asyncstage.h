@@ -440,7 +440,8 @@ int preference_loss(int64_t pairs, int64_t len, const float* logp, const float* 
 /* Key ranges of packed documents.  documents [batch, length] int32: a document is a run of equal ids >= 0; ids
  * below 0 are padding.  Query i sees the keys [key_start[i], key_end[i]) of its row: from the first token of
  * its document to itself; with prefix [batch, length] uint8 (or NULL), the tokens from a document's first one on
- * whose flag is not 0 see that whole run of them.  Padding sees nothing (0, 0).  batch in [0, 2^24], length in [0, 2^30]. */
+ * whose flag is not 0 see that whole run of them.  Padding sees nothing (0, 0).  batch in [0, 2^24], length in [0, 2^30]; the
+ * time grows with the square of a document's length beyond 2048 tokens. */
 int attention_key_ranges(int64_t batch, int64_t length, const int32_t* documents, const uint8_t* prefix,
                          int32_t* key_start, int32_t* key_end, void* hip_stream);
 
@@ -541,7 +542,7 @@ int stage_grad_norm(stage_t* s, int32_t which, float* norm_dev);
 /* Kernel-class timing.  While enabled, the stage records a HIP event pair on the launching
  * stream around every launch of a class and, when read, adds up the elapsed times and the algorithmic work of
  * those launches: GEMM and attention in flops (2 M N K per product; causal attention forward
- * 4 B Hq hd s(s+1)/2, backward twice that), the delayed update and the gradient norm in bytes of
+ * 4 B Hq hd s(s+1)/2, backward twice that, also where documents let a query see less), the delayed update and the gradient norm in bytes of
  * HBM traffic, the Newton-Schulz products of Muon (STAGE_PROF_NS) in flops.  Reading synchronises the stream and resets the counters.  Meant for measurement
  * passes; it adds two event records per launch. */
 typedef enum {

@@ -73,7 +73,7 @@ __device__ __forceinline__ f32x16 rows_product_parts(const RowFrag<HD>& a, const
 }
 
 // The same for dP, of which nothing is an exponential: in parts at 128 only (their registers spill: 1425 tokens, 32
-// heads of 128 on 8: backward 999 -> 1141 us, gradients 1.0e-6 off against 9.3e-7), one chain of 64 at most otherwise
+// heads of 128 on 8: backward 989 -> 1149 us captured, gradients 1.0e-6 off against 9.3e-7), one chain of 64 at most otherwise
 template <int HD>
 __device__ __forceinline__ f32x16 grad_product(const RowFrag<HD>& a, const RowFrag<HD>& b) {
   if constexpr (HD == 128) return rows_product_parts<HD>(a, b);
@@ -542,7 +542,9 @@ __global__ void __launch_bounds__(256) range_grad_join(RangeArgs a) {
 // position where a prefix ends is a running minimum from its end.  What lies outside the block's tokens is
 // searched for, outwards from them and no further than the document goes.  The block's tokens and the RT on either side
 // are loaded together, since the time is that of the round trips to memory (4 rows of 131072 tokens, 200 documents each:
-// 11.8 us with one after the other, 7.2 so).
+// 11.8 us of kernel time with one after the other, 7.2 so).  A document over many blocks is walked by each of them, RT tokens
+// a round trip: the work grows with the square of its length (one document a row, 4 x 131072 tokens: 55 us, 84 with prefixes; one
+// of 2^22: 2.7 ms).
 constexpr int RT = 2048, RTH = 256, PT = RT / RTH;
 
 // PT tokens of a row from i0 on (those below `end` exist) and the id before them

@@ -434,6 +434,9 @@ __global__ void __launch_bounds__(NT, 2) range_flash_fwd(RangeArgs a, int pack) 
 }
 
 // ------------------------------------------------------------------------------------------ backward
+// P and dS are rounded to bf16 for their products, as in the causal kernels: the gradients are 2.4e-3 of their norm off, of
+// which their own rounding is 1.7e-3.  In two parts each they would take three products more to the seven there are, in
+// kernels that the matrix cores and the vector work between them bound.
 // The tanh of a tile's products ahead of a softmax of the backward.  Behind the polynomial its slope is 1 - t^2, an
 // instruction of the softmax.  A t near 1 has lost it (at y = 8 it would be 6 % off, from y = 10 on 0), so in the other branch the
 // slope comes from e = exp(-2 |y|), as 4 e / (1 + e)^2, and is put where the softmax finds it for nothing more:
@@ -755,7 +758,7 @@ __device__ __forceinline__ void range_dq_block(const RangeArgs& a, int qb, int s
     const int key0 = blo + kt * KB;
     if (key0 < wk.hi && key0 + KB > wk.lo) {
       // frag_rows and frag_cols; with CAP at 128 their addresses are formed here, tile by tile: kept across the loop they
-      // push other registers out to memory (2 x 4096 tokens, 32 heads on 8: dQ 528 us, and 800 with the exact slopes)
+      // push other registers out to memory (2 x 4096 tokens, 32 heads on 8: dQ 800 us, 512 so)
       int at = lane;
       if constexpr (CAP && HD == 128) asm volatile("" : "+v"(at));
       auto rows_at = [&](const bf16* T, int r, int k) { return frag_rows_of<HD>(T, r, k, at); };
@@ -1326,8 +1329,8 @@ int range_mfma_dkv_splits(const RangeArgs& a) {
 }
 
 // Few query blocks share their keys' tiles, towards 512 items: a block of a long row alone is a chain of its tiles
-// (one sequence of 4096 tokens, one head of 64: backward 87 -> 38 us; 16 queries on 8192 keys, 8 heads of 128 on 1: 206 ->
-// 59)
+// (captured: one sequence of 4096 tokens, one head of 64: backward 89 -> 46 us; 16 queries on 8192 keys, 8 heads of 128 on
+// 1: 214 -> 59)
 int range_mfma_dq_splits(const RangeArgs& a) {
   const int64_t items = cdiv(a.Sq, QB) * a.Hq * a.B;
   return items == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, 512 / items, cdiv(a.Sk, KB) / tiles_per_share(items)}));

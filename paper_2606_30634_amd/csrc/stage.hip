@@ -622,11 +622,15 @@ AttnArgs attn_args(const stage* S, const BlockAct& b) {
   return a;
 }
 
+RangeArgs range_sizes(const stage_shape_t& sh) {
+  RangeArgs a{};
+  a.B = sh.micro_batch; a.Sq = a.Sk = sh.seq_len; a.Hq = sh.n_heads; a.Hkv = sh.n_kv_heads; a.hd = sh.head_dim;
+  return a;
+}
 // The variant's attention over the slot's packed projections
 RangeArgs range_args(const stage* S, const Slot& sl, const BlockAct& b) {
   const stage_shape_t& sh = S->sh;
-  RangeArgs a{};
-  a.B = sh.micro_batch; a.Sq = a.Sk = sh.seq_len; a.Hq = sh.n_heads; a.Hkv = sh.n_kv_heads; a.hd = sh.head_dim;
+  RangeArgs a = range_sizes(sh);
   auto heads = [&](void* base, int first) {
     return HeadRows{(char*)base + (size_t)first * sh.head_dim * S->esz, (int64_t)sh.seq_len * S->qkvw, sh.head_dim, S->qkvw};
   };
@@ -980,9 +984,7 @@ size_t variant_layout(stage* s, const stage_variant_t& v, char* p) {
     return r;
   };
   const size_t T = s->T, act = T * s->sh.d_model * s->esz;
-  RangeArgs a{};
-  a.B = s->sh.micro_batch; a.Sq = a.Sk = s->sh.seq_len;
-  a.Hq = s->sh.n_heads; a.Hkv = s->sh.n_kv_heads; a.hd = s->sh.head_dim;
+  const RangeArgs a = range_sizes(s->sh);
   void* ws = take(std::max(range_fwd_ws_bytes(s->bf, a), range_bwd_ws_bytes(s->bf, a)));
   const bool dropped = std::nearbyint(65536.0 * v.dropout) > 0;
   void* b[3];
@@ -1161,6 +1163,9 @@ int stage_set_variant(stage_t* s, const stage_variant_t* v, void* workspace, siz
     return STAGE_OK;
   }
   if (!workspace || (uintptr_t)workspace % ALIGN) return fail(STAGE_EINVAL, "workspace must be 256-byte aligned");
+  const RangeArgs a = range_sizes(s->sh);
+  if (std::max(range_fwd_blocks(s->bf, a), range_bwd_blocks(s->bf, a)) > MAX_BLOCKS_256)
+    return fail(STAGE_EINVAL, "micro_batch x seq_len x n_heads x head_dim is too large for a launch of the variant's attention");
   const size_t need = variant_layout(s, *v, nullptr);
   if (workspace_bytes < need)
     return fail(STAGE_ENOSPACE, "workspace holds " + std::to_string(workspace_bytes) + " bytes, needs " + std::to_string(need));
